@@ -389,6 +389,123 @@ int eden_profile_get(eden_ctx* ctx, uint32_t i, const char** name, uint64_t* lau
                      double* ms_total, double* bytes_total);
 const char* eden_strerror(int code);
 
+/* ---- the client's training step: linear layers and 8-bit activation checkpoints ----
+ *
+ * What a sender runs before it has a vector to send: the products of its feed-forward
+ * layers, with the activations that the backward pass needs kept in 8 bits, and the fp32
+ * weight gradients that eden_encode takes.  No formula of the paper is involved.
+ *
+ *   - Matrices are row-major; `*_stride` is the distance of two rows in elements, at least
+ *     the row length.  Rows may start anywhere that suits their element type.  All counts
+ *     are below 2^31; m = 0 (no tokens) is allowed, n = 0 and k = 0 are not.
+ *   - `type` is EDEN_TYPE_BF16 or EDEN_TYPE_FP16 (checkpoints also EDEN_TYPE_FP32): the type
+ *     of activations, weights, biases and activation gradients.  Sums are held in fp32 and
+ *     rounded once, where the result is stored.  Weight and bias gradients are fp32.
+ *   - Checkpoint: a row of features is cut into groups of EDEN_CHECKPOINT_GROUP; the last one
+ *     may be shorter.  A group keeps 2^e, e the smallest whole number with
+ *     max|v| <= 127 * 2^e (at least -126), as the byte e + 127, and per value the int8 code
+ *     v / 2^e rounded to nearest, ties to even.  A group that holds an infinity or a NaN has
+ *     the byte 255 and codes 0, and all its values are restored as NaN.  The value a code
+ *     stands for, code * 2^e, has seven significant bits: it is exact in every type, but for
+ *     values past the type's largest number, which are restored as that, and values below
+ *     2^-24 in fp16, which are rounded.
+ *   - NULL for an optional matrix leaves its term out.  An output may be the same matrix as
+ *     the residual or dy of the call (same pointer and stride); else nothing may overlap.
+ *   - Work is enqueued on the context's stream and uses the context's workspace, so the
+ *     figures of eden_client_stats are gone after these calls.  Results do not depend on the
+ *     order in which blocks run: there are no floating-point atomics. */
+#define EDEN_TYPE_BF16 0
+#define EDEN_TYPE_FP16 1
+#define EDEN_TYPE_FP32 2
+
+#define EDEN_ACT_NONE      0
+#define EDEN_ACT_RELU      1   /* max(z, 0); slope 0 at 0 */
+#define EDEN_ACT_GELU      2   /* z * Phi(z), Phi the normal distribution function */
+#define EDEN_ACT_GELU_TANH 3   /* z/2 * (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+#define EDEN_ACT_SILU      4   /* z / (1 + exp(-z)) */
+
+#define EDEN_SAVE_NONE 0
+#define EDEN_SAVE_PRE  1       /* z = x W^T + b, from its fp32 sums */
+#define EDEN_SAVE_OUT  2       /* y as it is stored */
+
+#define EDEN_CHECKPOINT_GROUP 32u
+
+/* ceil(features / 32): exponent bytes of one row. */
+uint64_t eden_checkpoint_groups(uint64_t features);
+/* Device workspace that holds every call of this section with m tokens and weights of n x k
+ * (act_backward: n features).  A call that needs less takes a smaller one. */
+uint64_t eden_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k);
+
+/* y [m, n] = act(x [m, k] W[n, k]^T + bias [n]) + residual [m, n]; `saved` receives the
+ * checkpoint of z or y (save). */
+typedef struct eden_linear_args {
+    const void* x;         uint64_t x_stride;
+    const void* weight;    uint64_t weight_stride;
+    const void* bias;                                   /* or NULL */
+    const void* residual;  uint64_t residual_stride;    /* or NULL */
+    void* y;               uint64_t y_stride;
+    int8_t* saved;         uint64_t saved_stride;       /* save != EDEN_SAVE_NONE */
+    uint8_t* saved_exp;    uint64_t saved_exp_stride;
+    uint64_t m, n, k;
+    int32_t type, act, save, reserved;
+} eden_linear_args;
+int eden_linear(eden_ctx* ctx, const eden_linear_args* args);
+
+/* codes [m, n], exps [m, groups(n)] <- x [m, n], and back. */
+typedef struct eden_checkpoint_args {
+    void* x;               uint64_t x_stride;           /* read by save, written by restore */
+    int8_t* codes;         uint64_t codes_stride;
+    uint8_t* exps;         uint64_t exps_stride;
+    uint64_t m, n;
+    int32_t type, reserved;
+} eden_checkpoint_args;
+int eden_checkpoint_save(eden_ctx* ctx, const eden_checkpoint_args* args);
+int eden_checkpoint_restore(eden_ctx* ctx, const eden_checkpoint_args* args);
+
+/* dz [m, n] = dy * act'(z), z the checkpointed pre-activation; bias_grad [n] = the column
+ * sums of dz before its rounding (accumulate: added to what bias_grad holds).  dz or
+ * bias_grad may be NULL. */
+typedef struct eden_act_backward_args {
+    const void* dy;        uint64_t dy_stride;
+    const int8_t* pre;     uint64_t pre_stride;         /* NULL with EDEN_ACT_NONE */
+    const uint8_t* pre_exp; uint64_t pre_exp_stride;
+    void* dz;              uint64_t dz_stride;          /* or NULL */
+    float* bias_grad;                                   /* or NULL */
+    uint64_t m, n;
+    int32_t type, act, accumulate, reserved;
+} eden_act_backward_args;
+int eden_act_backward(eden_ctx* ctx, const eden_act_backward_args* args);
+
+/* dx [m, k] = (dz [m, n] W[n, k] + residual) * act'(z): the gradient of a layer's input,
+ * plus what a residual branch brings, through the activation of the layer before it (z that
+ * layer's checkpointed pre-activation; NULL: dx is the input's gradient itself).
+ * bias_grad [k]: column sums of dx before its rounding. */
+typedef struct eden_linear_input_grad_args {
+    const void* dz;        uint64_t dz_stride;
+    const void* weight;    uint64_t weight_stride;
+    const void* residual;  uint64_t residual_stride;    /* or NULL */
+    const int8_t* pre;     uint64_t pre_stride;         /* or NULL with EDEN_ACT_NONE */
+    const uint8_t* pre_exp; uint64_t pre_exp_stride;
+    void* dx;              uint64_t dx_stride;
+    float* bias_grad;                                   /* or NULL */
+    uint64_t m, n, k;
+    int32_t type, act, accumulate, reserved;            /* accumulate: bias_grad += */
+} eden_linear_input_grad_args;
+int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_grad_args* args);
+
+/* weight_grad [n, k] (fp32) = dz [m, n]^T x [m, k], x either a matrix of dz's type (codes and
+ * exps NULL) or a checkpoint (x NULL).  accumulate: added to what weight_grad holds. */
+typedef struct eden_linear_weight_grad_args {
+    const void* dz;        uint64_t dz_stride;
+    const void* x;         uint64_t x_stride;
+    const int8_t* codes;   uint64_t codes_stride;
+    const uint8_t* exps;   uint64_t exps_stride;
+    float* weight_grad;    uint64_t weight_grad_stride;
+    uint64_t m, n, k;
+    int32_t type, accumulate;
+} eden_linear_weight_grad_args;
+int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_grad_args* args);
+
 #ifdef __cplusplus
 }
 #endif

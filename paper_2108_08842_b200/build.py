@@ -7,10 +7,11 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
+OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libeden.so")
-SOURCES = ["eden.cu", "lloyd_max.cpp", "uniform_family.cpp"]
+SOURCES = ["eden.cu", "train.cu", "lloyd_max.cpp", "uniform_family.cpp"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v"]
+              "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 
 
 def _newest_source() -> float:
@@ -21,20 +22,48 @@ def _newest_source() -> float:
     return newest
 
 
+def _fresh(obj: str) -> bool:
+    """Whether an object is newer than every file that the compiler read for it."""
+    try:
+        with open(obj + ".d") as f:
+            read = f.read().replace("\\\n", " ").split(":", 1)[1].split()
+        made = os.path.getmtime(obj)
+        return all(os.path.getmtime(p) <= made for p in read + [os.path.abspath(__file__)])
+    except (OSError, IndexError):
+        return False
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [nvcc] + NVCC_FLAGS + ["-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode:
+    os.makedirs(OBJ, exist_ok=True)
+    mark = ".tmp.%d" % os.getpid()
+    objects = [os.path.join(OBJ, s + ".o") for s in SOURCES]
+    running = []
+    for source, obj in zip(SOURCES, objects):           # one compiler per source, side by side
+        if force or not _fresh(obj):
+            cmd = [nvcc] + NVCC_FLAGS + ["-c", "-MMD", "-MF", obj + ".d", "-o", obj + mark, os.path.join(CSRC, source)]
+            running.append((obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    failed = False
+    for obj, p in running:
+        out, _ = p.communicate()
+        if verbose or p.returncode:
+            sys.stderr.write(out)
+        if p.returncode:
+            failed = True
+        else:
+            os.replace(obj + mark, obj)
+    if failed:
         raise RuntimeError("nvcc failed building libeden.so")
-    os.replace(tmp, LIB)
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB + mark] + objects
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("nvcc failed linking libeden.so")
+    os.replace(LIB + mark, LIB)
     return LIB
 
 
 if __name__ == "__main__":
-    print(build(force=True, verbose=True))
+    print(build(force="--force" in sys.argv[1:], verbose=True))

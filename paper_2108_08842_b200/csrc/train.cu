@@ -1,0 +1,284 @@
+// C ABI of the client's training step (declared in include/eden.h): argument checks,
+// workspace carving and launches.
+#include <algorithm>
+#include <new>
+
+#include "context.h"
+#include "kernels_checkpoint.cuh"
+#include "kernels_linear.cuh"
+
+using namespace eden;
+
+namespace {
+
+constexpr uint64_t kStatusBytes = 256;          // start of the workspace: the status word
+constexpr uint64_t kMaxCount = (1ull << 31) - 1;
+constexpr uint64_t kMaxRuns = 512;              // runs of rows that leave partial column sums
+
+uint64_t align_to(uint64_t v, uint64_t a) { return (v + a - 1) / a * a; }
+uint64_t groups_of(uint64_t n) { return (n + kGroup - 1) / kGroup; }
+uint64_t padded(uint64_t n) { return align_to(n, 8); }           // 16-byte rows of a 16-bit matrix
+
+// The caller's current device stays what it was.
+struct DeviceGuard {
+    int before = -1;
+    bool ok;
+    explicit DeviceGuard(int device)
+    {
+        ok = cudaGetDevice(&before) == cudaSuccess && (before == device || cudaSetDevice(device) == cudaSuccess);
+        if (before == device) before = -1;
+    }
+    ~DeviceGuard() { if (before >= 0) cudaSetDevice(before); }
+};
+
+// Scratch of one call, carved from the context's workspace behind the status word.
+struct Scratch {
+    char* base;
+    uint64_t used, size;
+    explicit Scratch(const eden_ctx* ctx) : base(ctx->ws), used(kStatusBytes), size(ctx->ws_bytes) {}
+    template <typename U> U* take(uint64_t count)
+    {
+        const uint64_t at = used, end = at + align_to(count * sizeof(U), 256);
+        if (end > size) return nullptr;
+        used = end;
+        return (U*)(base + at);
+    }
+};
+
+bool aligned(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
+
+bool half_type(int type) { return type == EDEN_TYPE_BF16 || type == EDEN_TYPE_FP16; }
+bool known_act(int act) { return act >= EDEN_ACT_NONE && act <= EDEN_ACT_SILU; }
+
+// a matrix of `size`-byte elements with rows of n
+bool matrix_ok(const void* p, uint64_t stride, uint64_t n, size_t size) { return p && aligned(p, size) && stride >= n; }
+bool optional_ok(const void* p, uint64_t stride, uint64_t n, size_t size) { return !p || matrix_ok(p, stride, n, size); }
+bool checkpoint_ok(const int8_t* codes, uint64_t cs, const uint8_t* exps, uint64_t es, uint64_t n)
+{
+    return codes && exps && cs >= n && es >= groups_of(n);
+}
+
+int counts_ok(uint64_t m, uint64_t n, uint64_t k)
+{
+    if (n == 0 || k == 0) return EDEN_ERR_INVALID_ARG;
+    return std::max(m, std::max(n, k)) > kMaxCount ? EDEN_ERR_TOO_LARGE : EDEN_OK;
+}
+
+// f(T{}) with the type behind an EDEN_TYPE_* of 16 bits
+#define EDEN_DISPATCH_HALF(type, CALL)                                      \
+    if ((type) == EDEN_TYPE_BF16) { using T_ = __nv_bfloat16; CALL; }        \
+    else { using T_ = __half; CALL; }
+
+#define EDEN_DISPATCH_TYPE(type, CALL)                                      \
+    if ((type) == EDEN_TYPE_BF16) { using T_ = __nv_bfloat16; CALL; }        \
+    else if ((type) == EDEN_TYPE_FP16) { using T_ = __half; CALL; }          \
+    else { using T_ = float; CALL; }
+
+size_t type_size(int type) { return type == EDEN_TYPE_FP32 ? 4 : 2; }
+
+CheckpointView view(const int8_t* codes, uint64_t cs, const uint8_t* exps, uint64_t es)
+{
+    return {const_cast<int8_t*>(codes), cs, const_cast<uint8_t*>(exps), es};
+}
+
+// partial [rows][n] -> out [n]
+int sum_columns(eden_ctx* ctx, const float* partial, uint64_t rows, uint64_t n, float* out, int accumulate)
+{
+    LAUNCH(ctx, "t_column_sum", 4.0 * (double)(rows + 1) * n, k_column_sum, (uint32_t)((n + kCkptThreads - 1) / kCkptThreads),
+           kCkptThreads, 0, partial, rows, n, out, accumulate);
+    return EDEN_OK;
+}
+
+template <typename T>
+int restore(eden_ctx* ctx, CheckpointView c, T* x, uint64_t x_stride, uint64_t m, uint64_t n)
+{
+    const uint64_t total = m * groups_of(n), blocks = (total + 7) / 8;
+    if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    LAUNCH(ctx, "t_restore", (double)m * (n * (1.0 + sizeof(T)) + groups_of(n)), k_checkpoint_restore<T>, (uint32_t)blocks,
+           kCkptThreads, 0, x, x_stride, c, n, groups_of(n), total);
+    return EDEN_OK;
+}
+
+template <int OP>
+int product(eden_ctx* ctx, const char* name, int type, const LinearOperands& g, const LinearEpilogue& p, double bytes)
+{
+    const uint64_t tiles = (p.rows + 127) / 128 * ((p.cols + 31) / 32);
+    if (tiles > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    EDEN_DISPATCH_HALF(type, LAUNCH(ctx, name, bytes, (k_linear_simple<OP, T_>), (uint32_t)tiles, 128, 0, g, p));
+    return EDEN_OK;
+}
+
+// Nothing throws across the C boundary: the launch records grow a vector while profiling.
+template <typename F>
+int guarded(eden_ctx* ctx, F&& f)
+{
+    DeviceGuard device(ctx->device);
+    if (!device.ok) return EDEN_ERR_CUDA;
+    ctx->order.clear();                          // the workspace no longer holds a call's client figures
+    try {
+        return f();
+    } catch (...) {
+        return EDEN_ERR_INVALID_ARG;
+    }
+}
+
+}  // namespace
+
+extern "C" uint64_t eden_checkpoint_groups(uint64_t features) { return groups_of(features); }
+
+extern "C" uint64_t eden_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k)
+{
+    // 16-bit copies of operands whose rows are not 16-byte aligned (or are restored from
+    // codes), and the partial column sums
+    const uint64_t mn = m * padded(n) * 2, mk = m * padded(k) * 2, nk = n * padded(k) * 2;
+    const uint64_t sums = std::max(std::max<uint64_t>((m + 31) / 32, 1) * k, kMaxRuns * n) * 4;
+    return kStatusBytes + std::max(mk + nk, std::max(mn + nk, mn + mk)) + sums + 4 * 256;
+}
+
+extern "C" int eden_linear(eden_ctx* ctx, const eden_linear_args* a)
+{
+    if (!ctx || !a) return EDEN_ERR_INVALID_ARG;
+    if (int rc = counts_ok(a->m, a->n, a->k)) return rc;
+    if (!half_type(a->type) || !known_act(a->act) || a->save < EDEN_SAVE_NONE || a->save > EDEN_SAVE_OUT) return EDEN_ERR_INVALID_ARG;
+    if (!matrix_ok(a->weight, a->weight_stride, a->k, 2) || !optional_ok(a->bias, a->n, a->n, 2)) return EDEN_ERR_INVALID_ARG;
+    if (a->m == 0) return EDEN_OK;
+    if (!matrix_ok(a->x, a->x_stride, a->k, 2) || !optional_ok(a->residual, a->residual_stride, a->n, 2) ||
+        !matrix_ok(a->y, a->y_stride, a->n, 2))
+        return EDEN_ERR_INVALID_ARG;
+    if (a->save != EDEN_SAVE_NONE && !checkpoint_ok(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride, a->n))
+        return EDEN_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> int {
+        LinearOperands g{a->x, a->weight, a->x_stride, a->weight_stride, a->k};
+        LinearEpilogue p{a->bias, a->residual, a->residual_stride, a->y, a->y_stride,
+                         view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride), nullptr, a->m, a->n, a->act, a->save, 0};
+        const double bytes = 2.0 * ((double)a->m * a->k + (double)a->n * a->k + a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
+                             (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
+        return product<kForward>(ctx, "t_linear", a->type, g, p, bytes);
+    });
+}
+
+extern "C" int eden_checkpoint_save(eden_ctx* ctx, const eden_checkpoint_args* a)
+{
+    if (!ctx || !a || a->n == 0 || a->type < EDEN_TYPE_BF16 || a->type > EDEN_TYPE_FP32) return EDEN_ERR_INVALID_ARG;
+    if (std::max(a->m, a->n) > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    if (a->m == 0) return EDEN_OK;
+    if (!matrix_ok(a->x, a->x_stride, a->n, type_size(a->type)) ||
+        !checkpoint_ok(a->codes, a->codes_stride, a->exps, a->exps_stride, a->n))
+        return EDEN_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> int {
+        const uint64_t groups = groups_of(a->n), total = a->m * groups, blocks = (total + 7) / 8;
+        if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
+        const CheckpointView c = view(a->codes, a->codes_stride, a->exps, a->exps_stride);
+        EDEN_DISPATCH_TYPE(a->type, LAUNCH(ctx, "t_save", (double)a->m * (a->n * (1.0 + sizeof(T_)) + groups), k_checkpoint_save<T_>,
+                                           (uint32_t)blocks, kCkptThreads, 0, (const T_*)a->x, a->x_stride, c, a->n, groups, total));
+        return EDEN_OK;
+    });
+}
+
+extern "C" int eden_checkpoint_restore(eden_ctx* ctx, const eden_checkpoint_args* a)
+{
+    if (!ctx || !a || a->n == 0 || a->type < EDEN_TYPE_BF16 || a->type > EDEN_TYPE_FP32) return EDEN_ERR_INVALID_ARG;
+    if (std::max(a->m, a->n) > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    if (a->m == 0) return EDEN_OK;
+    if (!matrix_ok(a->x, a->x_stride, a->n, type_size(a->type)) ||
+        !checkpoint_ok(a->codes, a->codes_stride, a->exps, a->exps_stride, a->n))
+        return EDEN_ERR_INVALID_ARG;
+    return guarded(ctx, [&]() -> int {
+        const CheckpointView c = view(a->codes, a->codes_stride, a->exps, a->exps_stride);
+        EDEN_DISPATCH_TYPE(a->type, return restore(ctx, c, (T_*)a->x, a->x_stride, a->m, a->n));
+    });
+}
+
+extern "C" int eden_act_backward(eden_ctx* ctx, const eden_act_backward_args* a)
+{
+    if (!ctx || !a || a->n == 0 || !half_type(a->type) || !known_act(a->act)) return EDEN_ERR_INVALID_ARG;
+    if (std::max(a->m, a->n) > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    if (!optional_ok(a->bias_grad, a->n, a->n, 4)) return EDEN_ERR_INVALID_ARG;
+    if (a->m > 0) {
+        if (!matrix_ok(a->dy, a->dy_stride, a->n, 2) || !optional_ok(a->dz, a->dz_stride, a->n, 2)) return EDEN_ERR_INVALID_ARG;
+        if (a->act != EDEN_ACT_NONE && !checkpoint_ok(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride, a->n)) return EDEN_ERR_INVALID_ARG;
+    }
+    return guarded(ctx, [&]() -> int {
+        const uint64_t groups = groups_of(a->n);
+        uint64_t runs = 0;
+        float* partial = nullptr;
+        if (a->m > 0 && (a->dz || a->bias_grad)) {
+            // about eight blocks of 8 warps for each SM, at least 8 rows (one per warp) to a run
+            const uint64_t want = std::min<uint64_t>(kMaxRuns, std::max<uint64_t>(1, (8ull * ctx->sm_count + groups - 1) / groups));
+            const uint64_t rows_per_run = std::max<uint64_t>(8, (a->m + want - 1) / want);
+            runs = (a->m + rows_per_run - 1) / rows_per_run;
+            if (a->bias_grad) {
+                partial = Scratch(ctx).take<float>(runs * a->n);
+                if (!partial) return EDEN_ERR_WORKSPACE;
+            }
+            EDEN_DISPATCH_HALF(a->type, LAUNCH(ctx, "t_act_backward", (double)a->m * (a->n * 5.0 + groups), k_act_backward<T_>,
+                                               dim3((uint32_t)groups, (uint32_t)runs), kCkptThreads, 0, (const T_*)a->dy, a->dy_stride,
+                                               view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), (T_*)a->dz, a->dz_stride,
+                                               partial, a->m, a->n, rows_per_run, a->act));
+        }
+        return a->bias_grad ? sum_columns(ctx, partial, runs, a->n, a->bias_grad, a->accumulate) : EDEN_OK;
+    });
+}
+
+extern "C" int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_grad_args* a)
+{
+    if (!ctx || !a) return EDEN_ERR_INVALID_ARG;
+    if (int rc = counts_ok(a->m, a->n, a->k)) return rc;
+    if (!half_type(a->type) || !known_act(a->act)) return EDEN_ERR_INVALID_ARG;
+    if (!matrix_ok(a->weight, a->weight_stride, a->k, 2) || !optional_ok(a->bias_grad, a->k, a->k, 4)) return EDEN_ERR_INVALID_ARG;
+    if (a->m > 0) {
+        if (!matrix_ok(a->dz, a->dz_stride, a->n, 2) || !optional_ok(a->residual, a->residual_stride, a->k, 2) ||
+            !matrix_ok(a->dx, a->dx_stride, a->k, 2))
+            return EDEN_ERR_INVALID_ARG;
+        if (a->act != EDEN_ACT_NONE && !checkpoint_ok(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride, a->k)) return EDEN_ERR_INVALID_ARG;
+    }
+    return guarded(ctx, [&]() -> int {
+        const uint64_t runs = (a->m + 31) / 32;
+        float* partial = nullptr;
+        if (a->m > 0) {
+            Scratch scratch(ctx);
+            if (a->bias_grad) {
+                partial = scratch.take<float>(runs * a->k);
+                if (!partial) return EDEN_ERR_WORKSPACE;
+            }
+            LinearOperands g{a->dz, a->weight, a->dz_stride, a->weight_stride, a->n};
+            LinearEpilogue p{nullptr, a->residual, a->residual_stride, a->dx, a->dx_stride,
+                             view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0};
+            const double bytes = 2.0 * ((double)a->m * a->n + (double)a->n * a->k + (double)a->m * a->k * (a->residual ? 2 : 1)) +
+                                 (a->act ? (double)a->m * (a->k + groups_of(a->k)) : 0.0);
+            if (int rc = product<kInputGrad>(ctx, "t_input_grad", a->type, g, p, bytes)) return rc;
+        }
+        return a->bias_grad ? sum_columns(ctx, partial, runs, a->k, a->bias_grad, a->accumulate) : EDEN_OK;
+    });
+}
+
+extern "C" int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_grad_args* a)
+{
+    if (!ctx || !a) return EDEN_ERR_INVALID_ARG;
+    if (int rc = counts_ok(a->m, a->n, a->k)) return rc;
+    if (!half_type(a->type) || !matrix_ok(a->weight_grad, a->weight_grad_stride, a->k, 4)) return EDEN_ERR_INVALID_ARG;
+    if (a->m > 0) {
+        if (!matrix_ok(a->dz, a->dz_stride, a->n, 2) || !!a->x == !!a->codes) return EDEN_ERR_INVALID_ARG;
+        if (a->x ? !matrix_ok(a->x, a->x_stride, a->k, 2) : !checkpoint_ok(a->codes, a->codes_stride, a->exps, a->exps_stride, a->k))
+            return EDEN_ERR_INVALID_ARG;
+    }
+    if (a->m == 0 && a->accumulate) return EDEN_OK;
+    return guarded(ctx, [&]() -> int {
+        LinearOperands g{a->dz, a->x, a->dz_stride, a->x_stride, a->m};
+        if (a->m > 0 && a->codes) {
+            const uint64_t stride = padded(a->k);
+            uint16_t* x = Scratch(ctx).take<uint16_t>(a->m * stride);
+            if (!x) return EDEN_ERR_WORKSPACE;
+            const CheckpointView c = view(a->codes, a->codes_stride, a->exps, a->exps_stride);
+            int rc = EDEN_OK;
+            EDEN_DISPATCH_HALF(a->type, rc = restore(ctx, c, (T_*)x, stride, a->m, a->k));
+            if (rc) return rc;
+            g.b = x;
+            g.b_stride = stride;
+        }
+        LinearEpilogue p{nullptr, nullptr, 0, a->weight_grad, a->weight_grad_stride, {}, nullptr, a->n, a->k, 0, 0, a->accumulate};
+        const double bytes = 2.0 * a->m * a->n + (double)a->m * (a->codes ? a->k + groups_of(a->k) : 2 * a->k) +
+                             4.0 * a->n * a->k * (a->accumulate ? 2 : 1);
+        return product<kWeightGrad>(ctx, "t_weight_grad", a->type, g, p, bytes);
+    });
+}
