@@ -5,6 +5,7 @@
 #pragma once
 
 #include "kernels_checkpoint.cuh"
+#include "tensor_core.cuh"
 
 namespace eden {
 
@@ -20,7 +21,128 @@ struct LinearEpilogue {
     float* column_sums;                // input grad: [ceil(rows / 32)][cols] sums of 32 rows, or null
     uint64_t rows, cols;
     int act, save, accumulate;
+    int wide;                          // kWide*
 };
+
+// Which matrices of an epilogue allow 32-byte accesses at multiples of 32 elements: their
+// rows start on 32-byte boundaries.
+enum { kWideOut = 1, kWideResidual = 2, kWideCodes = 4, kWideBias = 8 };
+
+template <typename T>
+__device__ __forceinline__ void unpack(uint32_t w, float& lo, float& hi)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        lo = __uint_as_float(w << 16);
+        hi = __uint_as_float(w & 0xFFFF0000u);
+    } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        lo = f.x;
+        hi = f.y;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack(float lo, float hi)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+
+// v[j] += from[j] for 32 values of a 16-bit type
+template <typename T>
+__device__ __forceinline__ void add_row(float (&v)[32], const T* from, int count, bool wide)
+{
+    if (wide && count == 32) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t w[8];
+            load_32b(from + 16 * i, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float lo, hi;
+                unpack<T>(w[j], lo, hi);
+                v[16 * i + 2 * j] += lo;
+                v[16 * i + 2 * j + 1] += hi;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < count) v[j] += to_float(from[j]);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(const float (&v)[32], T* to, int count, bool wide)
+{
+    if (wide && count == 32) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = pack<T>(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
+            store_32b(to + 16 * i, w);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < count) to[j] = from_float<T>(v[j]);
+    }
+}
+
+// the 8-bit form of a row's group
+__device__ __forceinline__ void save_group(const float (&v)[32], const CheckpointView& c, uint64_t row, uint64_t col0, int count, bool wide)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < count) most = max(most, magnitude_bits(v[j]));
+    const uint32_t e = group_exponent(most);
+    const float inverse = group_inverse(e);
+    c.exps[row * c.exps_stride + col0 / kGroup] = (uint8_t)e;
+    int8_t* codes = c.codes + row * c.codes_stride + col0;
+    if (wide && count == 32) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = group_code(v[4 * i], inverse) | group_code(v[4 * i + 1], inverse) << 8 | group_code(v[4 * i + 2], inverse) << 16 |
+                   group_code(v[4 * i + 3], inverse) << 24;
+        store_32b(codes, w);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < count) codes[j] = (int8_t)group_code(v[j], inverse);
+    }
+}
+
+// v[j] *= act'(z[j]) with z the checkpointed group
+__device__ __forceinline__ void apply_slopes(float (&v)[32], const CheckpointView& c, uint64_t row, uint64_t col0, int count, bool wide, int act)
+{
+    const int8_t* codes = c.codes + row * c.codes_stride + col0;
+    const float scale = group_scale(c.exps[row * c.exps_stride + col0 / kGroup]);
+    uint32_t w[8];
+    if (wide && count == 32) {
+        load_32b(codes, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (4 * i + j < count) w[i] |= (uint32_t)(uint8_t)codes[4 * i + j] << 8 * j;
+        }
+    }
+    with_act(act, [&](auto a) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            v[j] *= act_slope<decltype(a)::value>(code_value((int8_t)(w[j / 4] >> 8 * (j % 4)), scale));
+    });
+}
 
 // v[32]: fp32 sums of one row's columns col0 .. col0 + 31, held by the lane that owns the
 // row.  All 32 lanes of the warp call this together, for rows row0 + lane (row0 % 32 == 0)
@@ -33,62 +155,43 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row, ui
     if constexpr (OP == kWeightGrad) {
         if (!live) return;
         float* out = (float*)p.out + row * p.out_stride + col0;
+        if ((p.wide & kWideOut) && count == 32) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < count) out[j] = p.accumulate ? out[j] + v[j] : v[j];
+            for (int i = 0; i < 4; ++i) {
+                uint32_t w[8];
+                if (p.accumulate) {
+                    load_32b(out + 8 * i, w);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[8 * i + j] += __uint_as_float(w[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
+                store_32b(out + 8 * i, w);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < count) out[j] = p.accumulate ? out[j] + v[j] : v[j];
+        }
         return;
     }
     const T* residual = p.residual && live ? (const T*)p.residual + row * p.residual_stride + col0 : nullptr;
     if constexpr (OP == kForward) {
-        if (p.bias) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < count) v[j] += to_float(((const T*)p.bias)[col0 + j]);
-        }
-        auto save = [&]() {
-            if (!live) return;
-            uint32_t most = 0;
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < count) most = max(most, magnitude_bits(v[j]));
-            const uint32_t e = group_exponent(most);
-            const float inverse = group_inverse(e);
-            p.ckpt.exps[row * p.ckpt.exps_stride + col0 / kGroup] = (uint8_t)e;
-            int8_t* codes = p.ckpt.codes + row * p.ckpt.codes_stride + col0;
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < count) codes[j] = (int8_t)group_code(v[j], inverse);
-        };
-        if (p.save == EDEN_SAVE_PRE) save();
+        if (p.bias) add_row(v, (const T*)p.bias + col0, count, p.wide & kWideBias);
+        if (p.save == EDEN_SAVE_PRE && live) save_group(v, p.ckpt, row, col0, count, p.wide & kWideCodes);
         with_act(p.act, [&](auto a) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = act_value<decltype(a)::value>(v[j]);
         });
-        if (residual) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < count) v[j] += to_float(residual[j]);
-        }
-        if (p.save == EDEN_SAVE_OUT) {
+        if (residual) add_row(v, residual, count, p.wide & kWideResidual);
+        if (p.save == EDEN_SAVE_OUT && live) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = to_float(from_float<T>(v[j]));
-            save();
+            save_group(v, p.ckpt, row, col0, count, p.wide & kWideCodes);
         }
     } else {
-        if (residual) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < count) v[j] += to_float(residual[j]);
-        }
-        if (p.act != EDEN_ACT_NONE) {
-            const int8_t* codes = p.ckpt.codes + row * p.ckpt.codes_stride + col0;
-            const float scale = live ? group_scale(p.ckpt.exps[row * p.ckpt.exps_stride + col0 / kGroup]) : 0.f;
-            with_act(p.act, [&](auto a) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (live && j < count) v[j] *= act_slope<decltype(a)::value>(code_value(codes[j], scale));
-            });
-        }
+        if (residual) add_row(v, residual, count, p.wide & kWideResidual);
+        if (p.act != EDEN_ACT_NONE && live) apply_slopes(v, p.ckpt, row, col0, count, p.wide & kWideCodes, p.act);
         if (p.column_sums) {
             // lane j ends with the sum of column j: halves are exchanged and added five times
             float s[32];
@@ -104,55 +207,192 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row, ui
                     s[j] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, half);
                 }
             }
-            if (lane < count) p.column_sums[row / 32 * p.cols + col0 + lane] = s[0];
+            if (row - lane < p.rows && lane < count) p.column_sums[row / 32 * p.cols + col0 + lane] = s[0];
         }
     }
-    if (live) {
-        T* out = (T*)p.out + row * p.out_stride + col0;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < count) out[j] = from_float<T>(v[j]);
-    }
+    if (live) store_row(v, (T*)p.out + row * p.out_stride + col0, count, p.wide & kWideOut);
 }
 
-struct LinearOperands {
-    const void *a, *b;
-    uint64_t a_stride, b_stride;
-    uint64_t depth;                    // length of the sum
+// Tiles of the result, in the order in which they are handed out: bands of kBand tile rows,
+// column by column, so that the tiles in flight share few rows of A and of B in the L2 cache.
+struct TileGrid {
+    uint32_t rows, cols, count;        // tiles
+    uint32_t depth_steps;              // steps of 64 along the sum
 };
 
-// A block of 128 threads takes 128 rows x 32 columns, one row per thread.
-template <int OP, typename T>
-__global__ void __launch_bounds__(128) k_linear_simple(LinearOperands g, LinearEpilogue p)
+constexpr uint32_t kBand = 8;
+
+__device__ __forceinline__ void tile_at(const TileGrid& g, uint32_t t, uint32_t& row, uint32_t& col)
 {
-    __shared__ float sa[32][129], sb[32][32];
-    const uint64_t col_tiles = (p.cols + 31) / 32;
-    const uint64_t row0 = blockIdx.x / col_tiles * 128, col0 = blockIdx.x % col_tiles * 32;
-    const T *a = (const T*)g.a, *b = (const T*)g.b;
-    const int t = threadIdx.x;
-    float v[32];
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = 0.f;
-    for (uint64_t d0 = 0; d0 < g.depth; d0 += 32) {
-        for (int i = t; i < 32 * 128; i += 128) {
-            const int d = OP == kWeightGrad ? i / 128 : i % 32, r = OP == kWeightGrad ? i % 128 : i / 32;
-            const uint64_t row = row0 + r, dep = d0 + d;
-            sa[d][r] = row < p.rows && dep < g.depth ? to_float(a[OP == kWeightGrad ? dep * g.a_stride + row : row * g.a_stride + dep]) : 0.f;
+    const uint32_t per_band = kBand * g.cols, first = t / per_band * kBand;
+    const uint32_t height = min(kBand, g.rows - first), in_band = t % per_band;
+    row = first + in_band % height;
+    col = in_band / height;
+}
+
+// Shape of a block's share of a tile: 128 rows of A and BN / CG rows of B per step of 64.
+template <int CG, int BN>
+struct LinearShape {
+    static constexpr int kRowsB = BN / CG;
+    static constexpr uint32_t kBytesA = 128 * 128, kBytesB = kRowsB * 128, kStageBytes = kBytesA + kBytesB;
+    static constexpr int kStages = 6;
+    static constexpr uint32_t kSharedBytes = 1024 + kStages * kStageBytes + (2 * kStages + 5) * 8 + 16;
+    static constexpr uint32_t kColumns = 2 * BN;       // tensor memory: two tiles' sums
+};
+
+constexpr int kLinearThreads = 384;    // copies, products, tensor memory, one spare, eight epilogue warps
+
+// D = A B^T for tiles of 128 * CG x BN, persistent: block (pair) c takes tiles c, c + blocks, ...
+//   warp 0   one lane fills the stages with tensor copies, kStages ahead of the products
+//   warp 1   one lane (of the pair's first block) issues the products
+//   warps 4+ read finished sums from tensor memory and run the epilogue, while the products
+//            of the next tile fill the other half of tensor memory
+// CG = 2: the blocks of a pair hold 128 rows of A and half of the rows of B each; the first
+// one's barriers count both blocks' bytes, and its products write both blocks' sums.
+template <int OP, typename T, int CG, int BN>
+__global__ void __launch_bounds__(kLinearThreads, 1)
+k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, LinearEpilogue p, TileGrid grid,
+         uint32_t* __restrict__ status)
+{
+    using S = LinearShape<CG, BN>;
+    constexpr bool a_mn = OP == kWeightGrad, b_mn = OP != kForward;
+    constexpr uint32_t descriptor = product_descriptor(std::is_same_v<T, __nv_bfloat16>, a_mn, b_mn, 128 * CG, BN);
+
+    extern __shared__ char raw[];
+    const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + 8 * S::kStages;
+    const uint32_t sums_full = empty + 8 * S::kStages, sums_empty = sums_full + 16, drained = sums_empty + 16, slot = drained + 8;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0, first = blockIdx.x / CG, step = gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            barrier_init(full + 8 * i, 1);
+            barrier_init(empty + 8 * i, 1);
         }
-        for (int i = t; i < 32 * 32; i += 128) {
-            const int d = OP == kForward ? i % 32 : i / 32, c = OP == kForward ? i / 32 : i % 32;
-            const uint64_t col = col0 + c, dep = d0 + d;
-            sb[d][c] = col < p.cols && dep < g.depth ? to_float(b[OP == kForward ? col * g.b_stride + dep : dep * g.b_stride + col]) : 0.f;
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(sums_full + 8 * i, 1);
+            barrier_init(sums_empty + 8 * i, 8 * CG);
         }
-        __syncthreads();
-        for (int d = 0; d < 32; ++d) {
-            const float x = sa[d][t];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += x * sb[d][j];
-        }
-        __syncthreads();
+        barrier_init(drained, 1);
+        barrier_init_done();
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
     }
-    linear_epilogue<OP, T>(v, row0 + t, col0, p);
+    if (warp == 2) tmem_alloc<CG>(slot, S::kColumns);
+    tmem_fence_before();
+    if constexpr (CG == 2) cluster_arrive_wait(); else __syncthreads();
+    tmem_fence_after();
+    uint32_t sums;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sums) : "r"(slot));
+
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t n = 0;            // steps issued
+            for (uint32_t t = first; t < grid.count && ok; t += step) {
+                uint32_t tile_row, tile_col;
+                tile_at(grid, t, tile_row, tile_col);
+                const int row = (int)(tile_row * 128 * CG + rank * 128), col = (int)(tile_col * BN + rank * S::kRowsB);
+                for (uint32_t d = 0; d < grid.depth_steps; ++d, ++n) {
+                    const uint32_t s = n % S::kStages;
+                    if (!(ok = barrier_wait(empty + 8 * s, (n / S::kStages & 1) ^ 1))) break;
+                    const uint32_t bar = CG == 2 ? address_in(full + 8 * s, 0) : full + 8 * s;
+                    if (rank == 0) barrier_expect(full + 8 * s, CG * S::kStageBytes);
+                    const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
+                    const int depth = (int)d * 64;
+                    if constexpr (a_mn) {
+                        copy_box<CG>(a, &map_a, row, depth, bar);
+                        copy_box<CG>(a + 8192, &map_a, row + 64, depth, bar);
+                    } else {
+                        copy_box<CG>(a, &map_a, depth, row, bar);
+                    }
+                    if constexpr (b_mn) {
+#pragma unroll
+                        for (int i = 0; i < S::kRowsB / 64; ++i) copy_box<CG>(b + 8192 * i, &map_b, col + 64 * i, depth, bar);
+                    } else {
+                        copy_box<CG>(b, &map_b, depth, col, bar);
+                    }
+                }
+            }
+            // gave up: the copies still on their way (counted by the first block) land before the block ends
+            if (!ok && rank == 0)
+                for (uint32_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i) barrier_wait(full + 8 * (i % S::kStages), i / S::kStages & 1);
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            uint32_t n = 0, done = 0;
+            for (uint32_t t = first; t < grid.count && ok; t += step, ++done) {
+                const uint32_t half = done & 1, d_address = sums + half * BN;
+                if (!(ok = barrier_wait(sums_empty + 8 * half, (done / 2 & 1) ^ 1))) break;
+                tmem_fence_after();
+                for (uint32_t d = 0; d < grid.depth_steps; ++d, ++n) {
+                    const uint32_t s = n % S::kStages;
+                    if (!(ok = barrier_wait(full + 8 * s, n / S::kStages & 1))) break;
+                    tmem_fence_after();
+                    const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tile_product<CG>(d_address, tile_descriptor(a + k * (a_mn ? 2048 : 32), 8192, 1024),
+                                         tile_descriptor(b + k * (b_mn ? 2048 : 32), 8192, 1024), descriptor, d > 0 || k > 0);
+                    tile_commit<CG>(empty + 8 * s);
+                }
+                if (ok) tile_commit<CG>(sums_full + 8 * half);
+            }
+            if (!ok) {
+                tile_commit<CG>(drained);
+                barrier_wait(drained, 0);
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp % 4, side = (warp - 4) / 4;
+        uint32_t done = 0;
+        for (uint32_t t = first; t < grid.count; t += step, ++done) {
+            const uint32_t half = done & 1;
+            if (!(ok = barrier_wait(sums_full + 8 * half, done / 2 & 1))) break;
+            tmem_fence_after();
+            uint32_t tile_row, tile_col;
+            tile_at(grid, t, tile_row, tile_col);
+            const uint64_t row = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32 + lane;
+#pragma unroll 1
+            for (int c = 0; c < BN / 64; ++c) {
+                const uint32_t in_tile = side * (BN / 2) + c * 32;
+                const uint64_t col0 = (uint64_t)tile_col * BN + in_tile;
+                float v[32];
+                __syncwarp();
+                tmem_load(sums + ((uint32_t)quarter * 32 << 16) + half * BN + in_tile, v);
+                if (c == BN / 64 - 1) {
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive_remote(CG == 2 ? address_in(sums_empty + 8 * half, 0) : sums_empty + 8 * half);
+                }
+                if (col0 < p.cols) linear_epilogue<OP, T>(v, row, col0, p);
+            }
+        }
+    }
+    if (!ok) atomicOr(status, EDEN_STATUS_TIMEOUT);
+    __syncwarp();
+    tmem_fence_before();
+    if constexpr (CG == 2) cluster_arrive_wait(); else __syncthreads();
+    tmem_fence_after();
+    if (warp == 2) tmem_free<CG>(sums, S::kColumns);
+}
+
+// Copies rows of 16-bit values to rows of `stride` values (a multiple of 8) on a 16-byte boundary.
+__global__ void __launch_bounds__(256) k_align_rows(const uint16_t* __restrict__ from, uint64_t from_stride, uint16_t* __restrict__ to,
+                                                   uint64_t stride, uint64_t n, uint64_t total)
+{
+    const uint64_t chunk = (uint64_t)blockIdx.x * 256 + threadIdx.x;          // 8 values
+    if (chunk >= total) return;
+    const uint64_t per_row = stride / 8, row = chunk / per_row, col = chunk % per_row * 8;
+    const uint16_t* src = from + row * from_stride + col;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = col + 2 * i < n ? src[2 * i] : 0, hi = col + 2 * i + 1 < n ? src[2 * i + 1] : 0;
+        w[i] = lo | hi << 16;
+    }
+    *(uint4*)(to + row * stride + col) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 }  // namespace eden

@@ -99,13 +99,109 @@ int restore(eden_ctx* ctx, CheckpointView c, T* x, uint64_t x_stride, uint64_t m
     return EDEN_OK;
 }
 
-template <int OP>
-int product(eden_ctx* ctx, const char* name, int type, const LinearOperands& g, const LinearEpilogue& p, double bytes)
+// A 16-bit operand of a product: `rows` rows of `n` values.
+struct Operand {
+    const void* data;
+    uint64_t stride, rows, n;
+};
+
+// Tensor copies want 16-byte aligned rows: others are copied into the workspace first.
+int align_operand(eden_ctx* ctx, Scratch& scratch, Operand& o)
 {
-    const uint64_t tiles = (p.rows + 127) / 128 * ((p.cols + 31) / 32);
-    if (tiles > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    EDEN_DISPATCH_HALF(type, LAUNCH(ctx, name, bytes, (k_linear_simple<OP, T_>), (uint32_t)tiles, 128, 0, g, p));
+    if (o.rows == 1) o.stride = padded(o.n);
+    if (aligned(o.data, 16) && o.stride % 8 == 0) return EDEN_OK;
+    const uint64_t stride = padded(o.n), total = o.rows * (stride / 8), blocks = (total + 255) / 256;
+    if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    uint16_t* to = scratch.take<uint16_t>(o.rows * stride);
+    if (!to) return EDEN_ERR_WORKSPACE;
+    LAUNCH(ctx, "t_align_rows", 4.0 * o.rows * o.n, k_align_rows, (uint32_t)blocks, 256, 0, (const uint16_t*)o.data, o.stride, to, stride,
+           o.n, total);
+    o.data = to;
+    o.stride = stride;
     return EDEN_OK;
+}
+
+using EncodeMap = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeMap encode_map()
+{
+    static const EncodeMap fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) == cudaSuccess &&
+                        found == cudaDriverEntryPointSuccess;
+        return ok ? (EncodeMap)p : nullptr;
+    }();
+    return fn;
+}
+
+// boxes of 64 values x box_rows rows, 128-byte swizzle, zeros outside
+int make_map(CUtensorMap* map, int type, const Operand& o, uint32_t box_rows)
+{
+    const EncodeMap fn = encode_map();
+    if (!fn) return EDEN_ERR_CUDA;
+    const cuuint64_t dims[2] = {o.n, o.rows}, strides[1] = {o.stride * 2};
+    const cuuint32_t box[2] = {64, box_rows}, unit[2] = {1, 1};
+    const CUresult rc = fn(map, type == EDEN_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                           const_cast<void*>(o.data), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? EDEN_OK : EDEN_ERR_CUDA;
+}
+
+template <int OP, typename T, int CG, int BN>
+int launch_linear(eden_ctx* ctx, const char* name, int type, const Operand& a, const Operand& b, uint64_t depth, const LinearEpilogue& p,
+                  double bytes)
+{
+    using S = LinearShape<CG, BN>;
+    CUtensorMap map_a, map_b;
+    if (int rc = make_map(&map_a, type, a, OP == kWeightGrad ? 64 : 128)) return rc;
+    if (int rc = make_map(&map_b, type, b, OP == kForward ? S::kRowsB : 64)) return rc;
+    const uint64_t rows = (p.rows + 128 * CG - 1) / (128 * CG), cols = (p.cols + BN - 1) / BN;
+    if (rows * cols > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((depth + 63) / 64)};
+    const auto kernel = k_linear<OP, T, CG, BN>;
+    CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(rows * cols, ctx->sm_count / CG) * CG);
+    cfg.blockDim = dim3(kLinearThreads);
+    cfg.dynamicSmemBytes = S::kSharedBytes;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {CG, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = CG > 1 ? 1 : 0;
+    profile_begin(ctx, name, bytes);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, p, grid, (uint32_t*)ctx->ws);
+    profile_end(ctx);
+    ++ctx->launches;
+    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? EDEN_OK : EDEN_ERR_CUDA;
+}
+
+bool wide_rows(const void* p, uint64_t stride, size_t size) { return aligned(p, 32) && stride * size % 32 == 0; }
+
+// a: rows of the result (weight grad: steps of the sum) x ..., b: columns likewise
+template <int OP>
+int product(eden_ctx* ctx, Scratch& scratch, const char* name, int type, Operand a, Operand b, uint64_t depth, LinearEpilogue p, double bytes)
+{
+    if (int rc = align_operand(ctx, scratch, a)) return rc;
+    if (int rc = align_operand(ctx, scratch, b)) return rc;
+    p.wide = (wide_rows(p.out, p.out_stride, OP == kWeightGrad ? 4 : 2) ? kWideOut : 0) |
+             (wide_rows(p.residual, p.residual_stride, 2) ? kWideResidual : 0) |
+             (wide_rows(p.ckpt.codes, p.ckpt.codes_stride, 1) ? kWideCodes : 0) | (aligned(p.bias, 32) ? kWideBias : 0);
+    const auto waves = [&](uint64_t tile_rows, uint64_t tile_cols, uint64_t slots) {
+        return ((p.rows + tile_rows - 1) / tile_rows * ((p.cols + tile_cols - 1) / tile_cols) + slots - 1) / slots;
+    };
+    const double pair = 1.0 * waves(256, 256, ctx->sm_count / 2), one = 0.65 * waves(128, 128, ctx->sm_count),
+                 narrow = 0.45 * waves(128, 64, ctx->sm_count);
+    if (pair <= one && pair <= narrow) {
+        EDEN_DISPATCH_HALF(type, return (launch_linear<OP, T_, 2, 256>(ctx, name, type, a, b, depth, p, bytes)));
+    }
+    if (one <= narrow) {
+        EDEN_DISPATCH_HALF(type, return (launch_linear<OP, T_, 1, 128>(ctx, name, type, a, b, depth, p, bytes)));
+    }
+    EDEN_DISPATCH_HALF(type, return (launch_linear<OP, T_, 1, 64>(ctx, name, type, a, b, depth, p, bytes)));
 }
 
 // Nothing throws across the C boundary: the launch records grow a vector while profiling.
@@ -148,12 +244,13 @@ extern "C" int eden_linear(eden_ctx* ctx, const eden_linear_args* a)
     if (a->save != EDEN_SAVE_NONE && !checkpoint_ok(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride, a->n))
         return EDEN_ERR_INVALID_ARG;
     return guarded(ctx, [&]() -> int {
-        LinearOperands g{a->x, a->weight, a->x_stride, a->weight_stride, a->k};
+        Scratch scratch(ctx);
         LinearEpilogue p{a->bias, a->residual, a->residual_stride, a->y, a->y_stride,
-                         view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride), nullptr, a->m, a->n, a->act, a->save, 0};
+                         view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride), nullptr, a->m, a->n, a->act, a->save, 0, 0};
         const double bytes = 2.0 * ((double)a->m * a->k + (double)a->n * a->k + a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
                              (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
-        return product<kForward>(ctx, "t_linear", a->type, g, p, bytes);
+        return product<kForward>(ctx, scratch, "t_linear", a->type, {a->x, a->x_stride, a->m, a->k}, {a->weight, a->weight_stride, a->n, a->k},
+                                 a->k, p, bytes);
     });
 }
 
@@ -241,12 +338,13 @@ extern "C" int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_gra
                 partial = scratch.take<float>(runs * a->k);
                 if (!partial) return EDEN_ERR_WORKSPACE;
             }
-            LinearOperands g{a->dz, a->weight, a->dz_stride, a->weight_stride, a->n};
             LinearEpilogue p{nullptr, a->residual, a->residual_stride, a->dx, a->dx_stride,
-                             view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0};
+                             view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0, 0};
             const double bytes = 2.0 * ((double)a->m * a->n + (double)a->n * a->k + (double)a->m * a->k * (a->residual ? 2 : 1)) +
                                  (a->act ? (double)a->m * (a->k + groups_of(a->k)) : 0.0);
-            if (int rc = product<kInputGrad>(ctx, "t_input_grad", a->type, g, p, bytes)) return rc;
+            if (int rc = product<kInputGrad>(ctx, scratch, "t_input_grad", a->type, {a->dz, a->dz_stride, a->m, a->n},
+                                             {a->weight, a->weight_stride, a->n, a->k}, a->n, p, bytes))
+                return rc;
         }
         return a->bias_grad ? sum_columns(ctx, partial, runs, a->k, a->bias_grad, a->accumulate) : EDEN_OK;
     });
@@ -264,21 +362,25 @@ extern "C" int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_g
     }
     if (a->m == 0 && a->accumulate) return EDEN_OK;
     return guarded(ctx, [&]() -> int {
-        LinearOperands g{a->dz, a->x, a->dz_stride, a->x_stride, a->m};
-        if (a->m > 0 && a->codes) {
-            const uint64_t stride = padded(a->k);
-            uint16_t* x = Scratch(ctx).take<uint16_t>(a->m * stride);
-            if (!x) return EDEN_ERR_WORKSPACE;
+        if (a->m == 0) {
+            CUDA_OK(cudaMemset2DAsync(a->weight_grad, a->weight_grad_stride * 4, 0, a->k * 4, a->n, ctx->stream));
+            return EDEN_OK;
+        }
+        Scratch scratch(ctx);
+        Operand x{a->x, a->x_stride, a->m, a->k};
+        if (a->codes) {
+            x.stride = padded(a->k);
+            uint16_t* held = scratch.take<uint16_t>(a->m * x.stride);
+            if (!held) return EDEN_ERR_WORKSPACE;
             const CheckpointView c = view(a->codes, a->codes_stride, a->exps, a->exps_stride);
             int rc = EDEN_OK;
-            EDEN_DISPATCH_HALF(a->type, rc = restore(ctx, c, (T_*)x, stride, a->m, a->k));
+            EDEN_DISPATCH_HALF(a->type, rc = restore(ctx, c, (T_*)held, x.stride, a->m, a->k));
             if (rc) return rc;
-            g.b = x;
-            g.b_stride = stride;
+            x.data = held;
         }
-        LinearEpilogue p{nullptr, nullptr, 0, a->weight_grad, a->weight_grad_stride, {}, nullptr, a->n, a->k, 0, 0, a->accumulate};
+        LinearEpilogue p{nullptr, nullptr, 0, a->weight_grad, a->weight_grad_stride, {}, nullptr, a->n, a->k, 0, 0, a->accumulate, 0};
         const double bytes = 2.0 * a->m * a->n + (double)a->m * (a->codes ? a->k + groups_of(a->k) : 2 * a->k) +
                              4.0 * a->n * a->k * (a->accumulate ? 2 : 1);
-        return product<kWeightGrad>(ctx, "t_weight_grad", a->type, g, p, bytes);
+        return product<kWeightGrad>(ctx, scratch, "t_weight_grad", a->type, {a->dz, a->dz_stride, a->m, a->n}, x, a->m, p, bytes);
     });
 }
