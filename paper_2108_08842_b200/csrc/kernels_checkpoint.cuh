@@ -1,66 +1,274 @@
 // 8-bit checkpoints of activations: save, restore, and the gradient of an activation whose
-// argument is a checkpoint.
+// argument is a checkpoint.  All three move a few bytes per value and compute little: HBM
+// bounds them, so what counts is enough bytes in flight (32 bytes per thread and load).
 #pragma once
 
 #include "train_device.cuh"
 
 namespace eden {
 
-struct CheckpointView {
-    int8_t* codes;
-    uint64_t codes_stride;
-    uint8_t* exps;
-    uint64_t exps_stride;
-};
-
 constexpr int kCkptThreads = 256;
 
-// One warp per group, one value per lane: any alignment, any row length.
+// ---- rows on 32-byte boundaries -----------------------------------------------------
+// A thread takes half a group: 16 values, 32 bytes of a 16-bit type (fp32: 64) and 16 codes.
+// `halves` = 2 * groups of a row, so that the halves of a group sit in neighbouring lanes.
+
+// 16 values -> floats; past the row's end: zeros
 template <typename T>
-__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* __restrict__ x, uint64_t x_stride,
-                                                                 CheckpointView c, uint64_t n, uint64_t groups, uint64_t total)
+__device__ __forceinline__ void load_half_group(const T* p, int count, float (&v)[16])
 {
-    const uint64_t warp = (uint64_t)blockIdx.x * (kCkptThreads / 32) + threadIdx.x / 32;
-    if (warp >= total) return;
-    const uint64_t row = warp / groups, group = warp % groups, col = group * kGroup + threadIdx.x % 32;
-    const float v = col < n ? to_float(x[row * x_stride + col]) : 0.f;
-    const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, magnitude_bits(v)));
-    if (col < n) c.codes[row * c.codes_stride + col] = (int8_t)group_code(v, group_inverse(e));
-    if (threadIdx.x % 32 == 0) c.exps[row * c.exps_stride + group] = (uint8_t)e;
+    if (count >= 16) {
+        if constexpr (sizeof(T) == 4) {
+            uint32_t a[8], b[8];
+            load_32b(p, a);
+            load_32b(p + 8, b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = __uint_as_float(a[j]);
+                v[8 + j] = __uint_as_float(b[j]);
+            }
+        } else {
+            uint32_t a[8];
+            load_32b(p, a);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) unpack<T>(a[j], v[2 * j], v[2 * j + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = j < count ? to_float(p[j]) : 0.f;
+    }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* __restrict__ x, uint64_t x_stride,
-                                                                    CheckpointView c, uint64_t n, uint64_t groups, uint64_t total)
+__device__ __forceinline__ void store_half_group(T* p, int count, const float (&v)[16])
 {
-    const uint64_t warp = (uint64_t)blockIdx.x * (kCkptThreads / 32) + threadIdx.x / 32;
-    if (warp >= total) return;
-    const uint64_t row = warp / groups, group = warp % groups, col = group * kGroup + threadIdx.x % 32;
-    if (col >= n) return;
-    x[row * x_stride + col] = restored<T>(code_value(c.codes[row * c.codes_stride + col], group_scale(c.exps[row * c.exps_stride + group])));
+    if (count >= 16) {
+        uint32_t a[8];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) a[j] = __float_as_uint(v[8 * i + j]);
+                store_32b(p + 8 * i, a);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) a[j] = pack<T>(v[2 * j], v[2 * j + 1]);
+            store_32b(p, a);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < count) p[j] = from_float<T>(v[j]);
+    }
+}
+
+__device__ __forceinline__ uint4 load_codes(const int8_t* p, int count)
+{
+    if (count >= 16) return *(const uint4*)p;
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if (j < count) w[j / 4] |= (uint32_t)(uint8_t)p[j] << 8 * (j % 4);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save_wide(const T* __restrict__ x, uint64_t x_stride, CheckpointView c,
+                                                                      uint32_t n, uint32_t halves, uint64_t total)
+{
+    dependency_wait();
+    dependency_release();
+    const uint64_t i = (uint64_t)blockIdx.x * kCkptThreads + threadIdx.x;
+    const uint64_t row = total <= 0xFFFFFFFFull ? (uint32_t)i / halves : i / halves;
+    const uint32_t half = (uint32_t)(i - row * halves), col = half * 16;
+    const bool live = i < total;
+    const int count = live && col < n ? (int)min(n - col, 16u) : 0;
+    float v[16];
+    load_half_group(x + (live ? row * x_stride + col : 0), count, v);
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) most = max(most, magnitude_bits(v[j]));
+    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+    const uint32_t e = group_exponent(most);
+    const float inverse = group_inverse(e);
+    if (!live) return;
+    if ((half & 1) == 0) c.exps[row * c.exps_stride + half / 2] = (uint8_t)e;
+    int8_t* codes = c.codes + row * c.codes_stride + col;
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = group_codes(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3], inverse);
+    if (count == 16) {
+        *(uint4*)codes = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < count) codes[j] = (int8_t)(w[j / 4] >> 8 * (j % 4));
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore_wide(T* __restrict__ x, uint64_t x_stride, CheckpointView c,
+                                                                         uint32_t n, uint32_t halves, uint64_t total)
+{
+    dependency_wait();
+    dependency_release();
+    const uint64_t i = (uint64_t)blockIdx.x * kCkptThreads + threadIdx.x;
+    const uint64_t row = total <= 0xFFFFFFFFull ? (uint32_t)i / halves : i / halves;
+    const uint32_t half = (uint32_t)(i - row * halves), col = half * 16;
+    if (i >= total || col >= n) return;
+    const int count = (int)min(n - col, 16u);
+    const uint32_t e = c.exps[row * c.exps_stride + half / 2];
+    const uint4 q = load_codes(c.codes + row * c.codes_stride + col, count);
+    const float scale = group_scale(e);
+    float v[16];
+    code_values(q.x, scale, v[0], v[1], v[2], v[3]);
+    code_values(q.y, scale, v[4], v[5], v[6], v[7]);
+    code_values(q.z, scale, v[8], v[9], v[10], v[11]);
+    code_values(q.w, scale, v[12], v[13], v[14], v[15]);
+    if (e >= kSaturates<T>) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = saturated<T>(v[j]);
+    }
+    store_half_group(x + row * x_stride + col, count, v);
+}
+
+// dz = dy * act'(z).  A warp spans 32 half groups (512 columns) and walks down a run of rows,
+// eight warps to a block, each keeping the sums of its own rows; the block adds the eight up
+// and leaves the run's column sums in partial[run][n].
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kCkptThreads) k_act_backward_wide(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
+                                                                   uint64_t dz_stride, float* __restrict__ partial, uint32_t m, uint32_t n,
+                                                                   uint32_t rows_per_run)
+{
+    dependency_wait();
+    dependency_release();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t half = blockIdx.x * 32 + lane, col = half * 16;
+    const uint32_t begin = blockIdx.y * rows_per_run, end = min(m, begin + rows_per_run);
+    const int count = col < n ? (int)min(n - col, 16u) : 0;
+    float sum[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+    if (count > 0) {
+        // the next row is on its way while this one is worked on
+        float next[16];
+        uint4 next_codes = make_uint4(0, 0, 0, 0);
+        uint32_t next_exp = 0;
+        auto fetch = [&](uint32_t row) {
+            if (row >= end) return;
+            load_half_group(dy + (uint64_t)row * dy_stride + col, count, next);
+            if constexpr (ACT != EDEN_ACT_NONE) {
+                next_exp = pre.exps[(uint64_t)row * pre.exps_stride + half / 2];
+                next_codes = load_codes(pre.codes + (uint64_t)row * pre.codes_stride + col, count);
+            }
+        };
+        fetch(begin + warp);
+        for (uint32_t row = begin + warp; row < end; row += kCkptThreads / 32) {
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = next[j];
+            const uint32_t w[4] = {next_codes.x, next_codes.y, next_codes.z, next_codes.w};
+            const float scale = group_scale(next_exp);
+            fetch(row + kCkptThreads / 32);
+            if constexpr (ACT != EDEN_ACT_NONE) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float z[4];
+                    code_values(w[j], scale, z[0], z[1], z[2], z[3]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[4 * j + k] *= act_slope<ACT>(z[k]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[j] += v[j];
+            if (dz) store_half_group(dz + (uint64_t)row * dz_stride + col, count, v);
+        }
+    }
+    if (!partial) return;
+    __shared__ float sums[kCkptThreads / 32][16][33];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sums[warp][j][lane] = sum[j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 512; i += kCkptThreads) {
+        const uint32_t at = blockIdx.x * 512 + i;
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < kCkptThreads / 32; ++w) total += sums[w][i % 16][i / 16];
+        if (at < n) partial[(uint64_t)blockIdx.y * n + at] = total;
+    }
+}
+
+// ---- any alignment ------------------------------------------------------------------
+// One value per lane, a warp per group; four groups of a warp are in flight together.
+constexpr int kGroupsInFlight = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* __restrict__ x, uint64_t x_stride, CheckpointView c, uint64_t n,
+                                                                 uint32_t groups, uint64_t total)
+{
+    dependency_wait();
+    dependency_release();
+    const uint64_t first = ((uint64_t)blockIdx.x * (kCkptThreads / 32) + threadIdx.x / 32) * kGroupsInFlight;
+    const int lane = threadIdx.x % 32;
+    float v[kGroupsInFlight];
+#pragma unroll
+    for (int i = 0; i < kGroupsInFlight; ++i) {
+        const uint64_t row = (first + i) / groups, col = (first + i) % groups * kGroup + lane;
+        v[i] = first + i < total && col < n ? to_float(x[row * x_stride + col]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kGroupsInFlight; ++i) {
+        if (first + i >= total) return;
+        const uint64_t row = (first + i) / groups, group = (first + i) % groups, col = group * kGroup + lane;
+        const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, magnitude_bits(v[i])));
+        if (col < n) c.codes[row * c.codes_stride + col] = (int8_t)group_code(v[i], group_inverse(e));
+        if (lane == 0) c.exps[row * c.exps_stride + group] = (uint8_t)e;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* __restrict__ x, uint64_t x_stride, CheckpointView c, uint64_t n,
+                                                                    uint32_t groups, uint64_t total)
+{
+    dependency_wait();
+    dependency_release();
+    const uint64_t first = ((uint64_t)blockIdx.x * (kCkptThreads / 32) + threadIdx.x / 32) * kGroupsInFlight;
+    const int lane = threadIdx.x % 32;
+    float v[kGroupsInFlight];
+#pragma unroll
+    for (int i = 0; i < kGroupsInFlight; ++i) {
+        const uint64_t row = (first + i) / groups, group = (first + i) % groups, col = group * kGroup + lane;
+        v[i] = first + i < total && col < n ? code_value(c.codes[row * c.codes_stride + col], group_scale(c.exps[row * c.exps_stride + group])) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kGroupsInFlight; ++i) {
+        const uint64_t row = (first + i) / groups, col = (first + i) % groups * kGroup + lane;
+        if (first + i < total && col < n) x[row * x_stride + col] = from_float<T>(saturated<T>(v[i]));
+    }
 }
 
 // dz = dy * act'(z), one lane per column: a block takes 32 columns of a run of rows and
 // leaves the run's column sums in partial[run][n].
-template <typename T>
+template <typename T, int ACT>
 __global__ void __launch_bounds__(kCkptThreads) k_act_backward(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
-                                                              uint64_t dz_stride, float* __restrict__ partial, uint64_t m,
-                                                              uint64_t n, uint64_t rows_per_run, int act)
+                                                              uint64_t dz_stride, float* __restrict__ partial, uint32_t m, uint32_t n,
+                                                              uint32_t rows_per_run)
 {
-    const uint64_t group = blockIdx.x, col = group * kGroup + threadIdx.x % 32;
-    const uint64_t begin = (uint64_t)blockIdx.y * rows_per_run, end = begin + rows_per_run < m ? begin + rows_per_run : m;
+    dependency_wait();
+    dependency_release();
+    const uint32_t group = blockIdx.x, col = group * kGroup + threadIdx.x % 32;
+    const uint32_t begin = blockIdx.y * rows_per_run, end = min(m, begin + rows_per_run);
     float sum = 0.f;
     if (col < n) {
-        with_act(act, [&](auto a) {
-            for (uint64_t row = begin + threadIdx.x / 32; row < end; row += kCkptThreads / 32) {
-                float v = to_float(dy[row * dy_stride + col]);
-                if constexpr (decltype(a)::value != EDEN_ACT_NONE)
-                    v *= act_slope<decltype(a)::value>(code_value(pre.codes[row * pre.codes_stride + col],
-                                                                  group_scale(pre.exps[row * pre.exps_stride + group])));
-                sum += v;
-                if (dz) dz[row * dz_stride + col] = from_float<T>(v);
-            }
-        });
+#pragma unroll 4
+        for (uint64_t row = begin + threadIdx.x / 32; row < end; row += kCkptThreads / 32) {
+            float v = to_float(dy[row * dy_stride + col]);
+            if constexpr (ACT != EDEN_ACT_NONE)
+                v *= act_slope<ACT>(code_value(pre.codes[row * pre.codes_stride + col], group_scale(pre.exps[row * pre.exps_stride + group])));
+            sum += v;
+            if (dz) dz[row * dz_stride + col] = from_float<T>(v);
+        }
     }
     if (!partial) return;
     __shared__ float sums[kCkptThreads / 32][32];
@@ -73,15 +281,28 @@ __global__ void __launch_bounds__(kCkptThreads) k_act_backward(const T* dy, uint
     }
 }
 
-// out[n] (+)= the sum of partial's rows, in their order
+// out[n] (+)= the sum of partial's rows: 32 columns per block, each warp every eighth row,
+// the eight added in order
 __global__ void __launch_bounds__(kCkptThreads) k_column_sum(const float* __restrict__ partial, uint64_t rows, uint64_t n,
                                                             float* __restrict__ out, int accumulate)
 {
-    const uint64_t col = (uint64_t)blockIdx.x * kCkptThreads + threadIdx.x;
-    if (col >= n) return;
+    dependency_wait();
+    dependency_release();
+    const uint64_t col = (uint64_t)blockIdx.x * 32 + threadIdx.x % 32;
+    const int warp = threadIdx.x / 32;
     float sum = 0.f;
-    for (uint64_t r = 0; r < rows; ++r) sum += partial[r * n + col];
-    out[col] = accumulate ? out[col] + sum : sum;
+    if (col < n) {
+#pragma unroll 8
+        for (uint64_t r = warp; r < rows; r += kCkptThreads / 32) sum += partial[r * n + col];
+    }
+    __shared__ float sums[kCkptThreads / 32][32];
+    sums[warp][threadIdx.x % 32] = sum;
+    __syncthreads();
+    if (warp == 0 && col < n) {
+        float total = 0.f;
+        for (int w = 0; w < kCkptThreads / 32; ++w) total += sums[w][threadIdx.x];
+        out[col] = accumulate ? out[col] + total : total;
+    }
 }
 
 }  // namespace eden

@@ -28,31 +28,6 @@ struct LinearEpilogue {
 // rows start on 32-byte boundaries.
 enum { kWideOut = 1, kWideResidual = 2, kWideCodes = 4, kWideBias = 8 };
 
-template <typename T>
-__device__ __forceinline__ void unpack(uint32_t w, float& lo, float& hi)
-{
-    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
-        lo = __uint_as_float(w << 16);
-        hi = __uint_as_float(w & 0xFFFF0000u);
-    } else {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-        lo = f.x;
-        hi = f.y;
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ uint32_t pack(float lo, float hi)
-{
-    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    } else {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-}
-
 // v[j] += from[j] for 32 values of a 16-bit type
 template <typename T>
 __device__ __forceinline__ void add_row(float (&v)[32], const T* from, int count, bool wide)
@@ -110,8 +85,7 @@ __device__ __forceinline__ void save_group(const float (&v)[32], const Checkpoin
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            w[i] = group_code(v[4 * i], inverse) | group_code(v[4 * i + 1], inverse) << 8 | group_code(v[4 * i + 2], inverse) << 16 |
-                   group_code(v[4 * i + 3], inverse) << 24;
+            w[i] = group_codes(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
         store_32b(codes, w);
     } else {
 #pragma unroll
@@ -139,8 +113,12 @@ __device__ __forceinline__ void apply_slopes(float (&v)[32], const CheckpointVie
     }
     with_act(act, [&](auto a) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            v[j] *= act_slope<decltype(a)::value>(code_value((int8_t)(w[j / 4] >> 8 * (j % 4)), scale));
+        for (int i = 0; i < 8; ++i) {
+            float z[4];
+            code_values(w[i], scale, z[0], z[1], z[2], z[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * i + j] *= act_slope<decltype(a)::value>(z[j]);
+        }
     });
 }
 
@@ -283,6 +261,8 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     tmem_fence_before();
     if constexpr (CG == 2) cluster_arrive_wait(); else __syncthreads();
     tmem_fence_after();
+    dependency_wait();
+    dependency_release();
     uint32_t sums;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sums) : "r"(slot));
 
@@ -382,6 +362,8 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 __global__ void __launch_bounds__(256) k_align_rows(const uint16_t* __restrict__ from, uint64_t from_stride, uint16_t* __restrict__ to,
                                                    uint64_t stride, uint64_t n, uint64_t total)
 {
+    dependency_wait();
+    dependency_release();
     const uint64_t chunk = (uint64_t)blockIdx.x * 256 + threadIdx.x;          // 8 values
     if (chunk >= total) return;
     const uint64_t per_row = stride / 8, row = chunk / per_row, col = chunk % per_row * 8;

@@ -47,6 +47,8 @@ struct Scratch {
 
 bool aligned(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
 
+bool wide_rows(const void* p, uint64_t stride, size_t size) { return aligned(p, 32) && stride * size % 32 == 0; }
+
 bool half_type(int type) { return type == EDEN_TYPE_BF16 || type == EDEN_TYPE_FP16; }
 bool known_act(int act) { return act >= EDEN_ACT_NONE && act <= EDEN_ACT_SILU; }
 
@@ -81,23 +83,93 @@ CheckpointView view(const int8_t* codes, uint64_t cs, const uint8_t* exps, uint6
     return {const_cast<int8_t*>(codes), cs, const_cast<uint8_t*>(exps), es};
 }
 
+// A launch that may begin before the stream's previous kernel has ended: the kernels of this
+// file wait for it themselves (dependency_wait).  cluster = blocks per cluster.
+template <typename... KArgs, typename... Args>
+int launch(eden_ctx* ctx, const char* name, double bytes, void (*kernel)(KArgs...), dim3 grid, uint32_t block, uint32_t shared,
+           uint32_t cluster, Args&&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {cluster, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    profile_begin(ctx, name, bytes);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+    profile_end(ctx);
+    ++ctx->launches;
+    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? EDEN_OK : EDEN_ERR_CUDA;
+}
+
 // partial [rows][n] -> out [n]
 int sum_columns(eden_ctx* ctx, const float* partial, uint64_t rows, uint64_t n, float* out, int accumulate)
 {
-    LAUNCH(ctx, "t_column_sum", 4.0 * (double)(rows + 1) * n, k_column_sum, (uint32_t)((n + kCkptThreads - 1) / kCkptThreads),
-           kCkptThreads, 0, partial, rows, n, out, accumulate);
-    return EDEN_OK;
+    return launch(ctx, "t_column_sum", 4.0 * (double)(rows + 1) * n, k_column_sum, dim3((uint32_t)((n + 31) / 32)), kCkptThreads, 0, 1,
+                  partial, rows, n, out, accumulate);
+}
+
+// Rows on 32-byte boundaries and codes on 16-byte ones take the wide kernels: on 16384 x 4096
+// bf16 they restore in WIDE us against NARROW us for one value per lane.
+bool wide_checkpoint(const void* x, uint64_t x_stride, size_t size, const CheckpointView& c)
+{
+    return aligned(x, 32) && x_stride * size % 32 == 0 && aligned(c.codes, 16) && c.codes_stride % 16 == 0;
+}
+
+template <typename T>
+int save(eden_ctx* ctx, const T* x, uint64_t x_stride, CheckpointView c, uint64_t m, uint64_t n)
+{
+    const uint64_t groups = groups_of(n);
+    const double bytes = (double)m * (n * (1.0 + sizeof(T)) + groups);
+    if (wide_checkpoint(x, x_stride, sizeof(T), c)) {
+        const uint64_t total = m * groups * 2, blocks = (total + kCkptThreads - 1) / kCkptThreads;
+        if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
+        return launch(ctx, "t_save", bytes, k_checkpoint_save_wide<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n, groups * 2, total);
+    }
+    const uint64_t total = m * groups, blocks = (total + 8 * kGroupsInFlight - 1) / (8 * kGroupsInFlight);
+    if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    return launch(ctx, "t_save", bytes, k_checkpoint_save<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n, groups, total);
 }
 
 template <typename T>
 int restore(eden_ctx* ctx, CheckpointView c, T* x, uint64_t x_stride, uint64_t m, uint64_t n)
 {
-    const uint64_t total = m * groups_of(n), blocks = (total + 7) / 8;
+    const uint64_t groups = groups_of(n);
+    const double bytes = (double)m * (n * (1.0 + sizeof(T)) + groups);
+    if (wide_checkpoint(x, x_stride, sizeof(T), c)) {
+        const uint64_t total = m * groups * 2, blocks = (total + kCkptThreads - 1) / kCkptThreads;
+        if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
+        return launch(ctx, "t_restore", bytes, k_checkpoint_restore_wide<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n,
+                      groups * 2, total);
+    }
+    const uint64_t total = m * groups, blocks = (total + 8 * kGroupsInFlight - 1) / (8 * kGroupsInFlight);
     if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    LAUNCH(ctx, "t_restore", (double)m * (n * (1.0 + sizeof(T)) + groups_of(n)), k_checkpoint_restore<T>, (uint32_t)blocks,
-           kCkptThreads, 0, x, x_stride, c, n, groups_of(n), total);
-    return EDEN_OK;
+    return launch(ctx, "t_restore", bytes, k_checkpoint_restore<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n, groups, total);
 }
+
+template <typename T, int ACT>
+int act_backward(eden_ctx* ctx, const eden_act_backward_args* a, float* partial, bool wide, uint64_t strips, uint64_t runs, uint64_t rows_per_run)
+{
+    const double bytes = (double)a->m * a->n * (2.0 + (a->dz ? 2.0 : 0.0) + (ACT ? 1.0 : 0.0));
+    return launch(ctx, "t_act_backward", bytes, wide ? k_act_backward_wide<T, ACT> : k_act_backward<T, ACT>,
+                  dim3((uint32_t)strips, (uint32_t)runs), kCkptThreads, 0, 1, (const T*)a->dy, a->dy_stride,
+                  view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), (T*)a->dz, a->dz_stride, partial, a->m, a->n, rows_per_run);
+}
+
+#define EDEN_DISPATCH_ACT(act, CALL)                                                            \
+    switch (act) {                                                                              \
+        case EDEN_ACT_RELU: { constexpr int ACT_ = EDEN_ACT_RELU; CALL; } break;                \
+        case EDEN_ACT_GELU: { constexpr int ACT_ = EDEN_ACT_GELU; CALL; } break;                \
+        case EDEN_ACT_GELU_TANH: { constexpr int ACT_ = EDEN_ACT_GELU_TANH; CALL; } break;      \
+        case EDEN_ACT_SILU: { constexpr int ACT_ = EDEN_ACT_SILU; CALL; } break;                \
+        default: { constexpr int ACT_ = EDEN_ACT_NONE; CALL; } break;                           \
+    }
 
 // A 16-bit operand of a product: `rows` rows of `n` values.
 struct Operand {
@@ -114,8 +186,9 @@ int align_operand(eden_ctx* ctx, Scratch& scratch, Operand& o)
     if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
     uint16_t* to = scratch.take<uint16_t>(o.rows * stride);
     if (!to) return EDEN_ERR_WORKSPACE;
-    LAUNCH(ctx, "t_align_rows", 4.0 * o.rows * o.n, k_align_rows, (uint32_t)blocks, 256, 0, (const uint16_t*)o.data, o.stride, to, stride,
-           o.n, total);
+    if (int rc = launch(ctx, "t_align_rows", 4.0 * o.rows * o.n, k_align_rows, dim3((uint32_t)blocks), 256, 0, 1, (const uint16_t*)o.data,
+                        o.stride, to, stride, o.n, total))
+        return rc;
     o.data = to;
     o.stride = stride;
     return EDEN_OK;
@@ -162,24 +235,9 @@ int launch_linear(eden_ctx* ctx, const char* name, int type, const Operand& a, c
     const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((depth + 63) / 64)};
     const auto kernel = k_linear<OP, T, CG, BN>;
     CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(rows * cols, ctx->sm_count / CG) * CG);
-    cfg.blockDim = dim3(kLinearThreads);
-    cfg.dynamicSmemBytes = S::kSharedBytes;
-    cfg.stream = ctx->stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {CG, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = CG > 1 ? 1 : 0;
-    profile_begin(ctx, name, bytes);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, p, grid, (uint32_t*)ctx->ws);
-    profile_end(ctx);
-    ++ctx->launches;
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? EDEN_OK : EDEN_ERR_CUDA;
+    const uint32_t blocks = (uint32_t)std::min<uint64_t>(rows * cols, ctx->sm_count / CG) * CG;
+    return launch(ctx, name, bytes, kernel, dim3(blocks), kLinearThreads, S::kSharedBytes, CG, map_a, map_b, p, grid, (uint32_t*)ctx->ws);
 }
-
-bool wide_rows(const void* p, uint64_t stride, size_t size) { return aligned(p, 32) && stride * size % 32 == 0; }
 
 // a: rows of the result (weight grad: steps of the sum) x ..., b: columns likewise
 template <int OP>
@@ -263,12 +321,8 @@ extern "C" int eden_checkpoint_save(eden_ctx* ctx, const eden_checkpoint_args* a
         !checkpoint_ok(a->codes, a->codes_stride, a->exps, a->exps_stride, a->n))
         return EDEN_ERR_INVALID_ARG;
     return guarded(ctx, [&]() -> int {
-        const uint64_t groups = groups_of(a->n), total = a->m * groups, blocks = (total + 7) / 8;
-        if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
         const CheckpointView c = view(a->codes, a->codes_stride, a->exps, a->exps_stride);
-        EDEN_DISPATCH_TYPE(a->type, LAUNCH(ctx, "t_save", (double)a->m * (a->n * (1.0 + sizeof(T_)) + groups), k_checkpoint_save<T_>,
-                                           (uint32_t)blocks, kCkptThreads, 0, (const T_*)a->x, a->x_stride, c, a->n, groups, total));
-        return EDEN_OK;
+        EDEN_DISPATCH_TYPE(a->type, return save(ctx, (const T_*)a->x, a->x_stride, c, a->m, a->n));
     });
 }
 
@@ -296,22 +350,24 @@ extern "C" int eden_act_backward(eden_ctx* ctx, const eden_act_backward_args* a)
         if (a->act != EDEN_ACT_NONE && !checkpoint_ok(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride, a->n)) return EDEN_ERR_INVALID_ARG;
     }
     return guarded(ctx, [&]() -> int {
-        const uint64_t groups = groups_of(a->n);
         uint64_t runs = 0;
         float* partial = nullptr;
         if (a->m > 0 && (a->dz || a->bias_grad)) {
-            // about eight blocks of 8 warps for each SM, at least 8 rows (one per warp) to a run
-            const uint64_t want = std::min<uint64_t>(kMaxRuns, std::max<uint64_t>(1, (8ull * ctx->sm_count + groups - 1) / groups));
+            const CheckpointView c = view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride);
+            const bool wide = wide_rows(a->dy, a->dy_stride, 2) && (!a->dz || wide_rows(a->dz, a->dz_stride, 2)) &&
+                              (!a->act || (aligned(c.codes, 16) && c.codes_stride % 16 == 0));
+            // about six blocks of eight warps for each SM, at least 8 rows (one per warp) to a run
+            const uint64_t strips = wide ? (a->n + 511) / 512 : groups_of(a->n);
+            const uint64_t want = std::min<uint64_t>(kMaxRuns, std::max<uint64_t>(1, 6ull * ctx->sm_count / strips));
             const uint64_t rows_per_run = std::max<uint64_t>(8, (a->m + want - 1) / want);
             runs = (a->m + rows_per_run - 1) / rows_per_run;
             if (a->bias_grad) {
                 partial = Scratch(ctx).take<float>(runs * a->n);
                 if (!partial) return EDEN_ERR_WORKSPACE;
             }
-            EDEN_DISPATCH_HALF(a->type, LAUNCH(ctx, "t_act_backward", (double)a->m * (a->n * 5.0 + groups), k_act_backward<T_>,
-                                               dim3((uint32_t)groups, (uint32_t)runs), kCkptThreads, 0, (const T_*)a->dy, a->dy_stride,
-                                               view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), (T_*)a->dz, a->dz_stride,
-                                               partial, a->m, a->n, rows_per_run, a->act));
+            int rc = EDEN_OK;
+            EDEN_DISPATCH_HALF(a->type, EDEN_DISPATCH_ACT(a->act, rc = (act_backward<T_, ACT_>(ctx, a, partial, wide, strips, runs, rows_per_run))));
+            if (rc) return rc;
         }
         return a->bias_grad ? sum_columns(ctx, partial, runs, a->n, a->bias_grad, a->accumulate) : EDEN_OK;
     });

@@ -110,6 +110,24 @@ __device__ __forceinline__ uint32_t group_code(float v, float inverse)
 
 __device__ __forceinline__ float code_value(int8_t code, float scale) { return (float)code * scale; }
 
+// four codes in a word: the byte c + 128 under the exponent of 2^23 is 2^23 + 128 + c
+__device__ __forceinline__ void code_values(uint32_t w, float scale, float& v0, float& v1, float& v2, float& v3)
+{
+    w ^= 0x80808080u;
+    v0 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440)) - 8388736.f) * scale;
+    v1 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7441)) - 8388736.f) * scale;
+    v2 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7442)) - 8388736.f) * scale;
+    v3 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7443)) - 8388736.f) * scale;
+}
+
+__device__ __forceinline__ uint32_t group_codes(float v0, float v1, float v2, float v3, float inverse)
+{
+    const uint32_t b0 = __float_as_uint(__fmaf_rn(v0, inverse, 12582912.f)), b1 = __float_as_uint(__fmaf_rn(v1, inverse, 12582912.f));
+    const uint32_t b2 = __float_as_uint(__fmaf_rn(v2, inverse, 12582912.f)), b3 = __float_as_uint(__fmaf_rn(v3, inverse, 12582912.f));
+    const uint32_t w = __byte_perm(__byte_perm(b0, b1, 0x0040), __byte_perm(b2, b3, 0x0040), 0x5410);
+    return inverse == 0.f ? 0u : w;
+}
+
 // A restored value in the type of its activations.  A maximum close to the type's largest
 // number can round up to a code past it (64 * 2^122, 64 * 2^10): that saturates.
 template <typename T> struct Largest;
@@ -118,10 +136,65 @@ template <> struct Largest<__nv_bfloat16> { static constexpr float value = 3.389
 template <> struct Largest<__half> { static constexpr float value = 65504.f; };
 
 template <typename T>
-__device__ __forceinline__ T restored(float v)
+__device__ __forceinline__ float saturated(float v)
 {
-    if (fabsf(v) > Largest<T>::value) v = copysignf(Largest<T>::value, v);      // NaN compares false
-    return from_float<T>(v);
+    return fabsf(v) > Largest<T>::value ? copysignf(Largest<T>::value, v) : v;      // NaN compares false
 }
+
+// groups whose exponent byte is below this cannot pass the largest number: 128 * 2^e
+template <typename T> constexpr uint32_t kSaturates = std::is_same_v<T, __half> ? 127 + 9 : 127 + 121;
+
+// ---- 32-byte accesses ---------------------------------------------------------------
+__device__ __forceinline__ void load_32b(const void* p, uint32_t (&w)[8])
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p) : "memory");
+}
+
+__device__ __forceinline__ void store_32b(void* p, const uint32_t (&w)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack(uint32_t w, float& lo, float& hi)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        lo = __uint_as_float(w << 16);
+        hi = __uint_as_float(w & 0xFFFF0000u);
+    } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        lo = f.x;
+        hi = f.y;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack(float lo, float hi)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+
+struct CheckpointView {
+    int8_t* codes;
+    uint64_t codes_stride;
+    uint8_t* exps;
+    uint64_t exps_stride;
+};
+
+// ---- launches that overlap ----------------------------------------------------------
+// These kernels are launched before the stream's previous kernel has ended.  Each one waits
+// for it (and for its memory) before it touches global memory, and lets the next one start.
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dependency_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 }  // namespace eden
