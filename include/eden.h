@@ -368,6 +368,19 @@ int eden_force_generic_kernels(eden_ctx* ctx, int on);
                                      the context's stream, which waits for them where it needs them; 0: in line */
 #define EDEN_OPT_SLAB_STREAMS 5   /* 1 (default)..4: slabs are dealt round-robin to this many streams, so that
                                      one slab's second pass can overlap the next slab's first */
+/*   EDEN_OPT_LINEAR_FORM   EDEN_LINEAR_AUTO (default): the linear products choose their kernel by
+ *                          size; else that form wherever it can run (EDEN_LINEAR_FEW: up to 32
+ *                          tokens of eden_linear that save nothing).
+ *   EDEN_OPT_LINEAR_SPLITS 0 (default): by size; 1, 2, 4 or 8: parts that a tile's sum is cut
+ *                          into (at most one for each 64 of its length, and blocks of at most
+ *                          eight SMs). */
+#define EDEN_OPT_LINEAR_FORM   9
+#define EDEN_OPT_LINEAR_SPLITS 10
+#define EDEN_LINEAR_AUTO   0
+#define EDEN_LINEAR_PAIR   1   /* tiles of 256 x 256 on pairs of SMs */
+#define EDEN_LINEAR_SINGLE 2   /* tiles of 128 x 128 */
+#define EDEN_LINEAR_NARROW 3   /* tiles of 128 x 64 */
+#define EDEN_LINEAR_FEW    4   /* few tokens: weights straight to registers */
 int eden_set_option(eden_ctx* ctx, int option, int value);
 
 /* Host only, no GPU: the band of 32-bit keys [*lo, *hi] in which form 1 of the mask

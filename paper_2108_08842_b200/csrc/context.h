@@ -45,6 +45,8 @@ struct eden_ctx {
     int slab_sides;                  // bit 0: the sender uses the slab order, bit 1: the receiver
     std::vector<cudaStream_t> side;  // side streams of the slab order
     std::vector<cudaEvent_t> slab_events;   // fork (0) and join (1 + stream) events of the slab order
+    int linear_form;                 // EDEN_OPT_LINEAR_FORM
+    int linear_splits;               // EDEN_OPT_LINEAR_SPLITS
     int sm_count;
     std::vector<ProfileRecord> records;
     std::vector<std::pair<cudaEvent_t, cudaEvent_t>> event_pool;

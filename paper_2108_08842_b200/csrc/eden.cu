@@ -368,6 +368,8 @@ extern "C" int eden_create(eden_ctx** out, int cuda_device, void* cuda_stream,
     ctx->slab_mib = 0;
     ctx->slab_streams = 1;
     ctx->slab_sides = 3;
+    ctx->linear_form = EDEN_LINEAR_AUTO;
+    ctx->linear_splits = 0;
     ctx->sm_count = 0;
     if (cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, cuda_device) != cudaSuccess ||
         ctx->sm_count <= 0) {
@@ -456,6 +458,14 @@ extern "C" int eden_set_option(eden_ctx* ctx, int option, int value)
         case EDEN_OPT_SLAB_STREAMS:
             if (value < 1 || value > 4) return EDEN_ERR_INVALID_ARG;
             ctx->slab_streams = value;
+            return EDEN_OK;
+        case EDEN_OPT_LINEAR_FORM:
+            if (value < EDEN_LINEAR_AUTO || value > EDEN_LINEAR_FEW) return EDEN_ERR_INVALID_ARG;
+            ctx->linear_form = value;
+            return EDEN_OK;
+        case EDEN_OPT_LINEAR_SPLITS:
+            if (value != 0 && value != 1 && value != 2 && value != 4 && value != 8) return EDEN_ERR_INVALID_ARG;
+            ctx->linear_splits = value;
             return EDEN_OK;
         default:
             return EDEN_ERR_INVALID_ARG;

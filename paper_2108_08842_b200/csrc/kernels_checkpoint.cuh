@@ -74,7 +74,7 @@ __device__ __forceinline__ uint4 load_codes(const int8_t* p, int count)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save_wide(const T* __restrict__ x, uint64_t x_stride, CheckpointView c,
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save_wide(const T* x, uint64_t x_stride, CheckpointView c,
                                                                       uint32_t n, uint32_t halves, uint64_t total)
 {
     dependency_wait();
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save_wide(const T* 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore_wide(T* __restrict__ x, uint64_t x_stride, CheckpointView c,
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore_wide(T* x, uint64_t x_stride, CheckpointView c,
                                                                          uint32_t n, uint32_t halves, uint64_t total)
 {
     dependency_wait();
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore_wide(T* __r
 // and leaves the run's column sums in partial[run][n].
 template <typename T, int ACT>
 __global__ void __launch_bounds__(kCkptThreads) k_act_backward_wide(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
-                                                                   uint64_t dz_stride, float* __restrict__ partial, uint32_t m, uint32_t n,
+                                                                   uint64_t dz_stride, float* partial, uint32_t m, uint32_t n,
                                                                    uint32_t rows_per_run)
 {
     dependency_wait();
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_act_backward_wide(const T* dy,
 constexpr int kGroupsInFlight = 4;
 
 template <typename T>
-__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* __restrict__ x, uint64_t x_stride, CheckpointView c, uint64_t n,
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* x, uint64_t x_stride, CheckpointView c, uint64_t n,
                                                                  uint32_t groups, uint64_t total)
 {
     dependency_wait();
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* __res
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* __restrict__ x, uint64_t x_stride, CheckpointView c, uint64_t n,
+__global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* x, uint64_t x_stride, CheckpointView c, uint64_t n,
                                                                     uint32_t groups, uint64_t total)
 {
     dependency_wait();
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* __restri
 // leaves the run's column sums in partial[run][n].
 template <typename T, int ACT>
 __global__ void __launch_bounds__(kCkptThreads) k_act_backward(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
-                                                              uint64_t dz_stride, float* __restrict__ partial, uint32_t m, uint32_t n,
+                                                              uint64_t dz_stride, float* partial, uint32_t m, uint32_t n,
                                                               uint32_t rows_per_run)
 {
     dependency_wait();
@@ -283,8 +283,8 @@ __global__ void __launch_bounds__(kCkptThreads) k_act_backward(const T* dy, uint
 
 // out[n] (+)= the sum of partial's rows: 32 columns per block, each warp every eighth row,
 // the eight added in order
-__global__ void __launch_bounds__(kCkptThreads) k_column_sum(const float* __restrict__ partial, uint64_t rows, uint64_t n,
-                                                            float* __restrict__ out, int accumulate)
+__global__ void __launch_bounds__(kCkptThreads) k_column_sum(const float* partial, uint64_t rows, uint64_t n,
+                                                            float* out, int accumulate)
 {
     dependency_wait();
     dependency_release();

@@ -196,6 +196,7 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row, ui
 struct TileGrid {
     uint32_t rows, cols, count;        // tiles
     uint32_t depth_steps;              // steps of 64 along the sum
+    uint32_t splits;                   // parts of the sum, one block (pair) of a cluster each
 };
 
 constexpr uint32_t kBand = 8;
@@ -227,10 +228,13 @@ constexpr int kLinearThreads = 384;    // copies, products, tensor memory, one s
 //            of the next tile fill the other half of tensor memory
 // CG = 2: the blocks of a pair hold 128 rows of A and half of the rows of B each; the first
 // one's barriers count both blocks' bytes, and its products write both blocks' sums.
-template <int OP, typename T, int CG, int BN>
+// SPLIT: one tile per cluster.  Its blocks (pairs) take a part of the sum each, leave their
+// sums in shared memory, and then every block joins and finishes a share of the tile's 32 x 32
+// pieces, adding the parts in their order.
+template <int OP, typename T, int CG, int BN, bool SPLIT>
 __global__ void __launch_bounds__(kLinearThreads, 1)
 k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, LinearEpilogue p, TileGrid grid,
-         uint32_t* __restrict__ status)
+         uint32_t* status)
 {
     using S = LinearShape<CG, BN>;
     constexpr bool a_mn = OP == kWeightGrad, b_mn = OP != kForward;
@@ -241,7 +245,11 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + 8 * S::kStages;
     const uint32_t sums_full = empty + 8 * S::kStages, sums_empty = sums_full + 16, drained = sums_empty + 16, slot = drained + 8;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0, first = blockIdx.x / CG, step = gridDim.x / CG;
+    const uint32_t in_cluster = CG == 2 || SPLIT ? cluster_rank() : 0, rank = in_cluster % CG, leader = in_cluster - rank;
+    const uint32_t splits = SPLIT ? grid.splits : 1, part = in_cluster / CG;
+    const uint32_t first = blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
+    const uint32_t depth_begin = (uint32_t)((uint64_t)grid.depth_steps * part / splits);
+    const uint32_t depth_end = (uint32_t)((uint64_t)grid.depth_steps * (part + 1) / splits);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
@@ -259,7 +267,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     }
     if (warp == 2) tmem_alloc<CG>(slot, S::kColumns);
     tmem_fence_before();
-    if constexpr (CG == 2) cluster_arrive_wait(); else __syncthreads();
+    if constexpr (CG == 2 || SPLIT) cluster_arrive_wait(); else __syncthreads();
     tmem_fence_after();
     dependency_wait();
     dependency_release();
@@ -274,10 +282,10 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 uint32_t tile_row, tile_col;
                 tile_at(grid, t, tile_row, tile_col);
                 const int row = (int)(tile_row * 128 * CG + rank * 128), col = (int)(tile_col * BN + rank * S::kRowsB);
-                for (uint32_t d = 0; d < grid.depth_steps; ++d, ++n) {
+                for (uint32_t d = depth_begin; d < depth_end; ++d, ++n) {
                     const uint32_t s = n % S::kStages;
                     if (!(ok = barrier_wait(empty + 8 * s, (n / S::kStages & 1) ^ 1))) break;
-                    const uint32_t bar = CG == 2 ? address_in(full + 8 * s, 0) : full + 8 * s;
+                    const uint32_t bar = CG == 2 ? address_in(full + 8 * s, leader) : full + 8 * s;
                     if (rank == 0) barrier_expect(full + 8 * s, CG * S::kStageBytes);
                     const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
                     const int depth = (int)d * 64;
@@ -306,7 +314,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 const uint32_t half = done & 1, d_address = sums + half * BN;
                 if (!(ok = barrier_wait(sums_empty + 8 * half, (done / 2 & 1) ^ 1))) break;
                 tmem_fence_after();
-                for (uint32_t d = 0; d < grid.depth_steps; ++d, ++n) {
+                for (uint32_t d = depth_begin; d < depth_end; ++d, ++n) {
                     const uint32_t s = n % S::kStages;
                     if (!(ok = barrier_wait(full + 8 * s, n / S::kStages & 1))) break;
                     tmem_fence_after();
@@ -314,13 +322,13 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         tile_product<CG>(d_address, tile_descriptor(a + k * (a_mn ? 2048 : 32), 8192, 1024),
-                                         tile_descriptor(b + k * (b_mn ? 2048 : 32), 8192, 1024), descriptor, d > 0 || k > 0);
-                    tile_commit<CG>(empty + 8 * s);
+                                         tile_descriptor(b + k * (b_mn ? 2048 : 32), 8192, 1024), descriptor, d > depth_begin || k > 0);
+                    tile_commit<CG>(empty + 8 * s, leader);
                 }
-                if (ok) tile_commit<CG>(sums_full + 8 * half);
+                if (ok) tile_commit<CG>(sums_full + 8 * half, leader);
             }
             if (!ok) {
-                tile_commit<CG>(drained);
+                tile_commit<CG>(drained, leader);
                 barrier_wait(drained, 0);
             }
         }
@@ -341,25 +349,156 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 float v[32];
                 __syncwarp();
                 tmem_load(sums + ((uint32_t)quarter * 32 << 16) + half * BN + in_tile, v);
-                if (c == BN / 64 - 1) {
-                    tmem_fence_before();
-                    __syncwarp();
-                    if (lane == 0) barrier_arrive_remote(CG == 2 ? address_in(sums_empty + 8 * half, 0) : sums_empty + 8 * half);
+                if constexpr (SPLIT) {
+                    // [column][row], over the stages: every product that read them is done
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) shared_store(base + ((in_tile + j) * 128 + quarter * 32 + lane) * 4, v[j]);
+                } else {
+                    if (c == BN / 64 - 1) {
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive_remote(CG == 2 ? address_in(sums_empty + 8 * half, leader) : sums_empty + 8 * half);
+                    }
+                    if (col0 < p.cols) linear_epilogue<OP, T>(v, row, col0, p);
                 }
-                if (col0 < p.cols) linear_epilogue<OP, T>(v, row, col0, p);
             }
         }
+    }
+    __syncwarp();
+    if constexpr (SPLIT) {
+        cluster_arrive_wait();
+        if (warp >= 4) {
+            uint32_t tile_row, tile_col;
+            tile_at(grid, first, tile_row, tile_col);
+            for (uint32_t unit = part + splits * (warp - 4); unit < BN / 8; unit += splits * 8) {
+                const uint32_t quarter = unit % 4, in_tile = unit / 4 * 32;
+                const uint64_t row = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32 + lane, col0 = (uint64_t)tile_col * BN + in_tile;
+                if (col0 >= p.cols) continue;
+                float v[32];
+                for (uint32_t i = 0; i < splits; ++i) {
+                    const uint32_t from = address_in(base, i * CG + rank) + (in_tile * 128 + quarter * 32 + lane) * 4;
+                    float w[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) w[j] = cluster_load(from + j * 512);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = i == 0 ? w[j] : v[j] + w[j];
+                }
+                linear_epilogue<OP, T>(v, row, col0, p);
+            }
+        }
+        __syncwarp();
     }
     if (!ok) atomicOr(status, EDEN_STATUS_TIMEOUT);
     __syncwarp();
     tmem_fence_before();
-    if constexpr (CG == 2) cluster_arrive_wait(); else __syncthreads();
+    if constexpr (CG == 2 || SPLIT) cluster_arrive_wait(); else __syncthreads();
     tmem_fence_after();
     if (warp == 2) tmem_free<CG>(sums, S::kColumns);
 }
 
+// ---- few tokens ---------------------------------------------------------------------
+// y [m, n] for m <= 8 * NT: every weight is read once and used m times, so reading W is all
+// that takes time.  A block takes 16 rows of W; its 16 warps take steps of 64 along the sum in
+// turn, all loads of up to four steps on their way together, straight to registers in the
+// layout of the 16 x 8 x 16 product: the sum's index may be permuted alike in W and in x, so
+// each lane loads 16 consecutive bytes and feeds them as the fragments of two products.  The
+// 16 warps' sums are added in their order.
+constexpr int kFewThreads = 512;
+
+// 8 values at p, of which the first `count` exist
+template <bool VEC, typename T>
+__device__ __forceinline__ uint4 load_8(const T* p, int count)
+{
+    if constexpr (VEC) {                       // count is 8 or 0
+        return count > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = 2 * i < count ? ((const uint16_t*)p)[2 * i] : 0, hi = 2 * i + 1 < count ? ((const uint16_t*)p)[2 * i + 1] : 0;
+            w[i] = lo | hi << 16;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void few_product(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <typename T, int NT, bool VEC>
+__global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t x_stride, const T* w,
+                                                           uint64_t w_stride, uint32_t k, LinearEpilogue p)
+{
+    constexpr int kWarps = kFewThreads / 32, kAhead = NT == 1 ? 4 : 2;
+    dependency_wait();
+    dependency_release();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    const uint64_t n0 = (uint64_t)blockIdx.x * 16;
+    const uint64_t r0 = min(n0 + g, p.cols - 1), r1 = min(n0 + g + 8, p.cols - 1);     // past the end: any row, its sums are dropped
+    const T *w0 = w + r0 * w_stride, *w1 = w + r1 * w_stride;
+    float c[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
+
+    for (uint32_t k0 = warp * 64; k0 < k; k0 += kWarps * 64 * kAhead) {
+        uint4 a[kAhead][2][2], b[kAhead][NT][2];
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t at = k0 + s * kWarps * 64 + h * 32 + t * 8;
+                const int count = at < k ? (int)min(k - at, 8u) : 0;
+                a[s][h][0] = load_8<VEC>(w0 + at, count);
+                a[s][h][1] = load_8<VEC>(w1 + at, count);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const uint32_t token = i * 8 + g;
+                    b[s][i][h] = token < p.rows ? load_8<VEC>(x + token * x_stride + at, count) : make_uint4(0, 0, 0, 0);
+                }
+            }
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const uint4 u = a[s][h][0], v = a[s][h][1], z = b[s][i][h];
+                    few_product<T>(c[i], u.x, v.x, u.y, v.y, z.x, z.y);
+                    few_product<T>(c[i], u.z, v.z, u.w, v.w, z.z, z.w);
+                }
+    }
+    __shared__ float sums[kWarps][8 * NT][16 + 1];                 // [warp][token][row of W]
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        sums[warp][i * 8 + 2 * t][g] = c[i][0];
+        sums[warp][i * 8 + 2 * t + 1][g] = c[i][1];
+        sums[warp][i * 8 + 2 * t][g + 8] = c[i][2];
+        sums[warp][i * 8 + 2 * t + 1][g + 8] = c[i][3];
+    }
+    __syncthreads();
+    if (threadIdx.x >= 128 * NT) return;
+    const uint32_t token = threadIdx.x / 16, in = threadIdx.x % 16;
+    const uint64_t col = n0 + in;
+    if (token >= p.rows || col >= p.cols) return;
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) v += sums[i][token][in];
+    if (p.bias) v += to_float(((const T*)p.bias)[col]);
+    with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
+    if (p.residual) v += to_float(((const T*)p.residual)[token * p.residual_stride + col]);
+    ((T*)p.out)[token * p.out_stride + col] = from_float<T>(v);
+}
+
 // Copies rows of 16-bit values to rows of `stride` values (a multiple of 8) on a 16-byte boundary.
-__global__ void __launch_bounds__(256) k_align_rows(const uint16_t* __restrict__ from, uint64_t from_stride, uint16_t* __restrict__ to,
+__global__ void __launch_bounds__(256) k_align_rows(const uint16_t* from, uint64_t from_stride, uint16_t* to,
                                                    uint64_t stride, uint64_t n, uint64_t total)
 {
     dependency_wait();

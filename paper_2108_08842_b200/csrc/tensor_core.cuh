@@ -159,16 +159,30 @@ __device__ __forceinline__ void tile_product(uint32_t d, uint64_t a, uint64_t b,
                      ::"r"(d), "l"(a), "l"(b), "r"(descriptor), "r"((uint32_t)add) : "memory");
 }
 
-// an arrival on `bar` (with CG = 2 on both blocks' barriers at that address) when the
-// products issued so far are done
+// an arrival on `bar` (with CG = 2 on the barrier at that address in both blocks of the pair
+// that starts at rank `leader`) when the products issued so far are done
 template <int CG>
-__device__ __forceinline__ void tile_commit(uint32_t bar)
+__device__ __forceinline__ void tile_commit(uint32_t bar, uint32_t leader)
 {
     if constexpr (CG == 2)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+                     ::"r"(bar), "h"((uint16_t)(3u << leader)) : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// ---- shared memory by address -------------------------------------------------------
+__device__ __forceinline__ void shared_store(uint32_t address, float v)
+{
+    asm volatile("st.shared.f32 [%0], %1;" ::"r"(address), "f"(v) : "memory");
+}
+
+// address in the cluster's window (address_in)
+__device__ __forceinline__ float cluster_load(uint32_t address)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(address));
+    return v;
 }
 
 }  // namespace eden

@@ -222,44 +222,108 @@ int make_map(CUtensorMap* map, int type, const Operand& o, uint32_t box_rows)
     return rc == CUDA_SUCCESS ? EDEN_OK : EDEN_ERR_CUDA;
 }
 
-template <int OP, typename T, int CG, int BN>
-int launch_linear(eden_ctx* ctx, const char* name, int type, const Operand& a, const Operand& b, uint64_t depth, const LinearEpilogue& p,
-                  double bytes)
+struct Product {
+    const char* name;
+    int type;
+    Operand a, b;                      // rows of the result (weight grad: steps of the sum), columns likewise
+    uint64_t depth;                    // length of the sum
+    LinearEpilogue p;
+    double bytes;
+};
+
+template <int OP, typename T, int CG, int BN, bool SPLIT>
+int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
 {
     using S = LinearShape<CG, BN>;
     CUtensorMap map_a, map_b;
-    if (int rc = make_map(&map_a, type, a, OP == kWeightGrad ? 64 : 128)) return rc;
-    if (int rc = make_map(&map_b, type, b, OP == kForward ? S::kRowsB : 64)) return rc;
-    const uint64_t rows = (p.rows + 128 * CG - 1) / (128 * CG), cols = (p.cols + BN - 1) / BN;
-    if (rows * cols > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((depth + 63) / 64)};
-    const auto kernel = k_linear<OP, T, CG, BN>;
+    if (int rc = make_map(&map_a, q.type, q.a, OP == kWeightGrad ? 64 : 128)) return rc;
+    if (int rc = make_map(&map_b, q.type, q.b, OP == kForward ? S::kRowsB : 64)) return rc;
+    const uint64_t rows = (q.p.rows + 128 * CG - 1) / (128 * CG), cols = (q.p.cols + BN - 1) / BN;
+    if (rows * cols * CG * splits > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((q.depth + 63) / 64), splits};
+    const auto kernel = k_linear<OP, T, CG, BN, SPLIT>;
     CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
-    const uint32_t blocks = (uint32_t)std::min<uint64_t>(rows * cols, ctx->sm_count / CG) * CG;
-    return launch(ctx, name, bytes, kernel, dim3(blocks), kLinearThreads, S::kSharedBytes, CG, map_a, map_b, p, grid, (uint32_t*)ctx->ws);
+    const uint32_t groups = (uint32_t)(SPLIT ? rows * cols : std::min<uint64_t>(rows * cols, ctx->sm_count / CG));
+    return launch(ctx, q.name, q.bytes, kernel, dim3(groups * CG * splits), kLinearThreads, S::kSharedBytes, CG * splits, map_a, map_b, q.p,
+                  grid, (uint32_t*)ctx->ws);
 }
 
-// a: rows of the result (weight grad: steps of the sum) x ..., b: columns likewise
-template <int OP>
-int product(eden_ctx* ctx, Scratch& scratch, const char* name, int type, Operand a, Operand b, uint64_t depth, LinearEpilogue p, double bytes)
+template <int OP, int CG, int BN>
+int launch_tiles(eden_ctx* ctx, const Product& q, uint32_t splits)
 {
-    if (int rc = align_operand(ctx, scratch, a)) return rc;
-    if (int rc = align_operand(ctx, scratch, b)) return rc;
+    if (splits > 1) {
+        EDEN_DISPATCH_HALF(q.type, return (launch_linear<OP, T_, CG, BN, true>(ctx, q, splits)));
+    } else {
+        EDEN_DISPATCH_HALF(q.type, return (launch_linear<OP, T_, CG, BN, false>(ctx, q, 1)));
+    }
+}
+
+template <typename T, int NT>
+int launch_few(eden_ctx* ctx, const Product& q)
+{
+    const bool vec = aligned(q.a.data, 16) && aligned(q.b.data, 16) && q.depth % 8 == 0 && (q.a.stride % 8 == 0 || q.a.rows == 1) &&
+                     (q.b.stride % 8 == 0 || q.b.rows == 1);
+    return launch(ctx, q.name, q.bytes, vec ? k_linear_few<T, NT, true> : k_linear_few<T, NT, false>, dim3((uint32_t)((q.p.cols + 15) / 16)),
+                  kFewThreads, 0, 1, (const T*)q.a.data, q.a.stride, (const T*)q.b.data, q.b.stride, q.depth, q.p);
+}
+
+// How a product is cut up: a form (EDEN_LINEAR_*) and the parts of each tile's sum.
+struct Cut {
+    int form;
+    uint32_t splits;
+};
+
+template <int OP>
+Cut choose_cut(const eden_ctx* ctx, const Product& q)
+{
+    const uint64_t steps = (q.depth + 63) / 64;
+    const int form = ctx->linear_form;
+    if (OP == kForward && q.p.save == EDEN_SAVE_NONE && (form == EDEN_LINEAR_AUTO ? q.p.rows <= 16 : form == EDEN_LINEAR_FEW && q.p.rows <= 32))
+        return {EDEN_LINEAR_FEW, 1};
+    struct { int form; uint64_t rows, cols, blocks; double step; } tiles[] = {{EDEN_LINEAR_PAIR, 256, 256, 2, 560.},
+                                                                             {EDEN_LINEAR_SINGLE, 128, 128, 1, 380.},
+                                                                             {EDEN_LINEAR_NARROW, 128, 64, 1, 260.}};
+    Cut best{EDEN_LINEAR_PAIR, 1};
+    double least = 1e300;
+    for (const auto& t : tiles) {
+        if (form != EDEN_LINEAR_AUTO && form != EDEN_LINEAR_FEW && form != t.form) continue;
+        const uint64_t count = (q.p.rows + t.rows - 1) / t.rows * ((q.p.cols + t.cols - 1) / t.cols), slots = ctx->sm_count / t.blocks;
+        for (uint64_t splits = 1; splits * t.blocks <= 8 && splits <= steps; splits *= 2) {
+            if (ctx->linear_splits && (int)splits != ctx->linear_splits && (int)splits * 2 <= ctx->linear_splits && splits * 2 * t.blocks <= 8 && splits * 2 <= steps) continue;
+            if (ctx->linear_splits && (int)splits > ctx->linear_splits) break;
+            const double waves = (double)((count * splits + slots - 1) / slots);
+            const double cost = waves * ((double)(steps + splits - 1) / splits * t.step + (splits > 1 ? 2000. : 0.));
+            if (cost < least) {
+                least = cost;
+                best = {t.form, (uint32_t)splits};
+            }
+        }
+    }
+    return best;
+}
+
+template <int OP>
+int product(eden_ctx* ctx, Scratch& scratch, Product q)
+{
+    const Cut cut = choose_cut<OP>(ctx, q);
+    if constexpr (OP == kForward) {
+        if (cut.form == EDEN_LINEAR_FEW) {
+            if (q.p.rows <= 8) { EDEN_DISPATCH_HALF(q.type, return (launch_few<T_, 1>(ctx, q))); }
+            if (q.p.rows <= 16) { EDEN_DISPATCH_HALF(q.type, return (launch_few<T_, 2>(ctx, q))); }
+            EDEN_DISPATCH_HALF(q.type, return (launch_few<T_, 4>(ctx, q)));
+        }
+    }
+    if (int rc = align_operand(ctx, scratch, q.a)) return rc;
+    if (int rc = align_operand(ctx, scratch, q.b)) return rc;
+    LinearEpilogue& p = q.p;
     p.wide = (wide_rows(p.out, p.out_stride, OP == kWeightGrad ? 4 : 2) ? kWideOut : 0) |
              (wide_rows(p.residual, p.residual_stride, 2) ? kWideResidual : 0) |
              (wide_rows(p.ckpt.codes, p.ckpt.codes_stride, 1) ? kWideCodes : 0) | (aligned(p.bias, 32) ? kWideBias : 0);
-    const auto waves = [&](uint64_t tile_rows, uint64_t tile_cols, uint64_t slots) {
-        return ((p.rows + tile_rows - 1) / tile_rows * ((p.cols + tile_cols - 1) / tile_cols) + slots - 1) / slots;
-    };
-    const double pair = 1.0 * waves(256, 256, ctx->sm_count / 2), one = 0.65 * waves(128, 128, ctx->sm_count),
-                 narrow = 0.45 * waves(128, 64, ctx->sm_count);
-    if (pair <= one && pair <= narrow) {
-        EDEN_DISPATCH_HALF(type, return (launch_linear<OP, T_, 2, 256>(ctx, name, type, a, b, depth, p, bytes)));
+    switch (cut.form) {
+        case EDEN_LINEAR_PAIR: return launch_tiles<OP, 2, 256>(ctx, q, cut.splits);
+        case EDEN_LINEAR_SINGLE: return launch_tiles<OP, 1, 128>(ctx, q, cut.splits);
+        default: return launch_tiles<OP, 1, 64>(ctx, q, cut.splits);
     }
-    if (one <= narrow) {
-        EDEN_DISPATCH_HALF(type, return (launch_linear<OP, T_, 1, 128>(ctx, name, type, a, b, depth, p, bytes)));
-    }
-    EDEN_DISPATCH_HALF(type, return (launch_linear<OP, T_, 1, 64>(ctx, name, type, a, b, depth, p, bytes)));
 }
 
 // Nothing throws across the C boundary: the launch records grow a vector while profiling.
@@ -307,8 +371,8 @@ extern "C" int eden_linear(eden_ctx* ctx, const eden_linear_args* a)
                          view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride), nullptr, a->m, a->n, a->act, a->save, 0, 0};
         const double bytes = 2.0 * ((double)a->m * a->k + (double)a->n * a->k + a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
                              (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
-        return product<kForward>(ctx, scratch, "t_linear", a->type, {a->x, a->x_stride, a->m, a->k}, {a->weight, a->weight_stride, a->n, a->k},
-                                 a->k, p, bytes);
+        return product<kForward>(ctx, scratch, {"t_linear", a->type, {a->x, a->x_stride, a->m, a->k}, {a->weight, a->weight_stride, a->n, a->k},
+                                                a->k, p, bytes});
     });
 }
 
@@ -398,8 +462,8 @@ extern "C" int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_gra
                              view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0, 0};
             const double bytes = 2.0 * ((double)a->m * a->n + (double)a->n * a->k + (double)a->m * a->k * (a->residual ? 2 : 1)) +
                                  (a->act ? (double)a->m * (a->k + groups_of(a->k)) : 0.0);
-            if (int rc = product<kInputGrad>(ctx, scratch, "t_input_grad", a->type, {a->dz, a->dz_stride, a->m, a->n},
-                                             {a->weight, a->weight_stride, a->n, a->k}, a->n, p, bytes))
+            if (int rc = product<kInputGrad>(ctx, scratch, {"t_input_grad", a->type, {a->dz, a->dz_stride, a->m, a->n},
+                                                            {a->weight, a->weight_stride, a->n, a->k}, a->n, p, bytes}))
                 return rc;
         }
         return a->bias_grad ? sum_columns(ctx, partial, runs, a->k, a->bias_grad, a->accumulate) : EDEN_OK;
@@ -437,6 +501,6 @@ extern "C" int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_g
         LinearEpilogue p{nullptr, nullptr, 0, a->weight_grad, a->weight_grad_stride, {}, nullptr, a->n, a->k, 0, 0, a->accumulate, 0};
         const double bytes = 2.0 * a->m * a->n + (double)a->m * (a->codes ? a->k + groups_of(a->k) : 2 * a->k) +
                              4.0 * a->n * a->k * (a->accumulate ? 2 : 1);
-        return product<kWeightGrad>(ctx, scratch, "t_weight_grad", a->type, {a->dz, a->dz_stride, a->m, a->n}, x, a->m, p, bytes);
+        return product<kWeightGrad>(ctx, scratch, {"t_weight_grad", a->type, {a->dz, a->dz_stride, a->m, a->n}, x, a->m, p, bytes});
     });
 }

@@ -194,6 +194,8 @@ struct CheckpointView {
 // ---- launches that overlap ----------------------------------------------------------
 // These kernels are launched before the stream's previous kernel has ended.  Each one waits
 // for it (and for its memory) before it touches global memory, and lets the next one start.
+// What they read may be written while they already run, so no pointer is __restrict__: that
+// would allow loads through the read-only path, which assumes constant data.
 __device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dependency_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -93,6 +93,8 @@ _sig("eden_profile_get", _int, [_vp, _u32, ctypes.POINTER(ctypes.c_char_p), ctyp
 
 STATUS_ZERO_VECTOR, STATUS_NONFINITE, STATUS_NO_DATA, STATUS_TIMEOUT, STATUS_SCRATCH = 1, 2, 4, 8, 16
 OPT_PLAN_VARIANT, OPT_ROW_STAGING, OPT_SEL_ROUNDS, OPT_SLAB_MIB, OPT_SLAB_STREAMS, OPT_SLAB_SIDES, OPT_SEL_BAND, OPT_SEL_AHEAD = 1, 2, 3, 4, 5, 6, 7, 8
+OPT_LINEAR_FORM, OPT_LINEAR_SPLITS = 9, 10
+LINEAR_AUTO, LINEAR_PAIR, LINEAR_SINGLE, LINEAR_NARROW, LINEAR_FEW = range(5)
 PACKET_COORDS = 1024
 UNIFORM_MAX_INDEX = 127
 UNIFORM_MIN_DELTA = 0.0625

@@ -202,6 +202,38 @@ def test_linear_of_no_tokens(ctx):
     assert ctx.checkpoint_restore(ctx.checkpoint_save(normal(1, 0, 5)), torch.float32).shape == (0, 5)
 
 
+FORMS = [(f, s) for f in ("LINEAR_PAIR", "LINEAR_SINGLE", "LINEAR_NARROW") for s in (1, 2, 4, 8)]
+
+
+@pytest.fixture
+def forced(ctx, request):
+    from paper_2108_08842_b200 import eden
+
+    form, splits = request.param
+    ctx.set_option(eden.OPT_LINEAR_FORM, getattr(eden, form))
+    ctx.set_option(eden.OPT_LINEAR_SPLITS, splits)
+    yield request.param
+    ctx.set_option(eden.OPT_LINEAR_FORM, eden.LINEAR_AUTO)
+    ctx.set_option(eden.OPT_LINEAR_SPLITS, 0)
+
+
+@pytest.mark.parametrize("forced", FORMS, indirect=True)
+def test_every_form_at_every_size(ctx, forced):
+    """Each kernel form, with each number of parts, on sizes that the choice would give another."""
+    for m, n, k in ((1, 40, 72), (200, 300, 1000), (520, 264, 64), (300, 700, 520)):
+        check_linear(ctx, torch.bfloat16, m, n, k, "silu", True, True, "pre", seed=m)
+        check_input_grad(ctx, torch.float16, m, n, k, "gelu", True)
+        check_weight_grad(ctx, torch.bfloat16, m, n, k, True)
+    check_linear(ctx, torch.float16, 150, 333, 777, "relu", True, True, "out", 3, 1)
+    check_weight_grad(ctx, torch.float16, 1111, 130, 270, False, 1, 1)
+
+
+@pytest.mark.parametrize("forced", [("LINEAR_FEW", 0)], indirect=True)
+@pytest.mark.parametrize("m,n,k,extra,offset", [(17, 100, 1000, 0, 0), (24, 33, 4104, 8, 8), (31, 64, 200, 1, 1), (32, 16, 5000, 0, 0), (33, 64, 64, 0, 0)])
+def test_few_tokens_form(ctx, forced, m, n, k, extra, offset):
+    check_linear(ctx, torch.bfloat16, m, n, k, "gelu_tanh", True, True, "none", extra, offset)
+
+
 # ------------------------------------------------------------------------------- backward
 def pre_of(seed, m, n):
     codes, exps = R.code(R.f64(normal(seed, m, n, std=2.0)))
