@@ -47,6 +47,7 @@ struct eden_ctx {
     std::vector<cudaEvent_t> slab_events;   // fork (0) and join (1 + stream) events of the slab order
     int linear_form;                 // EDEN_OPT_LINEAR_FORM
     int linear_splits;               // EDEN_OPT_LINEAR_SPLITS
+    int cluster_slots[9];            // clusters of 1, 2, 4, 8 blocks that run at once; 0: not asked yet
     int sm_count;
     std::vector<ProfileRecord> records;
     std::vector<std::pair<cudaEvent_t, cudaEvent_t>> event_pool;

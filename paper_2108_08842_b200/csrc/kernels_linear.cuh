@@ -222,8 +222,8 @@ struct LinearShape {
 constexpr int kLinearThreads = 384;    // copies, products, tensor memory, one spare, eight epilogue warps
 
 // D = A B^T for tiles of 128 * CG x BN, persistent: block (pair) c takes tiles c, c + blocks, ...
-//   warp 0   one lane fills the stages with tensor copies, kStages ahead of the products
-//   warp 1   one lane (of the pair's first block) issues the products
+//   warp 0   fills the stages with tensor copies, kStages ahead of the products
+//   warp 1   (of the pair's first block) issues the products
 //   warps 4+ read finished sums from tensor memory and run the epilogue, while the products
 //            of the next tile fill the other half of tensor memory
 // CG = 2: the blocks of a pair hold 128 rows of A and half of the rows of B each; the first
@@ -276,15 +276,14 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 
     bool ok = true;
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t n = 0;            // steps issued
-            for (uint32_t t = first; t < grid.count && ok; t += step) {
-                uint32_t tile_row, tile_col;
-                tile_at(grid, t, tile_row, tile_col);
-                const int row = (int)(tile_row * 128 * CG + rank * 128), col = (int)(tile_col * BN + rank * S::kRowsB);
-                for (uint32_t d = depth_begin; d < depth_end; ++d, ++n) {
-                    const uint32_t s = n % S::kStages;
-                    if (!(ok = barrier_wait(empty + 8 * s, (n / S::kStages & 1) ^ 1))) break;
+        uint32_t s = 0, phase = 0, issued = 0;
+        for (uint32_t t = first; t < grid.count && ok; t += step) {
+            uint32_t tile_row, tile_col;
+            tile_at(grid, t, tile_row, tile_col);
+            const int row = (int)(tile_row * 128 * CG + rank * 128), col = (int)(tile_col * BN + rank * S::kRowsB);
+            for (uint32_t d = depth_begin; d < depth_end; ++d) {
+                if (!(ok = barrier_wait(empty + 8 * s, phase ^ 1))) break;
+                if (elected()) {
                     const uint32_t bar = CG == 2 ? address_in(full + 8 * s, leader) : full + 8 * s;
                     if (rank == 0) barrier_expect(full + 8 * s, CG * S::kStageBytes);
                     const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
@@ -302,33 +301,53 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                         copy_box<CG>(b, &map_b, depth, col, bar);
                     }
                 }
+                __syncwarp();
+                issued = min(issued + 1, (uint32_t)S::kStages);
+                if (++s == S::kStages) { s = 0; phase ^= 1; }
             }
-            // gave up: the copies still on their way (counted by the first block) land before the block ends
-            if (!ok && rank == 0)
-                for (uint32_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i) barrier_wait(full + 8 * (i % S::kStages), i / S::kStages & 1);
         }
+        // the products' last arrivals on this block's barriers land before the block ends
+        for (int i = 0; i < S::kStages && ok; ++i) {
+            ok = barrier_wait(empty + 8 * s, phase ^ 1);
+            if (++s == S::kStages) { s = 0; phase ^= 1; }
+        }
+        // gave up: the copies still on their way (counted by the pair's first block) land as well
+        if (!ok && rank == 0)
+            for (; issued > 0; --issued) {
+                if (s-- == 0) { s = S::kStages - 1; phase ^= 1; }
+                barrier_wait(full + 8 * s, phase);
+            }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            uint32_t n = 0, done = 0;
-            for (uint32_t t = first; t < grid.count && ok; t += step, ++done) {
-                const uint32_t half = done & 1, d_address = sums + half * BN;
-                if (!(ok = barrier_wait(sums_empty + 8 * half, (done / 2 & 1) ^ 1))) break;
+        if (rank == 0) {
+            uint32_t s = 0, phase = 0, half = 0, half_phase = 1;
+            const uint32_t low_a = descriptor_low(base), low_b = descriptor_low(base + S::kBytesA);
+            uint32_t a = low_a, b = low_b;
+            for (uint32_t t = first; t < grid.count && ok; t += step) {
+                const uint32_t d_address = sums + half * BN;
+                if (!(ok = barrier_wait(sums_empty + 8 * half, half_phase))) break;
                 tmem_fence_after();
-                for (uint32_t d = depth_begin; d < depth_end; ++d, ++n) {
-                    const uint32_t s = n % S::kStages;
-                    if (!(ok = barrier_wait(full + 8 * s, n / S::kStages & 1))) break;
+                for (uint32_t d = depth_begin; d < depth_end; ++d) {
+                    if (!(ok = barrier_wait(full + 8 * s, phase))) break;
                     tmem_fence_after();
-                    const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
+                    if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        tile_product<CG>(d_address, tile_descriptor(a + k * (a_mn ? 2048 : 32), 8192, 1024),
-                                         tile_descriptor(b + k * (b_mn ? 2048 : 32), 8192, 1024), descriptor, d > depth_begin || k > 0);
-                    tile_commit<CG>(empty + 8 * s, leader);
+                        for (int k = 0; k < 4; ++k)
+                            tile_product<CG>(d_address, tile_descriptor(a + k * (a_mn ? 2048 / 16 : 32 / 16)),
+                                             tile_descriptor(b + k * (b_mn ? 2048 / 16 : 32 / 16)), descriptor, k > 0 || d > depth_begin);
+                        tile_commit<CG>(empty + 8 * s, leader);
+                        if (d + 1 == depth_end) tile_commit<CG>(sums_full + 8 * half, leader);
+                    }
+                    __syncwarp();
+                    a += S::kStageBytes / 16;
+                    b += S::kStageBytes / 16;
+                    if (++s == S::kStages) { s = 0; phase ^= 1; a = low_a; b = low_b; }
                 }
-                if (ok) tile_commit<CG>(sums_full + 8 * half, leader);
+                half ^= 1;
+                half_phase ^= half ^ 1;
             }
             if (!ok) {
-                tile_commit<CG>(drained, leader);
+                if (elected()) tile_commit<CG>(drained, leader);
+                __syncwarp();
                 barrier_wait(drained, 0);
             }
         }
@@ -373,7 +392,9 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             for (uint32_t unit = part + splits * (warp - 4); unit < BN / 8; unit += splits * 8) {
                 const uint32_t quarter = unit % 4, in_tile = unit / 4 * 32;
                 const uint64_t row = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32 + lane, col0 = (uint64_t)tile_col * BN + in_tile;
-                if (col0 >= p.cols) continue;
+                // A piece without a row or column of the result is not read: its values would not be
+                // waited for, and the block that holds them could end before they are fetched.
+                if (col0 >= p.cols || row - lane >= p.rows) continue;
                 float v[32];
                 for (uint32_t i = 0; i < splits; ++i) {
                     const uint32_t from = address_in(base, i * CG + rank) + (in_tile * 128 + quarter * 32 + lane) * 4;

@@ -30,6 +30,17 @@ __device__ __forceinline__ void cluster_arrive_wait()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// One lane of a converged warp.  Copies and products are issued under this predicate, not under
+// lane == 0: the compiler then knows that one thread runs them and keeps their operands in
+// uniform registers (under lane == 0 a step of four products took 580 cycles of issue, which
+// bound every tile shape).
+__device__ __forceinline__ bool elected()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 // ---- mbarriers ----------------------------------------------------------------------
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
 {
@@ -53,15 +64,16 @@ __device__ __forceinline__ void barrier_arrive_remote(uint32_t bar)
 // gives up and the caller leaves its loop.
 constexpr uint32_t kWaitTries = 1u << 22;
 
+// All lanes of the warp wait together; the vote tells the compiler that they leave together.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
 {
     for (uint32_t i = 0; i < kWaitTries; ++i) {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\t"
-                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                     "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                      "selp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
+        if (__all_sync(0xFFFFFFFFu, done)) return true;
     }
     return false;
 }
@@ -132,12 +144,15 @@ __device__ __forceinline__ void tmem_load(uint32_t address, float (&v)[32])
 // (bit 46), swizzle code 2 (bits 61..63).  K-major tiles (rows of 64 values along the sum):
 // `stride` separates groups of 8 rows, `lead` is unused.  MN-major tiles (rows of 64 values
 // along the matrix, one row per step of the sum): `stride` separates groups of 8 steps,
-// `lead` blocks of 64 values.
-__device__ __forceinline__ uint64_t tile_descriptor(uint32_t address, uint32_t lead, uint32_t stride)
-{
-    return (uint64_t)((address >> 4) & 0x3FFF) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 |
-           (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// `lead` blocks of 64 values.  Only the low word changes from tile to tile: the address over
+// 16 lies in its low 14 bits (a block's shared memory ends below 2^18; the bits above name the
+// block within its cluster and are cut off), so an offset over 16 adds on.
+constexpr uint32_t kTileLead = 8192, kTileStride = 1024;
+constexpr uint32_t kDescriptorHigh = kTileStride >> 4 | 1u << 14 | 2u << 29;
+
+__device__ __forceinline__ uint32_t descriptor_low(uint32_t address) { return (address >> 4 & 0x3FFFu) | (kTileLead >> 4) << 16; }
+
+__device__ __forceinline__ uint64_t tile_descriptor(uint32_t low) { return (uint64_t)kDescriptorHigh << 32 | low; }
 
 // Instruction descriptor of kind::f16: fp32 sums, both operands bf16 or both fp16.
 __host__ __device__ constexpr uint32_t product_descriptor(bool bf16, bool a_mn_major, bool b_mn_major, int m, int n)

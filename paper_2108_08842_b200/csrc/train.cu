@@ -273,29 +273,62 @@ struct Cut {
     uint32_t splits;
 };
 
+// Clusters of 1, 2, 4 or 8 blocks with a tile's stages that the device runs at once: clusters do
+// not span the GPU's processing clusters, so fewer blocks fit than there are SMs.
+int cluster_slots(eden_ctx* ctx, uint32_t cluster)
+{
+    int& known = ctx->cluster_slots[cluster];
+    if (known > 0) return known;
+    const auto kernel = k_linear<kForward, __nv_bfloat16, 1, 128, true>;
+    using S = LinearShape<1, 128>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(cluster * ctx->sm_count);
+    cfg.blockDim = dim3(kLinearThreads);
+    cfg.dynamicSmemBytes = S::kSharedBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {cluster, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
+        cudaGetLastError();
+        n = std::max(1, ctx->sm_count / (int)cluster * 3 / 4);
+    }
+    return known = n;
+}
+
+// The cheapest form by a model of its time in microseconds, fitted to sums of 1024 and 4096 on
+// one to 512 tiles: a launch's fixed part, a step of 64 along the sum (the pair's is its
+// products' time, the others' the issue of four products and their barriers), the epilogue of
+// a tile where it outlasts the tile's steps, and the join of a split tile.
 template <int OP>
-Cut choose_cut(const eden_ctx* ctx, const Product& q)
+Cut choose_cut(eden_ctx* ctx, const Product& q)
 {
     const uint64_t steps = (q.depth + 63) / 64;
     const int form = ctx->linear_form;
     if (OP == kForward && q.p.save == EDEN_SAVE_NONE && (form == EDEN_LINEAR_AUTO ? q.p.rows <= 16 : form == EDEN_LINEAR_FEW && q.p.rows <= 32))
         return {EDEN_LINEAR_FEW, 1};
-    struct { int form; uint64_t rows, cols, blocks; double step; } tiles[] = {{EDEN_LINEAR_PAIR, 256, 256, 2, 560.},
-                                                                             {EDEN_LINEAR_SINGLE, 128, 128, 1, 380.},
-                                                                             {EDEN_LINEAR_NARROW, 128, 64, 1, 260.}};
+    static const struct { int form; uint64_t rows, cols; uint32_t blocks; double fixed, step, finish, join; } tiles[] = {
+        {EDEN_LINEAR_PAIR, 256, 256, 2, 6.8, 0.27, 2.4, 0.4},
+        {EDEN_LINEAR_SINGLE, 128, 128, 1, 4.8, 0.233, 1.2, 0.55},
+        {EDEN_LINEAR_NARROW, 128, 64, 1, 4.0, 0.215, 0.6, 0.45}};
     Cut best{EDEN_LINEAR_PAIR, 1};
     double least = 1e300;
     for (const auto& t : tiles) {
         if (form != EDEN_LINEAR_AUTO && form != EDEN_LINEAR_FEW && form != t.form) continue;
-        const uint64_t count = (q.p.rows + t.rows - 1) / t.rows * ((q.p.cols + t.cols - 1) / t.cols), slots = ctx->sm_count / t.blocks;
-        for (uint64_t splits = 1; splits * t.blocks <= 8 && splits <= steps; splits *= 2) {
-            if (ctx->linear_splits && (int)splits != ctx->linear_splits && (int)splits * 2 <= ctx->linear_splits && splits * 2 * t.blocks <= 8 && splits * 2 <= steps) continue;
-            if (ctx->linear_splits && (int)splits > ctx->linear_splits) break;
-            const double waves = (double)((count * splits + slots - 1) / slots);
-            const double cost = waves * ((double)(steps + splits - 1) / splits * t.step + (splits > 1 ? 2000. : 0.));
+        const uint64_t count = (q.p.rows + t.rows - 1) / t.rows * ((q.p.cols + t.cols - 1) / t.cols);
+        uint32_t most = 1;
+        while (2 * most * t.blocks <= 8 && 2 * most <= steps) most *= 2;
+        for (uint32_t splits = 1; splits <= most; splits *= 2) {
+            if (ctx->linear_splits && splits != std::min(most, (uint32_t)ctx->linear_splits)) continue;
+            const uint64_t slots = cluster_slots(ctx, splits * t.blocks), waves = (count + slots - 1) / slots;
+            const double sum = (double)((steps + splits - 1) / splits) * t.step;
+            const double cost = splits > 1 ? waves * (t.fixed + t.join * splits + sum) : t.fixed + waves * std::max(sum, t.finish);
             if (cost < least) {
                 least = cost;
-                best = {t.form, (uint32_t)splits};
+                best = {t.form, splits};
             }
         }
     }

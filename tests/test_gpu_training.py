@@ -220,7 +220,7 @@ def forced(ctx, request):
 @pytest.mark.parametrize("forced", FORMS, indirect=True)
 def test_every_form_at_every_size(ctx, forced):
     """Each kernel form, with each number of parts, on sizes that the choice would give another."""
-    for m, n, k in ((1, 40, 72), (200, 300, 1000), (520, 264, 64), (300, 700, 520)):
+    for m, n, k in ((1, 40, 72), (48, 1000, 520), (200, 300, 1000), (520, 264, 64), (300, 700, 520)):
         check_linear(ctx, torch.bfloat16, m, n, k, "silu", True, True, "pre", seed=m)
         check_input_grad(ctx, torch.float16, m, n, k, "gelu", True)
         check_weight_grad(ctx, torch.bfloat16, m, n, k, True)
