@@ -21,161 +21,232 @@ struct LinearEpilogue {
     float* column_sums;                // input grad: [ceil(rows / 32)][cols] sums of 32 rows, or null
     uint64_t rows, cols;
     int act, save, accumulate;
-    int wide;                          // kWide*
+    int grain_out, grain_residual, grain_codes, grain_bias;      // bytes that all rows start on, at most 32
 };
 
-// Which matrices of an epilogue allow 32-byte accesses at multiples of 32 elements: their
-// rows start on 32-byte boundaries.
-enum { kWideOut = 1, kWideResidual = 2, kWideCodes = 4, kWideBias = 8 };
+// ---- epilogue -----------------------------------------------------------------------
+// A warp finishes 32 rows x 32 columns at a time, a row per lane.  How it reaches a matrix
+// depends on the largest power of two (up to 32 bytes) that all its rows start on:
+//   32 bytes   the lane reads or writes its own row, whole 32-byte sectors
+//   less       through a buffer in shared memory, so that the lanes of an access take
+//              consecutive pieces (16 bytes, 4 bytes or one element) of a few rows; a lane
+//              per row would touch 32 sectors for 32 elements (8192 x 6088 results: 451 us
+//              against STAGED us)
+constexpr int kStageWords = 32 * 33;          // a warp's buffer: 32 rows of up to 32 words and one of padding
 
-// v[j] += from[j] for 32 values of a 16-bit type
-template <typename T>
-__device__ __forceinline__ void add_row(float (&v)[32], const T* from, int count, bool wide)
+// Rows of 32 elements of ELEM bytes in `buffer`, 8 * ELEM words and one of padding each.
+template <int ELEM>
+struct StagedRows {
+    static constexpr int kWords = 8 * ELEM, kPitch = kWords + 1;
+
+    // f(row, byte of the row, word of the buffer) for the pieces of GRAIN bytes, by 32 lanes
+    template <int GRAIN, typename F>
+    static __device__ __forceinline__ void pieces(F&& f)
+    {
+        constexpr int per_row = 32 * ELEM / GRAIN;
+        const int lane = threadIdx.x % 32;
+        if constexpr (per_row >= 32) {
+#pragma unroll 4
+            for (int r = 0; r < 32; ++r) f(r, lane * GRAIN);
+        } else {
+#pragma unroll 4
+            for (int i = 0; i < per_row; ++i) f(i * (32 / per_row) + lane / per_row, lane % per_row * GRAIN);
+        }
+    }
+
+    // global -> buffer; `rows` rows and `bytes` bytes of each exist
+    static __device__ __forceinline__ void fetch(uint32_t* buffer, const char* from, uint64_t stride, int rows, int bytes, int grain)
+    {
+        if (grain >= 16 && bytes == 32 * ELEM) {
+            pieces<16>([&](int r, int at) {
+                if (r >= rows) return;
+                const uint4 q = *(const uint4*)(from + r * stride + at);
+                uint32_t* to = buffer + r * kPitch + at / 4;
+                to[0] = q.x; to[1] = q.y; to[2] = q.z; to[3] = q.w;
+            });
+        } else if (ELEM == 4 || (grain >= 4 && bytes % 4 == 0)) {
+            pieces<4>([&](int r, int at) {
+                if (r < rows && at < bytes) buffer[r * kPitch + at / 4] = *(const uint32_t*)(from + r * stride + at);
+            });
+        } else {
+            pieces<ELEM>([&](int r, int at) {
+                if (r >= rows || at >= bytes) return;
+                if constexpr (ELEM == 2) ((uint16_t*)(buffer + r * kPitch))[at / 2] = *(const uint16_t*)(from + r * stride + at);
+                if constexpr (ELEM == 1) ((uint8_t*)(buffer + r * kPitch))[at] = *(const uint8_t*)(from + r * stride + at);
+            });
+        }
+        __syncwarp();
+    }
+
+    // buffer -> global
+    static __device__ __forceinline__ void flush(const uint32_t* buffer, char* to, uint64_t stride, int rows, int bytes, int grain)
+    {
+        __syncwarp();
+        if (grain >= 16 && bytes == 32 * ELEM) {
+            pieces<16>([&](int r, int at) {
+                if (r >= rows) return;
+                const uint32_t* q = buffer + r * kPitch + at / 4;
+                *(uint4*)(to + r * stride + at) = make_uint4(q[0], q[1], q[2], q[3]);
+            });
+        } else if (ELEM == 4 || (grain >= 4 && bytes % 4 == 0)) {
+            pieces<4>([&](int r, int at) {
+                if (r < rows && at < bytes) *(uint32_t*)(to + r * stride + at) = buffer[r * kPitch + at / 4];
+            });
+        } else {
+            pieces<ELEM>([&](int r, int at) {
+                if (r >= rows || at >= bytes) return;
+                if constexpr (ELEM == 2) *(uint16_t*)(to + r * stride + at) = ((const uint16_t*)(buffer + r * kPitch))[at / 2];
+                if constexpr (ELEM == 1) *(uint8_t*)(to + r * stride + at) = ((const uint8_t*)(buffer + r * kPitch))[at];
+            });
+        }
+        __syncwarp();
+    }
+};
+
+// The lane's row of a matrix, as 8 * ELEM words: row0 is the warp's first row, `at` its first
+// element in the matrix (row0, col0), count elements of `rows` rows exist.  Whole warps.
+template <int ELEM>
+__device__ __forceinline__ void read_row(uint32_t (&w)[8 * ELEM], const char* at, uint64_t stride, int rows, int count, int grain, uint32_t* buffer)
 {
-    if (wide && count == 32) {
+    const int lane = threadIdx.x % 32;
+    if (grain == 32 && count == 32) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t w[8];
-            load_32b(from + 16 * i, w);
+        for (int i = 0; i < ELEM; ++i) {
+            uint32_t q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (lane < rows) load_32b(at + lane * stride + 32 * i, q);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float lo, hi;
-                unpack<T>(w[j], lo, hi);
-                v[16 * i + 2 * j] += lo;
-                v[16 * i + 2 * j + 1] += hi;
-            }
+            for (int j = 0; j < 8; ++j) w[8 * i + j] = q[j];
         }
     } else {
+        StagedRows<ELEM>::fetch(buffer, at, stride, rows, count * ELEM, grain);
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < count) v[j] += to_float(from[j]);
+        for (int j = 0; j < 8 * ELEM; ++j) w[j] = buffer[lane * StagedRows<ELEM>::kPitch + j];
+        __syncwarp();
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void store_row(const float (&v)[32], T* to, int count, bool wide)
+template <int ELEM>
+__device__ __forceinline__ void write_row(const uint32_t (&w)[8 * ELEM], char* at, uint64_t stride, int rows, int count, int grain, uint32_t* buffer)
 {
-    if (wide && count == 32) {
+    const int lane = threadIdx.x % 32;
+    if (grain == 32 && count == 32) {
+        if (lane >= rows) return;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t w[8];
+        for (int i = 0; i < ELEM; ++i) {
+            uint32_t q[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = pack<T>(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
-            store_32b(to + 16 * i, w);
+            for (int j = 0; j < 8; ++j) q[j] = w[8 * i + j];
+            store_32b(at + lane * stride + 32 * i, q);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < count) to[j] = from_float<T>(v[j]);
+        for (int j = 0; j < 8 * ELEM; ++j) buffer[lane * StagedRows<ELEM>::kPitch + j] = w[j];
+        StagedRows<ELEM>::flush(buffer, at, stride, rows, count * ELEM, grain);
     }
-}
-
-// the 8-bit form of a row's group
-__device__ __forceinline__ void save_group(const float (&v)[32], const CheckpointView& c, uint64_t row, uint64_t col0, int count, bool wide)
-{
-    uint32_t most = 0;
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-        if (j < count) most = max(most, magnitude_bits(v[j]));
-    const uint32_t e = group_exponent(most);
-    const float inverse = group_inverse(e);
-    c.exps[row * c.exps_stride + col0 / kGroup] = (uint8_t)e;
-    int8_t* codes = c.codes + row * c.codes_stride + col0;
-    if (wide && count == 32) {
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            w[i] = group_codes(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
-        store_32b(codes, w);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < count) codes[j] = (int8_t)group_code(v[j], inverse);
-    }
-}
-
-// v[j] *= act'(z[j]) with z the checkpointed group
-__device__ __forceinline__ void apply_slopes(float (&v)[32], const CheckpointView& c, uint64_t row, uint64_t col0, int count, bool wide, int act)
-{
-    const int8_t* codes = c.codes + row * c.codes_stride + col0;
-    const float scale = group_scale(c.exps[row * c.exps_stride + col0 / kGroup]);
-    uint32_t w[8];
-    if (wide && count == 32) {
-        load_32b(codes, w);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            w[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (4 * i + j < count) w[i] |= (uint32_t)(uint8_t)codes[4 * i + j] << 8 * j;
-        }
-    }
-    with_act(act, [&](auto a) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float z[4];
-            code_values(w[i], scale, z[0], z[1], z[2], z[3]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[4 * i + j] *= act_slope<decltype(a)::value>(z[j]);
-        }
-    });
 }
 
 // v[32]: fp32 sums of one row's columns col0 .. col0 + 31, held by the lane that owns the
-// row.  All 32 lanes of the warp call this together, for rows row0 + lane (row0 % 32 == 0)
-// and the same col0 (col0 % 32 == 0), also where the row is past the last one.
+// row.  All 32 lanes of the warp call this together, for rows row0 + lane (row0 % 32 == 0,
+// row0 < rows) and the same col0 (col0 % 32 == 0); `buffer` is the warp's own.
 template <int OP, typename T>
-__device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row, uint64_t col0, const LinearEpilogue& p)
+__device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, uint64_t col0, const LinearEpilogue& p, uint32_t* buffer)
 {
-    const bool live = row < p.rows;
-    const int count = (int)(p.cols - col0 < 32 ? p.cols - col0 : 32);
+    const int lane = threadIdx.x % 32;
+    const int rows = (int)(p.rows - row0 < 32 ? p.rows - row0 : 32), count = (int)(p.cols - col0 < 32 ? p.cols - col0 : 32);
+    const bool live = lane < rows;
     if constexpr (OP == kWeightGrad) {
-        if (!live) return;
-        float* out = (float*)p.out + row * p.out_stride + col0;
-        if ((p.wide & kWideOut) && count == 32) {
+        char* out = (char*)p.out + (row0 * p.out_stride + col0) * 4;
+        uint32_t w[32];
+        if (p.accumulate) {
+            read_row<4>(w, out, p.out_stride * 4, rows, count, p.grain_out, buffer);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t w[8];
-                if (p.accumulate) {
-                    load_32b(out + 8 * i, w);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[8 * i + j] += __uint_as_float(w[j]);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
-                store_32b(out + 8 * i, w);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < count) out[j] = p.accumulate ? out[j] + v[j] : v[j];
+            for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
         }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) w[j] = __float_as_uint(v[j]);
+        write_row<4>(w, out, p.out_stride * 4, rows, count, p.grain_out, buffer);
         return;
     }
-    const T* residual = p.residual && live ? (const T*)p.residual + row * p.residual_stride + col0 : nullptr;
+    auto add_residual = [&]() {
+        if (!p.residual) return;
+        uint32_t w[16];
+        read_row<2>(w, (const char*)p.residual + (row0 * p.residual_stride + col0) * 2, p.residual_stride * 2, rows, count, p.grain_residual, buffer);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float lo, hi;
+            unpack<T>(w[j], lo, hi);
+            v[2 * j] += lo;
+            v[2 * j + 1] += hi;
+        }
+    };
     if constexpr (OP == kForward) {
-        if (p.bias) add_row(v, (const T*)p.bias + col0, count, p.wide & kWideBias);
-        if (p.save == EDEN_SAVE_PRE && live) save_group(v, p.ckpt, row, col0, count, p.wide & kWideCodes);
+        if (p.bias) {
+            const T* bias = (const T*)p.bias + col0;
+            if (count == 32 && p.grain_bias == 32) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t w[8];
+                    load_32b(bias + 16 * i, w);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float lo, hi;
+                        unpack<T>(w[j], lo, hi);
+                        v[16 * i + 2 * j] += lo;
+                        v[16 * i + 2 * j + 1] += hi;
+                    }
+                }
+            } else {
+                const float mine = lane < count ? to_float(bias[lane]) : 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xFFFFFFFFu, mine, j);
+            }
+        }
+        // the 8-bit form of the row's group
+        auto save = [&]() {
+            uint32_t most = 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < count) most = max(most, magnitude_bits(v[j]));
+            const uint32_t e = group_exponent(most);
+            const float inverse = group_inverse(e);
+            if (live) p.ckpt.exps[(row0 + lane) * p.ckpt.exps_stride + col0 / kGroup] = (uint8_t)e;
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = group_codes(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
+            write_row<1>(w, (char*)p.ckpt.codes + row0 * p.ckpt.codes_stride + col0, p.ckpt.codes_stride, rows, count, p.grain_codes, buffer);
+        };
+        if (p.save == EDEN_SAVE_PRE) save();
         with_act(p.act, [&](auto a) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = act_value<decltype(a)::value>(v[j]);
         });
-        if (residual) add_row(v, residual, count, p.wide & kWideResidual);
-        if (p.save == EDEN_SAVE_OUT && live) {
+        add_residual();
+        if (p.save == EDEN_SAVE_OUT) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = to_float(from_float<T>(v[j]));
-            save_group(v, p.ckpt, row, col0, count, p.wide & kWideCodes);
+            save();
         }
     } else {
-        if (residual) add_row(v, residual, count, p.wide & kWideResidual);
-        if (p.act != EDEN_ACT_NONE && live) apply_slopes(v, p.ckpt, row, col0, count, p.wide & kWideCodes, p.act);
+        add_residual();
+        if (p.act != EDEN_ACT_NONE) {
+            uint32_t w[8];
+            read_row<1>(w, (const char*)p.ckpt.codes + row0 * p.ckpt.codes_stride + col0, p.ckpt.codes_stride, rows, count, p.grain_codes, buffer);
+            const float scale = live ? group_scale(p.ckpt.exps[(row0 + lane) * p.ckpt.exps_stride + col0 / kGroup]) : 0.f;
+            with_act(p.act, [&](auto a) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float z[4];
+                    code_values(w[i], scale, z[0], z[1], z[2], z[3]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[4 * i + j] *= act_slope<decltype(a)::value>(z[j]);
+                }
+            });
+        }
         if (p.column_sums) {
             // lane j ends with the sum of column j: halves are exchanged and added five times
             float s[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) s[j] = live ? v[j] : 0.f;
-            const int lane = threadIdx.x % 32;
 #pragma unroll
             for (int half = 16; half >= 1; half /= 2) {
                 const bool upper = lane & half;
@@ -185,10 +256,13 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row, ui
                     s[j] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, half);
                 }
             }
-            if (row - lane < p.rows && lane < count) p.column_sums[row / 32 * p.cols + col0 + lane] = s[0];
+            if (lane < count) p.column_sums[row0 / 32 * p.cols + col0 + lane] = s[0];
         }
     }
-    if (live) store_row(v, (T*)p.out + row * p.out_stride + col0, count, p.wide & kWideOut);
+    uint32_t w[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = pack<T>(v[2 * j], v[2 * j + 1]);
+    write_row<2>(w, (char*)p.out + (row0 * p.out_stride + col0) * 2, p.out_stride * 2, rows, count, p.grain_out, buffer);
 }
 
 // Tiles of the result, in the order in which they are handed out: bands of kBand tile rows,
@@ -215,7 +289,8 @@ struct LinearShape {
     static constexpr int kRowsB = BN / CG;
     static constexpr uint32_t kBytesA = 128 * 128, kBytesB = kRowsB * 128, kStageBytes = kBytesA + kBytesB;
     static constexpr int kStages = 6;
-    static constexpr uint32_t kSharedBytes = 1024 + kStages * kStageBytes + (2 * kStages + 5) * 8 + 16;
+    static constexpr uint32_t kBuffers = kStages * kStageBytes, kBarriers = kBuffers + 8 * kStageWords * 4;
+    static constexpr uint32_t kSharedBytes = 1024 + kBarriers + (2 * kStages + 5) * 8 + 16;
     static constexpr uint32_t kColumns = 2 * BN;       // tensor memory: two tiles' sums
 };
 
@@ -242,9 +317,10 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 
     extern __shared__ char raw[];
     const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
-    const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + 8 * S::kStages;
+    const uint32_t full = base + S::kBarriers, empty = full + 8 * S::kStages;
     const uint32_t sums_full = empty + 8 * S::kStages, sums_empty = sums_full + 16, drained = sums_empty + 16, slot = drained + 8;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint32_t* const buffer = (uint32_t*)(raw + (base - shared_address(raw)) + S::kBuffers) + (warp % 8) * kStageWords;   // epilogue warps 4 .. 11
     const uint32_t in_cluster = CG == 2 || SPLIT ? cluster_rank() : 0, rank = in_cluster % CG, leader = in_cluster - rank;
     const uint32_t splits = SPLIT ? grid.splits : 1, part = in_cluster / CG;
     const uint32_t first = blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
@@ -360,7 +436,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             tmem_fence_after();
             uint32_t tile_row, tile_col;
             tile_at(grid, t, tile_row, tile_col);
-            const uint64_t row = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32 + lane;
+            const uint64_t row0 = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32;
 #pragma unroll 1
             for (int c = 0; c < BN / 64; ++c) {
                 const uint32_t in_tile = side * (BN / 2) + c * 32;
@@ -378,7 +454,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                         __syncwarp();
                         if (lane == 0) barrier_arrive_remote(CG == 2 ? address_in(sums_empty + 8 * half, leader) : sums_empty + 8 * half);
                     }
-                    if (col0 < p.cols) linear_epilogue<OP, T>(v, row, col0, p);
+                    if (col0 < p.cols && row0 < p.rows) linear_epilogue<OP, T>(v, row0, col0, p, buffer);
                 }
             }
         }
@@ -391,10 +467,10 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             tile_at(grid, first, tile_row, tile_col);
             for (uint32_t unit = part + splits * (warp - 4); unit < BN / 8; unit += splits * 8) {
                 const uint32_t quarter = unit % 4, in_tile = unit / 4 * 32;
-                const uint64_t row = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32 + lane, col0 = (uint64_t)tile_col * BN + in_tile;
+                const uint64_t row0 = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32, col0 = (uint64_t)tile_col * BN + in_tile;
                 // A piece without a row or column of the result is not read: its values would not be
                 // waited for, and the block that holds them could end before they are fetched.
-                if (col0 >= p.cols || row - lane >= p.rows) continue;
+                if (col0 >= p.cols || row0 >= p.rows) continue;
                 float v[32];
                 for (uint32_t i = 0; i < splits; ++i) {
                     const uint32_t from = address_in(base, i * CG + rank) + (in_tile * 128 + quarter * 32 + lane) * 4;
@@ -404,7 +480,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = i == 0 ? w[j] : v[j] + w[j];
                 }
-                linear_epilogue<OP, T>(v, row, col0, p);
+                linear_epilogue<OP, T>(v, row0, col0, p, buffer);
             }
         }
         __syncwarp();

@@ -231,6 +231,13 @@ struct Product {
     double bytes;
 };
 
+// the largest power of two, up to 32, of which every row's address is a multiple
+int row_grain(const void* p, uint64_t stride, size_t size)
+{
+    const uint64_t bits = (uint64_t)(uintptr_t)p | stride * size | 32;
+    return (int)(bits & (0 - bits));
+}
+
 template <int OP, typename T, int CG, int BN, bool SPLIT>
 int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
 {
@@ -311,9 +318,9 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
     if (OP == kForward && q.p.save == EDEN_SAVE_NONE && (form == EDEN_LINEAR_AUTO ? q.p.rows <= 16 : form == EDEN_LINEAR_FEW && q.p.rows <= 32))
         return {EDEN_LINEAR_FEW, 1};
     static const struct { int form; uint64_t rows, cols; uint32_t blocks; double fixed, step, finish, join; } tiles[] = {
-        {EDEN_LINEAR_PAIR, 256, 256, 2, 6.8, 0.27, 2.4, 0.4},
-        {EDEN_LINEAR_SINGLE, 128, 128, 1, 4.8, 0.233, 1.2, 0.55},
-        {EDEN_LINEAR_NARROW, 128, 64, 1, 4.0, 0.215, 0.6, 0.45}};
+        {EDEN_LINEAR_PAIR, 256, 256, 2, 6.8, 0.27, OP == kWeightGrad ? 3.5 : 2.2, 0.4},
+        {EDEN_LINEAR_SINGLE, 128, 128, 1, 4.8, 0.233, OP == kWeightGrad ? 2.7 : 1.3, 0.55},
+        {EDEN_LINEAR_NARROW, 128, 64, 1, 4.0, 0.215, OP == kWeightGrad ? 1.8 : 0.9, 0.45}};
     Cut best{EDEN_LINEAR_PAIR, 1};
     double least = 1e300;
     for (const auto& t : tiles) {
@@ -349,9 +356,10 @@ int product(eden_ctx* ctx, Scratch& scratch, Product q)
     if (int rc = align_operand(ctx, scratch, q.a)) return rc;
     if (int rc = align_operand(ctx, scratch, q.b)) return rc;
     LinearEpilogue& p = q.p;
-    p.wide = (wide_rows(p.out, p.out_stride, OP == kWeightGrad ? 4 : 2) ? kWideOut : 0) |
-             (wide_rows(p.residual, p.residual_stride, 2) ? kWideResidual : 0) |
-             (wide_rows(p.ckpt.codes, p.ckpt.codes_stride, 1) ? kWideCodes : 0) | (aligned(p.bias, 32) ? kWideBias : 0);
+    p.grain_out = row_grain(p.out, p.out_stride, OP == kWeightGrad ? 4 : 2);
+    p.grain_residual = row_grain(p.residual, p.residual_stride, 2);
+    p.grain_codes = row_grain(p.ckpt.codes, p.ckpt.codes_stride, 1);
+    p.grain_bias = row_grain(p.bias, 0, 2);
     switch (cut.form) {
         case EDEN_LINEAR_PAIR: return launch_tiles<OP, 2, 256>(ctx, q, cut.splits);
         case EDEN_LINEAR_SINGLE: return launch_tiles<OP, 1, 128>(ctx, q, cut.splits);
@@ -401,7 +409,7 @@ extern "C" int eden_linear(eden_ctx* ctx, const eden_linear_args* a)
     return guarded(ctx, [&]() -> int {
         Scratch scratch(ctx);
         LinearEpilogue p{a->bias, a->residual, a->residual_stride, a->y, a->y_stride,
-                         view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride), nullptr, a->m, a->n, a->act, a->save, 0, 0};
+                         view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride), nullptr, a->m, a->n, a->act, a->save, 0};
         const double bytes = 2.0 * ((double)a->m * a->k + (double)a->n * a->k + a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
                              (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
         return product<kForward>(ctx, scratch, {"t_linear", a->type, {a->x, a->x_stride, a->m, a->k}, {a->weight, a->weight_stride, a->n, a->k},
@@ -492,7 +500,7 @@ extern "C" int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_gra
                 if (!partial) return EDEN_ERR_WORKSPACE;
             }
             LinearEpilogue p{nullptr, a->residual, a->residual_stride, a->dx, a->dx_stride,
-                             view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0, 0};
+                             view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0};
             const double bytes = 2.0 * ((double)a->m * a->n + (double)a->n * a->k + (double)a->m * a->k * (a->residual ? 2 : 1)) +
                                  (a->act ? (double)a->m * (a->k + groups_of(a->k)) : 0.0);
             if (int rc = product<kInputGrad>(ctx, scratch, {"t_input_grad", a->type, {a->dz, a->dz_stride, a->m, a->n},
@@ -531,7 +539,7 @@ extern "C" int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_g
             if (rc) return rc;
             x.data = held;
         }
-        LinearEpilogue p{nullptr, nullptr, 0, a->weight_grad, a->weight_grad_stride, {}, nullptr, a->n, a->k, 0, 0, a->accumulate, 0};
+        LinearEpilogue p{nullptr, nullptr, 0, a->weight_grad, a->weight_grad_stride, {}, nullptr, a->n, a->k, 0, 0, a->accumulate};
         const double bytes = 2.0 * a->m * a->n + (double)a->m * (a->codes ? a->k + groups_of(a->k) : 2 * a->k) +
                              4.0 * a->n * a->k * (a->accumulate ? 2 : 1);
         return product<kWeightGrad>(ctx, scratch, {"t_weight_grad", a->type, {a->dz, a->dz_stride, a->m, a->n}, x, a->m, p, bytes});
