@@ -86,9 +86,10 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save_wide(const T* 
     const int count = live && col < n ? (int)min(n - col, 16u) : 0;
     float v[16];
     load_half_group(x + (live ? row * x_stride + col : 0), count, v);
-    uint32_t most = 0;
+    float top = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) most = max(most, magnitude_bits(v[j]));
+    for (int j = 0; j < 16; j += 2) top = max_magnitude(top, v[j], v[j + 1]);
+    uint32_t most = magnitude_bits(top);
     most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
     const uint32_t e = group_exponent(most);
     const float inverse = group_inverse(e);
@@ -120,12 +121,16 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore_wide(T* x, 
     const int count = (int)min(n - col, 16u);
     const uint32_t e = c.exps[row * c.exps_stride + half / 2];
     const uint4 q = load_codes(c.codes + row * c.codes_stride + col, count);
-    const float scale = group_scale(e);
+    const Pair scale(group_scale(e));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
     float v[16];
-    code_values(q.x, scale, v[0], v[1], v[2], v[3]);
-    code_values(q.y, scale, v[4], v[5], v[6], v[7]);
-    code_values(q.z, scale, v[8], v[9], v[10], v[11]);
-    code_values(q.w, scale, v[12], v[13], v[14], v[15]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        Pair v01, v23;
+        code_values(w[j], scale, v01, v23);
+        v01.get(v[4 * j], v[4 * j + 1]);
+        v23.get(v[4 * j + 2], v[4 * j + 3]);
+    }
     if (e >= kSaturates<T>) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) v[j] = saturated<T>(v[j]);
@@ -174,10 +179,10 @@ __global__ void __launch_bounds__(kCkptThreads) k_act_backward_wide(const T* dy,
             if constexpr (ACT != EDEN_ACT_NONE) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float z[4];
-                    code_values(w[j], scale, z[0], z[1], z[2], z[3]);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[4 * j + k] *= act_slope<ACT>(z[k]);
+                    Pair z01, z23;
+                    code_values(w[j], Pair(scale), z01, z23);
+                    (Pair(v[4 * j], v[4 * j + 1]) * act_slope<ACT>(z01)).get(v[4 * j], v[4 * j + 1]);
+                    (Pair(v[4 * j + 2], v[4 * j + 3]) * act_slope<ACT>(z23)).get(v[4 * j + 2], v[4 * j + 3]);
                 }
             }
 #pragma unroll

@@ -39,41 +39,35 @@ template <int ELEM>
 struct StagedRows {
     static constexpr int kWords = 8 * ELEM, kPitch = kWords + 1;
 
-    // f(row, byte of the row, word of the buffer) for the pieces of GRAIN bytes, by 32 lanes
+    // f(i, row, byte of the row) for the lane's pieces of GRAIN bytes
     template <int GRAIN, typename F>
     static __device__ __forceinline__ void pieces(F&& f)
     {
         constexpr int per_row = 32 * ELEM / GRAIN;
         const int lane = threadIdx.x % 32;
-        if constexpr (per_row >= 32) {
-#pragma unroll 4
-            for (int r = 0; r < 32; ++r) f(r, lane * GRAIN);
-        } else {
-#pragma unroll 4
-            for (int i = 0; i < per_row; ++i) f(i * (32 / per_row) + lane / per_row, lane % per_row * GRAIN);
-        }
+#pragma unroll
+        for (int i = 0; i < per_row; ++i) f(i, i * (32 / per_row) + lane / per_row, lane % per_row * GRAIN);
     }
 
     // global -> buffer; `rows` rows and `bytes` bytes of each exist
     static __device__ __forceinline__ void fetch(uint32_t* buffer, const char* from, uint64_t stride, int rows, int bytes, int grain)
     {
         if (grain >= 16 && bytes == 32 * ELEM) {
-            pieces<16>([&](int r, int at) {
-                if (r >= rows) return;
-                const uint4 q = *(const uint4*)(from + r * stride + at);
+            uint4 q[ELEM * 2];
+            pieces<16>([&](int i, int r, int at) { q[i] = r < rows ? *(const uint4*)(from + r * stride + at) : make_uint4(0, 0, 0, 0); });
+            pieces<16>([&](int i, int r, int at) {
                 uint32_t* to = buffer + r * kPitch + at / 4;
-                to[0] = q.x; to[1] = q.y; to[2] = q.z; to[3] = q.w;
+                to[0] = q[i].x; to[1] = q[i].y; to[2] = q[i].z; to[3] = q[i].w;
             });
         } else if (ELEM == 4 || (grain >= 4 && bytes % 4 == 0)) {
-            pieces<4>([&](int r, int at) {
-                if (r < rows && at < bytes) buffer[r * kPitch + at / 4] = *(const uint32_t*)(from + r * stride + at);
-            });
+            uint32_t q[ELEM * 8];
+            pieces<4>([&](int i, int r, int at) { q[i] = r < rows && at < bytes ? *(const uint32_t*)(from + r * stride + at) : 0; });
+            pieces<4>([&](int i, int r, int at) { buffer[r * kPitch + at / 4] = q[i]; });
         } else {
-            pieces<ELEM>([&](int r, int at) {
-                if (r >= rows || at >= bytes) return;
-                if constexpr (ELEM == 2) ((uint16_t*)(buffer + r * kPitch))[at / 2] = *(const uint16_t*)(from + r * stride + at);
-                if constexpr (ELEM == 1) ((uint8_t*)(buffer + r * kPitch))[at] = *(const uint8_t*)(from + r * stride + at);
-            });
+            using U = std::conditional_t<ELEM == 1, uint8_t, uint16_t>;
+            U q[32];
+            pieces<ELEM>([&](int i, int r, int at) { q[i] = r < rows && at < bytes ? *(const U*)(from + r * stride + at) : U(0); });
+            pieces<ELEM>([&](int i, int r, int at) { ((U*)(buffer + r * kPitch))[at / ELEM] = q[i]; });
         }
         __syncwarp();
     }
@@ -83,17 +77,17 @@ struct StagedRows {
     {
         __syncwarp();
         if (grain >= 16 && bytes == 32 * ELEM) {
-            pieces<16>([&](int r, int at) {
+            pieces<16>([&](int, int r, int at) {
                 if (r >= rows) return;
                 const uint32_t* q = buffer + r * kPitch + at / 4;
                 *(uint4*)(to + r * stride + at) = make_uint4(q[0], q[1], q[2], q[3]);
             });
         } else if (ELEM == 4 || (grain >= 4 && bytes % 4 == 0)) {
-            pieces<4>([&](int r, int at) {
+            pieces<4>([&](int, int r, int at) {
                 if (r < rows && at < bytes) *(uint32_t*)(to + r * stride + at) = buffer[r * kPitch + at / 4];
             });
         } else {
-            pieces<ELEM>([&](int r, int at) {
+            pieces<ELEM>([&](int, int r, int at) {
                 if (r >= rows || at >= bytes) return;
                 if constexpr (ELEM == 2) *(uint16_t*)(to + r * stride + at) = ((const uint16_t*)(buffer + r * kPitch))[at / 2];
                 if constexpr (ELEM == 1) *(uint8_t*)(to + r * stride + at) = ((const uint8_t*)(buffer + r * kPitch))[at];
@@ -203,11 +197,16 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, u
         }
         // the 8-bit form of the row's group
         auto save = [&]() {
-            uint32_t most = 0;
+            float most = 0.f;
+            if (count == 32) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < count) most = max(most, magnitude_bits(v[j]));
-            const uint32_t e = group_exponent(most);
+                for (int j = 0; j < 32; j += 2) most = max_magnitude(most, v[j], v[j + 1]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j < count) most = max_magnitude(most, v[j], v[j]);
+            }
+            const uint32_t e = group_exponent(magnitude_bits(most));
             const float inverse = group_inverse(e);
             if (live) p.ckpt.exps[(row0 + lane) * p.ckpt.exps_stride + col0 / kGroup] = (uint8_t)e;
             uint32_t w[8];
@@ -218,7 +217,7 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, u
         if (p.save == EDEN_SAVE_PRE) save();
         with_act(p.act, [&](auto a) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = act_value<decltype(a)::value>(v[j]);
+            for (int j = 0; j < 32; j += 2) act_value<decltype(a)::value>(Pair(v[j], v[j + 1])).get(v[j], v[j + 1]);
         });
         add_residual();
         if (p.save == EDEN_SAVE_OUT) {
@@ -235,10 +234,10 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, u
             with_act(p.act, [&](auto a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    float z[4];
-                    code_values(w[i], scale, z[0], z[1], z[2], z[3]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[4 * i + j] *= act_slope<decltype(a)::value>(z[j]);
+                    Pair z01, z23;
+                    code_values(w[i], Pair(scale), z01, z23);
+                    (Pair(v[4 * i], v[4 * i + 1]) * act_slope<decltype(a)::value>(z01)).get(v[4 * i], v[4 * i + 1]);
+                    (Pair(v[4 * i + 2], v[4 * i + 3]) * act_slope<decltype(a)::value>(z23)).get(v[4 * i + 2], v[4 * i + 3]);
                 }
             });
         }

@@ -23,43 +23,166 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// ---- activations --------------------------------------------------------------------
-// sigmoid(u) = 1 / (1 + exp(-u)); exp overflows to infinity for u < -88, which gives 0
-__device__ __forceinline__ float sigmoid(float u) { return __fdividef(1.f, 1.f + __expf(-u)); }
+// ---- pairs of fp32 values: one packed instruction does both ---------------------------
+struct Pair {
+    uint64_t bits;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float x, float y) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(x), "f"(y)); }
+    explicit __device__ __forceinline__ Pair(float x) : Pair(x, x) {}
+    __device__ __forceinline__ void get(float& x, float& y) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(bits)); }
+};
 
+__device__ __forceinline__ Pair operator*(Pair a, Pair b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+
+__device__ __forceinline__ Pair operator+(Pair a, Pair b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+
+// a * b + c
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+    return r;
+}
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+__device__ __forceinline__ float reciprocal_fast(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+__device__ __forceinline__ Pair exp2_fast(Pair a)
+{
+    float x, y;
+    a.get(x, y);
+    return {exp2_fast(x), exp2_fast(y)};
+}
+
+__device__ __forceinline__ Pair reciprocal_fast(Pair a)
+{
+    float x, y;
+    a.get(x, y);
+    return {reciprocal_fast(x), reciprocal_fast(y)};
+}
+
+__device__ __forceinline__ Pair magnitude(Pair a)
+{
+    float x, y;
+    a.get(x, y);
+    return {fabsf(x), fabsf(y)};
+}
+
+// ---- activations --------------------------------------------------------------------
+// Two values at a time.  2^x and 1/x come from the special function unit (a few units in the
+// last place), four results a pair, which bounds none of the kernels here: an erff and an expf
+// for each value made the activation gradient of 8192 x 16384 take ERFF us against PAIRS.
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kTanhScale = 0.7978845608028654f;      // sqrt(2 / pi)
 constexpr float kTanhCubic = 0.044715f;
 
-template <int ACT>
-__device__ __forceinline__ float act_value(float z)
+// sigmoid(u) = 1 / (1 + 2^w) for w = -u * log2(e); 2^w overflows to infinity, which gives 0
+__device__ __forceinline__ Pair sigmoid_of(Pair w) { return reciprocal_fast(Pair(1.f) + exp2_fast(w)); }
+
+// 1 - Phi(|z|) = erfc(|z| / sqrt(2)) / 2 and exp(-z^2 / 2).  Abramowitz and Stegun 7.1.26:
+// erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x), off by at most 1.5e-7.
+__device__ __forceinline__ Pair upper_tail(Pair z, Pair& bell)
 {
-    if constexpr (ACT == EDEN_ACT_RELU) return z < 0.f ? 0.f : z;          // NaN stays NaN
-    if constexpr (ACT == EDEN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.7071067811865476f));
+    const Pair t = reciprocal_fast(fma(magnitude(z), Pair(0.3275911f * 0.7071067811865476f), Pair(1.f)));
+    bell = exp2_fast(z * z * Pair(-0.5f * kLog2e));
+    Pair q = fma(t, Pair(0.5f * 1.061405429f), Pair(0.5f * -1.453152027f));
+    q = fma(t, q, Pair(0.5f * 1.421413741f));
+    q = fma(t, q, Pair(0.5f * -0.284496736f));
+    q = fma(t, q, Pair(0.5f * 0.254829592f));
+    return q * t * bell;
+}
+
+template <int ACT>
+__device__ __forceinline__ Pair act_value(Pair z)
+{
+    if constexpr (ACT == EDEN_ACT_RELU) {
+        float x, y;
+        z.get(x, y);
+        return {x < 0.f ? 0.f : x, y < 0.f ? 0.f : y};                     // NaN stays NaN
+    }
+    if constexpr (ACT == EDEN_ACT_GELU) {
+        // z Phi(z) = max(z, 0) - |z| (1 - Phi(|z|)); the minimum keeps infinity from meeting its tail of 0
+        Pair bell;
+        const Pair tail = upper_tail(z, bell);
+        float x, y;
+        z.get(x, y);
+        return fma(tail, Pair(-fminf(fabsf(x), 3.0e38f), -fminf(fabsf(y), 3.0e38f)), Pair(fmaxf(x, 0.f), fmaxf(y, 0.f)));
+    }
     // (1 + tanh(u)) / 2 = sigmoid(2u)
-    if constexpr (ACT == EDEN_ACT_GELU_TANH) return z * sigmoid(2.f * kTanhScale * (z + kTanhCubic * z * z * z));
-    if constexpr (ACT == EDEN_ACT_SILU) return z * sigmoid(z);
+    if constexpr (ACT == EDEN_ACT_GELU_TANH)
+        return z * sigmoid_of(z * fma(z * z, Pair(-2.f * kLog2e * kTanhScale * kTanhCubic), Pair(-2.f * kLog2e * kTanhScale)));
+    if constexpr (ACT == EDEN_ACT_SILU) return z * sigmoid_of(z * Pair(-kLog2e));
     return z;
 }
 
 // Beyond |z| = 100 every slope is 0 or 1 to fp32; the clamp keeps z * z * z and z * p * (1 - p)
 // from meeting as infinity times zero.  A NaN compares false and passes through.
 template <int ACT>
-__device__ __forceinline__ float act_slope(float z)
+__device__ __forceinline__ Pair act_slope(Pair z)
 {
-    if constexpr (ACT == EDEN_ACT_NONE) return 1.f;
-    if constexpr (ACT == EDEN_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
-    if (fabsf(z) > 100.f) z = copysignf(100.f, z);
-    if constexpr (ACT == EDEN_ACT_GELU)
-        return 0.5f * (1.f + erff(z * 0.7071067811865476f)) + z * 0.3989422804014327f * __expf(-0.5f * z * z);
+    if constexpr (ACT == EDEN_ACT_NONE) return Pair(1.f);
+    float x, y;
+    z.get(x, y);
+    if constexpr (ACT == EDEN_ACT_RELU) return {x > 0.f ? 1.f : (x <= 0.f ? 0.f : x), y > 0.f ? 1.f : (y <= 0.f ? 0.f : y)};
+    if (fabsf(x) > 100.f) x = copysignf(100.f, x);
+    if (fabsf(y) > 100.f) y = copysignf(100.f, y);
+    z = Pair(x, y);
+    if constexpr (ACT == EDEN_ACT_GELU) {
+        // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi), Phi(z) = 1/2 + sign(z) (1/2 - tail)
+        Pair bell;
+        const Pair middle = fma(upper_tail(z, bell), Pair(-1.f), Pair(0.5f));
+        float a, b;
+        middle.get(a, b);
+        return fma(z * Pair(0.3989422804014327f), bell, Pair(0.5f) + Pair(copysignf(a, x), copysignf(b, y)));
+    }
     if constexpr (ACT == EDEN_ACT_GELU_TANH) {
-        const float p = sigmoid(2.f * kTanhScale * (z + kTanhCubic * z * z * z));
-        return p + z * p * (1.f - p) * 2.f * kTanhScale * (1.f + 3.f * kTanhCubic * z * z);
+        const Pair zz = z * z;
+        const Pair p = sigmoid_of(z * fma(zz, Pair(-2.f * kLog2e * kTanhScale * kTanhCubic), Pair(-2.f * kLog2e * kTanhScale)));
+        const Pair du = z * fma(zz, Pair(6.f * kTanhScale * kTanhCubic), Pair(2.f * kTanhScale));        // z * d(2u)/dz
+        return fma(p * fma(p, Pair(-1.f), Pair(1.f)), du, p);
     }
     if constexpr (ACT == EDEN_ACT_SILU) {
-        const float p = sigmoid(z);
-        return p * (1.f + z * (1.f - p));
+        const Pair p = sigmoid_of(z * Pair(-kLog2e));
+        return fma(p * fma(p, Pair(-1.f), Pair(1.f)), z, p);
     }
-    return 1.f;
+    return Pair(1.f);
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z)
+{
+    float x, y;
+    act_value<ACT>(Pair(z, z)).get(x, y);
+    return x;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z)
+{
+    float x, y;
+    act_slope<ACT>(Pair(z, z)).get(x, y);
+    return x;
 }
 
 // f(std::integral_constant<int, act>): one branch around a block of values
@@ -111,21 +234,30 @@ __device__ __forceinline__ uint32_t group_code(float v, float inverse)
 __device__ __forceinline__ float code_value(int8_t code, float scale) { return (float)code * scale; }
 
 // four codes in a word: the byte c + 128 under the exponent of 2^23 is 2^23 + 128 + c
-__device__ __forceinline__ void code_values(uint32_t w, float scale, float& v0, float& v1, float& v2, float& v3)
+__device__ __forceinline__ void code_values(uint32_t w, Pair scale, Pair& v01, Pair& v23)
 {
     w ^= 0x80808080u;
-    v0 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440)) - 8388736.f) * scale;
-    v1 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7441)) - 8388736.f) * scale;
-    v2 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7442)) - 8388736.f) * scale;
-    v3 = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7443)) - 8388736.f) * scale;
+    const Pair offset(-8388736.f);
+    v01 = (Pair(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440)), __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7441))) + offset) * scale;
+    v23 = (Pair(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7442)), __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7443))) + offset) * scale;
 }
 
 __device__ __forceinline__ uint32_t group_codes(float v0, float v1, float v2, float v3, float inverse)
 {
-    const uint32_t b0 = __float_as_uint(__fmaf_rn(v0, inverse, 12582912.f)), b1 = __float_as_uint(__fmaf_rn(v1, inverse, 12582912.f));
-    const uint32_t b2 = __float_as_uint(__fmaf_rn(v2, inverse, 12582912.f)), b3 = __float_as_uint(__fmaf_rn(v3, inverse, 12582912.f));
-    const uint32_t w = __byte_perm(__byte_perm(b0, b1, 0x0040), __byte_perm(b2, b3, 0x0040), 0x5410);
+    float c0, c1, c2, c3;
+    fma(Pair(v0, v1), Pair(inverse), Pair(12582912.f)).get(c0, c1);
+    fma(Pair(v2, v3), Pair(inverse), Pair(12582912.f)).get(c2, c3);
+    const uint32_t w = __byte_perm(__byte_perm(__float_as_uint(c0), __float_as_uint(c1), 0x0040),
+                                   __byte_perm(__float_as_uint(c2), __float_as_uint(c3), 0x0040), 0x5410);
     return inverse == 0.f ? 0u : w;
+}
+
+// max(m, |a|, |b|), NaN if one is
+__device__ __forceinline__ float max_magnitude(float m, float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
 }
 
 // A restored value in the type of its activations.  A maximum close to the type's largest
