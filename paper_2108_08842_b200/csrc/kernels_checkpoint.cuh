@@ -13,29 +13,34 @@ constexpr int kCkptThreads = 256;
 // A thread takes half a group: 16 values, 32 bytes of a 16-bit type (fp32: 64) and 16 codes.
 // `halves` = 2 * groups of a row, so that the halves of a group sit in neighbouring lanes.
 
-// 16 values -> floats; past the row's end: zeros
+// 16 values as they lie in memory; past the row's end: zeros
 template <typename T>
-__device__ __forceinline__ void load_half_group(const T* p, int count, float (&v)[16])
+__device__ __forceinline__ void fetch_half_group(const T* p, int count, uint32_t (&w)[4 * sizeof(T)])
 {
     if (count >= 16) {
-        if constexpr (sizeof(T) == 4) {
-            uint32_t a[8], b[8];
-            load_32b(p, a);
-            load_32b(p + 8, b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = __uint_as_float(a[j]);
-                v[8 + j] = __uint_as_float(b[j]);
-            }
-        } else {
-            uint32_t a[8];
-            load_32b(p, a);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) load_32b((const char*)p + 32 * i, *(uint32_t(*)[8])(w + 8 * i));
+    } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) unpack<T>(a[j], v[2 * j], v[2 * j + 1]);
-        }
+        for (int j = 0; j < 16; ++j) w[j] = j < count ? ((const uint32_t*)p)[j] : 0;
     } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = j < count ? to_float(p[j]) : 0.f;
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t lo = 2 * j < count ? ((const uint16_t*)p)[2 * j] : 0, hi = 2 * j + 1 < count ? ((const uint16_t*)p)[2 * j + 1] : 0;
+            w[j] = lo | hi << 16;
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void widen_half_group(const uint32_t (&w)[4 * sizeof(T)], float (&v)[16])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(w[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) unpack<T>(w[j], v[2 * j], v[2 * j + 1]);
     }
 }
 
@@ -84,8 +89,10 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save_wide(const T* 
     const uint32_t half = (uint32_t)(i - row * halves), col = half * 16;
     const bool live = i < total;
     const int count = live && col < n ? (int)min(n - col, 16u) : 0;
+    uint32_t raw[4 * sizeof(T)];
     float v[16];
-    load_half_group(x + (live ? row * x_stride + col : 0), count, v);
+    fetch_half_group(x + (live ? row * x_stride + col : 0), count, raw);
+    widen_half_group<T>(raw, v);
     float top = 0.f;
 #pragma unroll
     for (int j = 0; j < 16; j += 2) top = max_magnitude(top, v[j], v[j + 1]);
@@ -142,7 +149,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore_wide(T* x, 
 // eight warps to a block, each keeping the sums of its own rows; the block adds the eight up
 // and leaves the run's column sums in partial[run][n].
 template <typename T, int ACT>
-__global__ void __launch_bounds__(kCkptThreads) k_act_backward_wide(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
+__global__ void __launch_bounds__(kCkptThreads, 4) k_act_backward_wide(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
                                                                    uint64_t dz_stride, float* partial, uint32_t m, uint32_t n,
                                                                    uint32_t rows_per_run)
 {
@@ -157,12 +164,12 @@ __global__ void __launch_bounds__(kCkptThreads) k_act_backward_wide(const T* dy,
     for (int j = 0; j < 16; ++j) sum[j] = 0.f;
     if (count > 0) {
         // the next row is on its way while this one is worked on
-        float next[16];
+        uint32_t next[8];
         uint4 next_codes = make_uint4(0, 0, 0, 0);
         uint32_t next_exp = 0;
         auto fetch = [&](uint32_t row) {
             if (row >= end) return;
-            load_half_group(dy + (uint64_t)row * dy_stride + col, count, next);
+            fetch_half_group(dy + (uint64_t)row * dy_stride + col, count, next);
             if constexpr (ACT != EDEN_ACT_NONE) {
                 next_exp = pre.exps[(uint64_t)row * pre.exps_stride + half / 2];
                 next_codes = load_codes(pre.codes + (uint64_t)row * pre.codes_stride + col, count);
@@ -171,10 +178,9 @@ __global__ void __launch_bounds__(kCkptThreads) k_act_backward_wide(const T* dy,
         fetch(begin + warp);
         for (uint32_t row = begin + warp; row < end; row += kCkptThreads / 32) {
             float v[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = next[j];
+            widen_half_group<T>(next, v);
             const uint32_t w[4] = {next_codes.x, next_codes.y, next_codes.z, next_codes.w};
-            const float scale = group_scale(next_exp);
+            const float scale = slope_scale(next_exp);
             fetch(row + kCkptThreads / 32);
             if constexpr (ACT != EDEN_ACT_NONE) {
 #pragma unroll
@@ -270,7 +276,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_act_backward(const T* dy, uint
         for (uint64_t row = begin + threadIdx.x / 32; row < end; row += kCkptThreads / 32) {
             float v = to_float(dy[row * dy_stride + col]);
             if constexpr (ACT != EDEN_ACT_NONE)
-                v *= act_slope<ACT>(code_value(pre.codes[row * pre.codes_stride + col], group_scale(pre.exps[row * pre.exps_stride + group])));
+                v *= act_slope<ACT>(code_value(pre.codes[row * pre.codes_stride + col], slope_scale(pre.exps[row * pre.exps_stride + group])));
             sum += v;
             if (dz) dz[row * dz_stride + col] = from_float<T>(v);
         }

@@ -230,7 +230,7 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, u
         if (p.act != EDEN_ACT_NONE) {
             uint32_t w[8];
             read_row<1>(w, (const char*)p.ckpt.codes + row0 * p.ckpt.codes_stride + col0, p.ckpt.codes_stride, rows, count, p.grain_codes, buffer);
-            const float scale = live ? group_scale(p.ckpt.exps[(row0 + lane) * p.ckpt.exps_stride + col0 / kGroup]) : 0.f;
+            const float scale = live ? slope_scale(p.ckpt.exps[(row0 + lane) * p.ckpt.exps_stride + col0 / kGroup]) : 0.f;
             with_act(p.act, [&](auto a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {

@@ -136,8 +136,7 @@ __device__ __forceinline__ Pair act_value(Pair z)
     return z;
 }
 
-// Beyond |z| = 100 every slope is 0 or 1 to fp32; the clamp keeps z * z * z and z * p * (1 - p)
-// from meeting as infinity times zero.  A NaN compares false and passes through.
+// For |z| below 2^28 (see slope_scale), so that z * z * z stays finite where p * (1 - p) is 0.
 template <int ACT>
 __device__ __forceinline__ Pair act_slope(Pair z)
 {
@@ -145,9 +144,6 @@ __device__ __forceinline__ Pair act_slope(Pair z)
     float x, y;
     z.get(x, y);
     if constexpr (ACT == EDEN_ACT_RELU) return {x > 0.f ? 1.f : (x <= 0.f ? 0.f : x), y > 0.f ? 1.f : (y <= 0.f ? 0.f : y)};
-    if (fabsf(x) > 100.f) x = copysignf(100.f, x);
-    if (fabsf(y) > 100.f) y = copysignf(100.f, y);
-    z = Pair(x, y);
     if constexpr (ACT == EDEN_ACT_GELU) {
         // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi), Phi(z) = 1/2 + sign(z) (1/2 - tail)
         Pair bell;
@@ -221,6 +217,14 @@ __device__ __forceinline__ float group_inverse(uint32_t exp_byte)
 __device__ __forceinline__ float group_scale(uint32_t exp_byte)
 {
     return __uint_as_float(exp_byte == 255u ? 0x7FC00000u : exp_byte << 23);
+}
+
+// The scale for slopes: at most 2^20.  Beyond |z| = 100 every slope is 0 or 1 to fp32, so codes
+// other than 0 have the same slopes under any larger scale.  NaN compares false and stays.
+__device__ __forceinline__ float slope_scale(uint32_t exp_byte)
+{
+    const float s = group_scale(exp_byte);
+    return s > 1048576.f ? 1048576.f : s;
 }
 
 // v * 2^-e as a whole number in the low byte: the sum with 1.5 * 2^23 rounds to nearest even.
