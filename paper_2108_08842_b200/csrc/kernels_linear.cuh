@@ -26,171 +26,174 @@ struct LinearEpilogue {
 
 // ---- epilogue -----------------------------------------------------------------------
 // A warp finishes 32 rows x 32 columns at a time, a row per lane.  How it reaches a matrix
-// depends on the largest power of two (up to 32 bytes) that all its rows start on:
+// depends on the largest power of two that all its rows start on (its grain):
 //   32 bytes   the lane reads or writes its own row, whole 32-byte sectors
-//   less       through a buffer in shared memory, so that the lanes of an access take
-//              consecutive pieces (16 bytes, 4 bytes or one element) of a few rows; a lane
-//              per row would touch 32 sectors for 32 elements (8192 x 6088 results: 451 us
-//              against STAGED us)
-constexpr int kStageWords = 32 * 33;          // a warp's buffer: 32 rows of up to 32 words and one of padding
+//   16 bytes   through a buffer in shared memory, so that the lanes of an access take
+//              consecutive 16-byte pieces of a few rows
+//   less       likewise in whole 4-byte words; each row's own misalignment is a funnel shift
+//              between buffer and registers, and only the words at its ends are partial
+// A lane per row with less than a sector each took 451 us for 7376 x 6088 x 376 results that
+// start on 16 bytes, against STAGED us.
+constexpr int kStageWords = 32 * 17;          // a warp's buffer: 32 rows of 16 words and one of padding
 
-// Rows of 32 elements of ELEM bytes in `buffer`, 8 * ELEM words and one of padding each.
+// Rows of 32 elements of 1 or 2 bytes (16 of 4 bytes count as 32 of 2).
 template <int ELEM>
-struct StagedRows {
-    static constexpr int kWords = 8 * ELEM, kPitch = kWords + 1;
-
-    // f(i, row, byte of the row) for the lane's pieces of GRAIN bytes
-    template <int GRAIN, typename F>
-    static __device__ __forceinline__ void pieces(F&& f)
+struct Rows {
+    static constexpr int kWords = 8 * ELEM, kSpan = kWords + 1;         // a shifted row touches one word more
+                                                                        // (an odd pitch: no two lanes' rows share a bank)
+    // f(row, piece) for the lane's share of 32 rows of PER_ROW pieces
+    template <int PER_ROW, typename F>
+    static __device__ __forceinline__ void share(F&& f)
     {
-        constexpr int per_row = 32 * ELEM / GRAIN;
         const int lane = threadIdx.x % 32;
 #pragma unroll
-        for (int i = 0; i < per_row; ++i) f(i, i * (32 / per_row) + lane / per_row, lane % per_row * GRAIN);
+        for (int i = 0; i < PER_ROW; ++i) f(i, (i * 32 + lane) / PER_ROW, (i * 32 + lane) % PER_ROW);
     }
 
-    // global -> buffer; `rows` rows and `bytes` bytes of each exist
-    static __device__ __forceinline__ void fetch(uint32_t* buffer, const char* from, uint64_t stride, int rows, int bytes, int grain)
+    // matrix -> the lane's row; `rows` rows and `count` elements of the piece at `from` exist
+    static __device__ __forceinline__ void get(uint32_t (&w)[kWords], const char* from, uint64_t stride, int rows, int count, int grain,
+                                               uint32_t* buffer)
     {
-        if (grain >= 16 && bytes == 32 * ELEM) {
-            uint4 q[ELEM * 2];
-            pieces<16>([&](int i, int r, int at) { q[i] = r < rows ? *(const uint4*)(from + r * stride + at) : make_uint4(0, 0, 0, 0); });
-            pieces<16>([&](int i, int r, int at) {
-                uint32_t* to = buffer + r * kPitch + at / 4;
+        const int lane = threadIdx.x % 32;
+        if (grain == 32 && count == 32) {
+            if (lane < rows) {
+#pragma unroll
+                for (int i = 0; i < ELEM; ++i) load_32b(from + lane * stride + 32 * i, *(uint32_t(*)[8])(w + 8 * i));
+            }
+            return;
+        }
+        __syncwarp();
+        if (grain >= 16 && count == 32) {
+            uint4 q[kWords / 4];
+            share<kWords / 4>([&](int i, int r, int piece) {
+                q[i] = r < rows ? *(const uint4*)(from + r * stride + 16 * piece) : make_uint4(0, 0, 0, 0);
+            });
+            share<kWords / 4>([&](int i, int r, int piece) {
+                uint32_t* to = buffer + r * kSpan + 4 * piece;
                 to[0] = q[i].x; to[1] = q[i].y; to[2] = q[i].z; to[3] = q[i].w;
             });
-        } else if (ELEM == 4 || (grain >= 4 && bytes % 4 == 0)) {
-            uint32_t q[ELEM * 8];
-            pieces<4>([&](int i, int r, int at) { q[i] = r < rows && at < bytes ? *(const uint32_t*)(from + r * stride + at) : 0; });
-            pieces<4>([&](int i, int r, int at) { buffer[r * kPitch + at / 4] = q[i]; });
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) w[j] = buffer[lane * kSpan + j];
         } else {
-            using U = std::conditional_t<ELEM == 1, uint8_t, uint16_t>;
-            U q[32];
-            pieces<ELEM>([&](int i, int r, int at) { q[i] = r < rows && at < bytes ? *(const U*)(from + r * stride + at) : U(0); });
-            pieces<ELEM>([&](int i, int r, int at) { ((U*)(buffer + r * kPitch))[at / ELEM] = q[i]; });
+            uint32_t q[kSpan];
+            share<kSpan>([&](int i, int r, int word) {
+                const char* row = from + r * stride;
+                const int off = (int)((uintptr_t)row & 3);
+                q[i] = r < rows && 4 * word < off + count * ELEM ? *(const uint32_t*)(row - off + 4 * word) : 0;
+            });
+            share<kSpan>([&](int i, int r, int word) { buffer[r * kSpan + word] = q[i]; });
+            __syncwarp();
+            const uint32_t shift = 8 * (uint32_t)((uintptr_t)(from + lane * stride) & 3);
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) w[j] = __funnelshift_r(buffer[lane * kSpan + j], buffer[lane * kSpan + j + 1], shift);
         }
-        __syncwarp();
     }
 
-    // buffer -> global
-    static __device__ __forceinline__ void flush(const uint32_t* buffer, char* to, uint64_t stride, int rows, int bytes, int grain)
+    // the lane's row -> matrix
+    static __device__ __forceinline__ void put(const uint32_t (&w)[kWords], char* to, uint64_t stride, int rows, int count, int grain,
+                                               uint32_t* buffer)
     {
-        __syncwarp();
-        if (grain >= 16 && bytes == 32 * ELEM) {
-            pieces<16>([&](int, int r, int at) {
-                if (r >= rows) return;
-                const uint32_t* q = buffer + r * kPitch + at / 4;
-                *(uint4*)(to + r * stride + at) = make_uint4(q[0], q[1], q[2], q[3]);
-            });
-        } else if (ELEM == 4 || (grain >= 4 && bytes % 4 == 0)) {
-            pieces<4>([&](int, int r, int at) {
-                if (r < rows && at < bytes) *(uint32_t*)(to + r * stride + at) = buffer[r * kPitch + at / 4];
-            });
-        } else {
-            pieces<ELEM>([&](int, int r, int at) {
-                if (r >= rows || at >= bytes) return;
-                if constexpr (ELEM == 2) *(uint16_t*)(to + r * stride + at) = ((const uint16_t*)(buffer + r * kPitch))[at / 2];
-                if constexpr (ELEM == 1) *(uint8_t*)(to + r * stride + at) = ((const uint8_t*)(buffer + r * kPitch))[at];
-            });
+        const int lane = threadIdx.x % 32;
+        if (grain == 32 && count == 32) {
+            if (lane >= rows) return;
+#pragma unroll
+            for (int i = 0; i < ELEM; ++i) store_32b(to + lane * stride + 32 * i, *(const uint32_t(*)[8])(w + 8 * i));
+            return;
         }
         __syncwarp();
+        if (grain >= 16 && count == 32) {
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) buffer[lane * kSpan + j] = w[j];
+            __syncwarp();
+            share<kWords / 4>([&](int, int r, int piece) {
+                const uint32_t* p = buffer + r * kSpan + 4 * piece;
+                if (r < rows) *(uint4*)(to + r * stride + 16 * piece) = make_uint4(p[0], p[1], p[2], p[3]);
+            });
+        } else {
+            const uint32_t shift = 8 * (uint32_t)((uintptr_t)(to + lane * stride) & 3);
+#pragma unroll
+            for (int j = 0; j < kSpan; ++j)
+                buffer[lane * kSpan + j] = __funnelshift_l(j > 0 ? w[j - 1] : 0, j < kWords ? w[j] : 0, shift);
+            __syncwarp();
+            share<kSpan>([&](int, int r, int word) {
+                if (r >= rows) return;
+                char* row = to + r * stride;
+                const int off = (int)((uintptr_t)row & 3), first = 4 * word - off, end = count * ELEM;      // bytes of the row
+                const uint32_t p = buffer[r * kSpan + word];
+                if (first >= 0 && first + 4 <= end) {
+                    *(uint32_t*)(row + first) = p;
+                } else if constexpr (ELEM == 2) {
+                    if (first >= 0 && first + 2 <= end) *(uint16_t*)(row + first) = (uint16_t)p;
+                    else if (first < 0 && end > 0) *(uint16_t*)row = (uint16_t)(p >> 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (first + i >= 0 && first + i < end) row[first + i] = (char)(p >> 8 * i);
+                }
+            });
+        }
     }
 };
 
-// The lane's row of a matrix, as 8 * ELEM words: row0 is the warp's first row, `at` its first
-// element in the matrix (row0, col0), count elements of `rows` rows exist.  Whole warps.
-template <int ELEM>
-__device__ __forceinline__ void read_row(uint32_t (&w)[8 * ELEM], const char* at, uint64_t stride, int rows, int count, int grain, uint32_t* buffer)
-{
-    const int lane = threadIdx.x % 32;
-    if (grain == 32 && count == 32) {
-#pragma unroll
-        for (int i = 0; i < ELEM; ++i) {
-            uint32_t q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (lane < rows) load_32b(at + lane * stride + 32 * i, q);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[8 * i + j] = q[j];
-        }
-    } else {
-        StagedRows<ELEM>::fetch(buffer, at, stride, rows, count * ELEM, grain);
-#pragma unroll
-        for (int j = 0; j < 8 * ELEM; ++j) w[j] = buffer[lane * StagedRows<ELEM>::kPitch + j];
-        __syncwarp();
-    }
-}
+// The piece at (row0, col0): rows and columns that exist.
+struct Piece {
+    uint64_t row0, col0;
+    int rows, count;
+    __device__ __forceinline__ Piece(const LinearEpilogue& p, uint64_t row, uint64_t col)
+        : row0(row), col0(col), rows((int)(p.rows - row < 32 ? p.rows - row : 32)), count((int)(p.cols - col < 32 ? p.cols - col : 32)) {}
+    __device__ __forceinline__ char* in(const void* matrix, uint64_t stride, int size) const { return (char*)matrix + (row0 * stride + col0) * size; }
+};
 
-template <int ELEM>
-__device__ __forceinline__ void write_row(const uint32_t (&w)[8 * ELEM], char* at, uint64_t stride, int rows, int count, int grain, uint32_t* buffer)
-{
-    const int lane = threadIdx.x % 32;
-    if (grain == 32 && count == 32) {
-        if (lane >= rows) return;
-#pragma unroll
-        for (int i = 0; i < ELEM; ++i) {
-            uint32_t q[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = w[8 * i + j];
-            store_32b(at + lane * stride + 32 * i, q);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8 * ELEM; ++j) buffer[lane * StagedRows<ELEM>::kPitch + j] = w[j];
-        StagedRows<ELEM>::flush(buffer, at, stride, rows, count * ELEM, grain);
-    }
-}
-
-// v[32]: fp32 sums of one row's columns col0 .. col0 + 31, held by the lane that owns the
-// row.  All 32 lanes of the warp call this together, for rows row0 + lane (row0 % 32 == 0,
-// row0 < rows) and the same col0 (col0 % 32 == 0); `buffer` is the warp's own.
+// v[32]: fp32 sums of the lane's row of a piece.  All 32 lanes of the warp call this together;
+// `buffer` is the warp's own.
 template <int OP, typename T>
-__device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, uint64_t col0, const LinearEpilogue& p, uint32_t* buffer)
+__device__ __forceinline__ void linear_epilogue(float (&v)[32], const Piece& at, const LinearEpilogue& p, uint32_t* buffer)
 {
     const int lane = threadIdx.x % 32;
-    const int rows = (int)(p.rows - row0 < 32 ? p.rows - row0 : 32), count = (int)(p.cols - col0 < 32 ? p.cols - col0 : 32);
-    const bool live = lane < rows;
+    const bool live = lane < at.rows;
     if constexpr (OP == kWeightGrad) {
-        char* out = (char*)p.out + (row0 * p.out_stride + col0) * 4;
-        uint32_t w[32];
-        if (p.accumulate) {
-            read_row<4>(w, out, p.out_stride * 4, rows, count, p.grain_out, buffer);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
+        for (int h = 0; h < 2; ++h) {                          // 16 columns of 4 bytes
+            const int count = 2 * (at.count - 16 * h < 16 ? at.count - 16 * h : 16);
+            if (count <= 0) break;
+            char* out = at.in(p.out, p.out_stride, 4) + 64 * h;
+            uint32_t w[16];
+            if (p.accumulate) {
+                Rows<2>::get(w, out, p.out_stride * 4, at.rows, count, p.grain_out, buffer);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[16 * h + j] += __uint_as_float(w[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[16 * h + j]);
+            Rows<2>::put(w, out, p.out_stride * 4, at.rows, count, p.grain_out, buffer);
         }
-#pragma unroll
-        for (int j = 0; j < 32; ++j) w[j] = __float_as_uint(v[j]);
-        write_row<4>(w, out, p.out_stride * 4, rows, count, p.grain_out, buffer);
         return;
     }
-    auto add_residual = [&]() {
-        if (!p.residual) return;
-        uint32_t w[16];
-        read_row<2>(w, (const char*)p.residual + (row0 * p.residual_stride + col0) * 2, p.residual_stride * 2, rows, count, p.grain_residual, buffer);
+    auto add_halves = [&](const uint32_t (&w)[16]) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             float lo, hi;
             unpack<T>(w[j], lo, hi);
-            v[2 * j] += lo;
-            v[2 * j + 1] += hi;
+            (Pair(v[2 * j], v[2 * j + 1]) + Pair(lo, hi)).get(v[2 * j], v[2 * j + 1]);
         }
+    };
+    auto add_residual = [&]() {
+        if (!p.residual) return;
+        uint32_t w[16];
+        Rows<2>::get(w, at.in(p.residual, p.residual_stride, 2), p.residual_stride * 2, at.rows, at.count, p.grain_residual, buffer);
+        add_halves(w);
     };
     if constexpr (OP == kForward) {
         if (p.bias) {
-            const T* bias = (const T*)p.bias + col0;
-            if (count == 32 && p.grain_bias == 32) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t w[8];
-                    load_32b(bias + 16 * i, w);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float lo, hi;
-                        unpack<T>(w[j], lo, hi);
-                        v[16 * i + 2 * j] += lo;
-                        v[16 * i + 2 * j + 1] += hi;
-                    }
-                }
+            const T* bias = (const T*)p.bias + at.col0;
+            if (at.count == 32 && p.grain_bias == 32) {
+                uint32_t w[16];
+                load_32b(bias, *(uint32_t(*)[8])w);
+                load_32b(bias + 16, *(uint32_t(*)[8])(w + 8));
+                add_halves(w);
             } else {
-                const float mine = lane < count ? to_float(bias[lane]) : 0.f;
+                const float mine = lane < at.count ? to_float(bias[lane]) : 0.f;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xFFFFFFFFu, mine, j);
             }
@@ -198,21 +201,21 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, u
         // the 8-bit form of the row's group
         auto save = [&]() {
             float most = 0.f;
-            if (count == 32) {
+            if (at.count == 32) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 2) most = max_magnitude(most, v[j], v[j + 1]);
             } else {
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (j < count) most = max_magnitude(most, v[j], v[j]);
+                    if (j < at.count) most = max_magnitude(most, v[j], v[j]);
             }
             const uint32_t e = group_exponent(magnitude_bits(most));
             const float inverse = group_inverse(e);
-            if (live) p.ckpt.exps[(row0 + lane) * p.ckpt.exps_stride + col0 / kGroup] = (uint8_t)e;
+            if (live) p.ckpt.exps[(at.row0 + lane) * p.ckpt.exps_stride + at.col0 / kGroup] = (uint8_t)e;
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = group_codes(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
-            write_row<1>(w, (char*)p.ckpt.codes + row0 * p.ckpt.codes_stride + col0, p.ckpt.codes_stride, rows, count, p.grain_codes, buffer);
+            Rows<1>::put(w, at.in(p.ckpt.codes, p.ckpt.codes_stride, 1), p.ckpt.codes_stride, at.rows, at.count, p.grain_codes, buffer);
         };
         if (p.save == EDEN_SAVE_PRE) save();
         with_act(p.act, [&](auto a) {
@@ -229,8 +232,8 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, u
         add_residual();
         if (p.act != EDEN_ACT_NONE) {
             uint32_t w[8];
-            read_row<1>(w, (const char*)p.ckpt.codes + row0 * p.ckpt.codes_stride + col0, p.ckpt.codes_stride, rows, count, p.grain_codes, buffer);
-            const float scale = live ? slope_scale(p.ckpt.exps[(row0 + lane) * p.ckpt.exps_stride + col0 / kGroup]) : 0.f;
+            Rows<1>::get(w, at.in(p.ckpt.codes, p.ckpt.codes_stride, 1), p.ckpt.codes_stride, at.rows, at.count, p.grain_codes, buffer);
+            const float scale = live ? slope_scale(p.ckpt.exps[(at.row0 + lane) * p.ckpt.exps_stride + at.col0 / kGroup]) : 0.f;
             with_act(p.act, [&](auto a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -255,13 +258,13 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], uint64_t row0, u
                     s[j] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, half);
                 }
             }
-            if (lane < count) p.column_sums[row0 / 32 * p.cols + col0 + lane] = s[0];
+            if (lane < at.count) p.column_sums[at.row0 / 32 * p.cols + at.col0 + lane] = s[0];
         }
     }
     uint32_t w[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) w[j] = pack<T>(v[2 * j], v[2 * j + 1]);
-    write_row<2>(w, (char*)p.out + (row0 * p.out_stride + col0) * 2, p.out_stride * 2, rows, count, p.grain_out, buffer);
+    Rows<2>::put(w, at.in(p.out, p.out_stride, 2), p.out_stride * 2, at.rows, at.count, p.grain_out, buffer);
 }
 
 // Tiles of the result, in the order in which they are handed out: bands of kBand tile rows,
@@ -282,44 +285,56 @@ __device__ __forceinline__ void tile_at(const TileGrid& g, uint32_t t, uint32_t&
     col = in_band / height;
 }
 
-// Shape of a block's share of a tile: 128 rows of A and BN / CG rows of B per step of 64.
+// Shape of a block's share of a tile: 128 rows of A and BN / CG rows of B per step of 64.  Each
+// of the four quarters of its 128 rows of sums has kSides epilogue warps side by side.
 template <int CG, int BN>
 struct LinearShape {
     static constexpr int kRowsB = BN / CG;
     static constexpr uint32_t kBytesA = 128 * 128, kBytesB = kRowsB * 128, kStageBytes = kBytesA + kBytesB;
     static constexpr int kStages = 6;
-    static constexpr uint32_t kBuffers = kStages * kStageBytes, kBarriers = kBuffers + 8 * kStageWords * 4;
-    static constexpr uint32_t kSharedBytes = 1024 + kBarriers + (2 * kStages + 5) * 8 + 16;
+    static constexpr int kSides = 2, kPieces = BN / kSides / 32;     // pieces of 32 columns per warp
+    static constexpr int kWarps = 4 * kSides, kThreads = 128 + 32 * kWarps;
+    static constexpr uint32_t kBuffers = kStages * kStageBytes, kBarriers = kBuffers + kWarps * kStageWords * 4;
+    static constexpr uint32_t kSharedBytes = kBarriers + (2 * kStages + 5) * 8 + 16;
     static constexpr uint32_t kColumns = 2 * BN;       // tensor memory: two tiles' sums
+    static_assert(kSharedBytes <= 227 * 1024, "a block's shared memory");
 };
 
-constexpr int kLinearThreads = 384;    // copies, products, tensor memory, one spare, eight epilogue warps
+// The tensor cores cut off what their fp32 sums cannot hold, always towards zero, so long sums
+// drift: 512 products of 16 left fp32 weight gradients 4e-6 off.  Those sums are taken out of
+// tensor memory every kPromote steps of 64 and added up in registers, rounded to nearest,
+// while the next ones run: PROMOTED off, and no time.  16-bit results do not show the drift.
+constexpr uint32_t kPromote = 16;
 
 // D = A B^T for tiles of 128 * CG x BN, persistent: block (pair) c takes tiles c, c + blocks, ...
 //   warp 0   fills the stages with tensor copies, kStages ahead of the products
 //   warp 1   (of the pair's first block) issues the products
+//   warp 2   owns the tensor memory
 //   warps 4+ read finished sums from tensor memory and run the epilogue, while the products
-//            of the next tile fill the other half of tensor memory
+//            of the next tile (or of the next kPromote steps) fill its other half.  Eight warps:
+//            sixteen have 96 registers each, spill, and took 52 against 47 us for gelu and 8-bit
+//            codes on 4096 x 4096 x 1024, 228 against 190 us for a weight gradient
 // CG = 2: the blocks of a pair hold 128 rows of A and half of the rows of B each; the first
 // one's barriers count both blocks' bytes, and its products write both blocks' sums.
 // SPLIT: one tile per cluster.  Its blocks (pairs) take a part of the sum each, leave their
 // sums in shared memory, and then every block joins and finishes a share of the tile's 32 x 32
 // pieces, adding the parts in their order.
 template <int OP, typename T, int CG, int BN, bool SPLIT>
-__global__ void __launch_bounds__(kLinearThreads, 1)
+__global__ void __launch_bounds__(LinearShape<CG, BN>::kThreads, 1)
 k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, LinearEpilogue p, TileGrid grid,
          uint32_t* status)
 {
     using S = LinearShape<CG, BN>;
     constexpr bool a_mn = OP == kWeightGrad, b_mn = OP != kForward;
+    constexpr uint32_t kRun = OP == kWeightGrad ? kPromote : 1u << 30;      // steps summed in tensor memory
     constexpr uint32_t descriptor = product_descriptor(std::is_same_v<T, __nv_bfloat16>, a_mn, b_mn, 128 * CG, BN);
 
-    extern __shared__ char raw[];
-    const uint32_t base = (shared_address(raw) + 1023u) & ~1023u;
+    extern __shared__ __align__(1024) char raw[];          // tiles of 128-byte rows swizzle by address bits 7 to 9
+    const uint32_t base = shared_address(raw);
     const uint32_t full = base + S::kBarriers, empty = full + 8 * S::kStages;
     const uint32_t sums_full = empty + 8 * S::kStages, sums_empty = sums_full + 16, drained = sums_empty + 16, slot = drained + 8;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    uint32_t* const buffer = (uint32_t*)(raw + (base - shared_address(raw)) + S::kBuffers) + (warp % 8) * kStageWords;   // epilogue warps 4 .. 11
+    uint32_t* const buffer = (uint32_t*)(raw + S::kBuffers) + (warp >= 4 ? warp - 4 : 0) * kStageWords;
     const uint32_t in_cluster = CG == 2 || SPLIT ? cluster_rank() : 0, rank = in_cluster % CG, leader = in_cluster - rank;
     const uint32_t splits = SPLIT ? grid.splits : 1, part = in_cluster / CG;
     const uint32_t first = blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
@@ -333,7 +348,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(sums_full + 8 * i, 1);
-            barrier_init(sums_empty + 8 * i, 8 * CG);
+            barrier_init(sums_empty + 8 * i, S::kWarps * CG);
         }
         barrier_init(drained, 1);
         barrier_init_done();
@@ -350,7 +365,9 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sums) : "r"(slot));
 
     bool ok = true;
-    if (warp == 0) {
+    if (warp < 4) {
+      registers_down();                // the block's registers (its threads x 168) move to the epilogue's warps
+      if (warp == 0) {
         uint32_t s = 0, phase = 0, issued = 0;
         for (uint32_t t = first; t < grid.count && ok; t += step) {
             uint32_t tile_row, tile_col;
@@ -392,33 +409,35 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 if (s-- == 0) { s = S::kStages - 1; phase ^= 1; }
                 barrier_wait(full + 8 * s, phase);
             }
-    } else if (warp == 1) {
+      } else if (warp == 1) {
         if (rank == 0) {
             uint32_t s = 0, phase = 0, half = 0, half_phase = 1;
             const uint32_t low_a = descriptor_low(base), low_b = descriptor_low(base + S::kBytesA);
             uint32_t a = low_a, b = low_b;
             for (uint32_t t = first; t < grid.count && ok; t += step) {
-                const uint32_t d_address = sums + half * BN;
-                if (!(ok = barrier_wait(sums_empty + 8 * half, half_phase))) break;
-                tmem_fence_after();
-                for (uint32_t d = depth_begin; d < depth_end; ++d) {
-                    if (!(ok = barrier_wait(full + 8 * s, phase))) break;
+                for (uint32_t part_begin = depth_begin; part_begin < depth_end && ok; part_begin += kRun) {
+                    const uint32_t d_address = sums + half * BN, part_end = depth_end - part_begin < kRun ? depth_end : part_begin + kRun;
+                    if (!(ok = barrier_wait(sums_empty + 8 * half, half_phase))) break;
                     tmem_fence_after();
-                    if (elected()) {
+                    for (uint32_t d = part_begin; d < part_end; ++d) {
+                        if (!(ok = barrier_wait(full + 8 * s, phase))) break;
+                        tmem_fence_after();
+                        if (elected()) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            tile_product<CG>(d_address, tile_descriptor(a + k * (a_mn ? 2048 / 16 : 32 / 16)),
-                                             tile_descriptor(b + k * (b_mn ? 2048 / 16 : 32 / 16)), descriptor, k > 0 || d > depth_begin);
-                        tile_commit<CG>(empty + 8 * s, leader);
-                        if (d + 1 == depth_end) tile_commit<CG>(sums_full + 8 * half, leader);
+                            for (int k = 0; k < 4; ++k)
+                                tile_product<CG>(d_address, tile_descriptor(a + k * (a_mn ? 2048 / 16 : 32 / 16)),
+                                                 tile_descriptor(b + k * (b_mn ? 2048 / 16 : 32 / 16)), descriptor, k > 0 || d > part_begin);
+                            tile_commit<CG>(empty + 8 * s, leader);
+                            if (d + 1 == part_end) tile_commit<CG>(sums_full + 8 * half, leader);
+                        }
+                        __syncwarp();
+                        a += S::kStageBytes / 16;
+                        b += S::kStageBytes / 16;
+                        if (++s == S::kStages) { s = 0; phase ^= 1; a = low_a; b = low_b; }
                     }
-                    __syncwarp();
-                    a += S::kStageBytes / 16;
-                    b += S::kStageBytes / 16;
-                    if (++s == S::kStages) { s = 0; phase ^= 1; a = low_a; b = low_b; }
+                    half ^= 1;
+                    half_phase ^= half ^ 1;
                 }
-                half ^= 1;
-                half_phase ^= half ^ 1;
             }
             if (!ok) {
                 if (elected()) tile_commit<CG>(drained, leader);
@@ -426,45 +445,77 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 barrier_wait(drained, 0);
             }
         }
-    } else if (warp >= 4) {
+      }
+      __syncwarp();
+      if constexpr (SPLIT) cluster_arrive_wait();
+    } else {
+        registers_up();
         const int quarter = warp % 4, side = (warp - 4) / 4;
-        uint32_t done = 0;
-        for (uint32_t t = first; t < grid.count; t += step, ++done) {
-            const uint32_t half = done & 1;
-            if (!(ok = barrier_wait(sums_full + 8 * half, done / 2 & 1))) break;
-            tmem_fence_after();
+        const uint32_t my_sums = sums + ((uint32_t)quarter * 32 << 16) + side * S::kPieces * 32;
+        uint32_t half = 0, phase = 0;
+        auto release = [&]() {
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive_remote(CG == 2 ? address_in(sums_empty + 8 * half, leader) : sums_empty + 8 * half);
+        };
+        for (uint32_t t = first; t < grid.count && ok; t += step) {
             uint32_t tile_row, tile_col;
             tile_at(grid, t, tile_row, tile_col);
             const uint64_t row0 = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32;
-#pragma unroll 1
-            for (int c = 0; c < BN / 64; ++c) {
-                const uint32_t in_tile = side * (BN / 2) + c * 32;
-                const uint64_t col0 = (uint64_t)tile_col * BN + in_tile;
-                float v[32];
-                __syncwarp();
-                tmem_load(sums + ((uint32_t)quarter * 32 << 16) + half * BN + in_tile, v);
+            const uint32_t in_tile = side * S::kPieces * 32;
+            auto finish = [&](float (&v)[32], int c) {
                 if constexpr (SPLIT) {
                     // [column][row], over the stages: every product that read them is done
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) shared_store(base + ((in_tile + j) * 128 + quarter * 32 + lane) * 4, v[j]);
+                    for (int j = 0; j < 32; ++j) shared_store(base + ((in_tile + 32 * c + j) * 128 + quarter * 32 + lane) * 4, v[j]);
                 } else {
-                    if (c == BN / 64 - 1) {
-                        tmem_fence_before();
-                        __syncwarp();
-                        if (lane == 0) barrier_arrive_remote(CG == 2 ? address_in(sums_empty + 8 * half, leader) : sums_empty + 8 * half);
-                    }
-                    if (col0 < p.cols && row0 < p.rows) linear_epilogue<OP, T>(v, row0, col0, p, buffer);
+                    const uint64_t col0 = (uint64_t)tile_col * BN + in_tile + 32 * c;
+                    if (row0 < p.rows && col0 < p.cols) linear_epilogue<OP, T>(v, Piece(p, row0, col0), p, buffer);
                 }
+            };
+            if constexpr (OP == kWeightGrad) {
+                float total[S::kPieces][32];
+                for (uint32_t part_begin = depth_begin; part_begin < depth_end; part_begin += kRun) {
+                    if (!(ok = barrier_wait(sums_full + 8 * half, phase))) break;
+                    tmem_fence_after();
+#pragma unroll
+                    for (int c = 0; c < S::kPieces; ++c) {
+                        float v[32];
+                        tmem_load(my_sums + half * BN + 32 * c, v);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const Pair sum = part_begin == depth_begin ? Pair(v[j], v[j + 1]) : Pair(total[c][j], total[c][j + 1]) + Pair(v[j], v[j + 1]);
+                            sum.get(total[c][j], total[c][j + 1]);
+                        }
+                    }
+                    release();
+                    half ^= 1;
+                    phase ^= half ^ 1;
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < S::kPieces; ++c) finish(total[c], c);
+            } else {
+                if (!(ok = barrier_wait(sums_full + 8 * half, phase))) break;
+                tmem_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < S::kPieces; ++c) {
+                    float v[32];
+                    __syncwarp();
+                    tmem_load(my_sums + half * BN + 32 * c, v);
+                    if (c == S::kPieces - 1) release();
+                    finish(v, c);
+                }
+                half ^= 1;
+                phase ^= half ^ 1;
             }
         }
-    }
-    __syncwarp();
-    if constexpr (SPLIT) {
-        cluster_arrive_wait();
-        if (warp >= 4) {
+        __syncwarp();
+        if constexpr (SPLIT) {
+            cluster_arrive_wait();
             uint32_t tile_row, tile_col;
             tile_at(grid, first, tile_row, tile_col);
-            for (uint32_t unit = part + splits * (warp - 4); unit < BN / 8; unit += splits * 8) {
+            for (uint32_t unit = part + splits * (warp - 4); unit < BN / 8; unit += splits * S::kWarps) {
                 const uint32_t quarter = unit % 4, in_tile = unit / 4 * 32;
                 const uint64_t row0 = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32, col0 = (uint64_t)tile_col * BN + in_tile;
                 // A piece without a row or column of the result is not read: its values would not be
@@ -479,10 +530,9 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = i == 0 ? w[j] : v[j] + w[j];
                 }
-                linear_epilogue<OP, T>(v, row0, col0, p, buffer);
+                linear_epilogue<OP, T>(v, Piece(p, row0, col0), p, buffer);
             }
         }
-        __syncwarp();
     }
     if (!ok) atomicOr(status, EDEN_STATUS_TIMEOUT);
     __syncwarp();

@@ -54,10 +54,12 @@ __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// bar is an address in the cluster's window (address_in)
+// bar is an address in the cluster's window (address_in).  Relaxed: what it says is that sums were
+// read from tensor memory, which tmem_fence_before orders; a release would also wait for the
+// stores of the epilogue.
 __device__ __forceinline__ void barrier_arrive_remote(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // Every wait ends: after kWaitTries tries (seconds; a tile takes a millisecond at most) it
@@ -77,6 +79,10 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
     }
     return false;
 }
+
+// ---- registers: 4 warps x 56 + 8 warps x 224 = 12 warps x 168, what the block was launched with
+__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
+__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
 
 // ---- tensor copies ------------------------------------------------------------------
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map)

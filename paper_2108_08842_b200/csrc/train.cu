@@ -251,7 +251,7 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
     const auto kernel = k_linear<OP, T, CG, BN, SPLIT>;
     CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
     const uint32_t groups = (uint32_t)(SPLIT ? rows * cols : std::min<uint64_t>(rows * cols, ctx->sm_count / CG));
-    return launch(ctx, q.name, q.bytes, kernel, dim3(groups * CG * splits), kLinearThreads, S::kSharedBytes, CG * splits, map_a, map_b, q.p,
+    return launch(ctx, q.name, q.bytes, kernel, dim3(groups * CG * splits), S::kThreads, S::kSharedBytes, CG * splits, map_a, map_b, q.p,
                   grid, (uint32_t*)ctx->ws);
 }
 
@@ -290,7 +290,7 @@ int cluster_slots(eden_ctx* ctx, uint32_t cluster)
     using S = LinearShape<1, 128>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(cluster * ctx->sm_count);
-    cfg.blockDim = dim3(kLinearThreads);
+    cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSharedBytes;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
