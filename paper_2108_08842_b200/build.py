@@ -1,4 +1,5 @@
-"""Builds libeden.so (the CUDA kernels and their C ABI) for sm_100a with nvcc, in-tree."""
+"""Builds libeden.so (the CUDA kernels and their C ABI) for sm_100a with nvcc, and _binding.so
+(the Python side of the training calls) with g++, both in-tree."""
 from __future__ import annotations
 
 import os
@@ -9,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libeden.so")
+BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["eden.cu", "train.cu", "lloyd_max.cpp", "uniform_family.cpp"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
@@ -33,8 +35,28 @@ def _fresh(obj: str) -> bool:
         return False
 
 
+def _fresh_binding() -> bool:
+    own = [os.path.join(CSRC, "binding.cpp"), os.path.join(os.path.dirname(HERE), "include", "eden.h"), os.path.abspath(__file__)]
+    return all(os.path.getmtime(p) <= os.path.getmtime(BINDING) for p in own)
+
+
+def _binding_command(out: str) -> list:
+    import sysconfig
+
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    includes = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    libs = os.path.join(root, "lib")
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)] +
+            ["-isystem" + i for i in includes] + ["-o", out,
+            os.path.join(CSRC, "binding.cpp"), "-L" + libs, "-Wl,-rpath," + libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source():
+    if not force and all(os.path.exists(p) and os.path.getmtime(p) >= _newest_source() for p in (LIB, BINDING)):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     os.makedirs(OBJ, exist_ok=True)
@@ -45,6 +67,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if force or not _fresh(obj):
             cmd = [nvcc] + NVCC_FLAGS + ["-c", "-MMD", "-MF", obj + ".d", "-o", obj + mark, os.path.join(CSRC, source)]
             running.append((obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    if force or not os.path.exists(BINDING) or not _fresh_binding():
+        running.append((BINDING, subprocess.Popen(_binding_command(BINDING + mark), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = False
     for obj, p in running:
         out, _ = p.communicate()
@@ -62,6 +86,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("nvcc failed linking libeden.so")
     os.replace(LIB + mark, LIB)
+    os.utime(BINDING)
     return LIB
 
 

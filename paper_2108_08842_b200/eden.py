@@ -1,7 +1,8 @@
-"""Thin ctypes binding over ``libeden.so`` (declared in ``include/eden.h``).
+"""Thin binding over ``libeden.so`` (declared in ``include/eden.h``): ctypes for the sender and
+the receiver, the extension ``_binding`` for the calls of the client's training step.
 
-Argument marshalling only: every step of EDEN's sender and receiver runs in the CUDA
-kernels of the library.  PyTorch supplies device memory and the stream.  Importing this
+Argument marshalling only: every step of EDEN's sender and receiver, and every product and
+checkpoint of the training step, runs in the CUDA kernels of the library.  PyTorch supplies device memory and the stream.  Importing this
 module fails loudly if the library has not been built (``python -m
 paper_2108_08842_b200.build``); there is no CPU fallback.
 """
@@ -9,7 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -18,9 +18,9 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libeden.so")
 
-if not os.path.exists(_LIB_PATH):
+if not (os.path.exists(_LIB_PATH) and os.path.exists(os.path.join(_HERE, "_binding.so"))):
     raise ImportError(
-        "libeden.so is missing: build it with `python -m paper_2108_08842_b200.build` "
+        "libeden.so or _binding.so is missing: build it with `python -m paper_2108_08842_b200.build` "
         "(needs nvcc); this package has no CPU fallback")
 
 _lib = ctypes.CDLL(_LIB_PATH)
@@ -84,9 +84,6 @@ _sig("eden_mean_sparsify_after", _int, [_vp, _vp, _vp, _vp, _vp, _u64, _u32, _vp
 _sig("eden_decode_accumulate_sparsify_after", _int, [_vp, _vp, _vp, _vp, _vp, _u64, _u32, _vp, _vp])
 _sig("eden_checkpoint_groups", _u64, [_u64])
 _sig("eden_linear_workspace_bytes", _u64, [_u64, _u64, _u64])
-for _name in ("eden_linear", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_act_backward",
-              "eden_linear_input_grad", "eden_linear_weight_grad"):
-    _sig(_name, _int, [_vp, ctypes.c_char_p])
 _sig("eden_profile_collect", _int, [_vp, ctypes.POINTER(_u32)])
 _sig("eden_profile_get", _int, [_vp, _u32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(_u64),
                                 ctypes.POINTER(_f64), ctypes.POINTER(_f64)])
@@ -100,17 +97,7 @@ UNIFORM_MAX_INDEX = 127
 UNIFORM_MIN_DELTA = 0.0625
 
 
-# the training step: codes of types, activations and what a layer saves, and the layouts of
-# the argument blocks (pointers and counts are 64-bit, the trailing switches 32-bit)
-TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
-SAVES = {"none": 0, "pre": 1, "out": 2}
 CHECKPOINT_GROUP = 32
-_LINEAR = struct.Struct("@16Q4i")
-_CHECKPOINT = struct.Struct("@8Q2i")
-_ACT_BACKWARD = struct.Struct("@11Q4i")
-_INPUT_GRAD = struct.Struct("@16Q4i")
-_WEIGHT_GRAD = struct.Struct("@13Q2i")
 
 
 class Checkpoint(NamedTuple):
@@ -123,6 +110,13 @@ class EdenError(RuntimeError):
     def __init__(self, code: int):
         self.code = code
         super().__init__("eden: %s (%d)" % (_lib.eden_strerror(code).decode(), code))
+
+
+from . import _binding  # noqa: E402  (built with the library; needs torch loaded)
+
+_binding.bind(*(ctypes.cast(getattr(_lib, name), _vp).value for name in (
+    "eden_linear", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_act_backward", "eden_linear_input_grad",
+    "eden_linear_weight_grad")), EdenError, Checkpoint)
 
 
 def _check(rc: int):
@@ -242,13 +236,6 @@ def _ptr_table(tensors: Sequence[Optional[torch.Tensor]]):
     return arr
 
 
-def _code_of(table, key, what):
-    try:
-        return table[key]
-    except (KeyError, TypeError):
-        raise ValueError("eden: %s %r is not one of %s" % (what, key, ", ".join(map(str, table)))) from None
-
-
 class Context:
     """One device, one stream, one caller-owned workspace (a torch uint8 tensor)."""
 
@@ -263,16 +250,18 @@ class Context:
         with torch.cuda.device(device):
             self.stream = stream if stream is not None else torch.cuda.current_stream()
             self.workspace = torch.empty(int(workspace_bytes_) + 256, dtype=torch.uint8, device="cuda:%d" % device)
-        self._device = torch.device("cuda", device)
         base = self.workspace.data_ptr()
         aligned = (base + 255) // 256 * 256
         self._h = _vp()
         self.workspace_bytes = int(workspace_bytes_)
         _check(_lib.eden_create(ctypes.byref(self._h), device, self.stream.cuda_stream,
                                 aligned, self.workspace_bytes))
+        self._native = _binding.native(self._h.value, device, self.stream.cuda_stream, self.stream.stream_id,
+                                       self.stream.device_index, self.stream.device_type)
 
     def close(self):
         if self._h:
+            _binding.close(self._native)
             _lib.eden_destroy(self._h)
             self._h = _vp()
 
@@ -439,124 +428,33 @@ class Context:
                                    mtab, d, n, out.ctypes.data))
 
     # ------------------------------------------------------------------ the client's training step
-    def _matrix(self, t: torch.Tensor, name: str, shape, dtype):
-        """(address, row stride) of a CUDA matrix with contiguous rows."""
-        if t.dtype != dtype or tuple(t.shape) != shape or t.get_device() != self.device:
-            raise ValueError("eden: %s has to be %s %s on cuda:%d, got %s %s on %s" % (
-                name, dtype, list(shape), self.device, t.dtype, list(t.shape), t.device))
-        row, col = t.stride()
-        if col != 1 and shape[1] > 1:
-            raise ValueError("eden: the rows of %s have to be contiguous" % name)
-        if shape[0] <= 1:
-            row = shape[1]
-        elif row < shape[1]:
-            raise ValueError("eden: the rows of %s overlap" % name)
-        return t.data_ptr(), row
-
-    def _vector(self, t: Optional[torch.Tensor], name: str, n: int, dtype) -> int:
-        if t is None:
-            return 0
-        if t.dtype != dtype or tuple(t.shape) != (n,) or t.get_device() != self.device or (n > 1 and t.stride(0) != 1):
-            raise ValueError("eden: %s has to be a contiguous %s [%d] on cuda:%d" % (name, dtype, n, self.device))
-        return t.data_ptr()
-
-    def _optional(self, t: Optional[torch.Tensor], name: str, shape, dtype):
-        return (0, 0) if t is None else self._matrix(t, name, shape, dtype)
-
-    def _checkpoint(self, c, name: str, m: int, n: int):
-        codes, exps = c
-        return (*self._matrix(codes, name + " codes", (m, n), torch.int8),
-                *self._matrix(exps, name + " exponents", (m, -(-n // CHECKPOINT_GROUP)), torch.uint8))
-
-    def _new(self, shape, dtype) -> torch.Tensor:
-        """An output made on the context's stream, whichever stream is current."""
-        if torch._C._cuda_getCurrentRawStream(self.device) == self.stream.cuda_stream:
-            return torch.empty(shape, dtype=dtype, device=self._device)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self._device)
-
-    def _call(self, fn, block: bytes, *tensors):
-        _check(fn(self._h, block))
-        if torch._C._cuda_getCurrentRawStream(self.device) != self.stream.cuda_stream:
-            for t in tensors:                     # their memory stays until this stream is done with it
-                if t is not None:
-                    t.record_stream(self.stream)
-
-    @staticmethod
-    def _rows(t: torch.Tensor, name: str):
-        if t.dim() != 2:
-            raise ValueError("eden: %s has to be a matrix" % name)
-        return t.shape
+    # Wrong types, shapes, devices or names raise ValueError before anything is launched.
+    # Outputs that are not given are made on the context's stream.
 
     def linear(self, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, save: str = "none",
                saved: Optional[Checkpoint] = None):
-        """eden_linear: act(x [m, k] weight [n, k]^T + bias [n]) + residual [m, n], bf16 or fp16.
-        save = "pre" or "out" also returns the 8-bit checkpoint of the pre-activation or of
-        the result: (out, saved)."""
-        m, k = self._rows(x, "x")
-        n = self._rows(weight, "weight")[0]
-        t = x.dtype
-        if out is None:
-            out = self._new((m, n), t)
-        s = _code_of(SAVES, save, "save")
-        codes = exps = None
-        c = (0, 0, 0, 0)
-        if s:
-            if saved is None:
-                saved = self.checkpoint_empty(m, n)
-            codes, exps = saved
-            c = self._checkpoint(saved, "saved", m, n)
-        block = _LINEAR.pack(*self._matrix(x, "x", (m, k), t), *self._matrix(weight, "weight", (n, k), t),
-                             self._vector(bias, "bias", n, t), *self._optional(residual, "residual", (m, n), t),
-                             *self._matrix(out, "out", (m, n), t), *c, m, n, k,
-                             _code_of(TYPES, t, "type"), _code_of(ACTS, act, "act"), s, 0)
-        self._call(_lib.eden_linear, block, x, weight, bias, residual, out, codes, exps)
-        return (out, saved) if s else out
+        """eden_linear: act(x [m, k] weight [n, k]^T + bias [n]) + residual [m, n], bf16 or fp16,
+        act one of none, relu, gelu, gelu_tanh, silu.  save = "pre" or "out" also returns the
+        8-bit checkpoint of the pre-activation or of the result: (out, saved)."""
+        return _binding.linear(self._native, x, weight, bias, act, residual, out, save, saved)
 
     def checkpoint_empty(self, m: int, n: int) -> Checkpoint:
-        return Checkpoint(self._new((m, n), torch.int8), self._new((m, -(-n // CHECKPOINT_GROUP)), torch.uint8))
+        return _binding.checkpoint_empty(self._native, m, n)
 
     def checkpoint_save(self, x: torch.Tensor, out: Optional[Checkpoint] = None) -> Checkpoint:
         """eden_checkpoint_save: the 8-bit form of x [m, n] (bf16, fp16 or fp32)."""
-        m, n = self._rows(x, "x")
-        if out is None:
-            out = self.checkpoint_empty(m, n)
-        block = _CHECKPOINT.pack(*self._matrix(x, "x", (m, n), x.dtype), *self._checkpoint(out, "out", m, n), m, n,
-                                 _code_of(TYPES, x.dtype, "type"), 0)
-        self._call(_lib.eden_checkpoint_save, block, x, *out)
-        return out
+        return _binding.checkpoint_save(self._native, x, out)
 
     def checkpoint_restore(self, saved: Checkpoint, dtype: torch.dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """eden_checkpoint_restore: the values that a checkpoint stands for."""
-        m, n = self._rows(saved[0], "saved codes")
-        if out is None:
-            out = self._new((m, n), dtype)
-        block = _CHECKPOINT.pack(*self._matrix(out, "out", (m, n), dtype), *self._checkpoint(saved, "saved", m, n), m, n,
-                                 _code_of(TYPES, dtype, "type"), 0)
-        self._call(_lib.eden_checkpoint_restore, block, out, *saved)
-        return out
+        return _binding.checkpoint_restore(self._native, saved, dtype, out)
 
     def act_backward(self, dy: torch.Tensor, pre: Optional[Checkpoint], act: str = "none", out: Optional[torch.Tensor] = None,
                      bias_grad: Optional[torch.Tensor] = None, accumulate: bool = False):
         """eden_act_backward: (dz, bias_grad) with dz = dy * act'(pre) and bias_grad its fp32
         column sums (accumulate: added to the given bias_grad)."""
-        m, n = self._rows(dy, "dy")
-        t = dy.dtype
-        if out is None:
-            out = self._new((m, n), t)
-        if bias_grad is None:
-            if accumulate:
-                raise ValueError("eden: accumulate needs a bias_grad to add to")
-            bias_grad = self._new((n,), torch.float32)
-        a = _code_of(ACTS, act, "act")
-        if a and pre is None:
-            raise ValueError("eden: the slope of %s needs its pre-activation" % act)
-        block = _ACT_BACKWARD.pack(*self._matrix(dy, "dy", (m, n), t), *(self._checkpoint(pre, "pre", m, n) if a else (0, 0, 0, 0)),
-                                   *self._matrix(out, "out", (m, n), t), self._vector(bias_grad, "bias_grad", n, torch.float32),
-                                   m, n, _code_of(TYPES, t, "type"), a, int(accumulate), 0)
-        self._call(_lib.eden_act_backward, block, dy, out, bias_grad, *(pre if a else ()))
-        return out, bias_grad
+        return _binding.act_backward(self._native, dy, pre, act, out, bias_grad, accumulate)
 
     def linear_input_grad(self, dz: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None,
                           pre: Optional[Checkpoint] = None, act: str = "none", out: Optional[torch.Tensor] = None,
@@ -564,44 +462,13 @@ class Context:
         """eden_linear_input_grad: dx = (dz [m, n] weight [n, k] + residual [m, k]) * act'(pre).
         With pre (the pre-activation of the layer that made the input) or bias_grad given,
         returns (dx, bias_grad), bias_grad the fp32 column sums of dx; else dx."""
-        m, n = self._rows(dz, "dz")
-        k = self._rows(weight, "weight")[1]
-        t = dz.dtype
-        if out is None:
-            out = self._new((m, k), t)
-        if bias_grad is None:
-            if accumulate:
-                raise ValueError("eden: accumulate needs a bias_grad to add to")
-            if pre is not None:
-                bias_grad = self._new((k,), torch.float32)
-        a = _code_of(ACTS, act, "act")
-        if a and pre is None:
-            raise ValueError("eden: the slope of %s needs its pre-activation" % act)
-        block = _INPUT_GRAD.pack(*self._matrix(dz, "dz", (m, n), t), *self._matrix(weight, "weight", (n, k), t),
-                                 *self._optional(residual, "residual", (m, k), t),
-                                 *(self._checkpoint(pre, "pre", m, k) if a else (0, 0, 0, 0)), *self._matrix(out, "out", (m, k), t),
-                                 self._vector(bias_grad, "bias_grad", k, torch.float32), m, n, k,
-                                 _code_of(TYPES, t, "type"), a, int(accumulate), 0)
-        self._call(_lib.eden_linear_input_grad, block, dz, weight, residual, out, bias_grad, *(pre if a else ()))
-        return out if bias_grad is None else (out, bias_grad)
+        return _binding.input_grad(self._native, dz, weight, residual, pre, act, out, bias_grad, accumulate)
 
     def linear_weight_grad(self, dz: torch.Tensor, x, out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
         """eden_linear_weight_grad: dz [m, n]^T x [m, k] in fp32; x is a Checkpoint or a matrix
         of dz's type.  out may be a view into the vector that encode takes (accumulate: added
         to what it holds)."""
-        m, n = self._rows(dz, "dz")
-        t = dz.dtype
-        held = not isinstance(x, torch.Tensor)
-        k = self._rows(x[0] if held else x, "x")[1]
-        if out is None:
-            if accumulate:
-                raise ValueError("eden: accumulate needs an out to add to")
-            out = self._new((n, k), torch.float32)
-        block = _WEIGHT_GRAD.pack(*self._matrix(dz, "dz", (m, n), t),
-                                  *((0, 0, *self._checkpoint(x, "x", m, k)) if held else (*self._matrix(x, "x", (m, k), t), 0, 0, 0, 0)),
-                                  *self._matrix(out, "out", (n, k), torch.float32), m, n, k, _code_of(TYPES, t, "type"), int(accumulate))
-        self._call(_lib.eden_linear_weight_grad, block, dz, out, *(x if held else (x,)))
-        return out
+        return _binding.weight_grad(self._native, dz, x, out, accumulate)
 
     # ------------------------------------------------------------------ status
     def status(self) -> int:

@@ -1,6 +1,5 @@
 """CPU checks of the training entry points: size rules, argument checks before any GPU work."""
 import ctypes
-import struct
 
 import pytest
 
@@ -37,25 +36,31 @@ def test_null_arguments_are_refused(lib, name):
     assert fn(None, None) == -1
 
 
-def test_binding_lays_out_the_argument_blocks_as_the_header_does():
-    import os
-    import subprocess
-    import tempfile
+def test_calls_of_a_context_refuse_before_any_gpu_work():
+    """Argument checks of the binding on CPU tensors: they come before the library is called."""
+    import torch
 
-    from paper_2108_08842_b200 import eden
+    from paper_2108_08842_b200 import _binding
 
-    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    fields = {"eden_linear_args": ("m", "reserved", eden._LINEAR, 13), "eden_checkpoint_args": ("m", "reserved", eden._CHECKPOINT, 6),
-              "eden_act_backward_args": ("m", "reserved", eden._ACT_BACKWARD, 9),
-              "eden_linear_input_grad_args": ("m", "reserved", eden._INPUT_GRAD, 13),
-              "eden_linear_weight_grad_args": ("m", "accumulate", eden._WEIGHT_GRAD, 10)}
-    body = "".join('printf("%%zu %%zu %%zu\\n", sizeof(%s), offsetof(%s, %s), offsetof(%s, %s));' % (s, s, f[0], s, f[1]) for s, f in fields.items())
-    with tempfile.TemporaryDirectory() as d:
-        src, exe = os.path.join(d, "a.c"), os.path.join(d, "a")
-        with open(src, "w") as f:
-            f.write('#include "%s"\n#include <stddef.h>\n#include <stdio.h>\nint main(void){%s return 0;}' % (os.path.join(root, "include", "eden.h"), body))
-        subprocess.run(["gcc", "-o", exe, src], check=True)
-        rows = subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()
-    rows = [tuple(map(int, rows[i:i + 3])) for i in range(0, len(rows), 3)]
-    for (_, _, block, count_at), (size, at, last) in zip(fields.values(), rows):
-        assert block.size == size and struct.calcsize("@%dQ" % count_at) == at and last == size - 4
+    native = _binding.native(0, 0, 0, 0, 0, 1)
+    x, w = torch.zeros(4, 32, dtype=torch.bfloat16), torch.zeros(8, 32, dtype=torch.bfloat16)
+    for bad in (lambda: _binding.linear(native, x, w, None, "none", None, None, "none", None),
+                lambda: _binding.linear(native, x, None, None, "none", None, None, "none", None),
+                lambda: _binding.linear(native, x[0], w, None, "none", None, None, "none", None),
+                lambda: _binding.linear(native, x.float(), w, None, "none", None, None, "none", None),
+                lambda: _binding.linear(native, x, w, None, "tanh", None, None, "none", None),
+                lambda: _binding.linear(native, x, w, None, None, None, None, "none", None),
+                lambda: _binding.linear(native, x, w, None, "none", None, None, 3, None),
+                lambda: _binding.checkpoint_empty(native, -1, 4),
+                lambda: _binding.checkpoint_save(native, x.double(), None),
+                lambda: _binding.checkpoint_restore(native, (x, x), torch.int8, None),
+                lambda: _binding.checkpoint_restore(native, [x, x], torch.float32, None),
+                lambda: _binding.act_backward(native, x, None, "gelu", None, None, False),
+                lambda: _binding.input_grad(native, x, w, None, None, "relu", None, None, False),
+                lambda: _binding.weight_grad(native, x, (x,), None, False)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        _binding.linear(native, x, w)
+    with pytest.raises(ValueError):
+        _binding.linear("native", x, w, None, "none", None, None, "none", None)
