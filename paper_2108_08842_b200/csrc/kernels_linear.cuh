@@ -34,23 +34,74 @@ struct LinearEpilogue {
 //              between buffer and registers, and only the words at its ends are partial
 // A lane per row with less than a sector each took 451 us for 7376 x 6088 x 376 results that
 // start on 16 bytes, against STAGED us.
-constexpr int kStageWords = 32 * 17;          // a warp's buffer: 32 rows of 16 words and one of padding
+constexpr int kOutWords = 32 * 20, kCodeWords = 32 * 12, kStageWords = kOutWords + kCodeWords;     // a warp's buffer
 
-// Rows of 32 elements of 1 or 2 bytes (16 of 4 bytes count as 32 of 2).
+__device__ __forceinline__ void copy_async_16(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
+__device__ __forceinline__ void copy_async_4(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Rows of 32 elements of 1 or 2 bytes (16 of 4 bytes count as 32 of 2).  In the buffer a row of
+// 16-byte pieces has 4 words of padding (128-bit accesses of eight lanes' rows then meet all
+// banks once), a row of words one (an odd pitch), the word that only shifted rows touch.
 template <int ELEM>
 struct Rows {
-    static constexpr int kWords = 8 * ELEM, kSpan = kWords + 1;         // a shifted row touches one word more
-                                                                        // (an odd pitch: no two lanes' rows share a bank)
-    // f(row, piece) for the lane's share of 32 rows of PER_ROW pieces
+    static constexpr int kWords = 8 * ELEM, kPiecePitch = kWords + 4, kPitch = kWords + 1;
+
+    // f(row, piece) for the lane's share of 32 rows of PER_ROW pieces, a power of two
     template <int PER_ROW, typename F>
     static __device__ __forceinline__ void share(F&& f)
     {
         const int lane = threadIdx.x % 32;
-#pragma unroll
-        for (int i = 0; i < PER_ROW; ++i) f(i, (i * 32 + lane) / PER_ROW, (i * 32 + lane) % PER_ROW);
+#pragma unroll 4
+        for (int i = 0; i < PER_ROW; ++i) f(i * (32 / PER_ROW) + lane / PER_ROW, lane % PER_ROW);
     }
 
-    // matrix -> the lane's row; `rows` rows and `count` elements of the piece at `from` exist
+    // matrix -> buffer, on its way; `rows` rows and `count` elements of the piece at `from` exist
+    static __device__ __forceinline__ void fetch(uint32_t* buffer, const char* from, uint64_t stride, int rows, int count, int grain)
+    {
+        const uint32_t to = shared_address(buffer);
+        if (grain >= 16 && count == 32) {
+            share<kWords / 4>([&](int r, int piece) {
+                if (r < rows) copy_async_16(to + (r * kPiecePitch + 4 * piece) * 4, from + r * stride + 16 * piece);
+            });
+        } else {
+            auto word = [&](int r, int at) {
+                const char* row = from + r * stride;
+                const int off = (int)((uintptr_t)row & 3);
+                if (r < rows && 4 * at < off + count * ELEM) copy_async_4(to + (r * kPitch + at) * 4, row - off + 4 * at);
+            };
+            share<kWords>(word);
+            word(threadIdx.x % 32, kWords);
+        }
+    }
+
+    // buffer -> the lane's row, once the fetch is in
+    static __device__ __forceinline__ void take(uint32_t (&w)[kWords], const uint32_t* buffer, const char* from, uint64_t stride, int count,
+                                                int grain)
+    {
+        const int lane = threadIdx.x % 32;
+        copy_async_wait();
+        __syncwarp();
+        if (grain >= 16 && count == 32) {
+#pragma unroll
+            for (int j = 0; j < kWords / 4; ++j) *(uint4*)(w + 4 * j) = *(const uint4*)(buffer + lane * kPiecePitch + 4 * j);
+        } else {
+            const uint32_t shift = 8 * (uint32_t)((uintptr_t)(from + lane * stride) & 3);
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) w[j] = __funnelshift_r(buffer[lane * kPitch + j], buffer[lane * kPitch + j + 1], shift);
+        }
+        __syncwarp();
+    }
+
+    // matrix -> the lane's row
     static __device__ __forceinline__ void get(uint32_t (&w)[kWords], const char* from, uint64_t stride, int rows, int count, int grain,
                                                uint32_t* buffer)
     {
@@ -62,32 +113,8 @@ struct Rows {
             }
             return;
         }
-        __syncwarp();
-        if (grain >= 16 && count == 32) {
-            uint4 q[kWords / 4];
-            share<kWords / 4>([&](int i, int r, int piece) {
-                q[i] = r < rows ? *(const uint4*)(from + r * stride + 16 * piece) : make_uint4(0, 0, 0, 0);
-            });
-            share<kWords / 4>([&](int i, int r, int piece) {
-                uint32_t* to = buffer + r * kSpan + 4 * piece;
-                to[0] = q[i].x; to[1] = q[i].y; to[2] = q[i].z; to[3] = q[i].w;
-            });
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) w[j] = buffer[lane * kSpan + j];
-        } else {
-            uint32_t q[kSpan];
-            share<kSpan>([&](int i, int r, int word) {
-                const char* row = from + r * stride;
-                const int off = (int)((uintptr_t)row & 3);
-                q[i] = r < rows && 4 * word < off + count * ELEM ? *(const uint32_t*)(row - off + 4 * word) : 0;
-            });
-            share<kSpan>([&](int i, int r, int word) { buffer[r * kSpan + word] = q[i]; });
-            __syncwarp();
-            const uint32_t shift = 8 * (uint32_t)((uintptr_t)(from + lane * stride) & 3);
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) w[j] = __funnelshift_r(buffer[lane * kSpan + j], buffer[lane * kSpan + j + 1], shift);
-        }
+        fetch(buffer, from, stride, rows, count, grain);
+        take(w, buffer, from, stride, count, grain);
     }
 
     // the lane's row -> matrix
@@ -101,38 +128,38 @@ struct Rows {
             for (int i = 0; i < ELEM; ++i) store_32b(to + lane * stride + 32 * i, *(const uint32_t(*)[8])(w + 8 * i));
             return;
         }
-        __syncwarp();
         if (grain >= 16 && count == 32) {
 #pragma unroll
-            for (int j = 0; j < kWords; ++j) buffer[lane * kSpan + j] = w[j];
+            for (int j = 0; j < kWords / 4; ++j) *(uint4*)(buffer + lane * kPiecePitch + 4 * j) = *(const uint4*)(w + 4 * j);
             __syncwarp();
-            share<kWords / 4>([&](int, int r, int piece) {
-                const uint32_t* p = buffer + r * kSpan + 4 * piece;
-                if (r < rows) *(uint4*)(to + r * stride + 16 * piece) = make_uint4(p[0], p[1], p[2], p[3]);
+            share<kWords / 4>([&](int r, int piece) {
+                if (r < rows) *(uint4*)(to + r * stride + 16 * piece) = *(const uint4*)(buffer + r * kPiecePitch + 4 * piece);
             });
         } else {
             const uint32_t shift = 8 * (uint32_t)((uintptr_t)(to + lane * stride) & 3);
 #pragma unroll
-            for (int j = 0; j < kSpan; ++j)
-                buffer[lane * kSpan + j] = __funnelshift_l(j > 0 ? w[j - 1] : 0, j < kWords ? w[j] : 0, shift);
+            for (int j = 0; j <= kWords; ++j) buffer[lane * kPitch + j] = __funnelshift_l(j > 0 ? w[j - 1] : 0, j < kWords ? w[j] : 0, shift);
             __syncwarp();
-            share<kSpan>([&](int, int r, int word) {
+            auto word = [&](int r, int at) {
                 if (r >= rows) return;
                 char* row = to + r * stride;
-                const int off = (int)((uintptr_t)row & 3), first = 4 * word - off, end = count * ELEM;      // bytes of the row
-                const uint32_t p = buffer[r * kSpan + word];
+                const int first = 4 * at - (int)((uintptr_t)row & 3), end = count * ELEM;           // bytes of the row
+                const uint32_t p = buffer[r * kPitch + at];
                 if (first >= 0 && first + 4 <= end) {
                     *(uint32_t*)(row + first) = p;
                 } else if constexpr (ELEM == 2) {
                     if (first >= 0 && first + 2 <= end) *(uint16_t*)(row + first) = (uint16_t)p;
-                    else if (first < 0 && end > 0) *(uint16_t*)row = (uint16_t)(p >> 16);
+                    else if (first < 0 && first + 2 >= 0 && end > 0) *(uint16_t*)row = (uint16_t)(p >> 16);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (first + i >= 0 && first + i < end) row[first + i] = (char)(p >> 8 * i);
                 }
-            });
+            };
+            share<kWords>(word);
+            word(lane, kWords);
         }
+        __syncwarp();
     }
 };
 
@@ -145,10 +172,22 @@ struct Piece {
     __device__ __forceinline__ char* in(const void* matrix, uint64_t stride, int size) const { return (char*)matrix + (row0 * stride + col0) * size; }
 };
 
+// The codes and exponents of a piece's pre-activation, set on their way while the piece before it
+// is finished.
+__device__ __forceinline__ void fetch_codes(const Piece& at, const LinearEpilogue& p, uint32_t* buffer, uint32_t& exp)
+{
+    const int lane = threadIdx.x % 32;
+    if (p.act == EDEN_ACT_NONE) return;
+    Rows<1>::fetch(buffer + kOutWords, at.in(p.ckpt.codes, p.ckpt.codes_stride, 1), p.ckpt.codes_stride, at.rows, at.count, p.grain_codes);
+    exp = lane < at.rows ? p.ckpt.exps[(at.row0 + lane) * p.ckpt.exps_stride + at.col0 / kGroup] : 0;
+}
+
 // v[32]: fp32 sums of the lane's row of a piece.  All 32 lanes of the warp call this together;
-// `buffer` is the warp's own.
+// `buffer` is the warp's own.  Input grad: the piece's codes were fetched, with their `exp`, and
+// `next`'s are, if there is a piece after it.
 template <int OP, typename T>
-__device__ __forceinline__ void linear_epilogue(float (&v)[32], const Piece& at, const LinearEpilogue& p, uint32_t* buffer)
+__device__ __forceinline__ void linear_epilogue(float (&v)[32], const Piece& at, const LinearEpilogue& p, uint32_t* buffer, uint32_t& exp,
+                                                const Piece* next)
 {
     const int lane = threadIdx.x % 32;
     const bool live = lane < at.rows;
@@ -232,8 +271,9 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], const Piece& at,
         add_residual();
         if (p.act != EDEN_ACT_NONE) {
             uint32_t w[8];
-            Rows<1>::get(w, at.in(p.ckpt.codes, p.ckpt.codes_stride, 1), p.ckpt.codes_stride, at.rows, at.count, p.grain_codes, buffer);
-            const float scale = live ? slope_scale(p.ckpt.exps[(at.row0 + lane) * p.ckpt.exps_stride + at.col0 / kGroup]) : 0.f;
+            Rows<1>::take(w, buffer + kOutWords, at.in(p.ckpt.codes, p.ckpt.codes_stride, 1), p.ckpt.codes_stride, at.count, p.grain_codes);
+            const float scale = live ? slope_scale(exp) : 0.f;
+            if (next) fetch_codes(*next, p, buffer, exp);
             with_act(p.act, [&](auto a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -463,6 +503,9 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             tile_at(grid, t, tile_row, tile_col);
             const uint64_t row0 = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32;
             const uint32_t in_tile = side * S::kPieces * 32;
+            uint32_t exp = 0;
+            if (OP == kInputGrad && !SPLIT && row0 < p.rows && (uint64_t)tile_col * BN + in_tile < p.cols)
+                fetch_codes(Piece(p, row0, (uint64_t)tile_col * BN + in_tile), p, buffer, exp);
             auto finish = [&](float (&v)[32], int c) {
                 if constexpr (SPLIT) {
                     // [column][row], over the stages: every product that read them is done
@@ -470,7 +513,10 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                     for (int j = 0; j < 32; ++j) shared_store(base + ((in_tile + 32 * c + j) * 128 + quarter * 32 + lane) * 4, v[j]);
                 } else {
                     const uint64_t col0 = (uint64_t)tile_col * BN + in_tile + 32 * c;
-                    if (row0 < p.rows && col0 < p.cols) linear_epilogue<OP, T>(v, Piece(p, row0, col0), p, buffer);
+                    if (row0 < p.rows && col0 < p.cols) {
+                        const Piece next(p, row0, col0 + 32);
+                        linear_epilogue<OP, T>(v, Piece(p, row0, col0), p, buffer, exp, c + 1 < S::kPieces && col0 + 32 < p.cols ? &next : nullptr);
+                    }
                 }
             };
             if constexpr (OP == kWeightGrad) {
@@ -521,6 +567,9 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 // A piece without a row or column of the result is not read: its values would not be
                 // waited for, and the block that holds them could end before they are fetched.
                 if (col0 >= p.cols || row0 >= p.rows) continue;
+                const Piece at(p, row0, col0);
+                uint32_t exp = 0;
+                if (OP == kInputGrad) fetch_codes(at, p, buffer, exp);
                 float v[32];
                 for (uint32_t i = 0; i < splits; ++i) {
                     const uint32_t from = address_in(base, i * CG + rank) + (in_tile * 128 + quarter * 32 + lane) * 4;
@@ -530,7 +579,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = i == 0 ? w[j] : v[j] + w[j];
                 }
-                linear_epilogue<OP, T>(v, Piece(p, row0, col0), p, buffer);
+                linear_epilogue<OP, T>(v, at, p, buffer, exp, nullptr);
             }
         }
     }
