@@ -30,8 +30,10 @@ struct LinearEpilogue {
 //   32 bytes   the lane reads or writes its own row, whole 32-byte sectors
 //   16 bytes   through a buffer in shared memory, so that the lanes of an access take
 //              consecutive 16-byte pieces of a few rows
-//   less       likewise in whole 4-byte words; each row's own misalignment is a funnel shift
-//              between buffer and registers, and only the words at its ends are partial
+//   less       likewise: reads take whole 4-byte words and undo each row's own misalignment by
+//              a funnel shift between buffer and registers; stores take words where all rows
+//              start on one, else single elements (words with partial ends branched, and took
+//              3750 cycles a piece)
 // A lane per row with less than a sector each took 451 us for 7376 x 6088 x 376 results that
 // start on 16 bytes, against STAGED us.
 constexpr int kOutWords = 32 * 20, kCodeWords = 32 * 12, kStageWords = kOutWords + kCodeWords;     // a warp's buffer
@@ -136,28 +138,34 @@ struct Rows {
                 if (r < rows) *(uint4*)(to + r * stride + 16 * piece) = *(const uint4*)(buffer + r * kPiecePitch + 4 * piece);
             });
         } else {
-            const uint32_t shift = 8 * (uint32_t)((uintptr_t)(to + lane * stride) & 3);
+            // no branches: every store is predicated, so that several are on their way
 #pragma unroll
-            for (int j = 0; j <= kWords; ++j) buffer[lane * kPitch + j] = __funnelshift_l(j > 0 ? w[j - 1] : 0, j < kWords ? w[j] : 0, shift);
+            for (int j = 0; j < kWords; ++j) buffer[lane * kPitch + j] = w[j];
             __syncwarp();
-            auto word = [&](int r, int at) {
-                if (r >= rows) return;
-                char* row = to + r * stride;
-                const int first = 4 * at - (int)((uintptr_t)row & 3), end = count * ELEM;           // bytes of the row
-                const uint32_t p = buffer[r * kPitch + at];
-                if (first >= 0 && first + 4 <= end) {
-                    *(uint32_t*)(row + first) = p;
-                } else if constexpr (ELEM == 2) {
-                    if (first >= 0 && first + 2 <= end) *(uint16_t*)(row + first) = (uint16_t)p;
-                    else if (first < 0 && first + 2 >= 0 && end > 0) *(uint16_t*)row = (uint16_t)(p >> 16);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (first + i >= 0 && first + i < end) row[first + i] = (char)(p >> 8 * i);
+            if (grain >= 4 && (count * ELEM & 3) == 0) {
+                constexpr int at_once = 32 / kWords;
+                const int word = lane % kWords;
+                char* row = to + (lane / kWords) * stride + 4 * word;
+                const uint32_t* from = buffer + (lane / kWords) * kPitch + word;
+                const int mine = 4 * word < count * ELEM ? rows - lane / kWords : 0;
+#pragma unroll 8
+                for (int r = 0; r < 32; r += at_once) {
+                    if (r < mine) *(uint32_t*)row = *from;
+                    row += at_once * stride;
+                    from += at_once * kPitch;
                 }
-            };
-            share<kWords>(word);
-            word(lane, kWords);
+            } else {
+                using U = std::conditional_t<ELEM == 1, uint8_t, uint16_t>;
+                char* row = to + lane * ELEM;
+                const U* from = (const U*)buffer + lane;
+                const int mine = lane < count ? rows : 0;
+#pragma unroll 8
+                for (int r = 0; r < 32; ++r) {
+                    if (r < mine) *(U*)row = *from;
+                    row += stride;
+                    from += kPitch * 4 / ELEM;
+                }
+            }
         }
         __syncwarp();
     }
