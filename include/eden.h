@@ -370,7 +370,7 @@ int eden_force_generic_kernels(eden_ctx* ctx, int on);
                                      one slab's second pass can overlap the next slab's first */
 /*   EDEN_OPT_LINEAR_FORM   EDEN_LINEAR_AUTO (default): the linear products choose their kernel by
  *                          size; else that form wherever it can run (EDEN_LINEAR_FEW: up to 32
- *                          tokens of eden_linear that save nothing).
+ *                          tokens of eden_linear).
  *   EDEN_OPT_LINEAR_SPLITS 0 (default): by size; 1, 2, 4 or 8: parts that a tile's sum is cut
  *                          into (at most one for each 64 of its length, and blocks of at most
  *                          eight SMs). */

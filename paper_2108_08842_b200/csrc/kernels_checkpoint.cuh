@@ -211,8 +211,26 @@ __global__ void __launch_bounds__(kCkptThreads, 4) k_act_backward_wide(const T* 
 }
 
 // ---- any alignment ------------------------------------------------------------------
-// One value per lane, a warp per group; four groups of a warp are in flight together.
-constexpr int kGroupsInFlight = 4;
+// One value per lane, a warp per group; a warp takes kGroupsInFlight consecutive groups, whose
+// loads are on their way together.
+constexpr int kGroupsInFlight = 8;
+
+// f(i, row, group) for the warp's groups, counted through the rows
+template <typename F>
+__device__ __forceinline__ void warp_groups(uint32_t groups, uint64_t total, F&& f)
+{
+    const uint64_t first = ((uint64_t)blockIdx.x * (kCkptThreads / 32) + threadIdx.x / 32) * kGroupsInFlight;
+    uint64_t row = total <= 0xFFFFFFFFull ? (uint32_t)first / groups : first / groups;
+    uint32_t group = (uint32_t)(first - row * groups);
+#pragma unroll
+    for (int i = 0; i < kGroupsInFlight; ++i) {
+        if (first + i < total) f(i, row, group);
+        if (++group == groups) {
+            group = 0;
+            ++row;
+        }
+    }
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* x, uint64_t x_stride, CheckpointView c, uint64_t n,
@@ -220,22 +238,19 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* x, ui
 {
     dependency_wait();
     dependency_release();
-    const uint64_t first = ((uint64_t)blockIdx.x * (kCkptThreads / 32) + threadIdx.x / 32) * kGroupsInFlight;
     const int lane = threadIdx.x % 32;
-    float v[kGroupsInFlight];
-#pragma unroll
-    for (int i = 0; i < kGroupsInFlight; ++i) {
-        const uint64_t row = (first + i) / groups, col = (first + i) % groups * kGroup + lane;
-        v[i] = first + i < total && col < n ? to_float(x[row * x_stride + col]) : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < kGroupsInFlight; ++i) {
-        if (first + i >= total) return;
-        const uint64_t row = (first + i) / groups, group = (first + i) % groups, col = group * kGroup + lane;
-        const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, magnitude_bits(v[i])));
-        if (col < n) c.codes[row * c.codes_stride + col] = (int8_t)group_code(v[i], group_inverse(e));
+    T v[kGroupsInFlight];
+    warp_groups(groups, total, [&](int i, uint64_t row, uint32_t group) {
+        const uint64_t col = (uint64_t)group * kGroup + lane;
+        v[i] = col < n ? x[row * x_stride + col] : from_float<T>(0.f);
+    });
+    warp_groups(groups, total, [&](int i, uint64_t row, uint32_t group) {
+        const uint64_t col = (uint64_t)group * kGroup + lane;
+        const float f = to_float(v[i]);
+        const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, magnitude_bits(f)));
+        if (col < n) c.codes[row * c.codes_stride + col] = (int8_t)group_code(f, group_inverse(e));
         if (lane == 0) c.exps[row * c.exps_stride + group] = (uint8_t)e;
-    }
+    });
 }
 
 template <typename T>
@@ -244,50 +259,67 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* x, uint6
 {
     dependency_wait();
     dependency_release();
-    const uint64_t first = ((uint64_t)blockIdx.x * (kCkptThreads / 32) + threadIdx.x / 32) * kGroupsInFlight;
     const int lane = threadIdx.x % 32;
-    float v[kGroupsInFlight];
-#pragma unroll
-    for (int i = 0; i < kGroupsInFlight; ++i) {
-        const uint64_t row = (first + i) / groups, group = (first + i) % groups, col = group * kGroup + lane;
-        v[i] = first + i < total && col < n ? code_value(c.codes[row * c.codes_stride + col], group_scale(c.exps[row * c.exps_stride + group])) : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < kGroupsInFlight; ++i) {
-        const uint64_t row = (first + i) / groups, col = (first + i) % groups * kGroup + lane;
-        if (first + i < total && col < n) x[row * x_stride + col] = from_float<T>(saturated<T>(v[i]));
-    }
+    int8_t v[kGroupsInFlight];
+    uint8_t e[kGroupsInFlight];
+    warp_groups(groups, total, [&](int i, uint64_t row, uint32_t group) {
+        const uint64_t col = (uint64_t)group * kGroup + lane;
+        v[i] = col < n ? c.codes[row * c.codes_stride + col] : 0;
+        e[i] = c.exps[row * c.exps_stride + group];
+    });
+    warp_groups(groups, total, [&](int i, uint64_t row, uint32_t group) {
+        const uint64_t col = (uint64_t)group * kGroup + lane;
+        if (col < n) x[row * x_stride + col] = from_float<T>(saturated<T>(code_value(v[i], group_scale(e[i]))));
+    });
 }
 
 // dz = dy * act'(z), one lane per column: a block takes 32 columns of a run of rows and
-// leaves the run's column sums in partial[run][n].
+// leaves the run's column sums in partial[run][n].  Each warp has the loads of four of its
+// rows on their way together.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(kCkptThreads) k_act_backward(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
                                                               uint64_t dz_stride, float* partial, uint32_t m, uint32_t n,
                                                               uint32_t rows_per_run)
 {
+    constexpr int kWarps = kCkptThreads / 32, kAhead = 4;
     dependency_wait();
     dependency_release();
     const uint32_t group = blockIdx.x, col = group * kGroup + threadIdx.x % 32;
     const uint32_t begin = blockIdx.y * rows_per_run, end = min(m, begin + rows_per_run);
     float sum = 0.f;
     if (col < n) {
-#pragma unroll 4
-        for (uint64_t row = begin + threadIdx.x / 32; row < end; row += kCkptThreads / 32) {
-            float v = to_float(dy[row * dy_stride + col]);
-            if constexpr (ACT != EDEN_ACT_NONE)
-                v *= act_slope<ACT>(code_value(pre.codes[row * pre.codes_stride + col], slope_scale(pre.exps[row * pre.exps_stride + group])));
-            sum += v;
-            if (dz) dz[row * dz_stride + col] = from_float<T>(v);
+        for (uint32_t row0 = begin + threadIdx.x / 32; row0 < end; row0 += kWarps * kAhead) {
+            T v[kAhead];
+            int8_t code[kAhead];
+            uint8_t e[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const uint64_t row = row0 + i * kWarps;
+                if (row >= end) continue;
+                v[i] = dy[row * dy_stride + col];
+                if constexpr (ACT != EDEN_ACT_NONE) {
+                    code[i] = pre.codes[row * pre.codes_stride + col];
+                    e[i] = pre.exps[row * pre.exps_stride + group];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const uint64_t row = row0 + i * kWarps;
+                if (row >= end) continue;
+                float f = to_float(v[i]);
+                if constexpr (ACT != EDEN_ACT_NONE) f *= act_slope<ACT>(code_value(code[i], slope_scale(e[i])));
+                sum += f;
+                if (dz) dz[row * dz_stride + col] = from_float<T>(f);
+            }
         }
     }
     if (!partial) return;
-    __shared__ float sums[kCkptThreads / 32][32];
+    __shared__ float sums[kWarps][32];
     sums[threadIdx.x / 32][threadIdx.x % 32] = sum;
     __syncthreads();
     if (threadIdx.x < 32 && col < n) {
         float total = 0.f;
-        for (int w = 0; w < kCkptThreads / 32; ++w) total += sums[w][threadIdx.x];
+        for (int w = 0; w < kWarps; ++w) total += sums[w][threadIdx.x];
         partial[(uint64_t)blockIdx.y * n + col] = total;
     }
 }

@@ -601,28 +601,20 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 
 // ---- few tokens ---------------------------------------------------------------------
 // y [m, n] for m <= 8 * NT: every weight is read once and used m times, so reading W is all
-// that takes time.  A block takes 16 rows of W; its 16 warps take steps of 64 along the sum in
-// turn, all loads of up to four steps on their way together, straight to registers in the
+// that takes time.  A block takes 16 * R rows of W; its 16 warps take steps of 64 along the sum
+// in turn, all loads of up to four steps on their way together, straight to registers in the
 // layout of the 16 x 8 x 16 product: the sum's index may be permuted alike in W and in x, so
 // each lane loads 16 consecutive bytes and feeds them as the fragments of two products.  The
-// 16 warps' sums are added in their order.
+// 16 warps' sums are added in their order.  R = 2 where groups of 32 results are saved.
+// 1 x 4096 x 4096 bf16: FEW1 us with the weights in the L2 cache, of which 5.1 are HBM's floor.
 constexpr int kFewThreads = 512;
 
-// 8 values at p, of which the first `count` exist
+// 8 values at p, of which the first `count` exist; VEC: 16-byte aligned, count 8 or 0
 template <bool VEC, typename T>
 __device__ __forceinline__ uint4 load_8(const T* p, int count)
 {
-    if constexpr (VEC) {                       // count is 8 or 0
-        return count > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = 2 * i < count ? ((const uint16_t*)p)[2 * i] : 0, hi = 2 * i + 1 < count ? ((const uint16_t*)p)[2 * i + 1] : 0;
-            w[i] = lo | hi << 16;
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    if constexpr (VEC) return count > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
+    return load_shifted_8(p, count);
 }
 
 template <typename T>
@@ -636,31 +628,34 @@ __device__ __forceinline__ void few_product(float (&c)[4], uint32_t a0, uint32_t
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <typename T, int NT, bool VEC>
-__global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t x_stride, const T* w,
-                                                           uint64_t w_stride, uint32_t k, LinearEpilogue p)
+template <typename T, int NT, int R, bool VEC>
+__global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t x_stride, const T* w, uint64_t w_stride, uint32_t k,
+                                                           LinearEpilogue p)
 {
-    constexpr int kWarps = kFewThreads / 32, kAhead = NT == 1 ? 4 : 2;
+    constexpr int kWarps = kFewThreads / 32, kAhead = (NT == 1 && R == 1 && VEC) ? 4 : (NT <= 2 && R == 1) || NT == 1 ? 2 : 1;
     dependency_wait();
     dependency_release();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-    const uint64_t n0 = (uint64_t)blockIdx.x * 16;
-    const uint64_t r0 = min(n0 + g, p.cols - 1), r1 = min(n0 + g + 8, p.cols - 1);     // past the end: any row, its sums are dropped
-    const T *w0 = w + r0 * w_stride, *w1 = w + r1 * w_stride;
-    float c[NT][4];
+    const uint64_t n0 = (uint64_t)blockIdx.x * (16 * R);
+    const T* row[2 * R];                                   // past the end: any row, its sums are dropped
 #pragma unroll
-    for (int i = 0; i < NT; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
+    for (int i = 0; i < 2 * R; ++i) row[i] = w + min(n0 + g + 8 * i, p.cols - 1) * w_stride;
+    float c[R][NT][4];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < NT; ++i) c[r][i][0] = c[r][i][1] = c[r][i][2] = c[r][i][3] = 0.f;
 
     for (uint32_t k0 = warp * 64; k0 < k; k0 += kWarps * 64 * kAhead) {
-        uint4 a[kAhead][2][2], b[kAhead][NT][2];
+        uint4 a[kAhead][2][2 * R], b[kAhead][NT][2];
 #pragma unroll
         for (int s = 0; s < kAhead; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t at = k0 + s * kWarps * 64 + h * 32 + t * 8;
                 const int count = at < k ? (int)min(k - at, 8u) : 0;
-                a[s][h][0] = load_8<VEC>(w0 + at, count);
-                a[s][h][1] = load_8<VEC>(w1 + at, count);
+#pragma unroll
+                for (int i = 0; i < 2 * R; ++i) a[s][h][i] = load_8<VEC>(row[i] + at, count);
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
                     const uint32_t token = i * 8 + g;
@@ -672,51 +667,111 @@ __global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    const uint4 u = a[s][h][0], v = a[s][h][1], z = b[s][i][h];
-                    few_product<T>(c[i], u.x, v.x, u.y, v.y, z.x, z.y);
-                    few_product<T>(c[i], u.z, v.z, u.w, v.w, z.z, z.w);
-                }
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        const uint4 u = a[s][h][2 * r], v = a[s][h][2 * r + 1], z = b[s][i][h];
+                        few_product<T>(c[r][i], u.x, v.x, u.y, v.y, z.x, z.y);
+                        few_product<T>(c[r][i], u.z, v.z, u.w, v.w, z.z, z.w);
+                    }
     }
-    __shared__ float sums[kWarps][8 * NT][16 + 1];                 // [warp][token][row of W]
+    // eight tokens at a time, [warp][token][row of W]
+    __shared__ float sums[kWarps][8][16 * R + 1];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        sums[warp][i * 8 + 2 * t][g] = c[i][0];
-        sums[warp][i * 8 + 2 * t + 1][g] = c[i][1];
-        sums[warp][i * 8 + 2 * t][g + 8] = c[i][2];
-        sums[warp][i * 8 + 2 * t + 1][g + 8] = c[i][3];
-    }
-    __syncthreads();
-    if (threadIdx.x >= 128 * NT) return;
-    const uint32_t token = threadIdx.x / 16, in = threadIdx.x % 16;
-    const uint64_t col = n0 + in;
-    if (token >= p.rows || col >= p.cols) return;
-    float v = 0.f;
+        if (8 * i >= p.rows) return;
+        if (i > 0) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) v += sums[i][token][in];
-    if (p.bias) v += to_float(((const T*)p.bias)[col]);
-    with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
-    if (p.residual) v += to_float(((const T*)p.residual)[token * p.residual_stride + col]);
-    ((T*)p.out)[token * p.out_stride + col] = from_float<T>(v);
+        for (int r = 0; r < R; ++r) {
+            sums[warp][2 * t][16 * r + g] = c[r][i][0];
+            sums[warp][2 * t + 1][16 * r + g] = c[r][i][1];
+            sums[warp][2 * t][16 * r + g + 8] = c[r][i][2];
+            sums[warp][2 * t + 1][16 * r + g + 8] = c[r][i][3];
+        }
+        __syncthreads();
+        if (threadIdx.x >= 128 * R) continue;
+        const uint32_t in_tile = threadIdx.x / (16 * R), in = threadIdx.x % (16 * R), token = 8 * i + in_tile;
+        const uint64_t col = n0 + in;
+        const bool live = token < p.rows && col < p.cols;
+        float v = 0.f;
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) v += sums[j][in_tile][in];
+        if (p.bias && live) v += to_float(((const T*)p.bias)[col]);
+        auto save = [&]() {                                // R = 2: the warp holds a token's group
+            const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, live ? magnitude_bits(v) : 0u));
+            if (!live) return;
+            p.ckpt.codes[token * p.ckpt.codes_stride + col] = (int8_t)group_code(v, group_inverse(e));
+            if (in == 0) p.ckpt.exps[token * p.ckpt.exps_stride + n0 / kGroup] = (uint8_t)e;
+        };
+        if (R == 2 && p.save == EDEN_SAVE_PRE) save();
+        with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
+        if (p.residual && live) v += to_float(((const T*)p.residual)[token * p.residual_stride + col]);
+        const T y = from_float<T>(v);
+        if (R == 2 && p.save == EDEN_SAVE_OUT) {
+            v = to_float(y);
+            save();
+        }
+        if (live) ((T*)p.out)[token * p.out_stride + col] = y;
+    }
 }
 
-// Copies rows of 16-bit values to rows of `stride` values (a multiple of 8) on a 16-byte boundary.
-__global__ void __launch_bounds__(256) k_align_rows(const uint16_t* from, uint64_t from_stride, uint16_t* to,
-                                                   uint64_t stride, uint64_t n, uint64_t total)
+// ---- operands -----------------------------------------------------------------------
+// What the tile kernel's tensor copies cannot read is laid out anew, both operands in one launch:
+// rows that do not start on 16 bytes are copied to such rows, checkpoints are restored to them.
+struct Layout {
+    const void* from;                  // 16-bit values, or null: a checkpoint
+    CheckpointView held;
+    uint64_t from_stride;
+    uint16_t* to;                      // rows of `stride` values, a multiple of 8
+    uint64_t stride, n, total;         // chunks of 8 values
+    bool wide;                         // codes on 8-byte boundaries
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_lay_out(Layout first, Layout second, uint32_t first_blocks)
 {
     dependency_wait();
     dependency_release();
-    const uint64_t chunk = (uint64_t)blockIdx.x * 256 + threadIdx.x;          // 8 values
-    if (chunk >= total) return;
-    const uint64_t per_row = stride / 8, row = chunk / per_row, col = chunk % per_row * 8;
-    const uint16_t* src = from + row * from_stride + col;
-    uint32_t w[4];
+    const bool is_second = blockIdx.x >= first_blocks;
+    const Layout& l = is_second ? second : first;
+    const uint64_t chunk = (uint64_t)(blockIdx.x - (is_second ? first_blocks : 0)) * 256 + threadIdx.x;
+    if (chunk >= l.total) return;
+    const uint32_t per_row = (uint32_t)(l.stride / 8);
+    const uint64_t row = l.total <= 0xFFFFFFFFull ? (uint32_t)chunk / per_row : chunk / per_row;
+    const uint64_t col = (chunk - row * per_row) * 8;
+    const int count = (int)min((uint64_t)8, l.n - col);
+    uint4 out;
+    if (l.from) {
+        out = load_shifted_8((const uint16_t*)l.from + row * l.from_stride + col, count);
+    } else {
+        const int8_t* codes = l.held.codes + row * l.held.codes_stride + col;
+        const uint32_t e = l.held.exps[row * l.held.exps_stride + col / kGroup];
+        uint2 w = make_uint2(0, 0);
+        if (l.wide && count == 8) {
+            w = *(const uint2*)codes;
+        } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = col + 2 * i < n ? src[2 * i] : 0, hi = col + 2 * i + 1 < n ? src[2 * i + 1] : 0;
-        w[i] = lo | hi << 16;
+            for (int j = 0; j < 8; ++j)
+                if (j < count) (j < 4 ? w.x : w.y) |= (uint32_t)(uint8_t)codes[j] << 8 * (j % 4);
+        }
+        const Pair scale(group_scale(e));
+        Pair p[4];
+        code_values(w.x, scale, p[0], p[1]);
+        code_values(w.y, scale, p[2], p[3]);
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x, y;
+            p[j].get(x, y);
+            if (e >= kSaturates<T>) {
+                x = saturated<T>(x);
+                y = saturated<T>(y);
+            }
+            o[j] = pack<T>(x, y);
+        }
+        out = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    *(uint4*)(to + row * stride + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    *(uint4*)(l.to + row * l.stride + col) = out;
 }
 
 }  // namespace eden

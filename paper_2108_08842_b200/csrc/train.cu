@@ -171,27 +171,38 @@ int act_backward(eden_ctx* ctx, const eden_act_backward_args* a, float* partial,
         default: { constexpr int ACT_ = EDEN_ACT_NONE; CALL; } break;                           \
     }
 
-// A 16-bit operand of a product: `rows` rows of `n` values.
+// An operand of a product: `rows` rows of `n` 16-bit values, or (data null) a checkpoint of them.
 struct Operand {
     const void* data;
     uint64_t stride, rows, n;
+    CheckpointView held;
 };
 
-// Tensor copies want 16-byte aligned rows: others are copied into the workspace first.
-int align_operand(eden_ctx* ctx, Scratch& scratch, Operand& o)
+// Tensor copies want 16-byte aligned rows of values: other operands are laid out so in the
+// workspace first, both in one launch.
+template <typename T>
+int lay_out(eden_ctx* ctx, Scratch& scratch, Operand& a, Operand& b)
 {
-    if (o.rows == 1) o.stride = padded(o.n);
-    if (aligned(o.data, 16) && o.stride % 8 == 0) return EDEN_OK;
-    const uint64_t stride = padded(o.n), total = o.rows * (stride / 8), blocks = (total + 255) / 256;
-    if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    uint16_t* to = scratch.take<uint16_t>(o.rows * stride);
-    if (!to) return EDEN_ERR_WORKSPACE;
-    if (int rc = launch(ctx, "t_align_rows", 4.0 * o.rows * o.n, k_align_rows, dim3((uint32_t)blocks), 256, 0, 1, (const uint16_t*)o.data,
-                        o.stride, to, stride, o.n, total))
-        return rc;
-    o.data = to;
-    o.stride = stride;
-    return EDEN_OK;
+    Layout job[2] = {};
+    uint64_t blocks[2] = {0, 0};
+    double bytes = 0;
+    int n = 0;
+    for (Operand* o : {&a, &b}) {
+        if (o->data && o->rows == 1) o->stride = padded(o->n);
+        if (o->data && aligned(o->data, 16) && o->stride % 8 == 0) continue;
+        const uint64_t stride = padded(o->n), total = o->rows * (stride / 8);
+        uint16_t* to = scratch.take<uint16_t>(o->rows * stride);
+        if (!to) return EDEN_ERR_WORKSPACE;
+        job[n] = {o->data, o->held, o->stride, to, stride, o->n, total, aligned(o->held.codes, 8) && o->held.codes_stride % 8 == 0};
+        blocks[n] = (total + 255) / 256;
+        bytes += (double)o->rows * o->n * (o->data ? 4 : 3);
+        o->data = to;
+        o->stride = stride;
+        ++n;
+    }
+    if (n == 0) return EDEN_OK;
+    if (blocks[0] + blocks[1] > kMaxCount) return EDEN_ERR_TOO_LARGE;
+    return launch(ctx, "t_lay_out", bytes, k_lay_out<T>, dim3((uint32_t)(blocks[0] + blocks[1])), 256, 0, 1, job[0], job[1], (uint32_t)blocks[0]);
 }
 
 using EncodeMap = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -265,13 +276,21 @@ int launch_tiles(eden_ctx* ctx, const Product& q, uint32_t splits)
     }
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int R>
 int launch_few(eden_ctx* ctx, const Product& q)
 {
     const bool vec = aligned(q.a.data, 16) && aligned(q.b.data, 16) && q.depth % 8 == 0 && (q.a.stride % 8 == 0 || q.a.rows == 1) &&
                      (q.b.stride % 8 == 0 || q.b.rows == 1);
-    return launch(ctx, q.name, q.bytes, vec ? k_linear_few<T, NT, true> : k_linear_few<T, NT, false>, dim3((uint32_t)((q.p.cols + 15) / 16)),
-                  kFewThreads, 0, 1, (const T*)q.a.data, q.a.stride, (const T*)q.b.data, q.b.stride, q.depth, q.p);
+    return launch(ctx, q.name, q.bytes, vec ? k_linear_few<T, NT, R, true> : k_linear_few<T, NT, R, false>,
+                  dim3((uint32_t)((q.p.cols + 16 * R - 1) / (16 * R))), kFewThreads, 0, 1, (const T*)q.a.data, q.a.stride, (const T*)q.b.data,
+                  q.b.stride, q.depth, q.p);
+}
+
+template <typename T>
+int launch_few(eden_ctx* ctx, const Product& q)
+{
+    if (q.p.save) return q.p.rows <= 8 ? launch_few<T, 1, 2>(ctx, q) : q.p.rows <= 16 ? launch_few<T, 2, 2>(ctx, q) : launch_few<T, 4, 2>(ctx, q);
+    return q.p.rows <= 8 ? launch_few<T, 1, 1>(ctx, q) : q.p.rows <= 16 ? launch_few<T, 2, 1>(ctx, q) : launch_few<T, 4, 1>(ctx, q);
 }
 
 // How a product is cut up: a form (EDEN_LINEAR_*) and the parts of each tile's sum.
@@ -315,8 +334,7 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
 {
     const uint64_t steps = (q.depth + 63) / 64;
     const int form = ctx->linear_form;
-    if (OP == kForward && q.p.save == EDEN_SAVE_NONE && (form == EDEN_LINEAR_AUTO ? q.p.rows <= 16 : form == EDEN_LINEAR_FEW && q.p.rows <= 32))
-        return {EDEN_LINEAR_FEW, 1};
+    if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 16))) return {EDEN_LINEAR_FEW, 1};
     static const struct { int form; uint64_t rows, cols; uint32_t blocks; double fixed, step, finish, join; } tiles[] = {
         {EDEN_LINEAR_PAIR, 256, 256, 2, 6.8, 0.27, OP == kWeightGrad ? 3.5 : 2.2, 0.4},
         {EDEN_LINEAR_SINGLE, 128, 128, 1, 4.8, 0.233, OP == kWeightGrad ? 2.7 : 1.3, 0.55},
@@ -339,6 +357,11 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
             }
         }
     }
+    // 17 to 32 tokens: every block of the form for few reads all of x, at about 20 TB/s from the caches
+    if (OP == kForward && form == EDEN_LINEAR_AUTO && q.p.rows <= 32) {
+        const double few = 2.5 + (double)q.p.cols * q.depth * 2 / 5e6 + (double)((q.p.cols + 15) / 16) * q.p.rows * q.depth * 2 / 20e6;
+        if (few < least) best = {EDEN_LINEAR_FEW, 1};
+    }
     return best;
 }
 
@@ -347,14 +370,11 @@ int product(eden_ctx* ctx, Scratch& scratch, Product q)
 {
     const Cut cut = choose_cut<OP>(ctx, q);
     if constexpr (OP == kForward) {
-        if (cut.form == EDEN_LINEAR_FEW) {
-            if (q.p.rows <= 8) { EDEN_DISPATCH_HALF(q.type, return (launch_few<T_, 1>(ctx, q))); }
-            if (q.p.rows <= 16) { EDEN_DISPATCH_HALF(q.type, return (launch_few<T_, 2>(ctx, q))); }
-            EDEN_DISPATCH_HALF(q.type, return (launch_few<T_, 4>(ctx, q)));
-        }
+        if (cut.form == EDEN_LINEAR_FEW) { EDEN_DISPATCH_HALF(q.type, return launch_few<T_>(ctx, q)); }
     }
-    if (int rc = align_operand(ctx, scratch, q.a)) return rc;
-    if (int rc = align_operand(ctx, scratch, q.b)) return rc;
+    int rc = EDEN_OK;
+    EDEN_DISPATCH_HALF(q.type, rc = lay_out<T_>(ctx, scratch, q.a, q.b));
+    if (rc) return rc;
     LinearEpilogue& p = q.p;
     p.grain_out = row_grain(p.out, p.out_stride, OP == kWeightGrad ? 4 : 2);
     p.grain_residual = row_grain(p.residual, p.residual_stride, 2);
@@ -412,7 +432,7 @@ extern "C" int eden_linear(eden_ctx* ctx, const eden_linear_args* a)
                          view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride), nullptr, a->m, a->n, a->act, a->save, 0};
         const double bytes = 2.0 * ((double)a->m * a->k + (double)a->n * a->k + a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
                              (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
-        return product<kForward>(ctx, scratch, {"t_linear", a->type, {a->x, a->x_stride, a->m, a->k}, {a->weight, a->weight_stride, a->n, a->k},
+        return product<kForward>(ctx, scratch, {"t_linear", a->type, {a->x, a->x_stride, a->m, a->k, {}}, {a->weight, a->weight_stride, a->n, a->k, {}},
                                                 a->k, p, bytes});
     });
 }
@@ -503,8 +523,8 @@ extern "C" int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_gra
                              view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0};
             const double bytes = 2.0 * ((double)a->m * a->n + (double)a->n * a->k + (double)a->m * a->k * (a->residual ? 2 : 1)) +
                                  (a->act ? (double)a->m * (a->k + groups_of(a->k)) : 0.0);
-            if (int rc = product<kInputGrad>(ctx, scratch, {"t_input_grad", a->type, {a->dz, a->dz_stride, a->m, a->n},
-                                                            {a->weight, a->weight_stride, a->n, a->k}, a->n, p, bytes}))
+            if (int rc = product<kInputGrad>(ctx, scratch, {"t_input_grad", a->type, {a->dz, a->dz_stride, a->m, a->n, {}},
+                                                            {a->weight, a->weight_stride, a->n, a->k, {}}, a->n, p, bytes}))
                 return rc;
         }
         return a->bias_grad ? sum_columns(ctx, partial, runs, a->k, a->bias_grad, a->accumulate) : EDEN_OK;
@@ -528,20 +548,10 @@ extern "C" int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_g
             return EDEN_OK;
         }
         Scratch scratch(ctx);
-        Operand x{a->x, a->x_stride, a->m, a->k};
-        if (a->codes) {
-            x.stride = padded(a->k);
-            uint16_t* held = scratch.take<uint16_t>(a->m * x.stride);
-            if (!held) return EDEN_ERR_WORKSPACE;
-            const CheckpointView c = view(a->codes, a->codes_stride, a->exps, a->exps_stride);
-            int rc = EDEN_OK;
-            EDEN_DISPATCH_HALF(a->type, rc = restore(ctx, c, (T_*)held, x.stride, a->m, a->k));
-            if (rc) return rc;
-            x.data = held;
-        }
+        const Operand x{a->x, a->x_stride, a->m, a->k, view(a->codes, a->codes_stride, a->exps, a->exps_stride)};
         LinearEpilogue p{nullptr, nullptr, 0, a->weight_grad, a->weight_grad_stride, {}, nullptr, a->n, a->k, 0, 0, a->accumulate};
         const double bytes = 2.0 * a->m * a->n + (double)a->m * (a->codes ? a->k + groups_of(a->k) : 2 * a->k) +
                              4.0 * a->n * a->k * (a->accumulate ? 2 : 1);
-        return product<kWeightGrad>(ctx, scratch, {"t_weight_grad", a->type, {a->dz, a->dz_stride, a->m, a->n}, x, a->m, p, bytes});
+        return product<kWeightGrad>(ctx, scratch, {"t_weight_grad", a->type, {a->dz, a->dz_stride, a->m, a->n, {}}, x, a->m, p, bytes});
     });
 }

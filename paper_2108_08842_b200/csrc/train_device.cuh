@@ -295,6 +295,37 @@ __device__ __forceinline__ void store_32b(void* p, const uint32_t (&w)[8])
                  : "memory");
 }
 
+// 8 values of 16 bits that start anywhere, of which the first `count` exist (zeros after them):
+// the one or two aligned 16-byte chunks that hold them, shifted.  Chunks without a value of
+// theirs are not touched.
+__device__ __forceinline__ uint4 load_shifted_8(const void* p, int count)
+{
+    const uintptr_t address = (uintptr_t)p;
+    const uint32_t off = (uint32_t)address & 15u;
+    const uint4* chunk = (const uint4*)(address - off);
+    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+    if (count > 0) lo = chunk[0];
+    if ((int)off + 2 * count > 16) hi = chunk[1];
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (off & 8u) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (off & 4u) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (off & 2u) * 8;
+    uint32_t v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j] = __funnelshift_r(w[j], w[j + 1], bits);
+        const int left = count - 2 * j;                      // values from this word on
+        v[j] &= left >= 2 ? 0xFFFFFFFFu : left == 1 ? 0xFFFFu : 0u;
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 template <typename T>
 __device__ __forceinline__ void unpack(uint32_t w, float& lo, float& hi)
 {

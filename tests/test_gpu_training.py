@@ -231,7 +231,14 @@ def test_every_form_at_every_size(ctx, forced):
 @pytest.mark.parametrize("forced", [("LINEAR_FEW", 0)], indirect=True)
 @pytest.mark.parametrize("m,n,k,extra,offset", [(17, 100, 1000, 0, 0), (24, 33, 4104, 8, 8), (31, 64, 200, 1, 1), (32, 16, 5000, 0, 0), (33, 64, 64, 0, 0)])
 def test_few_tokens_form(ctx, forced, m, n, k, extra, offset):
-    check_linear(ctx, torch.bfloat16, m, n, k, "gelu_tanh", True, True, "none", extra, offset)
+    for save in ("none", "pre", "out"):
+        check_linear(ctx, torch.bfloat16, m, n, k, "gelu_tanh", True, True, save, extra, offset)
+
+
+@pytest.mark.parametrize("offset", range(8))
+@pytest.mark.parametrize("m,k", [(1, 1001), (2, 1002), (3, 517), (9, 1028), (12, 71), (40, 333), (40, 334)])
+def test_linear_rows_at_every_alignment(ctx, m, k, offset):
+    check_linear(ctx, torch.float16, m, 50, k, "none", True, False, "pre" if offset % 2 else "none", 0, offset, seed=k)
 
 
 # ------------------------------------------------------------------------------- backward
