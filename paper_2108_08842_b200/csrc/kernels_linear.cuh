@@ -605,7 +605,10 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 // in turn, all loads of up to four steps on their way together, straight to registers in the
 // layout of the 16 x 8 x 16 product: the sum's index may be permuted alike in W and in x, so
 // each lane loads 16 consecutive bytes and feeds them as the fragments of two products.  The
-// 16 warps' sums are added in their order.  R = 2 where groups of 32 results are saved.
+// 16 warps' sums are added in their order.  R = 2 where groups of 32 results are saved.  Where
+// few rows of W meet a long sum, a cluster of blocks shares it: each block adds up its warps, and
+// the first one adds the blocks' sums, out of their shared memory, in their order (SHARED; the
+// same code with a cluster of one block took 7.4 us where this takes 4.8).
 // 1 x 4096 x 4096 bf16: FEW1 us with the weights in the L2 cache, of which 5.1 are HBM's floor.
 constexpr int kFewThreads = 512;
 
@@ -628,7 +631,7 @@ __device__ __forceinline__ void few_product(float (&c)[4], uint32_t a0, uint32_t
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <typename T, int NT, int R, bool VEC>
+template <typename T, int NT, int R, bool VEC, bool SHARED>
 __global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t x_stride, const T* w, uint64_t w_stride, uint32_t k,
                                                            LinearEpilogue p)
 {
@@ -646,7 +649,15 @@ __global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t
 #pragma unroll
         for (int i = 0; i < NT; ++i) c[r][i][0] = c[r][i][1] = c[r][i][2] = c[r][i][3] = 0.f;
 
-    for (uint32_t k0 = warp * 64; k0 < k; k0 += kWarps * 64 * kAhead) {
+    uint32_t blocks = 1, part = 0, first_step = 0;                          // of the cluster: 2, 4 or 8
+    if constexpr (SHARED) {
+        blocks = gridDim.y;
+        part = blockIdx.y;
+        const uint32_t steps = (k + 63) / 64, shift = 31 - __clz(blocks);
+        first_step = steps * part >> shift;
+        k = min(k, (steps * (part + 1) >> shift) * 64);
+    }
+    for (uint32_t k0 = (first_step + warp) * 64; k0 < k; k0 += kWarps * 64 * kAhead) {
         uint4 a[kAhead][2][2 * R], b[kAhead][NT][2];
 #pragma unroll
         for (int s = 0; s < kAhead; ++s)
@@ -675,11 +686,11 @@ __global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t
                         few_product<T>(c[r][i], u.z, v.z, u.w, v.w, z.z, z.w);
                     }
     }
-    // eight tokens at a time, [warp][token][row of W]
+    // eight tokens at a time, [warp][token][row of W]; warp 0's place then takes the block's sums
     __shared__ float sums[kWarps][8][16 * R + 1];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        if (8 * i >= p.rows) return;
+        if (8 * i >= p.rows) break;                        // alike in all blocks of a cluster
         if (i > 0) __syncthreads();
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -689,29 +700,42 @@ __global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t
             sums[warp][2 * t + 1][16 * r + g + 8] = c[r][i][3];
         }
         __syncthreads();
-        if (threadIdx.x >= 128 * R) continue;
+        const bool mine = threadIdx.x < 128 * R;
         const uint32_t in_tile = threadIdx.x / (16 * R), in = threadIdx.x % (16 * R), token = 8 * i + in_tile;
-        const uint64_t col = n0 + in;
-        const bool live = token < p.rows && col < p.cols;
         float v = 0.f;
+        if (mine) {
 #pragma unroll
-        for (int j = 0; j < kWarps; ++j) v += sums[j][in_tile][in];
-        if (p.bias && live) v += to_float(((const T*)p.bias)[col]);
-        auto save = [&]() {                                // R = 2: the warp holds a token's group
-            const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, live ? magnitude_bits(v) : 0u));
-            if (!live) return;
-            p.ckpt.codes[token * p.ckpt.codes_stride + col] = (int8_t)group_code(v, group_inverse(e));
-            if (in == 0) p.ckpt.exps[token * p.ckpt.exps_stride + n0 / kGroup] = (uint8_t)e;
-        };
-        if (R == 2 && p.save == EDEN_SAVE_PRE) save();
-        with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
-        if (p.residual && live) v += to_float(((const T*)p.residual)[token * p.residual_stride + col]);
-        const T y = from_float<T>(v);
-        if (R == 2 && p.save == EDEN_SAVE_OUT) {
-            v = to_float(y);
-            save();
+            for (int j = 0; j < kWarps; ++j) v += sums[j][in_tile][in];
         }
-        if (live) ((T*)p.out)[token * p.out_stride + col] = y;
+        if constexpr (SHARED) {
+            if (mine) sums[0][in_tile][in] = v;            // its own reader's value: no other thread's
+            cluster_arrive_wait();
+            if (mine && part == 0 && token < p.rows) {     // what is fetched is stored, and so waited for
+                for (uint32_t j = 1; j < blocks; ++j) v += cluster_load(address_in(shared_address(&sums[0][in_tile][in]), j));
+            }
+        }
+        if (mine && part == 0) {
+            const uint64_t col = n0 + in;
+            const bool live = token < p.rows && col < p.cols;
+            if (p.bias && live) v += to_float(((const T*)p.bias)[col]);
+            auto save = [&]() {                            // R = 2: the warp holds a token's group
+                const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, live ? magnitude_bits(v) : 0u));
+                if (!live) return;
+                p.ckpt.codes[token * p.ckpt.codes_stride + col] = (int8_t)group_code(v, group_inverse(e));
+                if (in == 0) p.ckpt.exps[token * p.ckpt.exps_stride + n0 / kGroup] = (uint8_t)e;
+            };
+            if (R == 2 && p.save == EDEN_SAVE_PRE) save();
+            with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
+            if (p.residual && live) v += to_float(((const T*)p.residual)[token * p.residual_stride + col]);
+            const T y = from_float<T>(v);
+            if (R == 2 && p.save == EDEN_SAVE_OUT) {
+                v = to_float(y);
+                save();
+            }
+            if (live) ((T*)p.out)[token * p.out_stride + col] = y;
+        }
+        // the sums were used (also where nothing was stored) before their blocks go on
+        if constexpr (SHARED) cluster_arrive_wait();
     }
 }
 
@@ -722,9 +746,9 @@ struct Layout {
     const void* from;                  // 16-bit values, or null: a checkpoint
     CheckpointView held;
     uint64_t from_stride;
-    uint16_t* to;                      // rows of `stride` values, a multiple of 8
-    uint64_t stride, n, total;         // chunks of 8 values
-    bool wide;                         // codes on 8-byte boundaries
+    uint16_t* to;                      // rows of `stride` values, a multiple of 16, on 32 bytes
+    uint64_t stride, n, total;         // chunks of 16 values
+    bool wide;                         // codes on 16-byte boundaries
 };
 
 template <typename T>
@@ -736,42 +760,37 @@ __global__ void __launch_bounds__(256) k_lay_out(Layout first, Layout second, ui
     const Layout& l = is_second ? second : first;
     const uint64_t chunk = (uint64_t)(blockIdx.x - (is_second ? first_blocks : 0)) * 256 + threadIdx.x;
     if (chunk >= l.total) return;
-    const uint32_t per_row = (uint32_t)(l.stride / 8);
+    const uint32_t per_row = (uint32_t)(l.stride / 16);
     const uint64_t row = l.total <= 0xFFFFFFFFull ? (uint32_t)chunk / per_row : chunk / per_row;
-    const uint64_t col = (chunk - row * per_row) * 8;
-    const int count = (int)min((uint64_t)8, l.n - col);
-    uint4 out;
+    const uint64_t col = (chunk - row * per_row) * 16;
+    const int count = (int)min((uint64_t)16, l.n - col);
+    uint32_t out[8];
     if (l.from) {
-        out = load_shifted_8((const uint16_t*)l.from + row * l.from_stride + col, count);
+        load_shifted((const uint16_t*)l.from + row * l.from_stride + col, 2 * count, out);
     } else {
         const int8_t* codes = l.held.codes + row * l.held.codes_stride + col;
         const uint32_t e = l.held.exps[row * l.held.exps_stride + col / kGroup];
-        uint2 w = make_uint2(0, 0);
-        if (l.wide && count == 8) {
-            w = *(const uint2*)codes;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < count) (j < 4 ? w.x : w.y) |= (uint32_t)(uint8_t)codes[j] << 8 * (j % 4);
-        }
+        uint32_t w[4];
+        if (l.wide && count == 16) *(uint4*)w = *(const uint4*)codes;
+        else load_shifted(codes, count, w);
         const Pair scale(group_scale(e));
-        Pair p[4];
-        code_values(w.x, scale, p[0], p[1]);
-        code_values(w.y, scale, p[2], p[3]);
-        uint32_t o[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float x, y;
-            p[j].get(x, y);
-            if (e >= kSaturates<T>) {
-                x = saturated<T>(x);
-                y = saturated<T>(y);
+            Pair p[2];
+            code_values(w[j], scale, p[0], p[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float x, y;
+                p[i].get(x, y);
+                if (e >= kSaturates<T>) {
+                    x = saturated<T>(x);
+                    y = saturated<T>(y);
+                }
+                out[2 * j + i] = pack<T>(x, y);
             }
-            o[j] = pack<T>(x, y);
         }
-        out = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    *(uint4*)(l.to + row * l.stride + col) = out;
+    store_32b(l.to + row * l.stride + col, out);
 }
 
 }  // namespace eden

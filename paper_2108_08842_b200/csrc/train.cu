@@ -17,7 +17,7 @@ constexpr uint64_t kMaxRuns = 512;              // runs of rows that leave parti
 
 uint64_t align_to(uint64_t v, uint64_t a) { return (v + a - 1) / a * a; }
 uint64_t groups_of(uint64_t n) { return (n + kGroup - 1) / kGroup; }
-uint64_t padded(uint64_t n) { return align_to(n, 8); }           // 16-byte rows of a 16-bit matrix
+uint64_t padded(uint64_t n) { return align_to(n, 16); }          // 32-byte rows of a 16-bit matrix
 
 // The caller's current device stays what it was.
 struct DeviceGuard {
@@ -84,7 +84,8 @@ CheckpointView view(const int8_t* codes, uint64_t cs, const uint8_t* exps, uint6
 }
 
 // A launch that may begin before the stream's previous kernel has ended: the kernels of this
-// file wait for it themselves (dependency_wait).  cluster = blocks per cluster.
+// file wait for it themselves (dependency_wait).  cluster = blocks per cluster, along x, or along
+// y where the grid is that high.
 template <typename... KArgs, typename... Args>
 int launch(eden_ctx* ctx, const char* name, double bytes, void (*kernel)(KArgs...), dim3 grid, uint32_t block, uint32_t shared,
            uint32_t cluster, Args&&... args)
@@ -98,7 +99,7 @@ int launch(eden_ctx* ctx, const char* name, double bytes, void (*kernel)(KArgs..
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim = {cluster, 1, 1};
+    attr[1].val.clusterDim = {grid.y == cluster ? 1 : cluster, grid.y == cluster ? cluster : 1, 1};
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     profile_begin(ctx, name, bytes);
@@ -115,42 +116,35 @@ int sum_columns(eden_ctx* ctx, const float* partial, uint64_t rows, uint64_t n, 
                   partial, rows, n, out, accumulate);
 }
 
-// Rows on 32-byte boundaries and codes on 16-byte ones take the wide kernels: on 16384 x 4096
-// bf16 they restore in WIDE us against NARROW us for one value per lane.
-bool wide_checkpoint(const void* x, uint64_t x_stride, size_t size, const CheckpointView& c)
-{
-    return aligned(x, 32) && x_stride * size % 32 == 0 && aligned(c.codes, 16) && c.codes_stride % 16 == 0;
-}
+// The kernels' WIDE forms: rows of values on 32-byte boundaries, rows of codes on 16-byte ones.
+// 16384 x 4096 bf16 is saved and restored in 65 us by them, in NARROW us by the others.
+bool wide_codes(const CheckpointView& c) { return aligned(c.codes, 16) && c.codes_stride % 16 == 0; }
 
 template <typename T>
 int save(eden_ctx* ctx, const T* x, uint64_t x_stride, CheckpointView c, uint64_t m, uint64_t n)
 {
-    const uint64_t groups = groups_of(n);
-    const double bytes = (double)m * (n * (1.0 + sizeof(T)) + groups);
-    if (wide_checkpoint(x, x_stride, sizeof(T), c)) {
-        const uint64_t total = m * groups * 2, blocks = (total + kCkptThreads - 1) / kCkptThreads;
-        if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
-        return launch(ctx, "t_save", bytes, k_checkpoint_save_wide<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n, groups * 2, total);
-    }
-    const uint64_t total = m * groups, blocks = (total + 8 * kGroupsInFlight - 1) / (8 * kGroupsInFlight);
+    const uint64_t groups = groups_of(n), total = m * groups * 2, blocks = (total + kCkptThreads - 1) / kCkptThreads;
     if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    return launch(ctx, "t_save", bytes, k_checkpoint_save<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n, groups, total);
+    const bool wide = wide_rows(x, x_stride, sizeof(T)) && wide_codes(c);
+    return launch(ctx, "t_save", (double)m * (n * (1.0 + sizeof(T)) + groups), wide ? k_checkpoint_save<T, true> : k_checkpoint_save<T, false>,
+                  dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n, groups * 2, total);
 }
 
 template <typename T>
 int restore(eden_ctx* ctx, CheckpointView c, T* x, uint64_t x_stride, uint64_t m, uint64_t n)
 {
-    const uint64_t groups = groups_of(n);
-    const double bytes = (double)m * (n * (1.0 + sizeof(T)) + groups);
-    if (wide_checkpoint(x, x_stride, sizeof(T), c)) {
-        const uint64_t total = m * groups * 2, blocks = (total + kCkptThreads - 1) / kCkptThreads;
-        if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
-        return launch(ctx, "t_restore", bytes, k_checkpoint_restore_wide<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n,
-                      groups * 2, total);
-    }
-    const uint64_t total = m * groups, blocks = (total + 8 * kGroupsInFlight - 1) / (8 * kGroupsInFlight);
+    const uint64_t groups = groups_of(n), total = m * groups * 2, blocks = (total + kCkptThreads - 1) / kCkptThreads;
     if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    return launch(ctx, "t_restore", bytes, k_checkpoint_restore<T>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c, n, groups, total);
+    const bool wide = wide_rows(x, x_stride, sizeof(T)) && wide_codes(c);
+    return launch(ctx, "t_restore", (double)m * (n * (1.0 + sizeof(T)) + groups),
+                  wide ? k_checkpoint_restore<T, true> : k_checkpoint_restore<T, false>, dim3((uint32_t)blocks), kCkptThreads, 0, 1, x, x_stride, c,
+                  n, groups * 2, total);
+}
+
+bool wide_backward(const eden_act_backward_args* a)
+{
+    return wide_rows(a->dy, a->dy_stride, 2) && (!a->dz || wide_rows(a->dz, a->dz_stride, 2)) &&
+           (a->act == EDEN_ACT_NONE || wide_codes(view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride)));
 }
 
 template <typename T, int ACT>
@@ -190,10 +184,10 @@ int lay_out(eden_ctx* ctx, Scratch& scratch, Operand& a, Operand& b)
     for (Operand* o : {&a, &b}) {
         if (o->data && o->rows == 1) o->stride = padded(o->n);
         if (o->data && aligned(o->data, 16) && o->stride % 8 == 0) continue;
-        const uint64_t stride = padded(o->n), total = o->rows * (stride / 8);
+        const uint64_t stride = padded(o->n), total = o->rows * (stride / 16);
         uint16_t* to = scratch.take<uint16_t>(o->rows * stride);
         if (!to) return EDEN_ERR_WORKSPACE;
-        job[n] = {o->data, o->held, o->stride, to, stride, o->n, total, aligned(o->held.codes, 8) && o->held.codes_stride % 8 == 0};
+        job[n] = {o->data, o->held, o->stride, to, stride, o->n, total, aligned(o->held.codes, 16) && o->held.codes_stride % 16 == 0};
         blocks[n] = (total + 255) / 256;
         bytes += (double)o->rows * o->n * (o->data ? 4 : 3);
         o->data = to;
@@ -281,9 +275,14 @@ int launch_few(eden_ctx* ctx, const Product& q)
 {
     const bool vec = aligned(q.a.data, 16) && aligned(q.b.data, 16) && q.depth % 8 == 0 && (q.a.stride % 8 == 0 || q.a.rows == 1) &&
                      (q.b.stride % 8 == 0 || q.b.rows == 1);
-    return launch(ctx, q.name, q.bytes, vec ? k_linear_few<T, NT, R, true> : k_linear_few<T, NT, R, false>,
-                  dim3((uint32_t)((q.p.cols + 16 * R - 1) / (16 * R))), kFewThreads, 0, 1, (const T*)q.a.data, q.a.stride, (const T*)q.b.data,
-                  q.b.stride, q.depth, q.p);
+    // a block for each SM where there are fewer rows of W than that, as long as its warps have a step each
+    const uint64_t blocks = (q.p.cols + 16 * R - 1) / (16 * R);
+    uint32_t parts = 1;
+    while (parts < 8 && blocks * parts * 2 <= (uint64_t)ctx->sm_count && (q.depth + 63) / 64 >= 16 * 2 * parts) parts *= 2;
+    const auto kernel = parts > 1 ? (vec ? k_linear_few<T, NT, R, true, true> : k_linear_few<T, NT, R, false, true>)
+                                  : (vec ? k_linear_few<T, NT, R, true, false> : k_linear_few<T, NT, R, false, false>);
+    return launch(ctx, q.name, q.bytes, kernel, dim3((uint32_t)blocks, parts), kFewThreads, 0, parts, (const T*)q.a.data, q.a.stride,
+                  (const T*)q.b.data, q.b.stride, q.depth, q.p);
 }
 
 template <typename T>
@@ -478,10 +477,8 @@ extern "C" int eden_act_backward(eden_ctx* ctx, const eden_act_backward_args* a)
         uint64_t runs = 0;
         float* partial = nullptr;
         if (a->m > 0 && (a->dz || a->bias_grad)) {
-            const CheckpointView c = view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride);
-            const bool wide = wide_rows(a->dy, a->dy_stride, 2) && (!a->dz || wide_rows(a->dz, a->dz_stride, 2)) &&
-                              (!a->act || (aligned(c.codes, 16) && c.codes_stride % 16 == 0));
             // about six blocks of eight warps for each SM, at least 8 rows (one per warp) to a run
+            const bool wide = wide_backward(a);
             const uint64_t strips = wide ? (a->n + 511) / 512 : groups_of(a->n);
             const uint64_t want = std::min<uint64_t>(kMaxRuns, std::max<uint64_t>(1, 6ull * ctx->sm_count / strips));
             const uint64_t rows_per_run = std::max<uint64_t>(8, (a->m + want - 1) / want);

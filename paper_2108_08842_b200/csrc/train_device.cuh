@@ -295,9 +295,64 @@ __device__ __forceinline__ void store_32b(void* p, const uint32_t (&w)[8])
                  : "memory");
 }
 
-// 8 values of 16 bits that start anywhere, of which the first `count` exist (zeros after them):
-// the one or two aligned 16-byte chunks that hold them, shifted.  Chunks without a value of
-// theirs are not touched.
+// ---- accesses at any address ----------------------------------------------------------
+// WORDS words from p on, of which the first `bytes` bytes exist (zeros after them): the aligned
+// 16-byte chunks that hold them, shifted.  Chunks without a byte of theirs are not touched.
+template <int WORDS>
+__device__ __forceinline__ void load_shifted(const void* p, int bytes, uint32_t (&v)[WORDS])
+{
+    const uintptr_t address = (uintptr_t)p;
+    const int off = (int)(address & 15u);
+    const uint4* chunk = (const uint4*)(address - off);
+    uint32_t w[WORDS + 4];
+#pragma unroll
+    for (int i = 0; i <= WORDS / 4; ++i) {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (bytes > 0 && off + bytes > 16 * i) q = chunk[i];
+        w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+    }
+    if (off & 8) {
+#pragma unroll
+        for (int i = 0; i < WORDS + 2; ++i) w[i] = w[i + 2];
+    }
+    if (off & 4) {
+#pragma unroll
+        for (int i = 0; i < WORDS + 1; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (off & 3) * 8;
+#pragma unroll
+    for (int j = 0; j < WORDS; ++j) v[j] = __funnelshift_r(w[j], w[j + 1], bits);
+    if (bytes < 4 * WORDS) {
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) {
+            const int left = bytes - 4 * j;
+            v[j] = left >= 4 ? v[j] : left > 0 ? v[j] & (0xFFFFFFFFu >> (32 - 8 * left)) : 0u;
+        }
+    }
+}
+
+// The first `bytes` bytes of v to p, in words where they are whole, in bytes at the ends.
+template <int WORDS>
+__device__ __forceinline__ void store_shifted(void* p, int bytes, const uint32_t (&v)[WORDS])
+{
+    const int off = (int)((uintptr_t)p & 3u);
+    char* base = (char*)p - off;
+#pragma unroll
+    for (int j = 0; j <= WORDS; ++j) {
+        const uint32_t w = __funnelshift_l(j > 0 ? v[j - 1] : 0u, j < WORDS ? v[j] : 0u, 8 * off);
+        const int first = 4 * j - off;                       // byte of v at the word's start
+        if (first >= 0 && first + 4 <= bytes) {
+            *(uint32_t*)(base + 4 * j) = w;
+        } else if (first + 4 > 0 && first < bytes) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (first + i >= 0 && first + i < bytes) base[4 * j + i] = (char)(w >> 8 * i);
+        }
+    }
+}
+
+// The same for 8 values of 16 bits, of which `count` exist, without a branch: several calls' loads
+// are on their way together (94 us for 4 x 12544 x 6046 through load_shifted, 67 through this).
 __device__ __forceinline__ uint4 load_shifted_8(const void* p, int count)
 {
     const uintptr_t address = (uintptr_t)p;
@@ -307,21 +362,16 @@ __device__ __forceinline__ uint4 load_shifted_8(const void* p, int count)
     if (count > 0) lo = chunk[0];
     if ((int)off + 2 * count > 16) hi = chunk[1];
     uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    if (off & 8u) {
 #pragma unroll
-        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-    }
-    if (off & 4u) {
+    for (int i = 0; i < 6; ++i) w[i] = off & 8u ? w[i + 2] : w[i];
 #pragma unroll
-        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-    }
+    for (int i = 0; i < 5; ++i) w[i] = off & 4u ? w[i + 1] : w[i];
     const uint32_t bits = (off & 2u) * 8;
     uint32_t v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        v[j] = __funnelshift_r(w[j], w[j + 1], bits);
         const int left = count - 2 * j;                      // values from this word on
-        v[j] &= left >= 2 ? 0xFFFFFFFFu : left == 1 ? 0xFFFFu : 0u;
+        v[j] = __funnelshift_r(w[j], w[j + 1], bits) & (left >= 2 ? 0xFFFFFFFFu : left == 1 ? 0xFFFFu : 0u);
     }
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
