@@ -10,6 +10,9 @@
 
 #include "../../include/eden.h"
 
+// the smallest workspace that eden_create takes
+uint64_t least_workspace();
+
 struct ProfileRecord {
     const char* name;
     double bytes;                    // algorithmic bytes of this launch

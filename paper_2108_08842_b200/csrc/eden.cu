@@ -276,6 +276,8 @@ uint64_t per_client_bytes() { return align_up(sizeof(ClientDesc), 16) + align_up
 
 }  // namespace
 
+uint64_t least_workspace() { return fixed_layout(1).end; }
+
 extern "C" uint64_t eden_workspace_bytes(uint64_t d_max, uint32_t n_batch)
 {
     if (n_batch == 0) n_batch = 1;

@@ -410,7 +410,7 @@ extern "C" uint64_t eden_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t
     // codes), and the partial column sums
     const uint64_t mn = m * padded(n) * 2, mk = m * padded(k) * 2, nk = n * padded(k) * 2;
     const uint64_t sums = std::max(std::max<uint64_t>((m + 31) / 32, 1) * k, kMaxRuns * n) * 4;
-    return kStatusBytes + std::max(mk + nk, std::max(mn + nk, mn + mk)) + sums + 4 * 256;
+    return std::max(least_workspace(), kStatusBytes + std::max(mk + nk, std::max(mn + nk, mn + mk)) + sums + 4 * 256);
 }
 
 extern "C" int eden_linear(eden_ctx* ctx, const eden_linear_args* a)
