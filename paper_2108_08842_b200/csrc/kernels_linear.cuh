@@ -349,9 +349,12 @@ struct LinearShape {
 };
 
 // The tensor cores cut off what their fp32 sums cannot hold, always towards zero, so long sums
-// drift: 512 products of 16 left fp32 weight gradients 4e-6 off.  Those sums are taken out of
-// tensor memory every kPromote steps of 64 and added up in registers, rounded to nearest,
-// while the next ones run: PROMOTED off, and no time.  16-bit results do not show the drift.
+// drift: 512 products of 16 left fp32 weight gradients 4e-6 off.  Where a result of 32 bits comes
+// of them (weight gradients, the column sums of input gradients) they are taken out of tensor
+// memory every kPromote steps of 64 and added up in registers, rounded to nearest, while the next
+// ones run: 5e-7 off, and within 3 % of the time (187 to 195 us for 4096 x 4096 over 8191 tokens).
+// 16-bit results do not show the drift.  RUNS: a kernel of its own, since its registers cost the
+// others' epilogue time (input gradient of 1999 x 1000 x 2731 with relu 37 against 43 us).
 constexpr uint32_t kPromote = 16;
 
 // D = A B^T for tiles of 128 * CG x BN, persistent: block (pair) c takes tiles c, c + blocks, ...
@@ -367,14 +370,13 @@ constexpr uint32_t kPromote = 16;
 // SPLIT: one tile per cluster.  Its blocks (pairs) take a part of the sum each, leave their
 // sums in shared memory, and then every block joins and finishes a share of the tile's 32 x 32
 // pieces, adding the parts in their order.
-template <int OP, typename T, int CG, int BN, bool SPLIT>
+template <int OP, typename T, int CG, int BN, bool SPLIT, bool RUNS>
 __global__ void __launch_bounds__(LinearShape<CG, BN>::kThreads, 1)
 k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, LinearEpilogue p, TileGrid grid,
          uint32_t* status)
 {
     using S = LinearShape<CG, BN>;
     constexpr bool a_mn = OP == kWeightGrad, b_mn = OP != kForward;
-    constexpr uint32_t kRun = OP == kWeightGrad ? kPromote : 1u << 30;      // steps summed in tensor memory
     constexpr uint32_t descriptor = product_descriptor(std::is_same_v<T, __nv_bfloat16>, a_mn, b_mn, 128 * CG, BN);
 
     extern __shared__ __align__(1024) char raw[];          // tiles of 128-byte rows swizzle by address bits 7 to 9
@@ -388,6 +390,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     const uint32_t first = blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
     const uint32_t depth_begin = (uint32_t)((uint64_t)grid.depth_steps * part / splits);
     const uint32_t depth_end = (uint32_t)((uint64_t)grid.depth_steps * (part + 1) / splits);
+    constexpr uint32_t run = RUNS ? kPromote : 1u << 30;                    // steps summed in tensor memory
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
@@ -463,8 +466,8 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             const uint32_t low_a = descriptor_low(base), low_b = descriptor_low(base + S::kBytesA);
             uint32_t a = low_a, b = low_b;
             for (uint32_t t = first; t < grid.count && ok; t += step) {
-                for (uint32_t part_begin = depth_begin; part_begin < depth_end && ok; part_begin += kRun) {
-                    const uint32_t d_address = sums + half * BN, part_end = depth_end - part_begin < kRun ? depth_end : part_begin + kRun;
+                for (uint32_t part_begin = depth_begin; part_begin < depth_end && ok; part_begin += run) {
+                    const uint32_t d_address = sums + half * BN, part_end = depth_end - part_begin < run ? depth_end : part_begin + run;
                     if (!(ok = barrier_wait(sums_empty + 8 * half, half_phase))) break;
                     tmem_fence_after();
                     for (uint32_t d = part_begin; d < part_end; ++d) {
@@ -527,11 +530,13 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                     }
                 }
             };
-            if constexpr (OP == kWeightGrad) {
+            if (RUNS && depth_end - depth_begin > run) {
+                // the runs added up, and the total put back in the last one's place
                 float total[S::kPieces][32];
-                for (uint32_t part_begin = depth_begin; part_begin < depth_end; part_begin += kRun) {
+                for (uint32_t part_begin = depth_begin;; part_begin += run) {
                     if (!(ok = barrier_wait(sums_full + 8 * half, phase))) break;
                     tmem_fence_after();
+                    const bool last = depth_end - part_begin <= run;
 #pragma unroll
                     for (int c = 0; c < S::kPieces; ++c) {
                         float v[32];
@@ -541,28 +546,28 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                             const Pair sum = part_begin == depth_begin ? Pair(v[j], v[j + 1]) : Pair(total[c][j], total[c][j + 1]) + Pair(v[j], v[j + 1]);
                             sum.get(total[c][j], total[c][j + 1]);
                         }
+                        if (last) tmem_store(my_sums + half * BN + 32 * c, total[c]);
                     }
+                    if (last) break;
                     release();
                     half ^= 1;
                     phase ^= half ^ 1;
                 }
-                if (!ok) break;
-#pragma unroll
-                for (int c = 0; c < S::kPieces; ++c) finish(total[c], c);
             } else {
-                if (!(ok = barrier_wait(sums_full + 8 * half, phase))) break;
-                tmem_fence_after();
-#pragma unroll 1
-                for (int c = 0; c < S::kPieces; ++c) {
-                    float v[32];
-                    __syncwarp();
-                    tmem_load(my_sums + half * BN + 32 * c, v);
-                    if (c == S::kPieces - 1) release();
-                    finish(v, c);
-                }
-                half ^= 1;
-                phase ^= half ^ 1;
+                ok = barrier_wait(sums_full + 8 * half, phase);
             }
+            if (!ok) break;
+            tmem_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < S::kPieces; ++c) {
+                float v[32];
+                __syncwarp();
+                tmem_load(my_sums + half * BN + 32 * c, v);
+                if (c == S::kPieces - 1) release();
+                finish(v, c);
+            }
+            half ^= 1;
+            phase ^= half ^ 1;
         }
         __syncwarp();
         if constexpr (SPLIT) {

@@ -243,7 +243,7 @@ int row_grain(const void* p, uint64_t stride, size_t size)
     return (int)(bits & (0 - bits));
 }
 
-template <int OP, typename T, int CG, int BN, bool SPLIT>
+template <int OP, typename T, int CG, int BN, bool SPLIT, bool RUNS>
 int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
 {
     using S = LinearShape<CG, BN>;
@@ -253,20 +253,29 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
     const uint64_t rows = (q.p.rows + 128 * CG - 1) / (128 * CG), cols = (q.p.cols + BN - 1) / BN;
     if (rows * cols * CG * splits > kMaxCount) return EDEN_ERR_TOO_LARGE;
     const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((q.depth + 63) / 64), splits};
-    const auto kernel = k_linear<OP, T, CG, BN, SPLIT>;
+    const auto kernel = k_linear<OP, T, CG, BN, SPLIT, RUNS>;
     CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
     const uint32_t groups = (uint32_t)(SPLIT ? rows * cols : std::min<uint64_t>(rows * cols, ctx->sm_count / CG));
     return launch(ctx, q.name, q.bytes, kernel, dim3(groups * CG * splits), S::kThreads, S::kSharedBytes, CG * splits, map_a, map_b, q.p,
                   grid, (uint32_t*)ctx->ws);
 }
 
+template <int OP, typename T, int CG, int BN, bool SPLIT>
+int launch_runs(eden_ctx* ctx, const Product& q, uint32_t splits)
+{
+    if constexpr (OP == kInputGrad) {
+        if (!q.p.column_sums || (q.depth + 63) / 64 <= (uint64_t)kPromote * splits) return launch_linear<OP, T, CG, BN, SPLIT, false>(ctx, q, splits);
+    }
+    return launch_linear<OP, T, CG, BN, SPLIT, OP != kForward>(ctx, q, splits);
+}
+
 template <int OP, int CG, int BN>
 int launch_tiles(eden_ctx* ctx, const Product& q, uint32_t splits)
 {
     if (splits > 1) {
-        EDEN_DISPATCH_HALF(q.type, return (launch_linear<OP, T_, CG, BN, true>(ctx, q, splits)));
+        EDEN_DISPATCH_HALF(q.type, return (launch_runs<OP, T_, CG, BN, true>(ctx, q, splits)));
     } else {
-        EDEN_DISPATCH_HALF(q.type, return (launch_linear<OP, T_, CG, BN, false>(ctx, q, 1)));
+        EDEN_DISPATCH_HALF(q.type, return (launch_runs<OP, T_, CG, BN, false>(ctx, q, 1)));
     }
 }
 
@@ -304,7 +313,7 @@ int cluster_slots(eden_ctx* ctx, uint32_t cluster)
 {
     int& known = ctx->cluster_slots[cluster];
     if (known > 0) return known;
-    const auto kernel = k_linear<kForward, __nv_bfloat16, 1, 128, true>;
+    const auto kernel = k_linear<kForward, __nv_bfloat16, 1, 128, true, false>;
     using S = LinearShape<1, 128>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(cluster * ctx->sm_count);
