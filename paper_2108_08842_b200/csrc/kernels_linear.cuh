@@ -319,7 +319,7 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], const Piece& at,
 // column by column, so that the tiles in flight share few rows of A and of B in the L2 cache.
 struct TileGrid {
     uint32_t rows, cols, count;        // tiles
-    uint32_t depth_steps;              // steps of 64 along the sum
+    uint32_t depth_steps;              // steps of the shape's kDepth along the sum
     uint32_t splits;                   // parts of the sum, one block (pair) of a cluster each
 };
 
@@ -333,13 +333,17 @@ __device__ __forceinline__ void tile_at(const TileGrid& g, uint32_t t, uint32_t&
     col = in_band / height;
 }
 
-// Shape of a block's share of a tile: 128 rows of A and BN / CG rows of B per step of 64.  Each
-// of the four quarters of its 128 rows of sums has kSides epilogue warps side by side.
+// Shape of a block's share of a tile: 128 rows of A and BN / CG rows of B per step along the sum.
+// Each of the four quarters of its 128 rows of sums has kSides epilogue warps side by side.  A
+// step is one box of 64 for pairs, whose four products outlast their issue (512 cycles), and two
+// for single blocks: waiting for a stage, releasing it and issuing four products takes 410 to 440
+// cycles whatever their size, of which 180 are the stage's.
 template <int CG, int BN>
 struct LinearShape {
-    static constexpr int kRowsB = BN / CG;
-    static constexpr uint32_t kBytesA = 128 * 128, kBytesB = kRowsB * 128, kStageBytes = kBytesA + kBytesB;
-    static constexpr int kStages = 6;
+    static constexpr int kRowsB = BN / CG, kBoxes = CG == 1 ? 2 : 1, kDepth = 64 * kBoxes;
+    static constexpr uint32_t kBoxA = 128 * 128, kBoxB = kRowsB * 128;
+    static constexpr uint32_t kBytesA = kBoxes * kBoxA, kStageBytes = kBoxes * (kBoxA + kBoxB);
+    static constexpr int kStages = CG == 2 ? 6 : BN == 128 ? 3 : 4;
     static constexpr int kSides = 2, kPieces = BN / kSides / 32;     // pieces of 32 columns per warp
     static constexpr int kWarps = 4 * kSides, kThreads = 128 + 32 * kWarps;
     static constexpr uint32_t kBuffers = kStages * kStageBytes, kBarriers = kBuffers + kWarps * kStageWords * 4;
@@ -351,7 +355,7 @@ struct LinearShape {
 // The tensor cores cut off what their fp32 sums cannot hold, always towards zero, so long sums
 // drift: 512 products of 16 left fp32 weight gradients 4e-6 off.  Where a result of 32 bits comes
 // of them (weight gradients, the column sums of input gradients) they are taken out of tensor
-// memory every kPromote steps of 64 and added up in registers, rounded to nearest, while the next
+// memory every kPromote products of 64 and added up in registers, rounded to nearest, while the next
 // ones run: 5e-7 off, and within 3 % of the time (187 to 195 us for 4096 x 4096 over 8191 tokens).
 // 16-bit results do not show the drift.  RUNS: a kernel of its own, since its registers cost the
 // others' epilogue time (input gradient of 1999 x 1000 x 2731 with relu 37 against 43 us).
@@ -390,7 +394,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     const uint32_t first = blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
     const uint32_t depth_begin = (uint32_t)((uint64_t)grid.depth_steps * part / splits);
     const uint32_t depth_end = (uint32_t)((uint64_t)grid.depth_steps * (part + 1) / splits);
-    constexpr uint32_t run = RUNS ? kPromote : 1u << 30;                    // steps summed in tensor memory
+    constexpr uint32_t run = RUNS ? kPromote / S::kBoxes : 1u << 30;        // steps summed in tensor memory
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
@@ -430,18 +434,22 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                     const uint32_t bar = CG == 2 ? address_in(full + 8 * s, leader) : full + 8 * s;
                     if (rank == 0) barrier_expect(full + 8 * s, CG * S::kStageBytes);
                     const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
-                    const int depth = (int)d * 64;
-                    if constexpr (a_mn) {
-                        copy_box<CG>(a, &map_a, row, depth, bar);
-                        copy_box<CG>(a + 8192, &map_a, row + 64, depth, bar);
-                    } else {
-                        copy_box<CG>(a, &map_a, depth, row, bar);
-                    }
-                    if constexpr (b_mn) {
 #pragma unroll
-                        for (int i = 0; i < S::kRowsB / 64; ++i) copy_box<CG>(b + 8192 * i, &map_b, col + 64 * i, depth, bar);
-                    } else {
-                        copy_box<CG>(b, &map_b, depth, col, bar);
+                    for (int box = 0; box < S::kBoxes; ++box) {
+                        const int depth = (int)d * S::kDepth + 64 * box;
+                        if constexpr (a_mn) {
+                            copy_box<CG>(a + box * S::kBoxA, &map_a, row, depth, bar);
+                            copy_box<CG>(a + box * S::kBoxA + 8192, &map_a, row + 64, depth, bar);
+                        } else {
+                            copy_box<CG>(a + box * S::kBoxA, &map_a, depth, row, bar);
+                        }
+                        if constexpr (b_mn) {
+#pragma unroll
+                            for (int i = 0; i < S::kRowsB / 64; ++i)
+                                copy_box<CG>(b + box * S::kBoxB + 8192 * i, &map_b, col + 64 * i, depth, bar);
+                        } else {
+                            copy_box<CG>(b + box * S::kBoxB, &map_b, depth, col, bar);
+                        }
                     }
                 }
                 __syncwarp();
@@ -475,9 +483,10 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                         tmem_fence_after();
                         if (elected()) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                tile_product<CG>(d_address, tile_descriptor(a + k * (a_mn ? 2048 / 16 : 32 / 16)),
-                                                 tile_descriptor(b + k * (b_mn ? 2048 / 16 : 32 / 16)), descriptor, k > 0 || d > part_begin);
+                            for (int k = 0; k < 4 * S::kBoxes; ++k)
+                                tile_product<CG>(d_address, tile_descriptor(a + k / 4 * (S::kBoxA / 16) + k % 4 * (a_mn ? 2048 / 16 : 32 / 16)),
+                                                 tile_descriptor(b + k / 4 * (S::kBoxB / 16) + k % 4 * (b_mn ? 2048 / 16 : 32 / 16)),
+                                                 descriptor, k > 0 || d > part_begin);
                             tile_commit<CG>(empty + 8 * s, leader);
                             if (d + 1 == part_end) tile_commit<CG>(sums_full + 8 * half, leader);
                         }

@@ -1,6 +1,7 @@
 // C ABI of the client's training step (declared in include/eden.h): argument checks,
 // workspace carving and launches.
 #include <algorithm>
+#include <cmath>
 #include <new>
 
 #include "context.h"
@@ -252,7 +253,7 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
     if (int rc = make_map(&map_b, q.type, q.b, OP == kForward ? S::kRowsB : 64)) return rc;
     const uint64_t rows = (q.p.rows + 128 * CG - 1) / (128 * CG), cols = (q.p.cols + BN - 1) / BN;
     if (rows * cols * CG * splits > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((q.depth + 63) / 64), splits};
+    const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((q.depth + S::kDepth - 1) / S::kDepth), splits};
     const auto kernel = k_linear<OP, T, CG, BN, SPLIT, RUNS>;
     CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
     const uint32_t groups = (uint32_t)(SPLIT ? rows * cols : std::min<uint64_t>(rows * cols, ctx->sm_count / CG));
@@ -335,39 +336,41 @@ int cluster_slots(eden_ctx* ctx, uint32_t cluster)
 
 // The cheapest form by a model of its time in microseconds, fitted to sums of 1024 and 4096 on
 // one to 512 tiles: a launch's fixed part, a step of 64 along the sum (the pair's is its
-// products' time, the others' the issue of four products and their barriers), the epilogue of
-// a tile where it outlasts the tile's steps, and the join of a split tile.
+// products' time, the others' the issue of their products and barriers), the epilogue of a tile
+// where it outlasts the tile's steps, and the join of a split tile.
 template <int OP>
 Cut choose_cut(eden_ctx* ctx, const Product& q)
 {
     const uint64_t steps = (q.depth + 63) / 64;
     const int form = ctx->linear_form;
-    if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 16))) return {EDEN_LINEAR_FEW, 1};
-    static const struct { int form; uint64_t rows, cols; uint32_t blocks; double fixed, step, finish, join; } tiles[] = {
-        {EDEN_LINEAR_PAIR, 256, 256, 2, 6.8, 0.27, OP == kWeightGrad ? 3.5 : 2.2, 0.4},
-        {EDEN_LINEAR_SINGLE, 128, 128, 1, 4.8, 0.233, OP == kWeightGrad ? 2.7 : 1.3, 0.55},
-        {EDEN_LINEAR_NARROW, 128, 64, 1, 4.0, 0.215, OP == kWeightGrad ? 1.8 : 0.9, 0.45}};
+    if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 8))) return {EDEN_LINEAR_FEW, 1};
+    static const struct { int form; uint64_t rows, cols, depth; uint32_t blocks; double fixed, step, finish, split, join; } tiles[] = {
+        {EDEN_LINEAR_PAIR, 256, 256, 64, 2, 6.0, 0.265, OP == kWeightGrad ? 3.5 : 2.2, 0.0, 0.5},
+        {EDEN_LINEAR_SINGLE, 128, 128, 128, 1, 4.9, 0.185, OP == kWeightGrad ? 2.7 : 1.3, 1.0, 0.5},
+        {EDEN_LINEAR_NARROW, 128, 64, 128, 1, 3.6, 0.159, OP == kWeightGrad ? 1.8 : 0.9, 1.2, 0.4}};
     Cut best{EDEN_LINEAR_PAIR, 1};
     double least = 1e300;
     for (const auto& t : tiles) {
         if (form != EDEN_LINEAR_AUTO && form != EDEN_LINEAR_FEW && form != t.form) continue;
         const uint64_t count = (q.p.rows + t.rows - 1) / t.rows * ((q.p.cols + t.cols - 1) / t.cols);
         uint32_t most = 1;
-        while (2 * most * t.blocks <= 8 && 2 * most <= steps) most *= 2;
+        while (2 * most * t.blocks <= 8 && 2 * most <= (steps * 64 + t.depth - 1) / t.depth) most *= 2;
         for (uint32_t splits = 1; splits <= most; splits *= 2) {
             if (ctx->linear_splits && splits != std::min(most, (uint32_t)ctx->linear_splits)) continue;
             const uint64_t slots = cluster_slots(ctx, splits * t.blocks), waves = (count + slots - 1) / slots;
             const double sum = (double)((steps + splits - 1) / splits) * t.step;
-            const double cost = splits > 1 ? waves * (t.fixed + t.join * splits + sum) : t.fixed + waves * std::max(sum, t.finish);
+            const double cost = splits > 1 ? waves * (t.fixed + t.split + t.join * splits + sum) : t.fixed + waves * std::max(sum, t.finish);
             if (cost < least) {
                 least = cost;
                 best = {t.form, splits};
             }
         }
     }
-    // 17 to 32 tokens: every block of the form for few reads all of x, at about 20 TB/s from the caches
+    // 9 to 32 tokens: the form for few takes W at HBM's rate, but its blocks (a wave of 148 costs 1.3 us
+    // up to 16 tokens, 2 us above) each read all of x, at about 20 TB/s from the caches
     if (OP == kForward && form == EDEN_LINEAR_AUTO && q.p.rows <= 32) {
-        const double few = 2.5 + (double)q.p.cols * q.depth * 2 / 5e6 + (double)((q.p.cols + 15) / 16) * q.p.rows * q.depth * 2 / 20e6;
+        const double blocks = (double)((q.p.cols + 15) / 16), waves = std::ceil(blocks / ctx->sm_count);
+        const double few = 1.5 + waves * (q.p.rows <= 16 ? 1.3 : 2.0) + (double)q.p.cols * q.depth * 2 / 6e6 + blocks * q.p.rows * q.depth * 2 / 20e6;
         if (few < least) best = {EDEN_LINEAR_FEW, 1};
     }
     return best;
