@@ -334,18 +334,18 @@ __device__ __forceinline__ void tile_at(const TileGrid& g, uint32_t t, uint32_t&
 }
 
 // Shape of a block's share of a tile: 128 rows of A and BN / CG rows of B per step along the sum.
-// Each of the four quarters of its 128 rows of sums has kSides epilogue warps side by side.  A
+// Each of the four quarters of its 128 rows of sums has SIDES epilogue warps side by side.  A
 // step is one box of 64 for pairs, whose four products outlast their issue (512 cycles), and two
 // for single blocks: waiting for a stage, releasing it and issuing four products takes 410 to 440
 // cycles whatever their size, of which 180 are the stage's.
-template <int CG, int BN>
+template <int CG, int BN, int SIDES>
 struct LinearShape {
     static constexpr int kRowsB = BN / CG, kBoxes = CG == 1 ? 2 : 1, kDepth = 64 * kBoxes;
     static constexpr uint32_t kBoxA = 128 * 128, kBoxB = kRowsB * 128;
     static constexpr uint32_t kBytesA = kBoxes * kBoxA, kStageBytes = kBoxes * (kBoxA + kBoxB);
-    static constexpr int kStages = CG == 2 ? 6 : BN == 128 ? 3 : 4;
-    static constexpr int kSides = 2, kPieces = BN / kSides / 32;     // pieces of 32 columns per warp
-    static constexpr int kWarps = 4 * kSides, kThreads = 128 + 32 * kWarps;
+    static constexpr int kStages = CG == 2 ? (SIDES == 2 ? 6 : 5) : BN == 128 ? 3 : 4;
+    static constexpr int kPieces = BN / SIDES / 32;      // pieces of 32 columns per warp
+    static constexpr int kWarps = 4 * SIDES, kThreads = 128 + 32 * kWarps;
     static constexpr uint32_t kBuffers = kStages * kStageBytes, kBarriers = kBuffers + kWarps * kStageWords * 4;
     static constexpr uint32_t kSharedBytes = kBarriers + (2 * kStages + 5) * 8 + 16;
     static constexpr uint32_t kColumns = 2 * BN;       // tensor memory: two tiles' sums
@@ -366,20 +366,21 @@ constexpr uint32_t kPromote = 16;
 //   warp 1   (of the pair's first block) issues the products
 //   warp 2   owns the tensor memory
 //   warps 4+ read finished sums from tensor memory and run the epilogue, while the products
-//            of the next tile (or of the next kPromote steps) fill its other half.  Eight warps:
-//            sixteen have 96 registers each, spill, and took 52 against 47 us for gelu and 8-bit
-//            codes on 4096 x 4096 x 1024, 228 against 190 us for a weight gradient
+//            of the next tile (or of the next kPromote steps) fill its other half.  Eight warps
+//            (SIDES = 2), or sixteen with 104 registers each and a stage less where an epilogue
+//            that is more than a store may outlast the products: 36 against 40 us for bias, gelu
+//            and 8-bit codes on 4096 x 4096 x 1024, but 176 against 171 us for 8192 x 4096 x 4096
 // CG = 2: the blocks of a pair hold 128 rows of A and half of the rows of B each; the first
 // one's barriers count both blocks' bytes, and its products write both blocks' sums.
 // SPLIT: one tile per cluster.  Its blocks (pairs) take a part of the sum each, leave their
 // sums in shared memory, and then every block joins and finishes a share of the tile's 32 x 32
 // pieces, adding the parts in their order.
-template <int OP, typename T, int CG, int BN, bool SPLIT, bool RUNS>
-__global__ void __launch_bounds__(LinearShape<CG, BN>::kThreads, 1)
+template <int OP, typename T, int CG, int BN, bool SPLIT, bool RUNS, int SIDES>
+__global__ void __launch_bounds__(LinearShape<CG, BN, SIDES>::kThreads, 1)
 k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, LinearEpilogue p, TileGrid grid,
          uint32_t* status)
 {
-    using S = LinearShape<CG, BN>;
+    using S = LinearShape<CG, BN, SIDES>;
     constexpr bool a_mn = OP == kWeightGrad, b_mn = OP != kForward;
     constexpr uint32_t descriptor = product_descriptor(std::is_same_v<T, __nv_bfloat16>, a_mn, b_mn, 128 * CG, BN);
 
@@ -421,7 +422,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 
     bool ok = true;
     if (warp < 4) {
-      registers_down();                // the block's registers (its threads x 168) move to the epilogue's warps
+      registers_down<SIDES>();         // the block's registers move to the epilogue's warps
       if (warp == 0) {
         uint32_t s = 0, phase = 0, issued = 0;
         for (uint32_t t = first; t < grid.count && ok; t += step) {
@@ -509,7 +510,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
       __syncwarp();
       if constexpr (SPLIT) cluster_arrive_wait();
     } else {
-        registers_up();
+        registers_up<SIDES>();
         const int quarter = warp % 4, side = (warp - 4) / 4;
         const uint32_t my_sums = sums + ((uint32_t)quarter * 32 << 16) + side * S::kPieces * 32;
         uint32_t half = 0, phase = 0;

@@ -80,9 +80,21 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
     return false;
 }
 
-// ---- registers: 4 warps x 56 + 8 warps x 224 = 12 warps x 168, what the block was launched with
-__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
-__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
+// ---- registers: 4 warps x 56 + 8 x 224 = 12 x 168, or 4 x 40 + 16 x 104 < 20 x 96: no more than
+// the block was launched with
+template <int SIDES>
+__device__ __forceinline__ void registers_down()
+{
+    if constexpr (SIDES == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+}
+
+template <int SIDES>
+__device__ __forceinline__ void registers_up()
+{
+    if constexpr (SIDES == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+}
 
 // ---- tensor copies ------------------------------------------------------------------
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map)

@@ -244,17 +244,17 @@ int row_grain(const void* p, uint64_t stride, size_t size)
     return (int)(bits & (0 - bits));
 }
 
-template <int OP, typename T, int CG, int BN, bool SPLIT, bool RUNS>
+template <int OP, typename T, int CG, int BN, bool SPLIT, bool RUNS, int SIDES = 2>
 int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
 {
-    using S = LinearShape<CG, BN>;
+    using S = LinearShape<CG, BN, SIDES>;
     CUtensorMap map_a, map_b;
     if (int rc = make_map(&map_a, q.type, q.a, OP == kWeightGrad ? 64 : 128)) return rc;
     if (int rc = make_map(&map_b, q.type, q.b, OP == kForward ? S::kRowsB : 64)) return rc;
     const uint64_t rows = (q.p.rows + 128 * CG - 1) / (128 * CG), cols = (q.p.cols + BN - 1) / BN;
     if (rows * cols * CG * splits > kMaxCount) return EDEN_ERR_TOO_LARGE;
     const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((q.depth + S::kDepth - 1) / S::kDepth), splits};
-    const auto kernel = k_linear<OP, T, CG, BN, SPLIT, RUNS>;
+    const auto kernel = k_linear<OP, T, CG, BN, SPLIT, RUNS, SIDES>;
     CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
     const uint32_t groups = (uint32_t)(SPLIT ? rows * cols : std::min<uint64_t>(rows * cols, ctx->sm_count / CG));
     return launch(ctx, q.name, q.bytes, kernel, dim3(groups * CG * splits), S::kThreads, S::kSharedBytes, CG * splits, map_a, map_b, q.p,
@@ -264,6 +264,11 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
 template <int OP, typename T, int CG, int BN, bool SPLIT>
 int launch_runs(eden_ctx* ctx, const Product& q, uint32_t splits)
 {
+    if constexpr (OP != kWeightGrad && CG == 2 && !SPLIT) {
+        // sums of up to 2048 do not hide such an epilogue behind their products (8200 cycles for 1024)
+        const bool more = q.p.act || q.p.save || q.p.residual || q.p.column_sums;
+        if (more && q.depth <= 2048 && (!q.p.column_sums || q.depth <= 64 * kPromote)) return launch_linear<OP, T, CG, BN, SPLIT, false, 4>(ctx, q, 1);
+    }
     if constexpr (OP == kInputGrad) {
         if (!q.p.column_sums || (q.depth + 63) / 64 <= (uint64_t)kPromote * splits) return launch_linear<OP, T, CG, BN, SPLIT, false>(ctx, q, splits);
     }
@@ -280,15 +285,21 @@ int launch_tiles(eden_ctx* ctx, const Product& q, uint32_t splits)
     }
 }
 
+// A block for each SM where there are fewer rows of W than that, as long as its warps have a step each.
+uint32_t few_parts(const eden_ctx* ctx, uint64_t blocks, uint64_t depth)
+{
+    uint32_t parts = 1;
+    while (parts < 8 && blocks * parts * 2 <= (uint64_t)ctx->sm_count && (depth + 63) / 64 >= 16 * 2 * parts) parts *= 2;
+    return parts;
+}
+
 template <typename T, int NT, int R>
 int launch_few(eden_ctx* ctx, const Product& q)
 {
     const bool vec = aligned(q.a.data, 16) && aligned(q.b.data, 16) && q.depth % 8 == 0 && (q.a.stride % 8 == 0 || q.a.rows == 1) &&
                      (q.b.stride % 8 == 0 || q.b.rows == 1);
-    // a block for each SM where there are fewer rows of W than that, as long as its warps have a step each
     const uint64_t blocks = (q.p.cols + 16 * R - 1) / (16 * R);
-    uint32_t parts = 1;
-    while (parts < 8 && blocks * parts * 2 <= (uint64_t)ctx->sm_count && (q.depth + 63) / 64 >= 16 * 2 * parts) parts *= 2;
+    const uint32_t parts = few_parts(ctx, blocks, q.depth);
     const auto kernel = parts > 1 ? (vec ? k_linear_few<T, NT, R, true, true> : k_linear_few<T, NT, R, false, true>)
                                   : (vec ? k_linear_few<T, NT, R, true, false> : k_linear_few<T, NT, R, false, false>);
     return launch(ctx, q.name, q.bytes, kernel, dim3((uint32_t)blocks, parts), kFewThreads, 0, parts, (const T*)q.a.data, q.a.stride,
@@ -314,8 +325,8 @@ int cluster_slots(eden_ctx* ctx, uint32_t cluster)
 {
     int& known = ctx->cluster_slots[cluster];
     if (known > 0) return known;
-    const auto kernel = k_linear<kForward, __nv_bfloat16, 1, 128, true, false>;
-    using S = LinearShape<1, 128>;
+    const auto kernel = k_linear<kForward, __nv_bfloat16, 1, 128, true, false, 2>;
+    using S = LinearShape<1, 128, 2>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(cluster * ctx->sm_count);
     cfg.blockDim = dim3(S::kThreads);
@@ -370,7 +381,8 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
     // up to 16 tokens, 2 us above) each read all of x, at about 20 TB/s from the caches
     if (OP == kForward && form == EDEN_LINEAR_AUTO && q.p.rows <= 32) {
         const double blocks = (double)((q.p.cols + 15) / 16), waves = std::ceil(blocks / ctx->sm_count);
-        const double few = 1.5 + waves * (q.p.rows <= 16 ? 1.3 : 2.0) + (double)q.p.cols * q.depth * 2 / 6e6 + blocks * q.p.rows * q.depth * 2 / 20e6;
+        const double few = 1.5 + waves * (q.p.rows <= 16 ? 1.3 : 2.0) + (double)q.p.cols * q.depth * 2 / 6e6 + blocks * q.p.rows * q.depth * 2 / 20e6 +
+                           (double)steps / (16 * few_parts(ctx, (uint64_t)blocks, q.depth)) * (q.p.rows <= 16 ? 0.4 : 0.8);
         if (few < least) best = {EDEN_LINEAR_FEW, 1};
     }
     return best;
