@@ -617,14 +617,16 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 // ---- few tokens ---------------------------------------------------------------------
 // y [m, n] for m <= 8 * NT: every weight is read once and used m times, so reading W is all
 // that takes time.  A block takes 16 * R rows of W; its 16 warps take steps of 64 along the sum
-// in turn, all loads of up to four steps on their way together, straight to registers in the
+// in turn, all loads of one or two steps on their way together, straight to registers in the
 // layout of the 16 x 8 x 16 product: the sum's index may be permuted alike in W and in x, so
 // each lane loads 16 consecutive bytes and feeds them as the fragments of two products.  The
 // 16 warps' sums are added in their order.  R = 2 where groups of 32 results are saved.  Where
 // few rows of W meet a long sum, a cluster of blocks shares it: each block adds up its warps, and
 // the first one adds the blocks' sums, out of their shared memory, in their order (SHARED; the
 // same code with a cluster of one block took 7.4 us where this takes 4.8).
-// 1 x 4096 x 4096 bf16: FEW1 us with the weights in the L2 cache, of which 5.1 are HBM's floor.
+// Two blocks on an SM hide each other's ends: one with twice the loads on their way took 5.8 us
+// against 4.1 for 13 x 2731 x 1000 and 7.7 against 4.0 for 1 x 2731 x 1001.  1 x 4096 x 4096 bf16
+// takes 4.9 us with the weights in the L2 cache (5.1 is HBM's floor), 1 x 16384 x 4096 25.7 us (21).
 constexpr int kFewThreads = 512;
 
 // 8 values at p, of which the first `count` exist; VEC: 16-byte aligned, count 8 or 0
@@ -647,10 +649,10 @@ __device__ __forceinline__ void few_product(float (&c)[4], uint32_t a0, uint32_t
 }
 
 template <typename T, int NT, int R, bool VEC, bool SHARED>
-__global__ void __launch_bounds__(kFewThreads) k_linear_few(const T* x, uint64_t x_stride, const T* w, uint64_t w_stride, uint32_t k,
+__global__ void __launch_bounds__(kFewThreads, NT <= 2 ? 2 : 1) k_linear_few(const T* x, uint64_t x_stride, const T* w, uint64_t w_stride, uint32_t k,
                                                            LinearEpilogue p)
 {
-    constexpr int kWarps = kFewThreads / 32, kAhead = (NT == 1 && R == 1 && VEC) ? 4 : (NT <= 2 && R == 1) || NT == 1 ? 2 : 1;
+    constexpr int kWarps = kFewThreads / 32, kAhead = NT == 1 && R == 1 && VEC ? 2 : 1;
     dependency_wait();
     dependency_release();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;

@@ -354,7 +354,7 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
 {
     const uint64_t steps = (q.depth + 63) / 64;
     const int form = ctx->linear_form;
-    if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 8))) return {EDEN_LINEAR_FEW, 1};
+    if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 16))) return {EDEN_LINEAR_FEW, 1};
     static const struct { int form; uint64_t rows, cols, depth; uint32_t blocks; double fixed, step, finish, split, join; } tiles[] = {
         {EDEN_LINEAR_PAIR, 256, 256, 64, 2, 6.0, 0.265, OP == kWeightGrad ? 3.5 : 2.2, 0.0, 0.5},
         {EDEN_LINEAR_SINGLE, 128, 128, 128, 1, 4.9, 0.185, OP == kWeightGrad ? 2.7 : 1.3, 1.0, 0.5},
@@ -377,12 +377,12 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
             }
         }
     }
-    // 9 to 32 tokens: the form for few takes W at HBM's rate, but its blocks (a wave of 148 costs 1.3 us
-    // up to 16 tokens, 2 us above) each read all of x, at about 20 TB/s from the caches
+    // 17 to 32 tokens: the form for few takes W at HBM's rate, but its blocks (a wave of 148 costs 2 us)
+    // each read all of x, at about 20 TB/s from the caches.  Up to 16 it was never behind by more than a tenth.
     if (OP == kForward && form == EDEN_LINEAR_AUTO && q.p.rows <= 32) {
         const double blocks = (double)((q.p.cols + 15) / 16), waves = std::ceil(blocks / ctx->sm_count);
-        const double few = 1.5 + waves * (q.p.rows <= 16 ? 1.3 : 2.0) + (double)q.p.cols * q.depth * 2 / 6e6 + blocks * q.p.rows * q.depth * 2 / 20e6 +
-                           (double)steps / (16 * few_parts(ctx, (uint64_t)blocks, q.depth)) * (q.p.rows <= 16 ? 0.4 : 0.8);
+        const double few = 1.5 + waves * 2.0 + (double)q.p.cols * q.depth * 2 / 6e6 + blocks * q.p.rows * q.depth * 2 / 20e6 +
+                           (double)steps / (16 * few_parts(ctx, (uint64_t)blocks, q.depth)) * 0.8;
         if (few < least) best = {EDEN_LINEAR_FEW, 1};
     }
     return best;
