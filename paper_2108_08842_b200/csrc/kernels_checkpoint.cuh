@@ -12,9 +12,9 @@ constexpr int kCkptThreads = 256;
 // A thread takes half a group: 16 values, 32 bytes of a 16-bit type (fp32: 64) and 16 codes.
 // `halves` = 2 * groups of a row, so that the halves of a group sit in neighbouring lanes.
 // WIDE: rows of values start on 32 bytes and rows of codes on 16, and full half groups move in
-// one access each; else every access is put together from the aligned words that it touches.
+// one access each; else loads are put together from the aligned chunks that they touch.
 // A value per lane, the simple form for any alignment, took 41 us to save and restore
-// 5368 x 1116 fp16, against ANYALIGN us.
+// 5368 x 1116 fp16, against 12 us.
 template <bool WIDE, typename T>
 __device__ __forceinline__ void load_values(const T* p, int count, uint32_t (&w)[4 * sizeof(T)])
 {
@@ -36,22 +36,20 @@ __device__ __forceinline__ void load_values(const T* p, int count, uint32_t (&w)
     }
 }
 
-template <bool WIDE, typename T>
+template <typename T>
 __device__ __forceinline__ void store_values(T* p, int count, const float (&v)[16])
 {
-    uint32_t w[4 * sizeof(T)];
-    if constexpr (sizeof(T) == 4) {
+    if (count >= 16) {
+        uint32_t w[4 * sizeof(T)];
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[j]);
-    } else {
+            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[j]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = pack<T>(v[2 * j], v[2 * j + 1]);
-    }
-    if (WIDE && count >= 16) {
+            for (int j = 0; j < 8; ++j) w[j] = pack<T>(v[2 * j], v[2 * j + 1]);
+        }
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) store_32b((char*)p + 32 * i, *(const uint32_t(*)[8])(w + 8 * i));
-    } else if constexpr (!WIDE) {
-        store_shifted(p, count * (int)sizeof(T), w);
     } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
@@ -119,6 +117,9 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_save(const T* x, ui
     else store_shifted(codes, count, w);
 }
 
+// Without WIDE the warp hands its 32 x 16 values round in shared memory and stores them one
+// after the other, a lane each: words put together by every thread for its own half group lie 32
+// bytes apart across the lanes, and took 206 us for 16384 x 4096 bf16 against 54 us.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* x, uint64_t x_stride, CheckpointView c, uint32_t n,
                                                                     uint32_t halves, uint64_t total)
@@ -128,36 +129,56 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* x, uint6
     const uint64_t i = (uint64_t)blockIdx.x * kCkptThreads + threadIdx.x;
     const uint64_t row = total <= 0xFFFFFFFFull ? (uint32_t)i / halves : i / halves;
     const uint32_t half = (uint32_t)(i - row * halves), col = half * 16;
-    if (i >= total || col >= n) return;
-    const int count = (int)min(n - col, 16u);
-    const uint32_t e = c.exps[row * c.exps_stride + half / 2];
-    uint32_t w[4];
-    load_codes<WIDE>(c.codes + row * c.codes_stride + col, count, w);
-    const Pair scale(group_scale(e));
+    const int count = i < total && col < n ? (int)min(n - col, 16u) : 0;
+    if (WIDE && count == 0) return;
     float v[16];
+    if (count > 0) {
+        const uint32_t e = c.exps[row * c.exps_stride + half / 2];
+        uint32_t w[4];
+        load_codes<WIDE>(c.codes + row * c.codes_stride + col, count, w);
+        const Pair scale(group_scale(e));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        Pair v01, v23;
-        code_values(w[j], scale, v01, v23);
-        v01.get(v[4 * j], v[4 * j + 1]);
-        v23.get(v[4 * j + 2], v[4 * j + 3]);
-    }
-    if (e >= kSaturates<T>) {
+        for (int j = 0; j < 4; ++j) {
+            Pair v01, v23;
+            code_values(w[j], scale, v01, v23);
+            v01.get(v[4 * j], v[4 * j + 1]);
+            v23.get(v[4 * j + 2], v[4 * j + 3]);
+        }
+        if (e >= kSaturates<T>) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = saturated<T>(v[j]);
+            for (int j = 0; j < 16; ++j) v[j] = saturated<T>(v[j]);
+        }
     }
-    store_values<WIDE>(x + row * x_stride + col, count, v);
+    T* to = x + row * x_stride + col;
+    if constexpr (WIDE) {
+        store_values(to, count, v);
+    } else {
+        __shared__ T values[kCkptThreads / 32][32][16 + 2];            // rows of an odd number of words for 16 bits
+        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+        if (count > 0) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) values[warp][lane][j] = from_float<T>(v[j]);
+        }
+        __syncwarp();
+#pragma unroll 4
+        for (int k = 0; k < 16; ++k) {
+            const int owner = 2 * k + lane / 16;
+            T* at = (T*)__shfl_sync(0xFFFFFFFFu, (unsigned long long)to, owner) + lane % 16;
+            if (lane % 16 < __shfl_sync(0xFFFFFFFFu, count, owner)) *at = values[warp][owner][lane % 16];
+        }
+    }
 }
 
 // dz = dy * act'(z).  A warp spans 32 half groups (512 columns) and walks down a run of rows,
 // eight warps to a block, each keeping the sums of its own rows; the block adds the eight up
 // and leaves the run's column sums in partial[run][n].  The next row waits in registers as it
 // lies in memory, so that four blocks fit on an SM: 8192 x 16384 bf16 with gelu takes 122 us (180
-// with two blocks), of which HBM's floor is 105.
-template <typename T, int ACT>
-__global__ void __launch_bounds__(kCkptThreads, 4) k_act_backward_wide(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
-                                                                       uint64_t dz_stride, float* partial, uint32_t m, uint32_t n,
-                                                                       uint32_t rows_per_run)
+// with two blocks), of which HBM's floor is 105.  Without WIDE the row goes round the warp to be
+// stored, as in the restore.
+template <typename T, int ACT, bool WIDE>
+__global__ void __launch_bounds__(kCkptThreads, WIDE ? 4 : 3) k_act_backward(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
+                                                                            uint64_t dz_stride, float* partial, uint32_t m, uint32_t n,
+                                                                            uint32_t rows_per_run)
 {
     dependency_wait();
     dependency_release();
@@ -168,35 +189,48 @@ __global__ void __launch_bounds__(kCkptThreads, 4) k_act_backward_wide(const T* 
     float sum[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) sum[j] = 0.f;
-    if (count > 0) {
-        uint32_t next[8], next_codes[4] = {0, 0, 0, 0}, next_exp = 0;
-        auto fetch = [&](uint32_t row) {
-            if (row >= end) return;
-            load_values<true>(dy + (uint64_t)row * dy_stride + col, count, next);
-            if constexpr (ACT != EDEN_ACT_NONE) {
-                next_exp = pre.exps[(uint64_t)row * pre.exps_stride + half / 2];
-                load_codes<true>(pre.codes + (uint64_t)row * pre.codes_stride + col, count, next_codes);
-            }
-        };
-        fetch(begin + warp);
-        for (uint32_t row = begin + warp; row < end; row += kCkptThreads / 32) {
-            float v[16];
-            widen<T>(next, v);
-            const uint32_t w[4] = {next_codes[0], next_codes[1], next_codes[2], next_codes[3]};
-            const float scale = slope_scale(next_exp);
-            fetch(row + kCkptThreads / 32);
-            if constexpr (ACT != EDEN_ACT_NONE) {
+    uint32_t next[8], next_codes[4] = {0, 0, 0, 0}, next_exp = 0;
+    auto fetch = [&](uint32_t row) {
+        if (row >= end || count == 0) return;
+        load_values<WIDE>(dy + (uint64_t)row * dy_stride + col, count, next);
+        if constexpr (ACT != EDEN_ACT_NONE) {
+            next_exp = pre.exps[(uint64_t)row * pre.exps_stride + half / 2];
+            load_codes<WIDE>(pre.codes + (uint64_t)row * pre.codes_stride + col, count, next_codes);
+        }
+    };
+    fetch(begin + warp);
+    for (uint32_t row = begin + warp; row < end; row += kCkptThreads / 32) {
+        if (WIDE && count == 0) break;
+        float v[16];
+        widen<T>(next, v);
+        const uint32_t w[4] = {next_codes[0], next_codes[1], next_codes[2], next_codes[3]};
+        const float scale = slope_scale(next_exp);
+        fetch(row + kCkptThreads / 32);
+        if constexpr (ACT != EDEN_ACT_NONE) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    Pair z01, z23;
-                    code_values(w[j], Pair(scale), z01, z23);
-                    (Pair(v[4 * j], v[4 * j + 1]) * act_slope<ACT>(z01)).get(v[4 * j], v[4 * j + 1]);
-                    (Pair(v[4 * j + 2], v[4 * j + 3]) * act_slope<ACT>(z23)).get(v[4 * j + 2], v[4 * j + 3]);
-                }
+            for (int j = 0; j < 4; ++j) {
+                Pair z01, z23;
+                code_values(w[j], Pair(scale), z01, z23);
+                (Pair(v[4 * j], v[4 * j + 1]) * act_slope<ACT>(z01)).get(v[4 * j], v[4 * j + 1]);
+                (Pair(v[4 * j + 2], v[4 * j + 3]) * act_slope<ACT>(z23)).get(v[4 * j + 2], v[4 * j + 3]);
             }
+        }
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sum[j] += v[j];
-            if (dz) store_values<true>(dz + (uint64_t)row * dz_stride + col, count, v);
+        for (int j = 0; j < 16; ++j) sum[j] += v[j];
+        if (!dz) continue;
+        if constexpr (WIDE) {
+            store_values(dz + (uint64_t)row * dz_stride + col, count, v);
+        } else {
+            __shared__ uint32_t values[kCkptThreads / 32][32][9];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) values[warp][lane][j] = pack<T>(v[2 * j], v[2 * j + 1]);
+            __syncwarp();
+            const uint32_t first = blockIdx.x * 512 + lane;
+            T* to = dz + (uint64_t)row * dz_stride + first;
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (first + 32 * k < n) to[32 * k] = ((const T*)values[warp][2 * k + lane / 16])[lane % 16];
+            __syncwarp();
         }
     }
     if (!partial) return;
@@ -210,57 +244,6 @@ __global__ void __launch_bounds__(kCkptThreads, 4) k_act_backward_wide(const T* 
 #pragma unroll
         for (int w = 0; w < kCkptThreads / 32; ++w) total += sums[w][i % 16][i / 16];
         if (at < n) partial[(uint64_t)blockIdx.y * n + at] = total;
-    }
-}
-
-// The same for rows at any alignment, one lane per column: a block takes 32 columns of a run of
-// rows, and each warp has the loads of four of its rows on their way together.  1505 x 10137
-// values take 27 us, 53 in half groups put together from shifted words.
-template <typename T, int ACT>
-__global__ void __launch_bounds__(kCkptThreads) k_act_backward(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,
-                                                              uint64_t dz_stride, float* partial, uint32_t m, uint32_t n,
-                                                              uint32_t rows_per_run)
-{
-    constexpr int kWarps = kCkptThreads / 32, kAhead = 4;
-    dependency_wait();
-    dependency_release();
-    const uint32_t group = blockIdx.x, col = group * kGroup + threadIdx.x % 32;
-    const uint32_t begin = blockIdx.y * rows_per_run, end = min(m, begin + rows_per_run);
-    float sum = 0.f;
-    if (col < n) {
-        for (uint32_t row0 = begin + threadIdx.x / 32; row0 < end; row0 += kWarps * kAhead) {
-            T v[kAhead];
-            int8_t code[kAhead];
-            uint8_t e[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const uint64_t row = row0 + i * kWarps;
-                if (row >= end) continue;
-                v[i] = dy[row * dy_stride + col];
-                if constexpr (ACT != EDEN_ACT_NONE) {
-                    code[i] = pre.codes[row * pre.codes_stride + col];
-                    e[i] = pre.exps[row * pre.exps_stride + group];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const uint64_t row = row0 + i * kWarps;
-                if (row >= end) continue;
-                float f = to_float(v[i]);
-                if constexpr (ACT != EDEN_ACT_NONE) f *= act_slope<ACT>(code_value(code[i], slope_scale(e[i])));
-                sum += f;
-                if (dz) dz[row * dz_stride + col] = from_float<T>(f);
-            }
-        }
-    }
-    if (!partial) return;
-    __shared__ float sums[kWarps][32];
-    sums[threadIdx.x / 32][threadIdx.x % 32] = sum;
-    __syncthreads();
-    if (threadIdx.x < 32 && col < n) {
-        float total = 0.f;
-        for (int w = 0; w < kWarps; ++w) total += sums[w][threadIdx.x];
-        partial[(uint64_t)blockIdx.y * n + col] = total;
     }
 }
 

@@ -35,7 +35,7 @@ struct LinearEpilogue {
 //              start on one, else single elements (words with partial ends branched, and took
 //              3750 cycles a piece)
 // A lane per row with less than a sector each took 451 us for 7376 x 6088 x 376 results that
-// start on 16 bytes, against STAGED us.
+// start on 16 bytes, against 48 us.
 constexpr int kOutWords = 32 * 20, kCodeWords = 32 * 12, kStageWords = kOutWords + kCodeWords;     // a warp's buffer
 
 __device__ __forceinline__ void copy_async_16(uint32_t to, const void* from)
