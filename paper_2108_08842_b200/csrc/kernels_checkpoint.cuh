@@ -186,9 +186,9 @@ __global__ void __launch_bounds__(kCkptThreads, WIDE ? 4 : 3) k_act_backward(con
     const uint32_t half = blockIdx.x * 32 + lane, col = half * 16;
     const uint32_t begin = blockIdx.y * rows_per_run, end = min(m, begin + rows_per_run);
     const int count = col < n ? (int)min(n - col, 16u) : 0;
-    float sum[16];
+    Pair sum[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+    for (int j = 0; j < 8; ++j) sum[j] = Pair(0.f);
     uint32_t next[8], next_codes[4] = {0, 0, 0, 0}, next_exp = 0;
     auto fetch = [&](uint32_t row) {
         if (row >= end || count == 0) return;
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kCkptThreads, WIDE ? 4 : 3) k_act_backward(con
             }
         }
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sum[j] += v[j];
+        for (int j = 0; j < 8; ++j) sum[j] = sum[j] + Pair(v[2 * j], v[2 * j + 1]);
         if (!dz) continue;
         if constexpr (WIDE) {
             store_values(dz + (uint64_t)row * dz_stride + col, count, v);
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kCkptThreads, WIDE ? 4 : 3) k_act_backward(con
     if (!partial) return;
     __shared__ float sums[kCkptThreads / 32][16][33];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) sums[warp][j][lane] = sum[j];
+    for (int j = 0; j < 8; ++j) sum[j].get(sums[warp][2 * j][lane], sums[warp][2 * j + 1][lane]);
     __syncthreads();
     for (int i = threadIdx.x; i < 512; i += kCkptThreads) {
         const uint32_t at = blockIdx.x * 512 + i;

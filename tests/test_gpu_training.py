@@ -451,6 +451,59 @@ def test_calls_on_another_stream(ctx):
     other.close()
 
 
+def test_offsets_past_32_bits(ctx):
+    """Matrices of more than 2^31 elements, and rows further apart than that in all."""
+    m, n = 70000, 32768
+    x = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    x.copy_(torch.arange(n, device="cuda").sub(n // 2).mul(2.0 ** -10).to(torch.bfloat16).expand(m, n))
+    x[-1] = x[-1].flip(0)
+    saved = ctx.checkpoint_save(x)
+    back = ctx.checkpoint_restore(saved, torch.bfloat16)
+    for r in (0, 40000, m - 1):
+        codes, exps = R.code(R.f64(x[r:r + 1]))
+        assert np.array_equal(saved.codes[r:r + 1].cpu().numpy(), codes) and np.array_equal(saved.exps[r:r + 1].cpu().numpy(), exps)
+        R.near(back[r:r + 1], R.value(codes, exps), 0.0)
+    dz, db = ctx.act_backward(x[-600:], (saved.codes[-600:], saved.exps[-600:]), act="relu", out=back[-600:])
+    z = R.held((saved.codes[-600:], saved.exps[-600:]))
+    R.near(dz, R.f64(x[-600:]) * (z > 0), R.rounding(R.f64(x[-600:]), torch.bfloat16))
+    del back, saved, dz
+    # 300 rows, 2^23 elements apart
+    step, k = 1 << 23, 200
+    wide = x.view(-1).as_strided((270, k), (step, 1))
+    assert wide.numel() == 270 * k and 269 * step > 2 ** 31
+    wide.copy_(normal(1, 270, k, dtype=torch.bfloat16))
+    w = normal(2, 96, k, dtype=torch.bfloat16, std=0.07)
+    xs, ws = R.f64(wide), R.f64(w).T
+    off = R.sum_bound(xs, ws)
+    out = x.view(-1).as_strided((270, 96), (step, 1), storage_offset=1024)
+    R.near(ctx.linear(wide, w, out=out), xs @ ws, off + R.rounding(np.abs(xs @ ws) + off, torch.bfloat16))
+    R.near(ctx.linear(wide[-3:], w, out=out[-3:]), (xs @ ws)[-3:], (off + R.rounding(np.abs(xs @ ws) + off, torch.bfloat16))[-3:])
+    ref = R.f64(out).T @ xs
+    R.near(ctx.linear_weight_grad(out, wide), ref, R.sum_bound(R.f64(out).T, xs))
+
+
+def test_two_contexts_at_once(ctx):
+    """Products on two streams whose kernels want the same SMs and tensor memory."""
+    from paper_2108_08842_b200 import eden
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = [eden.Context(0, workspace_bytes_=eden.linear_workspace_bytes(600, 1024, 1024), stream=s) for s in streams]
+    x, w = normal(1, 600, 1024, dtype=torch.bfloat16), normal(2, 1024, 1024, dtype=torch.bfloat16, std=0.03)
+    pre = pre_of(3, 600, 1024)
+    want = ctx.linear(x, w, act="gelu"), ctx.linear_weight_grad(x, pre), ctx.linear(x[:5], w)
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for c in both:
+            got.append((c.linear(x, w, act="gelu"), c.linear_weight_grad(x, pre), c.linear(x[:5], w)))
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+    for c in both:
+        assert c.status() == 0
+        c.close()
+
+
 def test_calls_in_a_graph():
     from paper_2108_08842_b200 import eden
 
