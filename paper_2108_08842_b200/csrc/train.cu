@@ -1,6 +1,7 @@
 // C ABI of the client's training step (declared in include/eden.h): argument checks,
 // workspace carving and launches.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <new>
 
@@ -251,7 +252,12 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
     if (rows * cols * CG * splits > kMaxCount) return EDEN_ERR_TOO_LARGE;
     const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((q.depth + S::kDepth - 1) / S::kDepth), splits};
     const auto kernel = k_linear<OP, T, CG, BN, SPLIT, RUNS, SIDES>;
-    CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
+    static std::atomic<uint64_t> asked{0};       // devices on which this kernel may use its shared memory
+    const uint64_t device = 1ull << (ctx->device & 63);
+    if (!(asked.load(std::memory_order_relaxed) & device) || ctx->device > 63) {
+        CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
+        asked.fetch_or(device, std::memory_order_relaxed);
+    }
     const uint32_t groups = (uint32_t)(SPLIT ? rows * cols : std::min<uint64_t>(rows * cols, ctx->sm_count / CG));
     return launch(ctx, q.name, q.bytes, kernel, dim3(groups * CG * splits), S::kThreads, S::kSharedBytes, CG * splits, map_a, map_b, q.p,
                   grid, (uint32_t*)ctx->ws);
@@ -500,17 +506,19 @@ extern "C" int eden_act_backward(eden_ctx* ctx, const eden_act_backward_args* a)
             // about six blocks of eight warps for each SM, at least 8 rows (one per warp) to a run
             const uint64_t strips = (a->n + 511) / 512;
             const uint64_t want = std::min<uint64_t>(kMaxRuns, std::max<uint64_t>(1, 6ull * ctx->sm_count / strips));
-            const uint64_t rows_per_run = std::max<uint64_t>(8, (a->m + want - 1) / want);
+            const uint64_t rows_per_run = std::max<uint64_t>(a->m <= 32 ? 32 : 8, (a->m + want - 1) / want);
             runs = (a->m + rows_per_run - 1) / rows_per_run;
-            if (a->bias_grad) {
+            if (a->bias_grad && (runs > 1 || a->accumulate)) {
                 partial = Scratch(ctx).take<float>(runs * a->n);
                 if (!partial) return EDEN_ERR_WORKSPACE;
+            } else {
+                partial = a->bias_grad;              // one run's sums are the result
             }
             int rc = EDEN_OK;
             EDEN_DISPATCH_HALF(a->type, EDEN_DISPATCH_ACT(a->act, rc = (act_backward<T_, ACT_>(ctx, a, partial, strips, runs, rows_per_run))));
             if (rc) return rc;
         }
-        return a->bias_grad ? sum_columns(ctx, partial, runs, a->n, a->bias_grad, a->accumulate) : EDEN_OK;
+        return partial != a->bias_grad ? sum_columns(ctx, partial, runs, a->n, a->bias_grad, a->accumulate) : EDEN_OK;
     });
 }
 
@@ -531,9 +539,11 @@ extern "C" int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_gra
         float* partial = nullptr;
         if (a->m > 0) {
             Scratch scratch(ctx);
-            if (a->bias_grad) {
+            if (a->bias_grad && (runs > 1 || a->accumulate)) {
                 partial = scratch.take<float>(runs * a->k);
                 if (!partial) return EDEN_ERR_WORKSPACE;
+            } else {
+                partial = a->bias_grad;              // 32 rows' sums are the result
             }
             LinearEpilogue p{nullptr, a->residual, a->residual_stride, a->dx, a->dx_stride,
                              view(a->pre, a->pre_stride, a->pre_exp, a->pre_exp_stride), partial, a->m, a->k, a->act, 0, 0};
@@ -543,7 +553,7 @@ extern "C" int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_gra
                                                             {a->weight, a->weight_stride, a->n, a->k, {}}, a->n, p, bytes}))
                 return rc;
         }
-        return a->bias_grad ? sum_columns(ctx, partial, runs, a->k, a->bias_grad, a->accumulate) : EDEN_OK;
+        return partial != a->bias_grad ? sum_columns(ctx, partial, runs, a->k, a->bias_grad, a->accumulate) : EDEN_OK;
     });
 }
 
