@@ -318,7 +318,8 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], const Piece& at,
 // Tiles of the result, in the order in which they are handed out: bands of kBand tile rows,
 // column by column, so that the tiles in flight share few rows of A and of B in the L2 cache.
 struct TileGrid {
-    uint32_t rows, cols, count;        // tiles
+    uint32_t rows, cols;               // tiles
+    uint32_t begin, end;               // those of this launch, in their order
     uint32_t depth_steps;              // steps of the shape's kDepth along the sum
     uint32_t splits;                   // parts of the sum, one block (pair) of a cluster each
 };
@@ -392,7 +393,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     uint32_t* const buffer = (uint32_t*)(raw + S::kBuffers) + (warp >= 4 ? warp - 4 : 0) * kStageWords;
     const uint32_t in_cluster = CG == 2 || SPLIT ? cluster_rank() : 0, rank = in_cluster % CG, leader = in_cluster - rank;
     const uint32_t splits = SPLIT ? grid.splits : 1, part = in_cluster / CG;
-    const uint32_t first = blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
+    const uint32_t first = grid.begin + blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
     const uint32_t depth_begin = (uint32_t)((uint64_t)grid.depth_steps * part / splits);
     const uint32_t depth_end = (uint32_t)((uint64_t)grid.depth_steps * (part + 1) / splits);
     constexpr uint32_t run = RUNS ? kPromote / S::kBoxes : 1u << 30;        // steps summed in tensor memory
@@ -425,7 +426,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
       registers_down<SIDES>();         // the block's registers move to the epilogue's warps
       if (warp == 0) {
         uint32_t s = 0, phase = 0, issued = 0;
-        for (uint32_t t = first; t < grid.count && ok; t += step) {
+        for (uint32_t t = first; t < grid.end && ok; t += step) {
             uint32_t tile_row, tile_col;
             tile_at(grid, t, tile_row, tile_col);
             const int row = (int)(tile_row * 128 * CG + rank * 128), col = (int)(tile_col * BN + rank * S::kRowsB);
@@ -474,7 +475,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             uint32_t s = 0, phase = 0, half = 0, half_phase = 1;
             const uint32_t low_a = descriptor_low(base), low_b = descriptor_low(base + S::kBytesA);
             uint32_t a = low_a, b = low_b;
-            for (uint32_t t = first; t < grid.count && ok; t += step) {
+            for (uint32_t t = first; t < grid.end && ok; t += step) {
                 for (uint32_t part_begin = depth_begin; part_begin < depth_end && ok; part_begin += run) {
                     const uint32_t d_address = sums + half * BN, part_end = depth_end - part_begin < run ? depth_end : part_begin + run;
                     if (!(ok = barrier_wait(sums_empty + 8 * half, half_phase))) break;
@@ -519,7 +520,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             __syncwarp();
             if (lane == 0) barrier_arrive_remote(CG == 2 ? address_in(sums_empty + 8 * half, leader) : sums_empty + 8 * half);
         };
-        for (uint32_t t = first; t < grid.count && ok; t += step) {
+        for (uint32_t t = first; t < grid.end && ok; t += step) {
             uint32_t tile_row, tile_col;
             tile_at(grid, t, tile_row, tile_col);
             const uint64_t row0 = (uint64_t)tile_row * 128 * CG + rank * 128 + quarter * 32;

@@ -242,7 +242,7 @@ int row_grain(const void* p, uint64_t stride, size_t size)
 }
 
 template <int OP, typename T, int CG, int BN, bool SPLIT, bool RUNS, int SIDES = 2>
-int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
+int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits, uint32_t begin, uint32_t end)
 {
     using S = LinearShape<CG, BN, SIDES>;
     CUtensorMap map_a, map_b;
@@ -250,7 +250,8 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
     if (int rc = make_map(&map_b, q.type, q.b, OP == kForward ? S::kRowsB : 64)) return rc;
     const uint64_t rows = (q.p.rows + 128 * CG - 1) / (128 * CG), cols = (q.p.cols + BN - 1) / BN;
     if (rows * cols * CG * splits > kMaxCount) return EDEN_ERR_TOO_LARGE;
-    const TileGrid grid{(uint32_t)rows, (uint32_t)cols, (uint32_t)(rows * cols), (uint32_t)((q.depth + S::kDepth - 1) / S::kDepth), splits};
+    if (end == 0) end = (uint32_t)(rows * cols);
+    const TileGrid grid{(uint32_t)rows, (uint32_t)cols, begin, end, (uint32_t)((q.depth + S::kDepth - 1) / S::kDepth), splits};
     const auto kernel = k_linear<OP, T, CG, BN, SPLIT, RUNS, SIDES>;
     static std::atomic<uint64_t> asked{0};       // devices on which this kernel may use its shared memory
     const uint64_t device = 1ull << (ctx->device & 63);
@@ -258,33 +259,45 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits)
         CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
         asked.fetch_or(device, std::memory_order_relaxed);
     }
-    const uint32_t groups = (uint32_t)(SPLIT ? rows * cols : std::min<uint64_t>(rows * cols, ctx->sm_count / CG));
+    const uint32_t groups = SPLIT ? end - begin : std::min<uint32_t>(end - begin, ctx->sm_count / CG);
     return launch(ctx, q.name, q.bytes, kernel, dim3(groups * CG * splits), S::kThreads, S::kSharedBytes, CG * splits, map_a, map_b, q.p,
                   grid, (uint32_t*)ctx->ws);
 }
 
 template <int OP, typename T, int CG, int BN, bool SPLIT>
-int launch_runs(eden_ctx* ctx, const Product& q, uint32_t splits)
+int launch_runs(eden_ctx* ctx, const Product& q, uint32_t splits, uint32_t begin = 0, uint32_t end = 0)
 {
     if constexpr (OP != kWeightGrad && CG == 2 && !SPLIT) {
         // sums of up to 2048 do not hide such an epilogue behind their products (8200 cycles for 1024)
         const bool more = q.p.act || q.p.save || q.p.residual || q.p.column_sums;
-        if (more && q.depth <= 2048 && (!q.p.column_sums || q.depth <= 64 * kPromote)) return launch_linear<OP, T, CG, BN, SPLIT, false, 4>(ctx, q, 1);
+        if (more && q.depth <= 2048 && (!q.p.column_sums || q.depth <= 64 * kPromote)) return launch_linear<OP, T, CG, BN, SPLIT, false, 4>(ctx, q, 1, begin, end);
     }
     if constexpr (OP == kInputGrad) {
-        if (!q.p.column_sums || (q.depth + 63) / 64 <= (uint64_t)kPromote * splits) return launch_linear<OP, T, CG, BN, SPLIT, false>(ctx, q, splits);
+        if (!q.p.column_sums || (q.depth + 63) / 64 <= (uint64_t)kPromote * splits) return launch_linear<OP, T, CG, BN, SPLIT, false>(ctx, q, splits, begin, end);
     }
-    return launch_linear<OP, T, CG, BN, SPLIT, OP != kForward>(ctx, q, splits);
+    return launch_linear<OP, T, CG, BN, SPLIT, OP != kForward>(ctx, q, splits, begin, end);
 }
 
+// How a product is cut up: a form (EDEN_LINEAR_*) and the parts of each tile's sum; and, where the
+// last wave of whole tiles would leave many SMs without one, the first of the tiles that a second
+// launch takes in `tail_splits` parts each.
+struct Cut {
+    int form;
+    uint32_t splits, tail, tail_splits;
+};
+
 template <int OP, int CG, int BN>
-int launch_tiles(eden_ctx* ctx, const Product& q, uint32_t splits)
+int launch_tiles(eden_ctx* ctx, const Product& q, const Cut& cut)
 {
-    if (splits > 1) {
-        EDEN_DISPATCH_HALF(q.type, return (launch_runs<OP, T_, CG, BN, true>(ctx, q, splits)));
-    } else {
-        EDEN_DISPATCH_HALF(q.type, return (launch_runs<OP, T_, CG, BN, false>(ctx, q, 1)));
+    int rc = EDEN_OK;
+    if (cut.splits > 1) {
+        EDEN_DISPATCH_HALF(q.type, rc = (launch_runs<OP, T_, CG, BN, true>(ctx, q, cut.splits)));
+        return rc;
     }
+    EDEN_DISPATCH_HALF(q.type, rc = (launch_runs<OP, T_, CG, BN, false>(ctx, q, 1, 0, cut.tail)));
+    if (rc || cut.tail == 0) return rc;
+    EDEN_DISPATCH_HALF(q.type, rc = (launch_runs<OP, T_, CG, BN, true>(ctx, q, cut.tail_splits, cut.tail)));
+    return rc;
 }
 
 // A block for each SM where there are fewer rows of W than that, as long as its warps have a step each.
@@ -314,12 +327,6 @@ int launch_few(eden_ctx* ctx, const Product& q)
     if (q.p.save) return q.p.rows <= 8 ? launch_few<T, 1, 2>(ctx, q) : q.p.rows <= 16 ? launch_few<T, 2, 2>(ctx, q) : launch_few<T, 4, 2>(ctx, q);
     return q.p.rows <= 8 ? launch_few<T, 1, 1>(ctx, q) : q.p.rows <= 16 ? launch_few<T, 2, 1>(ctx, q) : launch_few<T, 4, 1>(ctx, q);
 }
-
-// How a product is cut up: a form (EDEN_LINEAR_*) and the parts of each tile's sum.
-struct Cut {
-    int form;
-    uint32_t splits;
-};
 
 // Clusters of 1, 2, 4 or 8 blocks with a tile's stages that the device runs at once: clusters do
 // not span the GPU's processing clusters, so fewer blocks fit than there are SMs.
@@ -356,12 +363,12 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
 {
     const uint64_t steps = (q.depth + 63) / 64;
     const int form = ctx->linear_form;
-    if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 16))) return {EDEN_LINEAR_FEW, 1};
+    if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 16))) return {EDEN_LINEAR_FEW, 1, 0, 0};
     static const struct { int form; uint64_t rows, cols, depth; uint32_t blocks; double fixed, step, finish, split, join; } tiles[] = {
         {EDEN_LINEAR_PAIR, 256, 256, 64, 2, 6.0, 0.265, OP == kWeightGrad ? 3.5 : 2.2, 0.0, 0.5},
         {EDEN_LINEAR_SINGLE, 128, 128, 128, 1, 4.9, 0.185, OP == kWeightGrad ? 2.7 : 1.3, 1.0, 0.5},
         {EDEN_LINEAR_NARROW, 128, 64, 128, 1, 3.6, 0.159, OP == kWeightGrad ? 1.8 : 0.9, 1.2, 0.4}};
-    Cut best{EDEN_LINEAR_PAIR, 1};
+    Cut best{EDEN_LINEAR_PAIR, 1, 0, 0};
     double least = 1e300;
     for (const auto& t : tiles) {
         if (form != EDEN_LINEAR_AUTO && form != EDEN_LINEAR_FEW && form != t.form) continue;
@@ -375,7 +382,17 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
             const double cost = splits > 1 ? waves * (t.fixed + t.split + t.join * splits + sum) : t.fixed + waves * std::max(sum, t.finish);
             if (cost < least) {
                 least = cost;
-                best = {t.form, splits};
+                best = {t.form, splits, 0, 0};
+            }
+            // whole waves, and the rest in parts: 256 tiles on 74 pairs are 3 waves and 34 tiles
+            const uint64_t pairs = cluster_slots(ctx, t.blocks), whole = count / pairs * pairs;
+            if (splits == 1 || ctx->linear_splits || whole == 0 || whole == count) continue;
+            const uint64_t tail_waves = (count - whole + slots - 1) / slots;
+            const double with_tail = t.fixed + (double)(whole / pairs) * std::max((double)steps * t.step, t.finish) +
+                                     tail_waves * (t.fixed + t.split + t.join * splits + sum);
+            if (with_tail < least) {
+                least = with_tail;
+                best = {t.form, 1, (uint32_t)whole, splits};
             }
         }
     }
@@ -385,7 +402,7 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
         const double blocks = (double)((q.p.cols + 15) / 16), waves = std::ceil(blocks / ctx->sm_count);
         const double few = 1.5 + waves * 2.0 + (double)q.p.cols * q.depth * 2 / 6e6 + blocks * q.p.rows * q.depth * 2 / 20e6 +
                            (double)steps / (16 * few_parts(ctx, (uint64_t)blocks, q.depth)) * 0.8;
-        if (few < least) best = {EDEN_LINEAR_FEW, 1};
+        if (few < least) best = {EDEN_LINEAR_FEW, 1, 0, 0};
     }
     return best;
 }
@@ -406,9 +423,9 @@ int product(eden_ctx* ctx, Scratch& scratch, Product q)
     p.grain_codes = row_grain(p.ckpt.codes, p.ckpt.codes_stride, 1);
     p.grain_bias = row_grain(p.bias, 0, 2);
     switch (cut.form) {
-        case EDEN_LINEAR_PAIR: return launch_tiles<OP, 2, 256>(ctx, q, cut.splits);
-        case EDEN_LINEAR_SINGLE: return launch_tiles<OP, 1, 128>(ctx, q, cut.splits);
-        default: return launch_tiles<OP, 1, 64>(ctx, q, cut.splits);
+        case EDEN_LINEAR_PAIR: return launch_tiles<OP, 2, 256>(ctx, q, cut);
+        case EDEN_LINEAR_SINGLE: return launch_tiles<OP, 1, 128>(ctx, q, cut);
+        default: return launch_tiles<OP, 1, 64>(ctx, q, cut);
     }
 }
 

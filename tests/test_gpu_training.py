@@ -228,6 +228,38 @@ def test_every_form_at_every_size(ctx, forced):
     check_weight_grad(ctx, torch.float16, 1111, 130, 270, False, 1, 1)
 
 
+def test_last_wave_in_parts():
+    """80 tiles of 256 x 256 on 74 pairs of SMs: the rest of the tiles in a launch of their own."""
+    from paper_2108_08842_b200 import eden
+
+    c = eden.Context(0, workspace_bytes_=eden.linear_workspace_bytes(4096, 4096, 4096))
+    x, w = normal(1, 1270, 4096, dtype=torch.bfloat16), normal(2, 4000, 4096, dtype=torch.bfloat16, std=0.015)
+    b, r = normal(3, 4000, dtype=torch.bfloat16), normal(4, 1270, 4000, dtype=torch.bfloat16)
+    before = c.launch_count
+    y, saved = c.linear(x, w, b, act="silu", residual=r, save="pre")
+    assert c.launch_count == before + 2
+    c.set_option(eden.OPT_LINEAR_SPLITS, 1)
+    plain = c.linear(x, w, b, act="silu", residual=r)
+    assert c.launch_count == before + 3
+    c.set_option(eden.OPT_LINEAR_SPLITS, 0)
+    xs, ws = R.f64(x), R.f64(w).T
+    z = xs @ ws + R.f64(b)
+    off = R.sum_bound(xs, ws) + 2.0 ** -22 * np.abs(z)
+    ref = R.act(z, "silu") + R.f64(r)
+    bound = R.LIPSCHITZ * off + R.ACT * (1 + np.abs(z)) + 2.0 ** -23 * np.abs(ref)
+    for got in (y, plain):
+        R.near(got, ref, bound + R.rounding(np.abs(ref) + bound, torch.bfloat16))
+    step = 2.0 ** (saved.exps.cpu().numpy().astype(float)[:, np.arange(4000) // 32] - 127)
+    assert (np.abs(R.held(saved) - z) <= step / 2 + off).all()
+    # sums over 4096 tokens into 80 tiles
+    before = c.launch_count
+    dw = c.linear_weight_grad(x.t().contiguous(), w.t().contiguous())
+    assert c.launch_count == before + 3                # rows of 1270 values are laid out first
+    R.near(dw, xs @ ws, R.sum_bound(xs, ws))
+    assert c.status() == 0
+    c.close()
+
+
 @pytest.mark.parametrize("forced", [("LINEAR_FEW", 0)], indirect=True)
 @pytest.mark.parametrize("m,n,k,extra,offset", [(17, 100, 1000, 0, 0), (24, 33, 4104, 8, 8), (31, 64, 200, 1, 1), (32, 16, 5000, 0, 0), (33, 64, 64, 0, 0)])
 def test_few_tokens_form(ctx, forced, m, n, k, extra, offset):
