@@ -423,93 +423,93 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 
     bool ok = true;
     if (warp < 4) {
-      registers_down<SIDES>();         // the block's registers move to the epilogue's warps
-      if (warp == 0) {
-        uint32_t s = 0, phase = 0, issued = 0;
-        for (uint32_t t = first; t < grid.end && ok; t += step) {
-            uint32_t tile_row, tile_col;
-            tile_at(grid, t, tile_row, tile_col);
-            const int row = (int)(tile_row * 128 * CG + rank * 128), col = (int)(tile_col * BN + rank * S::kRowsB);
-            for (uint32_t d = depth_begin; d < depth_end; ++d) {
-                if (!(ok = barrier_wait(empty + 8 * s, phase ^ 1))) break;
-                if (elected()) {
-                    const uint32_t bar = CG == 2 ? address_in(full + 8 * s, leader) : full + 8 * s;
-                    if (rank == 0) barrier_expect(full + 8 * s, CG * S::kStageBytes);
-                    const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
+        registers_down<SIDES>();         // the block's registers move to the epilogue's warps
+        if (warp == 0) {
+            uint32_t s = 0, phase = 0, issued = 0;
+            for (uint32_t t = first; t < grid.end && ok; t += step) {
+                uint32_t tile_row, tile_col;
+                tile_at(grid, t, tile_row, tile_col);
+                const int row = (int)(tile_row * 128 * CG + rank * 128), col = (int)(tile_col * BN + rank * S::kRowsB);
+                for (uint32_t d = depth_begin; d < depth_end; ++d) {
+                    if (!(ok = barrier_wait(empty + 8 * s, phase ^ 1))) break;
+                    if (elected()) {
+                        const uint32_t bar = CG == 2 ? address_in(full + 8 * s, leader) : full + 8 * s;
+                        if (rank == 0) barrier_expect(full + 8 * s, CG * S::kStageBytes);
+                        const uint32_t a = base + s * S::kStageBytes, b = a + S::kBytesA;
 #pragma unroll
-                    for (int box = 0; box < S::kBoxes; ++box) {
-                        const int depth = (int)d * S::kDepth + 64 * box;
-                        if constexpr (a_mn) {
-                            copy_box<CG>(a + box * S::kBoxA, &map_a, row, depth, bar);
-                            copy_box<CG>(a + box * S::kBoxA + 8192, &map_a, row + 64, depth, bar);
-                        } else {
-                            copy_box<CG>(a + box * S::kBoxA, &map_a, depth, row, bar);
-                        }
-                        if constexpr (b_mn) {
+                        for (int box = 0; box < S::kBoxes; ++box) {
+                            const int depth = (int)d * S::kDepth + 64 * box;
+                            if constexpr (a_mn) {
+                                copy_box<CG>(a + box * S::kBoxA, &map_a, row, depth, bar);
+                                copy_box<CG>(a + box * S::kBoxA + 8192, &map_a, row + 64, depth, bar);
+                            } else {
+                                copy_box<CG>(a + box * S::kBoxA, &map_a, depth, row, bar);
+                            }
+                            if constexpr (b_mn) {
 #pragma unroll
-                            for (int i = 0; i < S::kRowsB / 64; ++i)
-                                copy_box<CG>(b + box * S::kBoxB + 8192 * i, &map_b, col + 64 * i, depth, bar);
-                        } else {
-                            copy_box<CG>(b + box * S::kBoxB, &map_b, depth, col, bar);
+                                for (int i = 0; i < S::kRowsB / 64; ++i)
+                                    copy_box<CG>(b + box * S::kBoxB + 8192 * i, &map_b, col + 64 * i, depth, bar);
+                            } else {
+                                copy_box<CG>(b + box * S::kBoxB, &map_b, depth, col, bar);
+                            }
                         }
                     }
+                    __syncwarp();
+                    issued = min(issued + 1, (uint32_t)S::kStages);
+                    if (++s == S::kStages) { s = 0; phase ^= 1; }
                 }
-                __syncwarp();
-                issued = min(issued + 1, (uint32_t)S::kStages);
+            }
+            // the products' last arrivals on this block's barriers land before the block ends
+            for (int i = 0; i < S::kStages && ok; ++i) {
+                ok = barrier_wait(empty + 8 * s, phase ^ 1);
                 if (++s == S::kStages) { s = 0; phase ^= 1; }
             }
-        }
-        // the products' last arrivals on this block's barriers land before the block ends
-        for (int i = 0; i < S::kStages && ok; ++i) {
-            ok = barrier_wait(empty + 8 * s, phase ^ 1);
-            if (++s == S::kStages) { s = 0; phase ^= 1; }
-        }
-        // gave up: the copies still on their way (counted by the pair's first block) land as well
-        if (!ok && rank == 0)
-            for (; issued > 0; --issued) {
-                if (s-- == 0) { s = S::kStages - 1; phase ^= 1; }
-                barrier_wait(full + 8 * s, phase);
-            }
-      } else if (warp == 1) {
-        if (rank == 0) {
-            uint32_t s = 0, phase = 0, half = 0, half_phase = 1;
-            const uint32_t low_a = descriptor_low(base), low_b = descriptor_low(base + S::kBytesA);
-            uint32_t a = low_a, b = low_b;
-            for (uint32_t t = first; t < grid.end && ok; t += step) {
-                for (uint32_t part_begin = depth_begin; part_begin < depth_end && ok; part_begin += run) {
-                    const uint32_t d_address = sums + half * BN, part_end = depth_end - part_begin < run ? depth_end : part_begin + run;
-                    if (!(ok = barrier_wait(sums_empty + 8 * half, half_phase))) break;
-                    tmem_fence_after();
-                    for (uint32_t d = part_begin; d < part_end; ++d) {
-                        if (!(ok = barrier_wait(full + 8 * s, phase))) break;
+            // gave up: the copies still on their way (counted by the pair's first block) land as well
+            if (!ok && rank == 0)
+                for (; issued > 0; --issued) {
+                    if (s-- == 0) { s = S::kStages - 1; phase ^= 1; }
+                    barrier_wait(full + 8 * s, phase);
+                }
+        } else if (warp == 1) {
+            if (rank == 0) {
+                uint32_t s = 0, phase = 0, half = 0, half_phase = 1;
+                const uint32_t low_a = descriptor_low(base), low_b = descriptor_low(base + S::kBytesA);
+                uint32_t a = low_a, b = low_b;
+                for (uint32_t t = first; t < grid.end && ok; t += step) {
+                    for (uint32_t part_begin = depth_begin; part_begin < depth_end && ok; part_begin += run) {
+                        const uint32_t d_address = sums + half * BN, part_end = depth_end - part_begin < run ? depth_end : part_begin + run;
+                        if (!(ok = barrier_wait(sums_empty + 8 * half, half_phase))) break;
                         tmem_fence_after();
-                        if (elected()) {
+                        for (uint32_t d = part_begin; d < part_end; ++d) {
+                            if (!(ok = barrier_wait(full + 8 * s, phase))) break;
+                            tmem_fence_after();
+                            if (elected()) {
 #pragma unroll
-                            for (int k = 0; k < 4 * S::kBoxes; ++k)
-                                tile_product<CG>(d_address, tile_descriptor(a + k / 4 * (S::kBoxA / 16) + k % 4 * (a_mn ? 2048 / 16 : 32 / 16)),
-                                                 tile_descriptor(b + k / 4 * (S::kBoxB / 16) + k % 4 * (b_mn ? 2048 / 16 : 32 / 16)),
-                                                 descriptor, k > 0 || d > part_begin);
-                            tile_commit<CG>(empty + 8 * s, leader);
-                            if (d + 1 == part_end) tile_commit<CG>(sums_full + 8 * half, leader);
+                                for (int k = 0; k < 4 * S::kBoxes; ++k)
+                                    tile_product<CG>(d_address, tile_descriptor(a + k / 4 * (S::kBoxA / 16) + k % 4 * (a_mn ? 2048 / 16 : 32 / 16)),
+                                                     tile_descriptor(b + k / 4 * (S::kBoxB / 16) + k % 4 * (b_mn ? 2048 / 16 : 32 / 16)),
+                                                     descriptor, k > 0 || d > part_begin);
+                                tile_commit<CG>(empty + 8 * s, leader);
+                                if (d + 1 == part_end) tile_commit<CG>(sums_full + 8 * half, leader);
+                            }
+                            __syncwarp();
+                            a += S::kStageBytes / 16;
+                            b += S::kStageBytes / 16;
+                            if (++s == S::kStages) { s = 0; phase ^= 1; a = low_a; b = low_b; }
                         }
-                        __syncwarp();
-                        a += S::kStageBytes / 16;
-                        b += S::kStageBytes / 16;
-                        if (++s == S::kStages) { s = 0; phase ^= 1; a = low_a; b = low_b; }
+                        half ^= 1;
+                        half_phase ^= half ^ 1;
                     }
-                    half ^= 1;
-                    half_phase ^= half ^ 1;
+                }
+                if (!ok) {
+                    if (elected()) tile_commit<CG>(drained, leader);
+                    __syncwarp();
+                    barrier_wait(drained, 0);
                 }
             }
-            if (!ok) {
-                if (elected()) tile_commit<CG>(drained, leader);
-                __syncwarp();
-                barrier_wait(drained, 0);
-            }
         }
-      }
-      __syncwarp();
-      if constexpr (SPLIT) cluster_arrive_wait();
+        __syncwarp();
+        if constexpr (SPLIT) cluster_arrive_wait();
     } else {
         registers_up<SIDES>();
         const int quarter = warp % 4, side = (warp - 4) / 4;
@@ -607,7 +607,10 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
             }
         }
     }
-    if (!ok) atomicOr(status, EDEN_STATUS_TIMEOUT);
+    if (!ok) {
+        copy_async_wait();
+        atomicOr(status, EDEN_STATUS_TIMEOUT);
+    }
     __syncwarp();
     tmem_fence_before();
     if constexpr (CG == 2 || SPLIT) cluster_arrive_wait(); else __syncthreads();

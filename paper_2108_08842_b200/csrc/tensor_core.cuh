@@ -81,7 +81,8 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
 }
 
 // ---- registers: 4 warps x 56 + 8 x 224 = 12 x 168, or 4 x 40 + 16 x 104 < 20 x 96: no more than
-// the block was launched with
+// the block was launched with, which the host checks before the first launch of a kernel
+constexpr int kLaunchRegisters[2] = {168, 96};           // a thread's at launch, for SIDES 2 and 4
 template <int SIDES>
 __device__ __forceinline__ void registers_down()
 {

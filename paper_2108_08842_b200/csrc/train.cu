@@ -256,6 +256,10 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits, uint32_t beg
     static std::atomic<uint64_t> asked{0};       // devices on which this kernel may use its shared memory
     const uint64_t device = 1ull << (ctx->device & 63);
     if (!(asked.load(std::memory_order_relaxed) & device) || ctx->device > 63) {
+        // a kernel compiled to fewer registers than its warps redistribute would wait for them for good
+        cudaFuncAttributes attributes;
+        CUDA_OK(cudaFuncGetAttributes(&attributes, kernel));
+        if ((attributes.numRegs + 7) / 8 * 8 < kLaunchRegisters[SIDES == 4]) return EDEN_ERR_CUDA;
         CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSharedBytes));
         asked.fetch_or(device, std::memory_order_relaxed);
     }
