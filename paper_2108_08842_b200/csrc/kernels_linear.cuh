@@ -50,7 +50,7 @@ __device__ __forceinline__ void copy_async_4(uint32_t to, const void* from)
 
 __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Rows of 32 elements of 1 or 2 bytes (16 of 4 bytes count as 32 of 2).  In the buffer a row of
+// Rows of 32 elements of 1 or 2 bytes.  In the buffer a row of
 // 16-byte pieces has 4 words of padding (128-bit accesses of eight lanes' rows then meet all
 // banks once), a row of words one (an odd pitch), the word that only shifted rows touch.
 template <int ELEM>
@@ -171,6 +171,69 @@ struct Rows {
     }
 };
 
+// Rows of 32 fp32 values, whole 128-byte lines where they are aligned, always through the buffer:
+// eight lanes to a row touch each line once, where a lane per row with 32 bytes a store touches
+// it four times (6656 x 1984 gradients of 64 tokens took 20 us so, 13.9 like this).  16-byte chunk c of row r
+// lies in place c ^ (r % 8) of its row: no two lanes of an access meet in a bank.
+struct WideRows {
+    static __device__ __forceinline__ float4* place(uint32_t* buffer, int row, int chunk) { return (float4*)buffer + row * 8 + (chunk ^ (row & 7)); }
+
+    // v[j] += the lane's row of the piece at `from`
+    static __device__ __forceinline__ void add(float (&v)[32], const char* from, uint64_t stride, int rows, int count, int grain, uint32_t* buffer)
+    {
+        const int lane = threadIdx.x % 32;
+        __syncwarp();
+        if (grain >= 16 && count == 32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = 4 * i + lane / 8;
+                if (r < rows) copy_async_16(shared_address(place(buffer, r, lane % 8)), from + r * stride + 16 * (lane % 8));
+            }
+        } else {
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (r < rows && lane < count) copy_async_4(shared_address((float*)place(buffer, r, lane / 4) + lane % 4), from + r * stride + 4 * lane);
+        }
+        copy_async_wait();
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const float4 f = *place(buffer, lane, c);
+            v[4 * c] += f.x;
+            v[4 * c + 1] += f.y;
+            v[4 * c + 2] += f.z;
+            v[4 * c + 3] += f.w;
+        }
+        __syncwarp();
+    }
+
+    static __device__ __forceinline__ void put(const float (&v)[32], char* to, uint64_t stride, int rows, int count, int grain, uint32_t* buffer)
+    {
+        const int lane = threadIdx.x % 32;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) *place(buffer, lane, c) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+        __syncwarp();
+        if (grain >= 16 && count == 32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = 4 * i + lane / 8;
+                if (r < rows) *(float4*)(to + r * stride + 16 * (lane % 8)) = *place(buffer, r, lane % 8);
+            }
+        } else if (grain >= 8 && count == 32) {
+            const int q = lane % 16;
+#pragma unroll 8
+            for (int r = lane / 16; r < 32; r += 2)
+                if (r < rows) *(float2*)(to + r * stride + 8 * q) = ((const float2*)place(buffer, r, q / 2))[q % 2];
+        } else {
+            const int mine = lane < count ? rows : 0;
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (r < mine) *(float*)(to + r * stride + 4 * lane) = ((const float*)place(buffer, r, lane / 4))[lane % 4];
+        }
+        __syncwarp();
+    }
+};
+
 // The piece at (row0, col0): rows and columns that exist.
 struct Piece {
     uint64_t row0, col0;
@@ -200,21 +263,9 @@ __device__ __forceinline__ void linear_epilogue(float (&v)[32], const Piece& at,
     const int lane = threadIdx.x % 32;
     const bool live = lane < at.rows;
     if constexpr (OP == kWeightGrad) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {                          // 16 columns of 4 bytes
-            const int count = 2 * (at.count - 16 * h < 16 ? at.count - 16 * h : 16);
-            if (count <= 0) break;
-            char* out = at.in(p.out, p.out_stride, 4) + 64 * h;
-            uint32_t w[16];
-            if (p.accumulate) {
-                Rows<2>::get(w, out, p.out_stride * 4, at.rows, count, p.grain_out, buffer);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[16 * h + j] += __uint_as_float(w[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(v[16 * h + j]);
-            Rows<2>::put(w, out, p.out_stride * 4, at.rows, count, p.grain_out, buffer);
-        }
+        char* out = at.in(p.out, p.out_stride, 4);
+        if (p.accumulate) WideRows::add(v, out, p.out_stride * 4, at.rows, at.count, p.grain_out, buffer);
+        WideRows::put(v, out, p.out_stride * 4, at.rows, at.count, p.grain_out, buffer);
         return;
     }
     auto add_halves = [&](const uint32_t (&w)[16]) {
