@@ -36,7 +36,7 @@ struct LinearEpilogue {
 //              3750 cycles a piece)
 // A lane per row with less than a sector each took 451 us for 7376 x 6088 x 376 results that
 // start on 16 bytes, against 48 us.
-constexpr int kOutWords = 32 * 20, kCodeWords = 32 * 12, kStageWords = kOutWords + kCodeWords;     // a warp's buffer
+constexpr int kOutWords = 32 * 20, kStageWords = kOutWords + 32 * 12;       // a warp's buffer: 16-bit rows, codes
 
 __device__ __forceinline__ void copy_async_16(uint32_t to, const void* from)
 {
@@ -50,9 +50,9 @@ __device__ __forceinline__ void copy_async_4(uint32_t to, const void* from)
 
 __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Rows of 32 elements of 1 or 2 bytes.  In the buffer a row of
-// 16-byte pieces has 4 words of padding (128-bit accesses of eight lanes' rows then meet all
-// banks once), a row of words one (an odd pitch), the word that only shifted rows touch.
+// Rows of 32 elements of 1 or 2 bytes.  In the buffer a row of 16-byte pieces has 4 words of
+// padding (128-bit accesses of eight lanes' rows then meet all banks once), a row of words one
+// (an odd pitch), the word that only shifted rows touch.
 template <int ELEM>
 struct Rows {
     static constexpr int kWords = 8 * ELEM, kPiecePitch = kWords + 4, kPitch = kWords + 1;

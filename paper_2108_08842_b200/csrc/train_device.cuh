@@ -175,14 +175,6 @@ __device__ __forceinline__ float act_value(float z)
     return x;
 }
 
-template <int ACT>
-__device__ __forceinline__ float act_slope(float z)
-{
-    float x, y;
-    act_slope<ACT>(Pair(z, z)).get(x, y);
-    return x;
-}
-
 // f(std::integral_constant<int, act>): one branch around a block of values
 template <typename F>
 __device__ __forceinline__ void with_act(int act, F&& f)
@@ -236,8 +228,6 @@ __device__ __forceinline__ uint32_t group_code(float v, float inverse)
     const uint32_t bits = __float_as_uint(__fmaf_rn(v, inverse, 12582912.f));
     return inverse == 0.f ? 0u : bits & 0xFFu;
 }
-
-__device__ __forceinline__ float code_value(int8_t code, float scale) { return (float)code * scale; }
 
 // four codes in a word: the byte c + 128 under the exponent of 2^23 is 2^23 + 128 + c
 __device__ __forceinline__ void code_values(uint32_t w, Pair scale, Pair& v01, Pair& v23)
