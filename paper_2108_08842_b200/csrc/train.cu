@@ -369,9 +369,12 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
     const int form = ctx->linear_form;
     if (OP == kForward && q.p.rows <= 32 && (form == EDEN_LINEAR_FEW || (form == EDEN_LINEAR_AUTO && q.p.rows <= 16))) return {EDEN_LINEAR_FEW, 1, 0, 0};
     static const struct { int form; uint64_t rows, cols, depth; uint32_t blocks; double fixed, step, finish, split, join; } tiles[] = {
-        {EDEN_LINEAR_PAIR, 256, 256, 64, 2, 6.0, 0.265, OP == kWeightGrad ? 3.5 : 2.2, 0.0, 0.5},
-        {EDEN_LINEAR_SINGLE, 128, 128, 128, 1, 4.9, 0.185, OP == kWeightGrad ? 2.7 : 1.3, 1.0, 0.5},
-        {EDEN_LINEAR_NARROW, 128, 64, 128, 1, 3.6, 0.159, OP == kWeightGrad ? 1.8 : 0.9, 1.2, 0.4}};
+        {EDEN_LINEAR_PAIR, 256, 256, 64, 2, 6.0, 0.265, OP == kWeightGrad ? 3.4 : 2.2, 0.0, 0.5},
+        {EDEN_LINEAR_SINGLE, 128, 128, 128, 1, 4.9, 0.185, OP == kWeightGrad ? 1.6 : 1.3, 1.0, 0.5},
+        {EDEN_LINEAR_NARROW, 128, 64, 128, 1, 3.6, 0.159, OP == kWeightGrad ? 0.95 : 0.9, 1.2, 0.4}};
+    // fp32 rows that start on 16, 8 or 4 bytes leave in more and smaller stores
+    const int grain = OP == kWeightGrad ? row_grain(q.p.out, q.p.out_stride, 4) : 32;
+    const double slower = grain >= 32 ? 1.0 : grain >= 16 ? 1.4 : grain >= 8 ? 1.75 : 2.7;
     Cut best{EDEN_LINEAR_PAIR, 1, 0, 0};
     double least = 1e300;
     for (const auto& t : tiles) {
@@ -383,7 +386,7 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
             if (ctx->linear_splits && splits != std::min(most, (uint32_t)ctx->linear_splits)) continue;
             const uint64_t slots = cluster_slots(ctx, splits * t.blocks), waves = (count + slots - 1) / slots;
             const double sum = (double)((steps + splits - 1) / splits) * t.step;
-            const double cost = splits > 1 ? waves * (t.fixed + t.split + t.join * splits + sum) : t.fixed + waves * std::max(sum, t.finish);
+            const double cost = splits > 1 ? waves * (t.fixed + t.split + t.join * splits + sum) : t.fixed + waves * std::max(sum, t.finish * slower);
             if (cost < least) {
                 least = cost;
                 best = {t.form, splits, 0, 0};
@@ -392,7 +395,7 @@ Cut choose_cut(eden_ctx* ctx, const Product& q)
             const uint64_t pairs = cluster_slots(ctx, t.blocks), whole = count / pairs * pairs;
             if (splits == 1 || ctx->linear_splits || whole == 0 || whole == count) continue;
             const uint64_t tail_waves = (count - whole + slots - 1) / slots;
-            const double with_tail = t.fixed + (double)(whole / pairs) * std::max((double)steps * t.step, t.finish) +
+            const double with_tail = t.fixed + (double)(whole / pairs) * std::max((double)steps * t.step, t.finish * slower) +
                                      tail_waves * (t.fixed + t.split + t.join * splits + sum);
             if (with_tail < least) {
                 least = with_tail;
