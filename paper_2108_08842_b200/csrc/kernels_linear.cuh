@@ -406,12 +406,17 @@ struct LinearShape {
 
 // The tensor cores cut off what their fp32 sums cannot hold, always towards zero, so long sums
 // drift: 512 products of 16 left fp32 weight gradients 4e-6 off.  Where a result of 32 bits comes
-// of them (weight gradients, the column sums of input gradients) they are taken out of tensor
-// memory every kPromote products of 64 and added up in registers, rounded to nearest, while the next
-// ones run: 5e-7 off, and within 3 % of the time (187 to 195 us for 4096 x 4096 over 8191 tokens).
-// 16-bit results do not show the drift.  RUNS: a kernel of its own, since its registers cost the
-// others' epilogue time (input gradient of 1999 x 1000 x 2731 with relu 37 against 43 us).
-constexpr uint32_t kPromote = 16;
+// of them (weight gradients, the column sums of input gradients) or codes do (a value between two
+// of them shows the smallest difference: of 16384 steps 6.5e-4 of the codes' values were off,
+// 1.5e-4 in fp32), they are taken out of tensor memory every kPromote products of 64 and added up,
+// rounded to nearest.  Weight gradients are 3e-7 off then (of 1024 steps; plain fp32 2.5e-7 over
+// 4096), column sums 6.5e-7 (1.3e-6 of 1024 steps), codes 1e-4 whatever the length.  Results of 16
+// bits alone do not show the drift: 1.66e-3 either way.
+//   Two runs: each has its half of the tensor memory; they are added up in the second one's place, and
+// the next tile's first run takes the other.  Linear 4096 x 4096 x 1024 with gelu and codes 45 -> 47 us.
+//   More: added up in registers while the next run is summed.  8192 x 4096 x 4096 with codes 198 -> 216 us.
+// RUNS: a kernel of its own, since its registers cost the others' epilogue time.
+template <int OP> constexpr uint32_t kPromote = OP == kWeightGrad ? 16 : 8;
 
 // D = A B^T for tiles of 128 * CG x BN, persistent: block (pair) c takes tiles c, c + blocks, ...
 //   warp 0   fills the stages with tensor copies, kStages ahead of the products
@@ -447,7 +452,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     const uint32_t first = grid.begin + blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
     const uint32_t depth_begin = (uint32_t)((uint64_t)grid.depth_steps * part / splits);
     const uint32_t depth_end = (uint32_t)((uint64_t)grid.depth_steps * (part + 1) / splits);
-    constexpr uint32_t run = RUNS ? kPromote / S::kBoxes : 1u << 30;        // steps summed in tensor memory
+    constexpr uint32_t run = RUNS ? kPromote<OP> / S::kBoxes : 1u << 30;        // steps summed in tensor memory
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
@@ -566,6 +571,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
         const int quarter = warp % 4, side = (warp - 4) / 4;
         const uint32_t my_sums = sums + ((uint32_t)quarter * 32 << 16) + side * S::kPieces * 32;
         uint32_t half = 0, phase = 0;
+        const bool both = RUNS && depth_end - depth_begin > run && depth_end - depth_begin <= 2 * run;
         auto release = [&]() {
             tmem_fence_before();
             __syncwarp();
@@ -592,7 +598,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                     }
                 }
             };
-            if (RUNS && depth_end - depth_begin > run) {
+            if (RUNS && SIDES == 2 && depth_end - depth_begin > 2 * run) {
                 // the runs added up, and the total put back in the last one's place
                 float total[S::kPieces][32];
                 for (uint32_t part_begin = depth_begin;; part_begin += run) {
@@ -617,6 +623,21 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 }
             } else {
                 ok = barrier_wait(sums_full + 8 * half, phase);
+                if (both && ok && (ok = barrier_wait(sums_full + 8, phase))) {   // half is 0 for every tile
+                    // the two runs added up in the second one's place
+                    tmem_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < S::kPieces; ++c) {
+                        float v[32], w[32];
+                        tmem_load(my_sums + 32 * c, v);
+                        tmem_load(my_sums + BN + 32 * c, w);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) (Pair(v[j], v[j + 1]) + Pair(w[j], w[j + 1])).get(v[j], v[j + 1]);
+                        tmem_store(my_sums + BN + 32 * c, v);
+                    }
+                    release();
+                    half = 1;
+                }
             }
             if (!ok) break;
             tmem_fence_after();

@@ -271,15 +271,21 @@ int launch_linear(eden_ctx* ctx, const Product& q, uint32_t splits, uint32_t beg
 template <int OP, typename T, int CG, int BN, bool SPLIT>
 int launch_runs(eden_ctx* ctx, const Product& q, uint32_t splits, uint32_t begin = 0, uint32_t end = 0)
 {
+    // codes and column sums are not left with the drift of long sums (kPromote)
+    const bool exact = OP == kInputGrad ? q.p.column_sums != nullptr : q.p.save != EDEN_SAVE_NONE;
+    const bool runs = exact && (q.depth + 63) / 64 > (uint64_t)kPromote<OP> * splits;
     if constexpr (OP != kWeightGrad && CG == 2 && !SPLIT) {
-        // sums of up to 2048 do not hide such an epilogue behind their products (8200 cycles for 1024)
-        const bool more = q.p.act || q.p.save || q.p.residual || q.p.column_sums;
-        if (more && q.depth <= 2048 && (!q.p.column_sums || q.depth <= 64 * kPromote)) return launch_linear<OP, T, CG, BN, SPLIT, false, 4>(ctx, q, 1, begin, end);
+        // sums of up to 2048 do not hide such an epilogue behind their products (8200 cycles for 1024);
+        // more than two runs do not fit the registers of sixteen epilogue warps
+        if ((q.p.act || q.p.residual || exact) && q.depth <= (runs ? 128 * kPromote<OP> : 2048)) {
+            if (runs) return launch_linear<OP, T, CG, BN, SPLIT, true, 4>(ctx, q, 1, begin, end);
+            return launch_linear<OP, T, CG, BN, SPLIT, false, 4>(ctx, q, 1, begin, end);
+        }
     }
-    if constexpr (OP == kInputGrad) {
-        if (!q.p.column_sums || (q.depth + 63) / 64 <= (uint64_t)kPromote * splits) return launch_linear<OP, T, CG, BN, SPLIT, false>(ctx, q, splits, begin, end);
+    if constexpr (OP != kWeightGrad) {
+        if (!runs) return launch_linear<OP, T, CG, BN, SPLIT, false>(ctx, q, splits, begin, end);
     }
-    return launch_linear<OP, T, CG, BN, SPLIT, OP != kForward>(ctx, q, splits, begin, end);
+    return launch_linear<OP, T, CG, BN, SPLIT, true>(ctx, q, splits, begin, end);
 }
 
 // How a product is cut up: a form (EDEN_LINEAR_*) and the parts of each tile's sum; and, where the
