@@ -90,11 +90,13 @@ __device__ __forceinline__ Pair magnitude(Pair a)
 }
 
 // ---- activations --------------------------------------------------------------------
-// Two values at a time.  2^x and 1/x come from the special function unit (a few units in the last
-// place), two results a value.  At 16 results a cycle that is 4096 cycles for the 128 x 256 values
-// of a product's epilogue and bounds the smooth activations there; one reciprocal shared by a pair
-// cost more in multiplications and selections than it saved.  An erff and an expf for each value
-// made the activation gradient of 8192 x 16384 take 257 us against 180, all else as it was.
+// Two values at a time.  2^x and 1/x come from the special function unit, good to a unit or two in
+// the last place of fp32, which the 16-bit types of the results do not show; it takes numbers below
+// 2^-126 for 0, so results below about 2^-119 (silu under -87, gelu under -13) may be 0 too.  Two
+// results a value: at 16 a cycle that is 4096 cycles for the 128 x 256 values of a product's epilogue
+// and bounds the smooth activations there; one reciprocal shared by a pair cost more in
+// multiplications and selections than it saved.  An erff and an expf for each value made the
+// activation gradient of 8192 x 16384 take 257 us against 180, all else as it was.
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kTanhScale = 0.7978845608028654f;      // sqrt(2 / pi)
 constexpr float kTanhCubic = 0.044715f;
@@ -102,16 +104,21 @@ constexpr float kTanhCubic = 0.044715f;
 // sigmoid(u) = 1 / (1 + 2^w) for w = -u * log2(e); 2^w overflows to infinity, which gives 0
 __device__ __forceinline__ Pair sigmoid_of(Pair w) { return reciprocal_fast(Pair(1.f) + exp2_fast(w)); }
 
-// 1 - Phi(|z|) = erfc(|z| / sqrt(2)) / 2 and exp(-z^2 / 2).  Abramowitz and Stegun 7.1.26:
-// erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x), off by at most 1.5e-7.
+// 1 - Phi(|z|) = erfc(|z| / sqrt(2)) / 2 = t P(t) exp(-z^2 / 2) with t = 1 / (1 + p |z|), and
+// exp(-z^2 / 2).  That form is Hastings' for erfc; P is the polynomial of degree 6 whose largest
+// relative error for |z| up to 14.5 is the least (7.9e-7; a linear programme over 4000 points, p by
+// search).  A fit of erfc's absolute error, with two terms less, was 5e-5 off at z = -3 and 9e-4 at
+// -4.5, past fp16's half unit.
 __device__ __forceinline__ Pair upper_tail(Pair z, Pair& bell)
 {
-    const Pair t = reciprocal_fast(fma(magnitude(z), Pair(0.3275911f * 0.7071067811865476f), Pair(1.f)));
+    const Pair t = reciprocal_fast(fma(magnitude(z), Pair(0.3625f), Pair(1.f)));
     bell = exp2_fast(z * z * Pair(-0.5f * kLog2e));
-    Pair q = fma(t, Pair(0.5f * 1.061405429f), Pair(0.5f * -1.453152027f));
-    q = fma(t, q, Pair(0.5f * 1.421413741f));
-    q = fma(t, q, Pair(0.5f * -0.284496736f));
-    q = fma(t, q, Pair(0.5f * 0.254829592f));
+    Pair q = fma(t, Pair(0.047876328f), Pair(-0.17912251f));
+    q = fma(t, q, Pair(0.17428418f));
+    q = fma(t, q, Pair(0.030232456f));
+    q = fma(t, q, Pair(0.13906018f));
+    q = fma(t, q, Pair(0.14297165f));
+    q = fma(t, q, Pair(0.14469792f));
     return q * t * bell;
 }
 
@@ -147,12 +154,14 @@ __device__ __forceinline__ Pair act_slope(Pair z)
     z.get(x, y);
     if constexpr (ACT == EDEN_ACT_RELU) return {x > 0.f ? 1.f : (x <= 0.f ? 0.f : x), y > 0.f ? 1.f : (y <= 0.f ? 0.f : y)};
     if constexpr (ACT == EDEN_ACT_GELU) {
-        // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi), Phi(z) = 1/2 + sign(z) (1/2 - tail)
+        // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi): g = tail - |z| exp(-z^2 / 2) / sqrt(2 pi) below 0 and 1 - g
+        // from 0 on, so that no difference of nearly equal numbers makes a small one
         Pair bell;
-        const Pair middle = fma(upper_tail(z, bell), Pair(-1.f), Pair(0.5f));
-        float a, b;
-        middle.get(a, b);
-        return fma(z * Pair(0.3989422804014327f), bell, Pair(0.5f) + Pair(copysignf(a, x), copysignf(b, y)));
+        const Pair tail = upper_tail(z, bell), g = fma(magnitude(z) * Pair(-0.3989422804014327f), bell, tail);
+        float a, b, c, d;
+        g.get(a, b);
+        fma(g, Pair(-1.f), Pair(1.f)).get(c, d);
+        return {x < 0.f ? a : c, y < 0.f ? b : d};
     }
     if constexpr (ACT == EDEN_ACT_GELU_TANH) {
         const Pair zz = z * z;
