@@ -25,8 +25,10 @@ __device__ __forceinline__ uint32_t address_in(uint32_t address, uint32_t rank)
     return r;
 }
 
+// The whole warp executes the aligned forms as one, so lanes that took different branches meet first.
 __device__ __forceinline__ void cluster_arrive_wait()
 {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
