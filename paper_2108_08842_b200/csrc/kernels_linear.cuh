@@ -516,11 +516,13 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
                 }
             }
             // the products' last arrivals on this block's barriers land before the block ends
+            uint32_t drain = s, drain_phase = phase;
             for (int i = 0; i < S::kStages && ok; ++i) {
-                ok = barrier_wait(empty + 8 * s, phase ^ 1);
-                if (++s == S::kStages) { s = 0; phase ^= 1; }
+                ok = barrier_wait(empty + 8 * drain, drain_phase ^ 1);
+                if (++drain == S::kStages) { drain = 0; drain_phase ^= 1; }
             }
-            // gave up: the copies still on their way (counted by the pair's first block) land as well
+            // gave up: the copies still on their way (counted by the pair's first block) land as well;
+            // s is the stage after the last one that was filled
             if (!ok && rank == 0)
                 for (; issued > 0; --issued) {
                     if (s-- == 0) { s = S::kStages - 1; phase ^= 1; }
