@@ -90,9 +90,14 @@ inline void profile_end(eden_ctx* ctx)
     ctx->profile_open = false;
 }
 
-#define CUDA_OK(expr)                                 \
-    do {                                              \
-        if ((expr) != cudaSuccess) return EDEN_ERR_CUDA; \
+// An error that is returned is taken off the runtime's record, or the next call's launch would
+// report it again.
+#define CUDA_OK(expr)              \
+    do {                           \
+        if ((expr) != cudaSuccess) { \
+            cudaGetLastError();    \
+            return EDEN_ERR_CUDA;  \
+        }                          \
     } while (0)
 
 // name and algorithmic bytes feed the optional per-kernel event timing (eden_profile_*)

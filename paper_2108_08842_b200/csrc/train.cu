@@ -108,7 +108,8 @@ int launch(eden_ctx* ctx, const char* name, double bytes, void (*kernel)(KArgs..
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
     profile_end(ctx);
     ++ctx->launches;
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? EDEN_OK : EDEN_ERR_CUDA;
+    CUDA_OK(e);
+    return EDEN_OK;
 }
 
 // partial [rows][n] -> out [n]
@@ -447,7 +448,7 @@ template <typename F>
 int guarded(eden_ctx* ctx, F&& f)
 {
     DeviceGuard device(ctx->device);
-    if (!device.ok) return EDEN_ERR_CUDA;
+    CUDA_OK(device.ok ? cudaSuccess : cudaErrorInvalidDevice);
     ctx->order.clear();                          // the workspace no longer holds a call's client figures
     try {
         return f();

@@ -1,0 +1,38 @@
+"""What training calls refuse, and what is left behind by a call that fails."""
+import ctypes
+
+import pytest
+import torch
+
+from tests.test_gpu_training import normal
+
+pytestmark = pytest.mark.gpu
+
+
+def test_an_error_is_reported_once():
+    """A launch that the runtime refuses (into a capture that was cut off) leaves nothing that the
+    next, good call would report."""
+    from paper_2108_08842_b200 import eden
+
+    runtime = ctypes.CDLL("libcudart.so.12")
+    side = torch.cuda.Stream()
+    stream = ctypes.c_void_p(side.cuda_stream)
+    c = eden.Context(0, workspace_bytes_=eden.linear_workspace_bytes(256, 256, 256), stream=side)
+    x, w = normal(1, 200, 256, dtype=torch.bfloat16), normal(2, 256, 256, dtype=torch.bfloat16)
+    out = torch.empty((200, 256), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        want = c.linear(x, w).clone()
+        side.synchronize()
+        assert runtime.cudaStreamBeginCapture(stream, 1) == 0
+        assert runtime.cudaStreamSynchronize(stream) != 0      # not allowed there: ends the capture
+        with pytest.raises(eden.EdenError):
+            c.linear(x, w, out=out)
+        graph = ctypes.c_void_p()
+        assert runtime.cudaStreamEndCapture(stream, ctypes.byref(graph)) != 0
+        runtime.cudaGetLastError()
+        c.linear(x, w, out=out)
+        c.checkpoint_save(x)
+        side.synchronize()
+    assert torch.equal(out, want) and c.status() == 0
+    c.close()
