@@ -81,7 +81,7 @@ class FeedForward:
         if gradient is None:
             gradient = torch.empty(self.d, device=dy.device)
         g = self.parts(gradient)
-        ctx.act_backward(dy, None, bias_grad=g[-1], accumulate=accumulate)
+        ctx.act_backward(dy, None, out=False, bias_grad=g[-1], accumulate=accumulate)
         for b in reversed(range(self.blocks)):
             w1, _, w2, _ = self.work[4 * b: 4 * b + 4]
             g_w1, g_b1, g_w2, _ = g[4 * b: 4 * b + 4]

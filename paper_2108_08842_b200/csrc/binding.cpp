@@ -57,6 +57,7 @@ Native* native_of(PyObject* o)
 }
 
 bool given(PyObject* o) { return o != Py_None; }
+bool left_out(PyObject* o) { return o == Py_False; }   // outputs that a call can do without
 
 const at::Tensor& tensor_of(PyObject* o, const char* name)
 {
@@ -183,6 +184,9 @@ PyObject* again(PyObject* o)
 }
 
 PyObject* wrapped(const at::Tensor& t) { return THPVariable_Wrap(t); }
+
+// what a call returns for an output
+PyObject* returned(PyObject* o, const at::Tensor& made) { return left_out(o) ? again(Py_None) : given(o) ? again(o) : wrapped(made); }
 
 PyObject* pair(PyObject* a, PyObject* b)             // takes both references
 {
@@ -350,14 +354,21 @@ PyObject* act_backward(PyObject*, PyObject* const* v, Py_ssize_t count)
             a.pre = (const int8_t*)pre.c.data; a.pre_stride = pre.c.stride;
             a.pre_exp = (const uint8_t*)pre.e.data; a.pre_exp_stride = pre.e.stride;
         }
-        const at::Tensor out = given(v[4]) ? matrix_of(v[4], "out") : fresh(n, {m, cols}, t);
-        const Matrix mo(n, out, "out", m, cols, t);
-        a.dz = mo.data; a.dz_stride = mo.stride;
-        const at::Tensor sums = sums_of(n, v[5], "bias_grad", cols, a.accumulate);
-        a.bias_grad = (float*)sums.data_ptr();
+        if (left_out(v[4]) && left_out(v[5])) refuse("out and bias_grad are both left out");
+        at::Tensor out, sums;
+        if (!left_out(v[4])) {
+            out = given(v[4]) ? matrix_of(v[4], "out") : fresh(n, {m, cols}, t);
+            const Matrix mo(n, out, "out", m, cols, t);
+            a.dz = mo.data; a.dz_stride = mo.stride;
+        }
+        if (left_out(v[5]) && a.accumulate) refuse("accumulate needs a bias_grad to add to");
+        if (!left_out(v[5])) {
+            sums = sums_of(n, v[5], "bias_grad", cols, a.accumulate);
+            a.bias_grad = (float*)sums.data_ptr();
+        }
         a.m = (uint64_t)m; a.n = (uint64_t)cols;
         done(n, lib.act_backward(n->ctx, &a), {&dy, &pre.codes, &pre.exps, &out, &sums});
-        return pair(given(v[4]) ? again(v[4]) : wrapped(out), given(v[5]) ? again(v[5]) : wrapped(sums));
+        return pair(returned(v[4], out), returned(v[5], sums));
     });
 }
 
@@ -394,7 +405,8 @@ PyObject* input_grad(PyObject*, PyObject* const* v, Py_ssize_t count)
         const Matrix mo(n, out, "out", m, k, t);
         a.dx = mo.data; a.dx_stride = mo.stride;
         at::Tensor sums;
-        const bool summed = given(v[4]) || given(v[7]) || a.accumulate;
+        const bool summed = !left_out(v[7]) && (given(v[4]) || given(v[7]) || a.accumulate);
+        if (left_out(v[7]) && a.accumulate) refuse("accumulate needs a bias_grad to add to");
         if (summed) {
             sums = sums_of(n, v[7], "bias_grad", k, a.accumulate);
             a.bias_grad = (float*)sums.data_ptr();

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import List, NamedTuple, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence, Union
 
 import numpy as np
 import torch
@@ -450,18 +450,20 @@ class Context:
         """eden_checkpoint_restore: the values that a checkpoint stands for."""
         return _binding.checkpoint_restore(self._native, saved, dtype, out)
 
-    def act_backward(self, dy: torch.Tensor, pre: Optional[Checkpoint], act: str = "none", out: Optional[torch.Tensor] = None,
-                     bias_grad: Optional[torch.Tensor] = None, accumulate: bool = False):
+    def act_backward(self, dy: torch.Tensor, pre: Optional[Checkpoint], act: str = "none", out: Union[torch.Tensor, bool, None] = None,
+                     bias_grad: Union[torch.Tensor, bool, None] = None, accumulate: bool = False):
         """eden_act_backward: (dz, bias_grad) with dz = dy * act'(pre) and bias_grad its fp32
-        column sums (accumulate: added to the given bias_grad)."""
+        column sums (accumulate: added to the given bias_grad).  out=False or bias_grad=False
+        leaves that one out: it is neither made nor computed, and None in the result."""
         return _binding.act_backward(self._native, dy, pre, act, out, bias_grad, accumulate)
 
     def linear_input_grad(self, dz: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None,
                           pre: Optional[Checkpoint] = None, act: str = "none", out: Optional[torch.Tensor] = None,
-                          bias_grad: Optional[torch.Tensor] = None, accumulate: bool = False):
+                          bias_grad: Union[torch.Tensor, bool, None] = None, accumulate: bool = False):
         """eden_linear_input_grad: dx = (dz [m, n] weight [n, k] + residual [m, k]) * act'(pre).
         With pre (the pre-activation of the layer that made the input) or bias_grad given,
-        returns (dx, bias_grad), bias_grad the fp32 column sums of dx; else dx."""
+        returns (dx, bias_grad), bias_grad the fp32 column sums of dx; else, and with
+        bias_grad=False, dx."""
         return _binding.input_grad(self._native, dz, weight, residual, pre, act, out, bias_grad, accumulate)
 
     def linear_weight_grad(self, dz: torch.Tensor, x, out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
