@@ -348,9 +348,9 @@ PyObject* act_backward(PyObject*, PyObject* const* v, Py_ssize_t count)
         const Matrix md(n, dy, "dy", m, cols, t);
         a.dy = md.data; a.dy_stride = md.stride;
         Checkpoint pre;
+        if (given(v[2])) pre = checkpoint_of(n, v[2], "pre", m, cols);
         if (a.act) {
             if (!given(v[2])) refuse("the slope of an activation needs its pre-activation");
-            pre = checkpoint_of(n, v[2], "pre", m, cols);
             a.pre = (const int8_t*)pre.c.data; a.pre_stride = pre.c.stride;
             a.pre_exp = (const uint8_t*)pre.e.data; a.pre_exp_stride = pre.e.stride;
         }
@@ -395,9 +395,9 @@ PyObject* input_grad(PyObject*, PyObject* const* v, Py_ssize_t count)
             a.residual = r.data; a.residual_stride = r.stride;
         }
         Checkpoint pre;
+        if (given(v[4])) pre = checkpoint_of(n, v[4], "pre", m, k);
         if (a.act) {
             if (!given(v[4])) refuse("the slope of an activation needs its pre-activation");
-            pre = checkpoint_of(n, v[4], "pre", m, k);
             a.pre = (const int8_t*)pre.c.data; a.pre_stride = pre.c.stride;
             a.pre_exp = (const uint8_t*)pre.e.data; a.pre_exp_stride = pre.e.stride;
         }

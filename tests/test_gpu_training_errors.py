@@ -36,3 +36,22 @@ def test_an_error_is_reported_once():
         side.synchronize()
     assert torch.equal(out, want) and c.status() == 0
     c.close()
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_a_pre_activation_is_looked_at_whatever_the_activation(act):
+    from paper_2108_08842_b200 import eden
+
+    c = eden.Context(0, workspace_bytes_=eden.linear_workspace_bytes(64, 64, 64))
+    dy, w = normal(1, 8, 64, dtype=torch.bfloat16), normal(2, 64, 48, dtype=torch.bfloat16)
+    good, other = c.checkpoint_save(normal(3, 8, 64)), c.checkpoint_save(normal(4, 8, 48))
+    c.act_backward(dy, good, act=act)
+    dx, db = c.linear_input_grad(dy, w, pre=other, act=act)
+    assert dx.shape == (8, 48) and db.shape == (48,)
+    for bad in ("pre", dy, (good[0],), (dy, dy), (good[0].cpu(), good[1].cpu()), (good[0], good[1][:, :1]), other, (good[0][:4], good[1][:4])):
+        with pytest.raises(ValueError):
+            c.act_backward(dy, bad, act=act)
+    for bad in ("pre", dy, (other[0], dy), good, (other[0].cpu(), other[1].cpu())):
+        with pytest.raises(ValueError):
+            c.linear_input_grad(dy, w, pre=bad, act=act)
+    c.close()
