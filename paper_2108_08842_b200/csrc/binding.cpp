@@ -248,6 +248,7 @@ PyObject* linear(PyObject*, PyObject* const* v, Py_ssize_t count)
         a.type = type_of(x, false, "x");
         a.act = act_of(v[4]);
         a.save = name_of(v[7], "save", kSaves, 3);
+        if (!a.save && given(v[8])) refuse("saved is given, but nothing is saved (save is none)");
         const Matrix mx(n, x, "x", m, k, t), mw(n, weight, "weight", cols, k, t);
         a.x = mx.data; a.x_stride = mx.stride;
         a.weight = mw.data; a.weight_stride = mw.stride;
