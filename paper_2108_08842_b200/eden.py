@@ -18,9 +18,9 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libeden.so")
 
-if not (os.path.exists(_LIB_PATH) and os.path.exists(os.path.join(_HERE, "_binding.so"))):
+if not os.path.exists(_LIB_PATH):
     raise ImportError(
-        "libeden.so or _binding.so is missing: build it with `python -m paper_2108_08842_b200.build` "
+        "libeden.so is missing: build it with `python -m paper_2108_08842_b200.build` "
         "(needs nvcc); this package has no CPU fallback")
 
 _lib = ctypes.CDLL(_LIB_PATH)
@@ -112,11 +112,26 @@ class EdenError(RuntimeError):
         super().__init__("eden: %s (%d)" % (_lib.eden_strerror(code).decode(), code))
 
 
-from . import _binding  # noqa: E402  (built with the library; needs torch loaded)
+class _NoBinding:
+    """In the extension's place where it cannot be loaded: the sender and the receiver do without
+    it, a training call says what is missing."""
 
-_binding.bind(*(ctypes.cast(getattr(_lib, name), _vp).value for name in (
-    "eden_linear", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_act_backward", "eden_linear_input_grad",
-    "eden_linear_weight_grad")), EdenError, Checkpoint)
+    def __init__(self, why):
+        self.why = why
+
+    def __getattr__(self, name):
+        raise ImportError("eden: the training calls need _binding.so, built for this torch: `python -m "
+                          "paper_2108_08842_b200.build` (%s)" % self.why)
+
+
+try:
+    from . import _binding  # built with the library; needs torch loaded
+except ImportError as _e:
+    _binding = _NoBinding(_e)
+else:
+    _binding.bind(*(ctypes.cast(getattr(_lib, name), _vp).value for name in (
+        "eden_linear", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_act_backward", "eden_linear_input_grad",
+        "eden_linear_weight_grad")), EdenError, Checkpoint)
 
 
 def _check(rc: int):
@@ -256,12 +271,15 @@ class Context:
         self.workspace_bytes = int(workspace_bytes_)
         _check(_lib.eden_create(ctypes.byref(self._h), device, self.stream.cuda_stream,
                                 aligned, self.workspace_bytes))
-        self._native = _binding.native(self._h.value, device, self.stream.cuda_stream, self.stream.stream_id,
-                                       self.stream.device_index, self.stream.device_type)
+        self._native = None
+        if not isinstance(_binding, _NoBinding):
+            self._native = _binding.native(self._h.value, device, self.stream.cuda_stream, self.stream.stream_id,
+                                           self.stream.device_index, self.stream.device_type)
 
     def close(self):
         if self._h:
-            _binding.close(self._native)
+            if self._native is not None:
+                _binding.close(self._native)
             _lib.eden_destroy(self._h)
             self._h = _vp()
 

@@ -13,3 +13,50 @@ def test_a_checkpoint_to_save_to_needs_a_save():
     saved = torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8)
     with pytest.raises(ValueError, match="saved is given"):
         _binding.linear(native, x, w, None, "none", None, None, "none", saved)
+
+
+WITHOUT_BINDING = """
+import sys
+sys.path.insert(0, %r)
+sys.modules["paper_2108_08842_b200._binding"] = None
+from paper_2108_08842_b200 import eden
+"""
+
+
+def in_a_process(code):
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    return subprocess.run([sys.executable, "-c", WITHOUT_BINDING % root + code], capture_output=True, text=True, timeout=300)
+
+
+def test_the_sender_is_there_without_the_extension():
+    done = in_a_process("""
+assert eden.code_bytes(1 << 20, 1.0) == 1 << 17 and eden.checkpoint_groups(33) == 2
+ctx = object.__new__(eden.Context)
+ctx._h, ctx._native = None, None
+for call in (lambda: ctx.linear(1, 2), lambda: ctx.checkpoint_empty(1, 2), lambda: eden.eden_act_backward(ctx, 1, 2)):
+    try:
+        call()
+    except ImportError as e:
+        assert "_binding.so" in str(e)
+    else:
+        raise SystemExit("not refused")
+""")
+    assert done.returncode == 0, done.stderr
+
+
+@pytest.mark.gpu
+def test_rounds_without_the_extension():
+    done = in_a_process("""
+import torch
+ctx = eden.Context(0, d_max=1 << 16, n_batch=2)
+x = torch.randn((2, 1 << 16), device="cuda")
+codes, scales = ctx.encode(x, [4.0, 4.0], [1, 2])
+mean = ctx.mean(codes, scales, [4.0, 4.0], [1, 2], 1 << 16)
+assert (mean - x.mean(dim=0)).norm() < 0.2 * x.mean(dim=0).norm() and ctx.status() == 0
+ctx.close()
+""")
+    assert done.returncode == 0, done.stderr
