@@ -90,5 +90,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def main():
+    print(build(force=True, verbose=True))
+
+
 if __name__ == "__main__":
-    print(build(force="--force" in sys.argv[1:], verbose=True))
+    main()

@@ -60,3 +60,13 @@ assert (mean - x.mean(dim=0)).norm() < 0.2 * x.mean(dim=0).norm() and ctx.status
 ctx.close()
 """)
     assert done.returncode == 0, done.stderr
+
+
+# ------------------------------------------------------------------------------- the build
+def test_the_command_builds_anew(monkeypatch, capsys):
+    from paper_2108_08842_b200 import build
+
+    calls = []
+    monkeypatch.setattr(build, "build", lambda **how: calls.append(how) or "libeden.so")
+    build.main()
+    assert calls == [dict(force=True, verbose=True)] and capsys.readouterr().out == "libeden.so\n"
