@@ -69,16 +69,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
             running.append((obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     if force or not os.path.exists(BINDING) or not _fresh_binding():
         running.append((BINDING, subprocess.Popen(_binding_command(BINDING + mark), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    failed = False
-    for obj, p in running:
+    failed = []
+    for made, p in running:
         out, _ = p.communicate()
         if verbose or p.returncode:
             sys.stderr.write(out)
         if p.returncode:
-            failed = True
+            failed.append(made)
         else:
-            os.replace(obj + mark, obj)
-    if failed:
+            os.replace(made + mark, made)
+    if any(made != BINDING for made in failed):
         raise RuntimeError("nvcc failed building libeden.so")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB + mark] + objects
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -86,6 +86,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("nvcc failed linking libeden.so")
     os.replace(LIB + mark, LIB)
+    if failed:
+        if os.path.exists(BINDING):                     # made for what was there before
+            os.remove(BINDING)
+        raise RuntimeError("g++ failed building _binding.so, which the training calls need; libeden.so is built")
     os.utime(BINDING)
     return LIB
 

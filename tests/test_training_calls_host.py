@@ -70,3 +70,17 @@ def test_the_command_builds_anew(monkeypatch, capsys):
     monkeypatch.setattr(build, "build", lambda **how: calls.append(how) or "libeden.so")
     build.main()
     assert calls == [dict(force=True, verbose=True)] and capsys.readouterr().out == "libeden.so\n"
+
+
+def test_a_failed_extension_is_named_and_the_library_is_there(monkeypatch, tmp_path):
+    from paper_2108_08842_b200 import build
+
+    build.build()                                        # the objects are there: only the link is left
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "libeden.so"))
+    monkeypatch.setattr(build, "BINDING", str(tmp_path / "_binding.so"))
+    monkeypatch.setattr(build, "_binding_command", lambda out: ["false"])
+    monkeypatch.setattr(build, "_fresh_binding", lambda: False)
+    (tmp_path / "_binding.so").write_text("an older one")
+    with pytest.raises(RuntimeError, match=r"g\+\+ failed building _binding.so"):
+        build.build()
+    assert (tmp_path / "libeden.so").exists() and not (tmp_path / "_binding.so").exists()
