@@ -35,7 +35,17 @@ def _fresh(obj: str) -> bool:
         return False
 
 
+def built_for() -> str:
+    """What the extension depends on besides its sources: it holds this, and is only loaded by the same."""
+    import torch
+
+    return "torch %s, python %d.%d" % ((torch.__version__,) + sys.version_info[:2])
+
+
 def _fresh_binding() -> bool:
+    with open(BINDING, "rb") as f:
+        if built_for().encode() not in f.read():
+            return False
     own = [os.path.join(CSRC, "binding.cpp"), os.path.join(os.path.dirname(HERE), "include", "eden.h"), os.path.abspath(__file__)]
     return all(os.path.getmtime(p) <= os.path.getmtime(BINDING) for p in own)
 
@@ -50,13 +60,13 @@ def _binding_command(out: str) -> list:
     includes = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                 sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
     libs = os.path.join(root, "lib")
-    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)] +
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", '-DEDEN_BUILT_FOR="%s"' % built_for(), "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)] +
             ["-isystem" + i for i in includes] + ["-o", out,
             os.path.join(CSRC, "binding.cpp"), "-L" + libs, "-Wl,-rpath," + libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and all(os.path.exists(p) and os.path.getmtime(p) >= _newest_source() for p in (LIB, BINDING)):
+    if not force and all(os.path.exists(p) and os.path.getmtime(p) >= _newest_source() for p in (LIB, BINDING)) and _fresh_binding():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     os.makedirs(OBJ, exist_ok=True)

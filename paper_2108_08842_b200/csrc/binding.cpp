@@ -513,4 +513,10 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__binding(void) { return PyModule_Create(&module_def); }
+// `built_for`: the torch and the Python whose interfaces this was compiled against
+PyMODINIT_FUNC PyInit__binding(void)
+{
+    PyObject* module = PyModule_Create(&module_def);
+    if (module && PyModule_AddStringConstant(module, "built_for", EDEN_BUILT_FOR) != 0) Py_CLEAR(module);
+    return module;
+}

@@ -15,6 +15,8 @@ from typing import List, NamedTuple, Optional, Sequence, Union
 import numpy as np
 import torch
 
+from . import build as _build
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libeden.so")
 
@@ -126,6 +128,8 @@ class _NoBinding:
 
 try:
     from . import _binding  # built with the library; needs torch loaded
+    if getattr(_binding, "built_for", None) != _build.built_for():
+        raise ImportError("it was built for %s" % getattr(_binding, "built_for", "something older"))
 except ImportError as _e:
     _binding = _NoBinding(_e)
 else:

@@ -84,3 +84,31 @@ def test_a_failed_extension_is_named_and_the_library_is_there(monkeypatch, tmp_p
     with pytest.raises(RuntimeError, match=r"g\+\+ failed building _binding.so"):
         build.build()
     assert (tmp_path / "libeden.so").exists() and not (tmp_path / "_binding.so").exists()
+
+
+def test_an_extension_for_another_torch_is_stale(monkeypatch):
+    from paper_2108_08842_b200 import _binding, build
+
+    build.build()
+    assert _binding.built_for == build.built_for() and torch.__version__ in build.built_for() and build._fresh_binding()
+    monkeypatch.setattr(torch, "__version__", "1.0")
+    assert not build._fresh_binding()
+
+
+def test_an_extension_for_another_torch_is_not_used():
+    done = in_a_process("""
+import types
+for name in [n for n in sys.modules if n.startswith("paper_2108_08842_b200")]:
+    del sys.modules[name]
+other = types.ModuleType("paper_2108_08842_b200._binding")
+other.built_for = "torch 1.0, python 2.7"
+sys.modules[other.__name__] = other
+from paper_2108_08842_b200 import eden
+try:
+    eden._binding.linear
+except ImportError as e:
+    assert "torch 1.0" in str(e)
+else:
+    raise SystemExit("not refused")
+""")
+    assert done.returncode == 0, done.stderr
