@@ -409,14 +409,16 @@ struct LinearShape {
 // of them (weight gradients, the column sums of input gradients) or codes do (a value between two
 // of them shows the smallest difference: of 16384 steps 6.5e-4 of the codes' values were off,
 // 1.5e-4 in fp32), they are taken out of tensor memory every kPromote products of 64 and added up,
-// rounded to nearest.  Weight gradients are 3e-7 off then (of 1024 steps; plain fp32 2.5e-7 over
-// 4096), column sums 6.5e-7 (1.3e-6 of 1024 steps), codes 1e-4 whatever the length.  Results of 16
-// bits alone do not show the drift: 1.66e-3 either way.
+// rounded to nearest.  Whatever the length, weight gradients are 1.4e-7 off then in bf16 and 4.3e-7
+// in fp16, whose products have bits to cut off too (2.9e-7 and 8e-7 in runs of 1024; plain fp32 over
+// 4096 steps 2.5e-7 and 6.2e-7), column sums 6.5e-7 (1.3e-6 of 1024 steps in one run), codes 1e-4.
+// Results of 16 bits alone do not show the drift: 1.66e-3 either way.
 //   Two runs: each has its half of the tensor memory; they are added up in the second one's place, and
 // the next tile's first run takes the other.  Linear 4096 x 4096 x 1024 with gelu and codes 45 -> 47 us.
-//   More: added up in registers while the next run is summed.  8192 x 4096 x 4096 with codes 198 -> 216 us.
+//   More: added up in registers while the next run is summed.  8192 x 4096 x 4096 with codes 198 -> 216
+// us, weight gradients 4096 x 4096 over 8191 tokens 209 -> 211 against runs of 1024.
 // RUNS: a kernel of its own, since its registers cost the others' epilogue time.
-template <int OP> constexpr uint32_t kPromote = OP == kWeightGrad ? 16 : 8;
+constexpr uint32_t kPromote = 8;
 
 // D = A B^T for tiles of 128 * CG x BN, persistent: block (pair) c takes tiles c, c + blocks, ...
 //   warp 0   fills the stages with tensor copies, kStages ahead of the products
@@ -452,7 +454,7 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
     const uint32_t first = grid.begin + blockIdx.x / (CG * splits), step = gridDim.x / (CG * splits);
     const uint32_t depth_begin = (uint32_t)((uint64_t)grid.depth_steps * part / splits);
     const uint32_t depth_end = (uint32_t)((uint64_t)grid.depth_steps * (part + 1) / splits);
-    constexpr uint32_t run = RUNS ? kPromote<OP> / S::kBoxes : 1u << 30;        // steps summed in tensor memory
+    constexpr uint32_t run = RUNS ? kPromote / S::kBoxes : 1u << 30;        // steps summed in tensor memory
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {

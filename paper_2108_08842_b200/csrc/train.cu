@@ -274,11 +274,11 @@ int launch_runs(eden_ctx* ctx, const Product& q, uint32_t splits, uint32_t begin
 {
     // codes and column sums are not left with the drift of long sums (kPromote)
     const bool exact = OP == kInputGrad ? q.p.column_sums != nullptr : q.p.save != EDEN_SAVE_NONE;
-    const bool runs = exact && (q.depth + 63) / 64 > (uint64_t)kPromote<OP> * splits;
+    const bool runs = exact && (q.depth + 63) / 64 > (uint64_t)kPromote * splits;
     if constexpr (OP != kWeightGrad && CG == 2 && !SPLIT) {
         // sums of up to 2048 do not hide such an epilogue behind their products (8200 cycles for 1024);
         // more than two runs do not fit the registers of sixteen epilogue warps
-        if ((q.p.act || q.p.residual || exact) && q.depth <= (runs ? 128 * kPromote<OP> : 2048)) {
+        if ((q.p.act || q.p.residual || exact) && q.depth <= (runs ? 128 * kPromote : 2048)) {
             if (runs) return launch_linear<OP, T, CG, BN, SPLIT, true, 4>(ctx, q, 1, begin, end);
             return launch_linear<OP, T, CG, BN, SPLIT, false, 4>(ctx, q, 1, begin, end);
         }

@@ -45,7 +45,7 @@ def splits(ctx, request):
 # ------------------------------------------------------------------------------- long sums
 # The tensor cores cut their fp32 sums off after every product of 16 steps.  A sum of like signs
 # that grows evenly over N products loses N / 4 units of its last place in the mean (half a unit of
-# what it has reached), a unit being at most 2^-23 of it.  Codes and bias gradients are to come of at
+# what it has reached), a unit being at most 2^-23 of it.  Codes and 32-bit results are to come of at
 # most 512 steps at a time, N = 32: 2^-20; the additions of the parts round by 2^-24 each.  (What is
 # added is cut off as well; products with 1 have too few bits for that.)
 CUT = 2.0 ** -20
@@ -92,6 +92,23 @@ def test_bias_gradients_of_long_sums(ctx, form, dtype, n):
         parts += R.f64(part)
     ctx.set_option(eden.OPT_LINEAR_SPLITS, 0)
     assert (np.abs(R.f64(whole) - parts) <= (n / 512 - 1 + 2 * 13) * 2.0 ** -24 * parts).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m", [1024, 1536, 4096])
+def test_weight_gradients_of_many_tokens(ctx, form, dtype, m):
+    """As above: between the whole and its parts of 512 tokens lie the additions of the parts."""
+    from paper_2108_08842_b200 import eden
+
+    n, k = 96, 200
+    g = torch.Generator(device="cuda").manual_seed(m)
+    dz = torch.rand((m, n), generator=g, device="cuda").add_(0.5).to(dtype)
+    x = torch.rand((m, k), generator=g, device="cuda").add_(0.5).to(dtype)
+    ctx.set_option(eden.OPT_LINEAR_SPLITS, 1)
+    whole = R.f64(ctx.linear_weight_grad(dz, x))
+    parts = sum(R.f64(ctx.linear_weight_grad(dz[i:i + 512], x[i:i + 512])) for i in range(0, m, 512))
+    ctx.set_option(eden.OPT_LINEAR_SPLITS, 0)
+    assert (np.abs(whole - parts) <= (m / 512 - 1) * 2.0 ** -24 * parts).all()
 
 
 # ------------------------------------------------------------------------------- small results
