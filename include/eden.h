@@ -413,7 +413,9 @@ const char* eden_strerror(int code);
  *     are below 2^31; m = 0 (no tokens) is allowed, n = 0 and k = 0 are not.
  *   - `type` is EDEN_TYPE_BF16 or EDEN_TYPE_FP16 (checkpoints also EDEN_TYPE_FP32): the type
  *     of activations, weights, biases and activation gradients.  Sums are held in fp32 and
- *     rounded once, where the result is stored.  Weight and bias gradients are fp32.
+ *     rounded once, where the result is stored.  The tensor cores cut fp32 sums off instead of
+ *     rounding them; where that would show (codes, 32-bit results) they are added up in parts
+ *     of 512, rounded to nearest.  Weight and bias gradients are fp32.
  *   - Checkpoint: a row of features is cut into groups of EDEN_CHECKPOINT_GROUP; the last one
  *     may be shorter.  A group keeps 2^e, e the smallest whole number with
  *     max|v| <= 127 * 2^e (at least -126), as the byte e + 127, and per value the int8 code
@@ -507,7 +509,9 @@ typedef struct eden_linear_input_grad_args {
 int eden_linear_input_grad(eden_ctx* ctx, const eden_linear_input_grad_args* args);
 
 /* weight_grad [n, k] (fp32) = dz [m, n]^T x [m, k], x either a matrix of dz's type (codes and
- * exps NULL) or a checkpoint (x NULL).  accumulate: added to what weight_grad holds. */
+ * exps NULL) or a checkpoint (x NULL), which stands for what eden_checkpoint_restore makes of it
+ * in dz's type: every value in bf16; in fp16 values past 65504 are that and values below 2^-24
+ * are rounded.  accumulate: added to what weight_grad holds. */
 typedef struct eden_linear_weight_grad_args {
     const void* dz;        uint64_t dz_stride;
     const void* x;         uint64_t x_stride;
