@@ -451,7 +451,9 @@ class Context:
 
     # ------------------------------------------------------------------ the client's training step
     # Wrong types, shapes, devices or names raise ValueError before anything is launched.
-    # Outputs that are not given are made on the context's stream.
+    # Outputs that are not given are made on the context's stream.  No autograd graph is recorded:
+    # tensors that require gradients are taken as they are, results require none, and the
+    # gradients are those of the calls below.
 
     def linear(self, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, save: str = "none",
@@ -490,8 +492,9 @@ class Context:
 
     def linear_weight_grad(self, dz: torch.Tensor, x, out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
         """eden_linear_weight_grad: dz [m, n]^T x [m, k] in fp32; x is a Checkpoint or a matrix
-        of dz's type.  out may be a view into the vector that encode takes (accumulate: added
-        to what it holds)."""
+        of dz's type (a Checkpoint stands for its values in that type: fp16 saturates and rounds
+        what it cannot hold).  out may be a view into the vector that encode takes (accumulate:
+        added to what it holds)."""
         return _binding.weight_grad(self._native, dz, x, out, accumulate)
 
     # ------------------------------------------------------------------ status

@@ -55,3 +55,16 @@ def test_a_pre_activation_is_looked_at_whatever_the_activation(act):
         with pytest.raises(ValueError):
             c.linear_input_grad(dy, w, pre=bad, act=act)
     c.close()
+
+
+def test_no_autograd_graph_is_recorded():
+    """Parameters are taken as they are: gradients come from the calls for them."""
+    from paper_2108_08842_b200 import eden
+
+    c = eden.Context(0, workspace_bytes_=eden.linear_workspace_bytes(64, 64, 64))
+    x, w = normal(1, 8, 64, dtype=torch.bfloat16), torch.nn.Parameter(normal(2, 64, 64, dtype=torch.bfloat16))
+    y, pre = c.linear(x, w, act="gelu", save="pre")
+    dx, db = c.linear_input_grad(y, w, pre=pre, act="gelu")
+    assert not any(t.requires_grad for t in (y, *pre, dx, db)) and w.grad is None
+    assert torch.equal(y, c.linear(x, w.detach(), act="gelu"))
+    c.close()
