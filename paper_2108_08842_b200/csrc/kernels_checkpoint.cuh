@@ -172,8 +172,9 @@ __global__ void __launch_bounds__(kCkptThreads) k_checkpoint_restore(T* x, uint6
 // dz = dy * act'(z).  A warp spans 32 half groups (512 columns) and walks down a run of rows,
 // eight warps to a block, each keeping the sums of its own rows; the block adds the eight up
 // and leaves the run's column sums in partial[run][n].  The next row waits in registers as it
-// lies in memory, so that four blocks fit on an SM: 8192 x 16384 bf16 with gelu takes 122 us (180
-// with two blocks), of which HBM's floor is 105.  Without WIDE the row goes round the warp to be
+// lies in memory, so that four blocks fit on an SM: 8192 x 16384 bf16 with gelu takes 131 us on the
+// device (138 to 144 a call with three states in turn), HBM's floor being 103; with two blocks and a shorter polynomial in
+// gelu's tail it took 180, with four 123.  Without WIDE the row goes round the warp to be
 // stored, as in the restore.
 template <typename T, int ACT, bool WIDE>
 __global__ void __launch_bounds__(kCkptThreads, WIDE ? 4 : 3) k_act_backward(const T* dy, uint64_t dy_stride, CheckpointView pre, T* dz,

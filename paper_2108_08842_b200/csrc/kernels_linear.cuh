@@ -428,7 +428,8 @@ constexpr uint32_t kPromote = 8;
 //            of the next tile (or of the next kPromote steps) fill its other half.  Eight warps
 //            (SIDES = 2), or sixteen with 104 registers each and a stage less where an epilogue
 //            that is more than a store may outlast the products: 36 against 40 us for bias, gelu
-//            and 8-bit codes on 4096 x 4096 x 1024, but 176 against 171 us for 8192 x 4096 x 4096
+//            and 8-bit codes on 4096 x 4096 x 1024 in one run, but 176 against 171 us for
+//            8192 x 4096 x 4096
 // CG = 2: the blocks of a pair hold 128 rows of A and half of the rows of B each; the first
 // one's barriers count both blocks' bytes, and its products write both blocks' sums.
 // SPLIT: one tile per cluster.  Its blocks (pairs) take a part of the sum each, leave their
@@ -706,7 +707,8 @@ k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUte
 // same code with a cluster of one block took 7.4 us where this takes 4.8).
 // Two blocks on an SM hide each other's ends: one with twice the loads on their way took 5.8 us
 // against 4.1 for 13 x 2731 x 1000 and 7.7 against 4.0 for 1 x 2731 x 1001.  1 x 4096 x 4096 bf16
-// takes 4.9 us with the weights in the L2 cache (5.1 is HBM's floor), 1 x 16384 x 4096 25.7 us (21).
+// takes 8.2 us with weights from HBM, whose floor is 5.1 (4.9 with the weights in the L2 cache, hot),
+// 1 x 16384 x 4096 25.7 us (21).
 constexpr int kFewThreads = 512;
 
 // 8 values at p, of which the first `count` exist; VEC: 16-byte aligned, count 8 or 0
