@@ -523,6 +523,201 @@ typedef struct eden_linear_weight_grad_args {
 } eden_linear_weight_grad_args;
 int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_grad_args* args);
 
+/* ---- what joins a client's blocks: norms, gate, dropout, residual ------------------------------
+ *
+ *   u = after(h)      x = scale * residual + gate * dropout(u)      y = before(x)
+ *
+ * in one pass over the rows: the norm behind a block, its gate and dropout, the residual stream and
+ * the norm in front of the next block.  Every part can be left out, so that the same calls are a
+ * norm alone, dropout alone, or a residual sum and a norm.
+ *
+ *   - Norm of a row v of n values: (v - mean) * rate * weight + bias with
+ *       EDEN_NORM_RMS    mean = 0, rate = 1 / sqrt(sum(v^2) / n + eps)
+ *       EDEN_NORM_LAYER  rate = 1 / sqrt(sum((v - mean)^2) / n + eps)
+ *     `stats` holds mean and rate of each row in fp32, for the backward pass.  Rows with norms
+ *     have at most EDEN_NORM_MAX_FEATURES values.
+ *   - Dropout: value (row, col) is kept where the 16-bit number that belongs to it is below
+ *     round(65536 * (1 - rate)), and divided by the exact chance of that; else it is 0, whatever it
+ *     was.  The number is half number col % 8 (word by word, the low half first) of Philox4x32-10
+ *     with counter (col / 8, first_row + row, 3, 0) and the seed as key (low word first).  Nothing
+ *     of it is stored: the backward pass makes the mask again.  It depends on no stride, type or
+ *     number of rows, so a batch cut into parts (first_row) has the mask of the whole.  seed_at:
+ *     the seed is read from device memory when the call runs, so that a captured call can be
+ *     replayed with another one.
+ *   - gate: a vector of n values, or (gate_per_value) a matrix.
+ *   - Everything is computed in fp32 and rounded once, where it is stored; y comes from x before
+ *     its rounding.
+ *   - As above: `type` is EDEN_TYPE_BF16 or EDEN_TYPE_FP16 (also of weights, biases and gates),
+ *     strides count elements, counts are below 2^31, m = 0 is allowed.  An output may be the same
+ *     matrix as an input (same pointer and stride) that has a value for every one of its own; else
+ *     nothing may overlap. */
+#define EDEN_NORM_NONE  0
+#define EDEN_NORM_RMS   1
+#define EDEN_NORM_LAYER 2
+#define EDEN_NORM_MAX_FEATURES 32768u
+
+typedef struct eden_norm {
+    const void* weight;                                 /* n values, or NULL: 1 */
+    const void* bias;                                   /* n values, or NULL: 0 */
+    float eps;                                          /* at least 0 */
+    int32_t kind;
+} eden_norm;
+
+typedef struct eden_drop {
+    double rate;                                        /* 0 to 1; 0: no dropout */
+    uint64_t seed;
+    const uint64_t* seed_at;                            /* dev, or NULL: seed */
+    uint64_t first_row;
+} eden_drop;
+
+/* Device workspace of eden_block_join_backward for rows of n values (eden_block_join needs none). */
+uint64_t eden_block_workspace_bytes(uint64_t n);
+
+typedef struct eden_block_join_args {
+    const void* h;         uint64_t h_stride;
+    const void* residual;  uint64_t residual_stride;    /* or NULL */
+    const void* gate;      uint64_t gate_stride;        /* or NULL; stride: gate_per_value */
+    void* x;               uint64_t x_stride;           /* or NULL with a norm before */
+    void* y;               uint64_t y_stride;           /* with a norm before */
+    float* after_stats;                                 /* [m][2] or NULL */
+    float* before_stats;
+    eden_norm after, before;
+    eden_drop drop;
+    uint64_t m, n;
+    float scale;
+    int32_t type, gate_per_value, reserved;
+} eden_block_join_args;
+int eden_block_join(eden_ctx* ctx, const eden_block_join_args* args);
+
+/* An activation that was kept for the backward pass: a matrix, or (data NULL) its checkpoint. */
+typedef struct eden_kept {
+    const void* data;      uint64_t stride;
+    const int8_t* codes;   uint64_t codes_stride;
+    const uint8_t* exps;   uint64_t exps_stride;
+} eden_kept;
+
+/* The gradients, from dx (of x; NULL: 0) and dy (of y).  With t = dx + the gradient of the norm before:
+ *   d_residual = scale * t, dh, and d_gate (gate_per_value), in `type`;
+ *   the sums over the rows in fp32 (accumulate: added to what is there): the norms' weights and
+ *   biases, gate_sum (a vector gate).
+ * Each output may be NULL.  h: with a norm after or a gate; x: with a norm before. */
+typedef struct eden_block_join_backward_args {
+    const void* dx;        uint64_t dx_stride;
+    const void* dy;        uint64_t dy_stride;
+    eden_kept h, x;
+    const void* gate;      uint64_t gate_stride;
+    const float* after_stats;
+    const float* before_stats;
+    void* d_residual;      uint64_t d_residual_stride;
+    void* dh;              uint64_t dh_stride;
+    void* d_gate;          uint64_t d_gate_stride;
+    float* gate_sum;
+    float* after_weight_grad;
+    float* after_bias_grad;
+    float* before_weight_grad;
+    float* before_bias_grad;
+    eden_norm after, before;
+    eden_drop drop;
+    uint64_t m, n;
+    float scale;
+    int32_t type, gate_per_value, accumulate;
+} eden_block_join_backward_args;
+int eden_block_join_backward(eden_ctx* ctx, const eden_block_join_backward_args* args);
+
+/* ---- microscaled 4-bit floating point: quantisation and products --------------------------------
+ *
+ * The training step's products with both operands in groups of EDEN_CHECKPOINT_GROUP values along
+ * the sum: a group keeps 2^e, e the smallest whole number with max|v| <= 6 * 2^e (at least -126), and
+ * per value a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 for v / 2^e, rounded to nearest, ties to
+ * the even code (0, 1, 2, 4 and their like).  A group that holds an infinity or a NaN is NaN as a
+ * whole.
+ *
+ *   - A matrix of `rows` rows of `features` values in this form (eden_mx4): codes, two a byte, the
+ *     low half first, code = sign << 3 | place of the magnitude in the list, rows of
+ *     eden_mx4_code_bytes(features) bytes, codes past the last value 0; exponents, the byte e + 127
+ *     (255: NaN; 0 stands for 2^-127), in tiles of 128 rows x 256 values: group g of row r is byte
+ *         (r / 128 * ceil(features / 256) + g / 8) * 1024 + g / 4 % 2 * 512 + r % 32 * 16 + r / 32 % 4 * 4 + g % 4
+ *     of eden_mx4_exponent_bytes(rows, features); no byte of a tile may be 255 but for a NaN group.
+ *     Codes start on 16 bytes, as do their rows (codes_stride, in bytes) and the exponents.
+ *   - The sums run along the groups, so each product of a layer's training step reads its operands in
+ *     another form, and eden_mx4_quantize writes one or both from one read of the matrix: `rows` has
+ *     the groups along the rows of x [m, n], `columns` is the form of x^T [n, m].
+ *       forward       y  = x W^T     x and W by rows
+ *       input grad    dx = dz W      dz by rows, W by columns (weight_t [k, n])
+ *       weight grad   dW = dz^T x    dz and x by columns (dz_t [n, m], x_t [k, m])
+ *   - The products of two codes and their scales are exact, sums are held in fp32 as for the
+ *     products above (codes and 32-bit results: in parts of 2048 added up, rounded to nearest). */
+typedef struct eden_mx4 {
+    uint8_t* codes;        uint64_t codes_stride;
+    uint8_t* exps;
+} eden_mx4;
+
+/* bytes of a row's codes, and of the exponents */
+uint64_t eden_mx4_code_bytes(uint64_t features);
+uint64_t eden_mx4_exponent_bytes(uint64_t rows, uint64_t features);
+/* Device workspace that holds every call of this section with m tokens and weights of n x k. */
+uint64_t eden_mx4_workspace_bytes(uint64_t m, uint64_t n, uint64_t k);
+
+typedef struct eden_mx4_quantize_args {
+    const void* x;         uint64_t x_stride;           /* [m, n] */
+    eden_mx4 rows;                                      /* of x, or codes NULL */
+    eden_mx4 columns;                                   /* of x^T, or codes NULL */
+    uint64_t m, n;
+    int32_t type, reserved;                             /* also EDEN_TYPE_FP32 */
+} eden_mx4_quantize_args;
+int eden_mx4_quantize(eden_ctx* ctx, const eden_mx4_quantize_args* args);
+
+/* x [m, n] <- the values, rounded once to `type` (also EDEN_TYPE_FP32); values past the type's
+ * largest number are restored as that. */
+typedef struct eden_mx4_restore_args {
+    void* x;               uint64_t x_stride;
+    eden_mx4 q;
+    uint64_t m, n;
+    int32_t type, reserved;
+} eden_mx4_restore_args;
+int eden_mx4_restore(eden_ctx* ctx, const eden_mx4_restore_args* args);
+
+/* eden_linear with x [m, k] and weight [n, k] in 4 bits: x a matrix of `type`, which the call
+ * quantises, or (NULL) held. */
+typedef struct eden_mx4_linear_args {
+    const void* x;         uint64_t x_stride;
+    eden_mx4 held;                                      /* x NULL */
+    eden_mx4 weight;
+    const void* bias;                                   /* or NULL */
+    const void* residual;  uint64_t residual_stride;    /* or NULL */
+    void* y;               uint64_t y_stride;
+    int8_t* saved;         uint64_t saved_stride;       /* save != EDEN_SAVE_NONE */
+    uint8_t* saved_exp;    uint64_t saved_exp_stride;
+    uint64_t m, n, k;
+    int32_t type, act, save, reserved;
+} eden_mx4_linear_args;
+int eden_mx4_linear(eden_ctx* ctx, const eden_mx4_linear_args* args);
+
+/* eden_linear_input_grad with dz [m, n] (a matrix of `type`, which the call quantises, or held) and
+ * the weights by columns, weight_t [k, n]. */
+typedef struct eden_mx4_linear_input_grad_args {
+    const void* dz;        uint64_t dz_stride;
+    eden_mx4 held;                                      /* dz NULL */
+    eden_mx4 weight_t;
+    const void* residual;  uint64_t residual_stride;    /* or NULL */
+    const int8_t* pre;     uint64_t pre_stride;         /* or NULL with EDEN_ACT_NONE */
+    const uint8_t* pre_exp; uint64_t pre_exp_stride;
+    void* dx;              uint64_t dx_stride;
+    float* bias_grad;                                   /* or NULL */
+    uint64_t m, n, k;
+    int32_t type, act, accumulate, reserved;            /* accumulate: bias_grad += */
+} eden_mx4_linear_input_grad_args;
+int eden_mx4_linear_input_grad(eden_ctx* ctx, const eden_mx4_linear_input_grad_args* args);
+
+/* weight_grad [n, k] (fp32) = dz_t [n, m] x_t [k, m]^T; accumulate: added to what it holds. */
+typedef struct eden_mx4_linear_weight_grad_args {
+    eden_mx4 dz_t, x_t;
+    float* weight_grad;    uint64_t weight_grad_stride;
+    uint64_t m, n, k;
+    int32_t accumulate, reserved;
+} eden_mx4_linear_weight_grad_args;
+int eden_mx4_linear_weight_grad(eden_ctx* ctx, const eden_mx4_linear_weight_grad_args* args);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,8 +33,16 @@ struct Library {
     int (*act_backward)(eden_ctx*, const eden_act_backward_args*);
     int (*input_grad)(eden_ctx*, const eden_linear_input_grad_args*);
     int (*weight_grad)(eden_ctx*, const eden_linear_weight_grad_args*);
+    int (*join)(eden_ctx*, const eden_block_join_args*);
+    int (*join_backward)(eden_ctx*, const eden_block_join_backward_args*);
+    int (*mx4_quantize)(eden_ctx*, const eden_mx4_quantize_args*);
+    int (*mx4_restore)(eden_ctx*, const eden_mx4_restore_args*);
+    int (*mx4_linear)(eden_ctx*, const eden_mx4_linear_args*);
+    int (*mx4_input_grad)(eden_ctx*, const eden_mx4_linear_input_grad_args*);
+    int (*mx4_weight_grad)(eden_ctx*, const eden_mx4_linear_weight_grad_args*);
 } lib;
-PyObject *error_type = nullptr, *checkpoint_type = nullptr;
+constexpr int kCalls = sizeof(Library) / sizeof(void*);
+PyObject *error_type = nullptr, *checkpoint_type = nullptr, *mx4_type = nullptr;
 
 [[noreturn]] void refuse(const std::string& what)
 {
@@ -458,6 +466,508 @@ PyObject* weight_grad(PyObject*, PyObject* const* v, Py_ssize_t count)
     });
 }
 
+// ---- what joins the blocks ----------------------------------------------------------------
+const char* const kNorms[] = {"none", "rms", "layer"};
+
+double number_of(PyObject* o, const char* name)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse(std::string(name) + " has to be a number");
+    }
+    return v;
+}
+
+uint64_t count_of(PyObject* o, const char* name)
+{
+    const unsigned long long v = PyLong_Check(o) ? PyLong_AsUnsignedLongLong(o) : (unsigned long long)-1;
+    if (!PyLong_Check(o) || PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse(std::string(name) + " has to be a whole number from 0 to 2^64 - 1");
+    }
+    return v;
+}
+
+// a norm (weight, bias, kind, eps), or None
+eden_norm norm_of(const Native* n, PyObject* o, const char* name, int64_t cols, at::ScalarType t)
+{
+    eden_norm r;
+    std::memset(&r, 0, sizeof(r));
+    if (!given(o)) return r;
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) refuse(std::string(name) + " has to be a Norm");
+    const std::string at = std::string(" of ") + name;
+    if (given(PyTuple_GET_ITEM(o, 0))) r.weight = vector_of(n, PyTuple_GET_ITEM(o, 0), ("the weight" + at).c_str(), cols, t);
+    if (given(PyTuple_GET_ITEM(o, 1))) r.bias = vector_of(n, PyTuple_GET_ITEM(o, 1), ("the bias" + at).c_str(), cols, t);
+    r.kind = name_of(PyTuple_GET_ITEM(o, 2), ("the kind" + at).c_str(), kNorms, 3);
+    r.eps = (float)number_of(PyTuple_GET_ITEM(o, 3), ("eps" + at).c_str());
+    if (!(r.eps >= 0.f) || r.eps > 1e30f) refuse("eps" + at + " has to be a finite number from 0 on");
+    if (r.kind == EDEN_NORM_NONE) r.weight = r.bias = nullptr;
+    return r;
+}
+
+eden_drop drop_of(const Native* n, PyObject* rate, PyObject* seed, PyObject* first_row)
+{
+    eden_drop d;
+    std::memset(&d, 0, sizeof(d));
+    d.rate = number_of(rate, "drop");
+    if (!(d.rate >= 0.0 && d.rate <= 1.0)) refuse("drop has to be from 0 to 1");
+    d.first_row = count_of(first_row, "first_row");
+    if (THPVariable_Check(seed)) {
+        const at::Tensor& t = THPVariable_Unpack(seed);
+        if (t.scalar_type() != at::kLong || t.numel() != 1 || !t.is_cuda() || t.get_device() != n->device)
+            refuse("seed has to be a whole number, or one int64 on cuda:" + std::to_string(n->device) + ", got " + described(t));
+        d.seed_at = (const uint64_t*)t.data_ptr();
+    } else {
+        d.seed = count_of(seed, "seed");
+    }
+    return d;
+}
+
+// a gate: one value per column, or a matrix
+const void* gate_of(const Native* n, PyObject* o, int64_t rows, int64_t cols, at::ScalarType t, uint64_t* stride, int32_t* per_value)
+{
+    *stride = 0;
+    *per_value = 0;
+    if (!given(o)) return nullptr;
+    const at::Tensor& gate = tensor_of(o, "gate");
+    if (gate.dim() != 2) return vector_of(n, o, "gate", cols, t);
+    const Matrix m(n, gate, "gate", rows, cols, t);
+    *stride = m.stride;
+    *per_value = 1;
+    return m.data;
+}
+
+const at::Tensor* tensor_in(PyObject* o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
+const at::Tensor* tensor_in(PyObject* o, int i) { return PyTuple_Check(o) && PyTuple_GET_SIZE(o) > i ? tensor_in(PyTuple_GET_ITEM(o, i)) : nullptr; }
+
+float* stats_of(const Native* n, PyObject* o, const char* name, int64_t rows)
+{
+    const at::Tensor& t = tensor_of(o, name);
+    if (t.dim() != 2 || t.scalar_type() != at::kFloat || t.size(0) != rows || t.size(1) != 2 || !t.is_cuda() || t.get_device() != n->device || !t.is_contiguous())
+        refuse(std::string(name) + " has to be a contiguous Float [" + std::to_string(rows) + ", 2] on cuda:" + std::to_string(n->device) + ", got " + described(t));
+    if ((uintptr_t)t.data_ptr() & 7) refuse(std::string(name) + " has to start on 8 bytes");
+    return (float*)t.data_ptr();
+}
+
+// (native, h, residual, after, before, gate, scale, drop, seed, first_row, out, normed, stats)
+//   -> (x, y, after_stats, before_stats)
+PyObject* join(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 13, [&]() -> PyObject* {
+        const Native* n = native_of(v[0]);
+        const at::Tensor& h = matrix_of(v[1], "h");
+        const int64_t m = h.size(0), cols = h.size(1);
+        const at::ScalarType t = h.scalar_type();
+        eden_block_join_args a;
+        std::memset(&a, 0, sizeof(a));
+        a.type = type_of(h, false, "h");
+        const Matrix mh(n, h, "h", m, cols, t);
+        a.h = mh.data; a.h_stride = mh.stride;
+        a.after = norm_of(n, v[3], "after", cols, t);
+        a.before = norm_of(n, v[4], "before", cols, t);
+        a.gate = gate_of(n, v[5], m, cols, t, &a.gate_stride, &a.gate_per_value);
+        a.scale = (float)number_of(v[6], "scale");
+        a.drop = drop_of(n, v[7], v[8], v[9]);
+        at::Tensor residual, x, y, after_stats, before_stats;
+        if (given(v[2])) {
+            residual = matrix_of(v[2], "residual");
+            const Matrix r(n, residual, "residual", m, cols, t);
+            a.residual = r.data; a.residual_stride = r.stride;
+        }
+        if (!left_out(v[10])) {
+            x = given(v[10]) ? matrix_of(v[10], "out") : fresh(n, {m, cols}, t);
+            const Matrix mx(n, x, "out", m, cols, t);
+            a.x = mx.data; a.x_stride = mx.stride;
+        } else if (!a.before.kind) {
+            refuse("out is left out, and there is no norm before");
+        }
+        if (a.before.kind) {
+            if (left_out(v[11])) refuse("normed cannot be left out of a call with a norm before");
+            y = given(v[11]) ? matrix_of(v[11], "normed") : fresh(n, {m, cols}, t);
+            const Matrix my(n, y, "normed", m, cols, t);
+            a.y = my.data; a.y_stride = my.stride;
+        } else if (given(v[11]) && !left_out(v[11])) {
+            refuse("normed is given, but there is no norm before");
+        }
+        if (flag_of(v[12])) {
+            if (a.after.kind) a.after_stats = (float*)(after_stats = fresh(n, {m, 2}, at::kFloat)).data_ptr();
+            if (a.before.kind) a.before_stats = (float*)(before_stats = fresh(n, {m, 2}, at::kFloat)).data_ptr();
+        }
+        a.m = (uint64_t)m; a.n = (uint64_t)cols;
+        done(n, lib.join(n->ctx, &a), {&h, &residual, &x, &y, &after_stats, &before_stats, tensor_in(v[3], 0), tensor_in(v[3], 1), tensor_in(v[4], 0),
+                                       tensor_in(v[4], 1), tensor_in(v[5]), tensor_in(v[8])});
+        PyObject* r = PyTuple_New(4);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, returned(v[10], x));
+        PyTuple_SET_ITEM(r, 1, !a.before.kind ? again(Py_None) : given(v[11]) ? again(v[11]) : wrapped(y));
+        PyTuple_SET_ITEM(r, 2, after_stats.defined() ? wrapped(after_stats) : again(Py_None));
+        PyTuple_SET_ITEM(r, 3, before_stats.defined() ? wrapped(before_stats) : again(Py_None));
+        return r;
+    });
+}
+
+// an activation that was kept: a matrix of type t, or a checkpoint
+eden_kept kept_of(const Native* n, PyObject* o, const char* name, int64_t rows, int64_t cols, at::ScalarType t)
+{
+    eden_kept k;
+    std::memset(&k, 0, sizeof(k));
+    if (THPVariable_Check(o)) {
+        const Matrix m(n, THPVariable_Unpack(o), name, rows, cols, t);
+        k.data = m.data; k.stride = m.stride;
+    } else {
+        const Checkpoint c = checkpoint_of(n, o, name, rows, cols);
+        k.codes = (const int8_t*)c.c.data; k.codes_stride = c.c.stride;
+        k.exps = (const uint8_t*)c.e.data; k.exps_stride = c.e.stride;
+    }
+    return k;
+}
+
+// (native, dx, dy, h, x, after_stats, before_stats, after, before, gate, scale, drop, seed, first_row, residual, out, gate_grad,
+//  after_weight_grad, after_bias_grad, before_weight_grad, before_bias_grad, accumulate)
+//   -> (residual, h, gate, after weight, after bias, before weight, before bias)
+PyObject* join_backward(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 22, [&]() -> PyObject* {
+        const Native* n = native_of(v[0]);
+        if (!given(v[1]) && !given(v[2])) refuse("dx and dy are both left out");
+        const at::Tensor& leading = given(v[1]) ? matrix_of(v[1], "dx") : matrix_of(v[2], "dy");
+        const int64_t m = leading.size(0), cols = leading.size(1);
+        const at::ScalarType t = leading.scalar_type();
+        eden_block_join_backward_args a;
+        std::memset(&a, 0, sizeof(a));
+        a.type = type_of(leading, false, given(v[1]) ? "dx" : "dy");
+        a.after = norm_of(n, v[7], "after", cols, t);
+        a.before = norm_of(n, v[8], "before", cols, t);
+        a.gate = gate_of(n, v[9], m, cols, t, &a.gate_stride, &a.gate_per_value);
+        a.scale = (float)number_of(v[10], "scale");
+        a.drop = drop_of(n, v[11], v[12], v[13]);
+        a.accumulate = flag_of(v[21]);
+        if (given(v[1])) {
+            const Matrix d(n, leading, "dx", m, cols, t);
+            a.dx = d.data; a.dx_stride = d.stride;
+        }
+        if (given(v[2])) {
+            if (!a.before.kind) refuse("dy is given, but there is no norm before");
+            const Matrix d(n, matrix_of(v[2], "dy"), "dy", m, cols, t);
+            a.dy = d.data; a.dy_stride = d.stride;
+        } else if (a.before.kind) {
+            refuse("a norm before needs its gradient dy");
+        }
+        if (a.before.kind) {
+            if (!given(v[4])) refuse("the gradient of the norm before needs x");
+            a.x = kept_of(n, v[4], "x", m, cols, t);
+            a.before_stats = stats_of(n, v[6], "before_stats", m);
+        }
+        if (a.after.kind || a.gate) {
+            if (!given(v[3])) refuse("the gradients of a norm after and of a gate need h");
+            a.h = kept_of(n, v[3], "h", m, cols, t);
+        }
+        if (a.after.kind) a.after_stats = stats_of(n, v[5], "after_stats", m);
+        auto matrix = [&](PyObject* o, const char* name, at::Tensor& made, void*& data, uint64_t& stride) {
+            if (left_out(o)) return;
+            made = given(o) ? matrix_of(o, name) : fresh(n, {m, cols}, t);
+            const Matrix d(n, made, name, m, cols, t);
+            data = d.data; stride = d.stride;
+        };
+        at::Tensor residual, dh, gate, sums[4];
+        matrix(v[14], "residual", residual, a.d_residual, a.d_residual_stride);
+        matrix(v[15], "out", dh, a.dh, a.dh_stride);
+        if (!a.gate && given(v[16]) && !left_out(v[16])) refuse("gate_grad is given, but there is no gate");
+        auto vector = [&](PyObject* o, const char* name, bool wanted, bool there, at::Tensor& made, float*& data) {
+            if (left_out(o)) return;
+            if (given(o) && !there) refuse(std::string(name) + " is given, but there is nothing that it is the gradient of");
+            if (!given(o) && !wanted) return;
+            made = sums_of(n, o, name, cols, a.accumulate);
+            data = (float*)made.data_ptr();
+        };
+        if (a.gate && a.gate_per_value) matrix(v[16], "gate_grad", gate, a.d_gate, a.d_gate_stride);
+        else if (a.gate) vector(v[16], "gate_grad", true, true, gate, a.gate_sum);
+        vector(v[17], "after_weight_grad", a.after.weight != nullptr, a.after.kind != 0, sums[0], a.after_weight_grad);
+        vector(v[18], "after_bias_grad", a.after.bias != nullptr, a.after.kind != 0, sums[1], a.after_bias_grad);
+        vector(v[19], "before_weight_grad", a.before.weight != nullptr, a.before.kind != 0, sums[2], a.before_weight_grad);
+        vector(v[20], "before_bias_grad", a.before.bias != nullptr, a.before.kind != 0, sums[3], a.before_bias_grad);
+        a.m = (uint64_t)m; a.n = (uint64_t)cols;
+        done(n, lib.join_backward(n->ctx, &a),
+             {tensor_in(v[1]), tensor_in(v[2]), tensor_in(v[3]), tensor_in(v[3], 0), tensor_in(v[3], 1), tensor_in(v[4]), tensor_in(v[4], 0), tensor_in(v[4], 1),
+              tensor_in(v[5]), tensor_in(v[6]), tensor_in(v[7], 0), tensor_in(v[7], 1), tensor_in(v[8], 0), tensor_in(v[8], 1), tensor_in(v[9]), tensor_in(v[12]),
+              &residual, &dh, &gate, &sums[0], &sums[1], &sums[2], &sums[3]});
+        const at::Tensor* const made[7] = {&residual, &dh, &gate, &sums[0], &sums[1], &sums[2], &sums[3]};
+        PyObject* r = PyTuple_New(7);
+        if (!r) return nullptr;
+        for (int i = 0; i < 7; ++i) {
+            PyObject* const o = v[14 + i];
+            PyTuple_SET_ITEM(r, i, !made[i]->defined() ? again(Py_None) : given(o) ? again(o) : wrapped(*made[i]));
+        }
+        return r;
+    });
+}
+
+// ---- 4 bits -------------------------------------------------------------------------------
+int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+
+struct Mx4 {
+    at::Tensor codes, exps;
+    int64_t features = 0;
+    eden_mx4 view() const { return {(uint8_t*)codes.data_ptr(), (uint64_t)(codes.size(0) > 1 ? codes.stride(0) : codes.size(1)), (uint8_t*)exps.data_ptr()}; }
+};
+
+bool is_mx4(PyObject* o) { return PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 3; }
+
+// rows or features below 0: any
+Mx4 mx4_of(const Native* n, PyObject* o, const char* name, int64_t rows, int64_t features)
+{
+    if (!is_mx4(o)) refuse(std::string(name) + " has to be an Mx4");
+    Mx4 q;
+    q.codes = tensor_of(PyTuple_GET_ITEM(o, 0), name);
+    q.exps = tensor_of(PyTuple_GET_ITEM(o, 1), name);
+    q.features = PyLong_Check(PyTuple_GET_ITEM(o, 2)) ? PyLong_AsLongLong(PyTuple_GET_ITEM(o, 2)) : -1;
+    if (PyErr_Occurred() || q.features < 1 || q.features > 0x7FFFFFFF) {
+        PyErr_Clear();
+        refuse(std::string("the features of ") + name + " have to be a whole number from 1 on");
+    }
+    const std::string at = std::string(" of ") + name;
+    if (q.codes.dim() != 2 || (features >= 0 && q.features != features) || (rows >= 0 && q.codes.size(0) != rows))
+        refuse(std::string(name) + " has to hold [" + (rows >= 0 ? std::to_string(rows) : "rows") + ", " + (features >= 0 ? std::to_string(features) : "features") +
+               "] values, got features " + std::to_string(q.features) + " and codes " + described(q.codes));
+    const Matrix codes(n, q.codes, ("the codes" + at).c_str(), q.codes.size(0), groups_of(q.features) * 16, at::kByte);
+    if ((uintptr_t)codes.data & 15 || codes.stride & 15) refuse("the rows of the codes" + at + " have to start on 16 bytes");
+    const int64_t across = tiles_of(q.codes.size(0), 128), along = tiles_of(q.features, 256);
+    if (q.exps.dim() != 3 || q.exps.scalar_type() != at::kByte || q.exps.size(0) != across || q.exps.size(1) != along || q.exps.size(2) != 1024 || !q.exps.is_cuda() ||
+        q.exps.get_device() != n->device || !q.exps.is_contiguous() || (uintptr_t)q.exps.data_ptr() & 15)
+        refuse("the exponents" + at + " have to be contiguous Byte [" + std::to_string(across) + ", " + std::to_string(along) + ", 1024] on cuda:" +
+               std::to_string(n->device) + " and 16 bytes, got " + described(q.exps));
+    return q;
+}
+
+Mx4 fresh_mx4(const Native* n, int64_t rows, int64_t features)
+{
+    Mx4 q;
+    q.codes = fresh(n, {rows, groups_of(features) * 16}, at::kByte);
+    q.exps = fresh(n, {tiles_of(rows, 128), tiles_of(features, 256), 1024}, at::kByte);
+    q.features = features;
+    return q;
+}
+
+PyObject* wrapped_mx4(const Mx4& q)
+{
+    PyObject *codes = wrapped(q.codes), *exps = wrapped(q.exps), *features = PyLong_FromLongLong(q.features);
+    PyObject* r = codes && exps && features ? PyObject_CallFunctionObjArgs(mx4_type, codes, exps, features, nullptr) : nullptr;
+    Py_XDECREF(codes);
+    Py_XDECREF(exps);
+    Py_XDECREF(features);
+    return r;
+}
+
+// (native, rows, features)
+PyObject* mx4_empty(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 3, [&]() -> PyObject* {
+        const int64_t m = PyLong_AsLongLong(v[1]), n = PyLong_AsLongLong(v[2]);
+        if (PyErr_Occurred()) throw Refused();
+        if (m < 0 || n < 1) refuse("an Mx4 has rows from 0 and features from 1 on");
+        return wrapped_mx4(fresh_mx4(native_of(v[0]), m, n));
+    });
+}
+
+// (native, x, rows, columns): each an Mx4, None (made) or False (left out)
+PyObject* mx4_quantize(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 4, [&]() -> PyObject* {
+        const Native* n = native_of(v[0]);
+        const at::Tensor& x = matrix_of(v[1], "x");
+        const int64_t m = x.size(0), cols = x.size(1);
+        eden_mx4_quantize_args a;
+        std::memset(&a, 0, sizeof(a));
+        a.type = type_of(x, true, "x");
+        const Matrix mx(n, x, "x", m, cols, x.scalar_type());
+        a.x = mx.data; a.x_stride = mx.stride;
+        if (cols < 1) refuse("x has no features");
+        if (!left_out(v[3]) && m < 1) refuse("the columns of a matrix without rows have no groups");
+        Mx4 rows, columns;
+        if (!left_out(v[2])) {
+            rows = given(v[2]) ? mx4_of(n, v[2], "out", m, cols) : fresh_mx4(n, m, cols);
+            a.rows = rows.view();
+        }
+        if (!left_out(v[3])) {
+            columns = given(v[3]) ? mx4_of(n, v[3], "out", cols, m) : fresh_mx4(n, cols, m);
+            a.columns = columns.view();
+        }
+        a.m = (uint64_t)m; a.n = (uint64_t)cols;
+        if (m > 0) done(n, lib.mx4_quantize(n->ctx, &a), {&x, &rows.codes, &rows.exps, &columns.codes, &columns.exps});
+        auto result = [&](PyObject* o, const Mx4& q) { return given(o) ? again(o) : wrapped_mx4(q); };
+        if (left_out(v[3])) return result(v[2], rows);
+        if (left_out(v[2])) return result(v[3], columns);
+        return pair(result(v[2], rows), result(v[3], columns));
+    });
+}
+
+at::ScalarType scalar_of(PyObject* o, const char* what, bool with_fp32)
+{
+    if (!THPDtype_Check(o)) refuse(std::string(what) + " has to be a dtype");
+    const at::ScalarType t = ((THPDtype*)o)->scalar_type;
+    if (t != at::kBFloat16 && t != at::kHalf && !(with_fp32 && t == at::kFloat)) refuse(std::string(what) + " has to be bf16" + (with_fp32 ? ", fp16 or fp32" : " or fp16"));
+    return t;
+}
+
+// (native, q, dtype, out)
+PyObject* mx4_restore(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 4, [&]() -> PyObject* {
+        const Native* n = native_of(v[0]);
+        const at::ScalarType t = scalar_of(v[2], "dtype", true);
+        const Mx4 q = mx4_of(n, v[1], "q", -1, -1);
+        const int64_t m = q.codes.size(0);
+        const at::Tensor out = given(v[3]) ? matrix_of(v[3], "out") : fresh(n, {m, q.features}, t);
+        const Matrix mo(n, out, "out", m, q.features, t);
+        const eden_mx4_restore_args a{mo.data, mo.stride, q.view(), (uint64_t)m, (uint64_t)q.features, type_of(out, true, "out"), 0};
+        if (m > 0) done(n, lib.mx4_restore(n->ctx, &a), {&out, &q.codes, &q.exps});
+        return given(v[3]) ? again(v[3]) : wrapped(out);
+    });
+}
+
+// An operand [m, k]: a matrix of a 16-bit type, or an Mx4, whose product has the given type, else
+// that of the first tensor that the call brings, else bf16.
+struct Operand4 {
+    at::Tensor matrix;
+    Matrix view;
+    Mx4 held;
+    int64_t m, k;
+    at::ScalarType t;
+    Operand4(const Native* n, PyObject* o, const char* name, PyObject* dtype, std::initializer_list<PyObject*> brought)
+    {
+        if (THPVariable_Check(o)) {
+            matrix = matrix_of(o, name);
+            m = matrix.size(0);
+            k = matrix.size(1);
+            t = matrix.scalar_type();
+            type_of(matrix, false, name);
+            if (given(dtype) && scalar_of(dtype, "dtype", false) != t) refuse(std::string("dtype is another one than that of ") + name);
+            view = Matrix(n, matrix, name, m, k, t);
+        } else {
+            held = mx4_of(n, o, name, -1, -1);
+            m = held.codes.size(0);
+            k = held.features;
+            t = at::kBFloat16;
+            for (PyObject* b : brought)
+                if (const at::Tensor* tensor = tensor_in(b)) {
+                    t = tensor->scalar_type() == at::kHalf ? at::kHalf : at::kBFloat16;
+                    break;
+                }
+            if (given(dtype)) t = scalar_of(dtype, "dtype", false);
+        }
+    }
+};
+
+// (native, x, weight, bias, act, residual, out, save, saved, dtype)
+PyObject* mx4_linear(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 10, [&]() -> PyObject* {
+        const Native* n = native_of(v[0]);
+        eden_mx4_linear_args a;
+        std::memset(&a, 0, sizeof(a));
+        const Operand4 x(n, v[1], "x", v[9], {v[6], v[5], v[3]});
+        const Mx4 weight = mx4_of(n, v[2], "weight", -1, x.k);
+        const int64_t m = x.m, cols = weight.codes.size(0);
+        const at::ScalarType t = x.t;
+        a.type = t == at::kBFloat16 ? EDEN_TYPE_BF16 : EDEN_TYPE_FP16;
+        a.act = act_of(v[4]);
+        a.save = name_of(v[7], "save", kSaves, 3);
+        if (!a.save && given(v[8])) refuse("saved is given, but nothing is saved (save is none)");
+        if (x.matrix.defined()) a.x = x.view.data, a.x_stride = x.view.stride;
+        else a.held = x.held.view();
+        a.weight = weight.view();
+        if (given(v[3])) a.bias = vector_of(n, v[3], "bias", cols, t);
+        at::Tensor residual, out = given(v[6]) ? matrix_of(v[6], "out") : fresh(n, {m, cols}, t);
+        if (given(v[5])) {
+            residual = matrix_of(v[5], "residual");
+            const Matrix r(n, residual, "residual", m, cols, t);
+            a.residual = r.data; a.residual_stride = r.stride;
+        }
+        const Matrix mo(n, out, "out", m, cols, t);
+        a.y = mo.data; a.y_stride = mo.stride;
+        Checkpoint c;
+        if (a.save) {
+            c = given(v[8]) ? checkpoint_of(n, v[8], "saved", m, cols) : fresh_checkpoint(n, m, cols);
+            a.saved = (int8_t*)c.c.data; a.saved_stride = c.c.stride;
+            a.saved_exp = (uint8_t*)c.e.data; a.saved_exp_stride = c.e.stride;
+        }
+        a.m = (uint64_t)m; a.n = (uint64_t)cols; a.k = (uint64_t)x.k;
+        done(n, lib.mx4_linear(n->ctx, &a), {&x.matrix, &x.held.codes, &x.held.exps, &weight.codes, &weight.exps, tensor_in(v[3]), &residual, &out, &c.codes, &c.exps});
+        PyObject* y = given(v[6]) ? again(v[6]) : wrapped(out);
+        return a.save ? pair(y, given(v[8]) ? again(v[8]) : wrapped_checkpoint(c)) : y;
+    });
+}
+
+// (native, dz, weight_t, residual, pre, act, out, bias_grad, accumulate, dtype)
+PyObject* mx4_input_grad(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 10, [&]() -> PyObject* {
+        const Native* n = native_of(v[0]);
+        eden_mx4_linear_input_grad_args a;
+        std::memset(&a, 0, sizeof(a));
+        const Operand4 dz(n, v[1], "dz", v[9], {v[6], v[3]});
+        const Mx4 weight = mx4_of(n, v[2], "weight_t", -1, dz.k);
+        const int64_t m = dz.m, k = weight.codes.size(0);
+        const at::ScalarType t = dz.t;
+        a.type = t == at::kBFloat16 ? EDEN_TYPE_BF16 : EDEN_TYPE_FP16;
+        a.act = act_of(v[5]);
+        a.accumulate = flag_of(v[8]);
+        if (dz.matrix.defined()) a.dz = dz.view.data, a.dz_stride = dz.view.stride;
+        else a.held = dz.held.view();
+        a.weight_t = weight.view();
+        at::Tensor residual;
+        if (given(v[3])) {
+            residual = matrix_of(v[3], "residual");
+            const Matrix r(n, residual, "residual", m, k, t);
+            a.residual = r.data; a.residual_stride = r.stride;
+        }
+        Checkpoint pre;
+        if (given(v[4])) pre = checkpoint_of(n, v[4], "pre", m, k);
+        if (a.act) {
+            if (!given(v[4])) refuse("the slope of an activation needs its pre-activation");
+            a.pre = (const int8_t*)pre.c.data; a.pre_stride = pre.c.stride;
+            a.pre_exp = (const uint8_t*)pre.e.data; a.pre_exp_stride = pre.e.stride;
+        }
+        const at::Tensor out = given(v[6]) ? matrix_of(v[6], "out") : fresh(n, {m, k}, t);
+        const Matrix mo(n, out, "out", m, k, t);
+        a.dx = mo.data; a.dx_stride = mo.stride;
+        at::Tensor sums;
+        const bool summed = !left_out(v[7]) && (given(v[4]) || given(v[7]) || a.accumulate);
+        if (left_out(v[7]) && a.accumulate) refuse("accumulate needs a bias_grad to add to");
+        if (summed) {
+            sums = sums_of(n, v[7], "bias_grad", k, a.accumulate);
+            a.bias_grad = (float*)sums.data_ptr();
+        }
+        a.m = (uint64_t)m; a.n = (uint64_t)dz.k; a.k = (uint64_t)k;
+        done(n, lib.mx4_input_grad(n->ctx, &a), {&dz.matrix, &dz.held.codes, &dz.held.exps, &weight.codes, &weight.exps, &residual, &pre.codes, &pre.exps, &out, &sums});
+        PyObject* dx = given(v[6]) ? again(v[6]) : wrapped(out);
+        return summed ? pair(dx, given(v[7]) ? again(v[7]) : wrapped(sums)) : dx;
+    });
+}
+
+// (native, dz_t, x_t, out, accumulate)
+PyObject* mx4_weight_grad(PyObject*, PyObject* const* v, Py_ssize_t count)
+{
+    return called(count, 5, [&]() -> PyObject* {
+        const Native* n = native_of(v[0]);
+        eden_mx4_linear_weight_grad_args a;
+        std::memset(&a, 0, sizeof(a));
+        a.accumulate = flag_of(v[4]);
+        const Mx4 dz = mx4_of(n, v[1], "dz_t", -1, -1), x = mx4_of(n, v[2], "x_t", -1, dz.features);
+        const int64_t cols = dz.codes.size(0), k = x.codes.size(0);
+        a.dz_t = dz.view();
+        a.x_t = x.view();
+        if (a.accumulate && !given(v[3])) refuse("accumulate needs an out to add to");
+        const at::Tensor out = given(v[3]) ? matrix_of(v[3], "out") : fresh(n, {cols, k}, at::kFloat);
+        const Matrix mo(n, out, "out", cols, k, at::kFloat);
+        a.weight_grad = (float*)mo.data; a.weight_grad_stride = mo.stride;
+        a.m = (uint64_t)dz.features; a.n = (uint64_t)cols; a.k = (uint64_t)k;
+        done(n, lib.mx4_weight_grad(n->ctx, &a), {&dz.codes, &dz.exps, &x.codes, &x.exps, &out});
+        return given(v[3]) ? again(v[3]) : wrapped(out);
+    });
+}
+
 // (context, device, stream, stream's id, device index and device type) -> handle
 PyObject* native(PyObject*, PyObject* const* v, Py_ssize_t count)
 {
@@ -481,18 +991,19 @@ PyObject* close_native(PyObject*, PyObject* const* v, Py_ssize_t count)
     });
 }
 
-// (the six entry points' addresses in the order of Library, EdenError, Checkpoint)
+// (the entry points' addresses in the order of Library, EdenError, Checkpoint, Mx4)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t count)
 {
-    return called(count, 8, [&]() -> PyObject* {
-        void* f[6];
-        for (int i = 0; i < 6; ++i) f[i] = PyLong_AsVoidPtr(v[i]);
+    return called(count, kCalls + 3, [&]() -> PyObject* {
+        void* f[kCalls];
+        for (int i = 0; i < kCalls; ++i) f[i] = PyLong_AsVoidPtr(v[i]);
         if (PyErr_Occurred()) throw Refused();
         std::memcpy(&lib, f, sizeof(lib));
-        Py_XDECREF(error_type);
-        Py_XDECREF(checkpoint_type);
-        error_type = again(v[6]);
-        checkpoint_type = again(v[7]);
+        PyObject** const types[3] = {&error_type, &checkpoint_type, &mx4_type};
+        for (int i = 0; i < 3; ++i) {
+            Py_XDECREF(*types[i]);
+            *types[i] = again(v[kCalls + i]);
+        }
         Py_RETURN_NONE;
     });
 }
@@ -508,6 +1019,14 @@ PyMethodDef methods[] = {EDEN_METHOD("bind", bind),
                          EDEN_METHOD("act_backward", act_backward),
                          EDEN_METHOD("input_grad", input_grad),
                          EDEN_METHOD("weight_grad", weight_grad),
+                         EDEN_METHOD("join", join),
+                         EDEN_METHOD("join_backward", join_backward),
+                         EDEN_METHOD("mx4_empty", mx4_empty),
+                         EDEN_METHOD("mx4_quantize", mx4_quantize),
+                         EDEN_METHOD("mx4_restore", mx4_restore),
+                         EDEN_METHOD("mx4_linear", mx4_linear),
+                         EDEN_METHOD("mx4_input_grad", mx4_input_grad),
+                         EDEN_METHOD("mx4_weight_grad", mx4_weight_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kCkptThreads, WIDE ? 4 : 3) k_act_backward(con
 
 // out[n] (+)= the sum of partial's rows: 32 columns per block, each warp every eighth row,
 // the eight added in order
-__global__ void __launch_bounds__(kCkptThreads) k_column_sum(const float* partial, uint64_t rows, uint64_t n,
+static __global__ void __launch_bounds__(kCkptThreads) k_column_sum(const float* partial, uint64_t rows, uint64_t n,
                                                             float* out, int accumulate)
 {
     dependency_wait();

@@ -86,6 +86,8 @@ _sig("eden_mean_sparsify_after", _int, [_vp, _vp, _vp, _vp, _vp, _u64, _u32, _vp
 _sig("eden_decode_accumulate_sparsify_after", _int, [_vp, _vp, _vp, _vp, _vp, _u64, _u32, _vp, _vp])
 _sig("eden_checkpoint_groups", _u64, [_u64])
 _sig("eden_linear_workspace_bytes", _u64, [_u64, _u64, _u64])
+_sig("eden_block_workspace_bytes", _u64, [_u64])
+_sig("eden_mx4_workspace_bytes", _u64, [_u64, _u64, _u64])
 _sig("eden_profile_collect", _int, [_vp, ctypes.POINTER(_u32)])
 _sig("eden_profile_get", _int, [_vp, _u32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(_u64),
                                 ctypes.POINTER(_f64), ctypes.POINTER(_f64)])
@@ -106,6 +108,44 @@ class Checkpoint(NamedTuple):
     """Activations [m, n] in 8 bits: int8 codes [m, n], uint8 exponents [m, ceil(n / 32)]."""
     codes: torch.Tensor
     exps: torch.Tensor
+
+
+class Norm(NamedTuple):
+    """A norm of rows: (v - mean) * rate * weight + bias, weight and bias of the activations' type.
+    kind "rms": mean 0, rate = 1 / sqrt(mean(v^2) + eps); "layer": the mean off first."""
+    weight: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    kind: str = "rms"
+    eps: float = 1e-6
+
+
+class Joined(NamedTuple):
+    """What block_join makes; what was not asked for is None.  Statistics are fp32 [m, 2]: mean and rate."""
+    x: Optional[torch.Tensor]
+    y: Optional[torch.Tensor]
+    after_stats: Optional[torch.Tensor]
+    before_stats: Optional[torch.Tensor]
+
+
+class JoinGradients(NamedTuple):
+    """What block_join_backward makes: residual, h and a matrix gate in the activations' type, the
+    sums over the rows in fp32; None where there is none or it was left out."""
+    residual: Optional[torch.Tensor]
+    h: Optional[torch.Tensor]
+    gate: Optional[torch.Tensor]
+    after_weight: Optional[torch.Tensor]
+    after_bias: Optional[torch.Tensor]
+    before_weight: Optional[torch.Tensor]
+    before_bias: Optional[torch.Tensor]
+
+
+class Mx4(NamedTuple):
+    """A matrix [rows, features] in microscaled 4-bit floating point: uint8 codes [rows, 16 * ceil(features / 32)],
+    two a byte, and uint8 exponents [ceil(rows / 128), ceil(features / 256), 1024] in the order that
+    include/eden.h gives."""
+    codes: torch.Tensor
+    exps: torch.Tensor
+    features: int
 
 
 class EdenError(RuntimeError):
@@ -135,7 +175,8 @@ except ImportError as _e:
 else:
     _binding.bind(*(ctypes.cast(getattr(_lib, name), _vp).value for name in (
         "eden_linear", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_act_backward", "eden_linear_input_grad",
-        "eden_linear_weight_grad")), EdenError, Checkpoint)
+        "eden_linear_weight_grad", "eden_block_join", "eden_block_join_backward", "eden_mx4_quantize", "eden_mx4_restore", "eden_mx4_linear",
+        "eden_mx4_linear_input_grad", "eden_mx4_linear_weight_grad")), EdenError, Checkpoint, Mx4)
 
 
 def _check(rc: int):
@@ -202,6 +243,16 @@ def checkpoint_groups(features: int) -> int:
 def linear_workspace_bytes(m: int, n: int, k: int) -> int:
     """Workspace of a Context for the training calls with up to m tokens and n x k weights."""
     return int(_lib.eden_linear_workspace_bytes(m, n, k))
+
+
+def block_workspace_bytes(n: int) -> int:
+    """Workspace of a Context for block_join_backward (and its parts) on rows of n values."""
+    return int(_lib.eden_block_workspace_bytes(n))
+
+
+def mx4_workspace_bytes(m: int, n: int, k: int) -> int:
+    """Workspace of a Context for the 4-bit calls with up to m tokens and n x k weights."""
+    return int(_lib.eden_mx4_workspace_bytes(m, n, k))
 
 
 def pass_plan(d: int, bits: float):
@@ -496,6 +547,88 @@ class Context:
         what it cannot hold).  out may be a view into the vector that encode takes (accumulate:
         added to what it holds)."""
         return _binding.weight_grad(self._native, dz, x, out, accumulate)
+
+    # ------------------------------------------------------------------ what joins the client's blocks
+    def block_join(self, h: torch.Tensor, residual: Optional[torch.Tensor] = None, after: Optional[Norm] = None, before: Optional[Norm] = None,
+                   gate: Optional[torch.Tensor] = None, scale: float = 1.0, drop: float = 0.0, seed: Union[int, torch.Tensor] = 0, first_row: int = 0,
+                   out: Union[torch.Tensor, bool, None] = None, normed: Optional[torch.Tensor] = None, stats: bool = False) -> Joined:
+        """eden_block_join: x = scale * residual + gate * dropout(after(h)) and y = before(x), bf16 or
+        fp16 [m, n], every part but h optional.  gate: [n] or [m, n].  drop is the chance of a 0; the
+        mask belongs to the seed (a number, or one int64 on the device that is read when the call
+        runs, for captured calls) and to first_row + row.  out=False leaves x out; stats: the norms'
+        statistics are made, for block_join_backward."""
+        return Joined(*_binding.join(self._native, h, residual, after, before, gate, scale, drop, seed, first_row, out, normed, stats))
+
+    def block_join_backward(self, dx: Optional[torch.Tensor], dy: Optional[torch.Tensor], h=None, x=None, after_stats: Optional[torch.Tensor] = None,
+                            before_stats: Optional[torch.Tensor] = None, after: Optional[Norm] = None, before: Optional[Norm] = None,
+                            gate: Optional[torch.Tensor] = None, scale: float = 1.0, drop: float = 0.0, seed: Union[int, torch.Tensor] = 0, first_row: int = 0,
+                            residual: Union[torch.Tensor, bool, None] = None, out: Union[torch.Tensor, bool, None] = None,
+                            gate_grad: Union[torch.Tensor, bool, None] = None, after_weight_grad: Union[torch.Tensor, bool, None] = None,
+                            after_bias_grad: Union[torch.Tensor, bool, None] = None, before_weight_grad: Union[torch.Tensor, bool, None] = None,
+                            before_bias_grad: Union[torch.Tensor, bool, None] = None, accumulate: bool = False) -> JoinGradients:
+        """eden_block_join_backward: the gradients of block_join from those of x (dx, or None) and y
+        (dy, with a norm before).  h (with a norm after or a gate) and x (with a norm before) are
+        matrices or Checkpoints.  An output is made where there is something that it is the gradient
+        of, written where it is given, and neither made nor computed where it is False; accumulate:
+        the sums over the rows are added to the given ones."""
+        return JoinGradients(*_binding.join_backward(self._native, dx, dy, h, x, after_stats, before_stats, after, before, gate, scale, drop, seed, first_row,
+                                                     residual, out, gate_grad, after_weight_grad, after_bias_grad, before_weight_grad, before_bias_grad,
+                                                     accumulate))
+
+    def norm(self, x: torch.Tensor, norm: Norm, out: Optional[torch.Tensor] = None, stats: bool = False):
+        """The norm of x's rows alone; stats: (y, statistics)."""
+        j = _binding.join(self._native, x, None, None, norm, None, 1.0, 0.0, 0, 0, False, out, stats)
+        return (j[1], j[3]) if stats else j[1]
+
+    def norm_backward(self, dy: torch.Tensor, x, stats: torch.Tensor, norm: Norm, dx: Optional[torch.Tensor] = None,
+                      out: Union[torch.Tensor, bool, None] = None, weight_grad: Union[torch.Tensor, bool, None] = None,
+                      bias_grad: Union[torch.Tensor, bool, None] = None, accumulate: bool = False):
+        """(gradient of x, of the weight, of the bias); x a matrix or a Checkpoint; dx is added to the first."""
+        d = _binding.join_backward(self._native, dx, dy, None, x, None, stats, None, norm, None, 1.0, 0.0, 0, 0, False, out, None, None, None,
+                                   weight_grad, bias_grad, accumulate)
+        return d[1], d[5], d[6]
+
+    def dropout(self, x: torch.Tensor, drop: float, seed: Union[int, torch.Tensor], first_row: int = 0, residual: Optional[torch.Tensor] = None,
+                scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """scale * residual + dropout(x).  Its own gradient: dropout(dy) with the same seed."""
+        return _binding.join(self._native, x, residual, None, None, None, scale, drop, seed, first_row, out, None, False)[0]
+
+    # ------------------------------------------------------------------ products in 4 bits
+    def mx4_empty(self, rows: int, features: int) -> Mx4:
+        return _binding.mx4_empty(self._native, rows, features)
+
+    def mx4_quantize(self, x: torch.Tensor, out: Optional[Mx4] = None) -> Mx4:
+        """eden_mx4_quantize: the 4-bit form of x [m, n] (bf16, fp16 or fp32), groups along its rows."""
+        return _binding.mx4_quantize(self._native, x, out, False)
+
+    def mx4_quantize_transposed(self, x: torch.Tensor, out: Optional[Mx4] = None) -> Mx4:
+        """eden_mx4_quantize: the 4-bit form of x^T [n, m], groups along x's columns."""
+        return _binding.mx4_quantize(self._native, x, False, out)
+
+    def mx4_quantize_both(self, x: torch.Tensor, rows: Optional[Mx4] = None, columns: Optional[Mx4] = None):
+        """Both from one read of x: (mx4_quantize(x), mx4_quantize_transposed(x))."""
+        return _binding.mx4_quantize(self._native, x, rows, columns)
+
+    def mx4_restore(self, q: Mx4, dtype: torch.dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """eden_mx4_restore: the values that a 4-bit form stands for."""
+        return _binding.mx4_restore(self._native, q, dtype, out)
+
+    def mx4_linear(self, x, weight: Mx4, bias: Optional[torch.Tensor] = None, act: str = "none", residual: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None, save: str = "none", saved: Optional[Checkpoint] = None, dtype: Optional[torch.dtype] = None):
+        """eden_mx4_linear: `linear` with both operands in 4 bits.  x [m, k] is a matrix (bf16 or
+        fp16), which the call quantises, or an Mx4; the rest is then of dtype, else of the type of the
+        tensors that are given, else bf16."""
+        return _binding.mx4_linear(self._native, x, weight, bias, act, residual, out, save, saved, dtype)
+
+    def mx4_linear_input_grad(self, dz, weight_t: Mx4, residual: Optional[torch.Tensor] = None, pre: Optional[Checkpoint] = None, act: str = "none",
+                              out: Optional[torch.Tensor] = None, bias_grad: Union[torch.Tensor, bool, None] = None, accumulate: bool = False,
+                              dtype: Optional[torch.dtype] = None):
+        """eden_mx4_linear_input_grad: `linear_input_grad` in 4 bits, weight_t = mx4_quantize_transposed(weight)."""
+        return _binding.mx4_input_grad(self._native, dz, weight_t, residual, pre, act, out, bias_grad, accumulate, dtype)
+
+    def mx4_linear_weight_grad(self, dz_t: Mx4, x_t: Mx4, out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
+        """eden_mx4_linear_weight_grad: dz^T x in fp32 from mx4_quantize_transposed of both."""
+        return _binding.mx4_weight_grad(self._native, dz_t, x_t, out, accumulate)
 
     # ------------------------------------------------------------------ status
     def status(self) -> int:
