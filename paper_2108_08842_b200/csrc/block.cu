@@ -9,8 +9,9 @@ using namespace eden;
 
 namespace {
 
-constexpr uint64_t kMaxSlots = 192;             // blocks of a backward launch, whatever the device
-constexpr uint64_t kMaxNormColumns = (uint64_t)kBlockColumns * kBlockCluster;
+constexpr uint64_t kMaxSlots = 192;             // blocks of a launch with norms, whatever the device
+constexpr uint64_t kMaxRuns = 512;              // runs of rows of a backward launch without norms
+constexpr uint64_t kMaxNormColumns = 512ull * kTeamWarps * kBlockCluster;
 static_assert(kMaxNormColumns == EDEN_NORM_MAX_FEATURES, "as documented");
 
 bool rows_on_16(const void* p, uint64_t stride) { return !p || (aligned(p, 16) && stride % 8 == 0); }
@@ -37,68 +38,90 @@ DropView drop_view(const eden_drop& d, int* has)
 // stride 0 where one vector serves all rows
 uint64_t gate_stride(const void* gate, int per_value, uint64_t stride) { return gate && per_value ? stride : 0; }
 
+Source matrix_source(const void* p, uint64_t stride) { return {(const char*)p, stride * 2, 2, 1, 0, rows_on_16(p, stride)}; }
+Source stats_source(const float* p) { return {(const char*)p, 8, 8, 0, 0, 0}; }
+
 // Rows over teams, blocks and clusters: see kernels_block.cuh.
 struct Grid {
     BlockShape s;
-    dim3 grid;
-    uint32_t threads, cluster, parts;
+    uint32_t blocks, threads, shared, pieces, parts;
+    bool wide;                         // of the sources; the outputs' rows count as well
 };
 
-Grid grid_of(uint64_t m, uint64_t n, bool sums, uint64_t slots)
+// What a block has beside its rows and vectors: places for sums, store buffers and barriers.
+constexpr uint32_t kRowsShared = (227 - 17) * 1024;
+
+Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)[kMaxSources], uint32_t warps, bool full)
 {
-    Grid g;
-    uint32_t blocks = 1;
-    while ((uint64_t)blocks * kBlockColumns < n && blocks < (sums ? (uint32_t)kBlockCluster : 1u << 30)) blocks *= 2;
-    if (!sums) blocks = (uint32_t)((n + kBlockColumns - 1) / kBlockColumns);
-    g.s.m = (uint32_t)m;
-    g.s.n = (uint32_t)n;
-    g.s.warps = (uint32_t)(((n + blocks - 1) / blocks + 255) / 256);
-    g.s.teams = kBlockWarps / g.s.warps;
-    g.s.span = g.s.warps * 256;
-    g.s.blocks = sums ? blocks : 1;
-    const uint32_t strips = sums ? 1 : (uint32_t)((n + g.s.span - 1) / g.s.span);
-    const uint64_t want = (m + g.s.teams - 1) / g.s.teams, most = std::max<uint64_t>(1, slots / blocks);
-    const uint32_t groups = (uint32_t)std::min(want, most);
-    g.grid = dim3(groups * g.s.blocks, strips);
-    g.threads = g.s.teams * g.s.warps * 32;
-    g.cluster = g.s.blocks;
-    g.parts = groups * g.s.teams;
+    Grid g{};
+    g.wide = n % 8 == 0;
+    BlockShape& s = g.s;
+    s.m = (uint32_t)m;
+    s.n = (uint32_t)n;
+    const uint64_t sms = std::min<uint64_t>(ctx->sm_count, kMaxSlots);
+    // Two pieces a thread where that leaves a row for every SM, or where one would need a cluster.
+    g.pieces = n > 256 * kTeamWarps || (n > 256 && m >= sms) ? 2 : 1;
+    const uint64_t columns = 256ull * kTeamWarps * g.pieces;
+    s.blocks = 1;
+    while (s.blocks * columns < n) s.blocks *= 2;
+    s.warps = (uint32_t)(((n + s.blocks - 1) / s.blocks + 256 * g.pieces - 1) / (256 * g.pieces));
+    s.teams = s.blocks > 1 ? 1 : warps / s.warps;                  // a cluster's blocks work on one row
+    s.span = s.warps * 256 * g.pieces;
+    const uint32_t width = (uint32_t)std::min<uint64_t>(n, s.span);
+    for (int i = 0; i < kMaxSources; ++i) {
+        s.source[i] = source[i];
+        if (!source[i].base) continue;
+        s.source[i].at = s.row_bytes;
+        // up to 15 bytes of a neighbour, and whole words behind the last value; all of the team's columns
+        s.row_bytes += (uint32_t)align_to(std::max(source[i].bytes_of(width) + 48, source[i].bytes_of(s.span)), 16);
+        if (source[i].columns && source[i].columns != (uint32_t)kGroup) g.wide = g.wide && source[i].aligned;
+    }
+    // few rows: a team of each block has one before a block has two
+    const uint32_t vectors = (full ? kVectors<true> : kVectors<false>) * s.span * 2;
+    while (s.teams > 1 && (2 * s.row_bytes * s.teams + vectors > kRowsShared || (uint64_t)s.teams * (sms / s.blocks) >= 2 * m)) s.teams = (s.teams + 1) / 2;
+    s.stages = std::min<uint32_t>(kMaxStages, (kRowsShared - vectors) / (s.row_bytes * s.teams));
+    s.vectors = s.teams * s.stages * s.row_bytes;
+    const uint64_t groups = std::min<uint64_t>((m + s.teams - 1) / s.teams, std::max<uint64_t>(1, sms / s.blocks));
+    g.blocks = (uint32_t)groups * s.blocks;
+    g.threads = s.teams * s.warps * 32;
+    g.shared = s.vectors + vectors;
+    g.parts = (uint32_t)groups * s.teams;
     return g;
 }
 
-uint64_t slots_of(const eden_ctx* ctx) { return std::min<uint64_t>(ctx->sm_count, kMaxSlots); }
-
-template <typename T, bool AFTER, bool BEFORE>
-int join(eden_ctx* ctx, const JoinView& p, const Grid& g, double bytes)
+template <typename View>
+int launch_rows(eden_ctx* ctx, const char* name, double bytes, void (*kernel)(View, BlockShape, uint32_t*), const View& p, const Grid& g)
 {
-    const bool wide = rows_on_16(p.h, p.h_stride) && rows_on_16(p.residual, p.residual_stride) && rows_on_16(p.gate_stride ? p.gate : nullptr, p.gate_stride) &&
-                      rows_on_16(p.x, p.x_stride) && rows_on_16(p.y, p.y_stride);
-    return launch(ctx, "t_join", bytes, wide ? k_join<T, true, AFTER, BEFORE> : k_join<T, false, AFTER, BEFORE>, g.grid, g.threads, 0, g.cluster, p, g.s);
+    CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowsShared));
+    return launch(ctx, name, bytes, kernel, dim3(g.blocks), g.threads, g.shared, g.s.blocks, p, g.s, (uint32_t*)ctx->ws);
 }
 
-bool kept_wide(const KeptView& k)
+bool full(const eden_norm& n) { return n.kind == EDEN_NORM_LAYER || (n.kind != EDEN_NORM_NONE && n.bias); }
+
+#define EDEN_JOIN_PIECES(kernel, f, w, pieces) ((pieces) == 2 ? kernel<T, AFTER, BEFORE, f, w, 2> : kernel<T, AFTER, BEFORE, f, w, 1>)
+#define EDEN_JOIN_KERNEL(kernel, f, w, pieces)                                                                  \
+    ((f) ? ((w) ? EDEN_JOIN_PIECES(kernel, true, true, pieces) : EDEN_JOIN_PIECES(kernel, true, false, pieces))  \
+         : ((w) ? EDEN_JOIN_PIECES(kernel, false, true, pieces) : EDEN_JOIN_PIECES(kernel, false, false, pieces)))
+
+template <typename T, bool AFTER, bool BEFORE>
+int join(eden_ctx* ctx, const JoinView& p, const Grid& g, bool f, double bytes)
 {
-    return k.data ? rows_on_16(k.data, k.stride) : aligned(k.held.codes, 8) && k.held.codes_stride % 8 == 0;
+    const bool wide = g.wide && rows_on_16(p.x, p.x_stride) && rows_on_16(p.y, p.y_stride);
+    return launch_rows(ctx, "t_join", bytes, EDEN_JOIN_KERNEL(k_join, f, wide, g.pieces), p, g);
 }
 
 template <typename T, bool AFTER, bool BEFORE>
-int join_backward(eden_ctx* ctx, const JoinBackwardView& p, const Grid& g, double bytes)
+int join_backward(eden_ctx* ctx, const JoinBackwardView& p, const Grid& g, bool f, double bytes)
 {
-    const bool wide = rows_on_16(p.dx, p.dx_stride) && rows_on_16(p.dy, p.dy_stride) && rows_on_16(p.gate_stride ? p.gate : nullptr, p.gate_stride) &&
-                      rows_on_16(p.d_residual, p.d_residual_stride) && rows_on_16(p.dh, p.dh_stride) && rows_on_16(p.d_gate, p.d_gate_stride) &&
-                      kept_wide(p.h) && kept_wide(p.x);
-    return launch(ctx, "t_join_backward", bytes, wide ? k_join_backward<T, true, AFTER, BEFORE> : k_join_backward<T, false, AFTER, BEFORE>, g.grid, g.threads,
-                  0, g.cluster, p, g.s);
+    const bool wide = g.wide && rows_on_16(p.d_residual, p.d_residual_stride) && rows_on_16(p.dh, p.dh_stride) && rows_on_16(p.d_gate, p.d_gate_stride);
+    return launch_rows(ctx, "t_join_backward", bytes, EDEN_JOIN_KERNEL(k_join_backward, f, wide, g.pieces), p, g);
 }
 
 #define EDEN_DISPATCH_NORMS(after, before, CALL)                                                   \
     if (after) {                                                                                  \
         if (before) { constexpr bool AFTER_ = true, BEFORE_ = true; CALL; }                       \
         else { constexpr bool AFTER_ = true, BEFORE_ = false; CALL; }                             \
-    } else {                                                                                      \
-        if (before) { constexpr bool AFTER_ = false, BEFORE_ = true; CALL; }                      \
-        else { constexpr bool AFTER_ = false, BEFORE_ = false; CALL; }                            \
-    }
+    } else { constexpr bool AFTER_ = false, BEFORE_ = true; CALL; }
 
 int sizes_ok(uint64_t m, uint64_t n, bool sums)
 {
@@ -117,7 +140,7 @@ KeptView kept_view(const eden_kept& k) { return {k.data, k.stride, view(k.codes,
 
 extern "C" uint64_t eden_block_workspace_bytes(uint64_t n)
 {
-    return std::max(least_workspace(), kStatusBytes + kJoinSums * 4 * std::max<uint64_t>(kMaxSlots * kBlockColumns, n) + 256);
+    return std::max(least_workspace(), kStatusBytes + 4 * std::max<uint64_t>(kJoinSums * kMaxSlots * 512 * kTeamWarps, kMaxRuns * n) + 256);
 }
 
 extern "C" int eden_block_join(eden_ctx* ctx, const eden_block_join_args* a)
@@ -132,13 +155,30 @@ extern "C" int eden_block_join(eden_ctx* ctx, const eden_block_join_args* a)
         !aligned(a->after_stats, 8) || !aligned(a->before_stats, 8))
         return EDEN_ERR_INVALID_ARG;
     return guarded(ctx, [&]() -> int {
-        JoinView p{a->h, a->h_stride, a->residual, a->residual_stride, a->gate, gate_stride(a->gate, a->gate_per_value, a->gate_stride), a->x, a->x_stride,
-                   before ? a->y : nullptr, a->y_stride, {a->after.weight, a->after.bias, a->after_stats, a->after.eps, a->after.kind},
+        const uint64_t per_value = gate_stride(a->gate, a->gate_per_value, a->gate_stride);
+        const double bytes = 2.0 * a->m * a->n * (1 + (a->residual ? 1 : 0) + (per_value ? 1 : 0) + (a->x ? 1 : 0) + (before ? 1 : 0));
+        if (!after && !before) {
+            PlainView p{a->h, a->h_stride, a->residual, a->residual_stride, a->gate, per_value, a->x, a->x_stride, {}, a->scale, 0,
+                        (uint32_t)a->m, (uint32_t)a->n, (uint32_t)((a->n + 255) / 256)};
+            p.drop = drop_view(a->drop, &p.has_drop);
+            const bool wide = rows_on_16(p.h, p.h_stride) && rows_on_16(p.residual, p.residual_stride) && (!per_value || rows_on_16(p.gate, per_value)) &&
+                              rows_on_16(p.x, p.x_stride);
+            const uint64_t blocks = ((a->m + kPlainRows - 1) / kPlainRows * p.warps_across + kPlainThreads / 32 - 1) / (kPlainThreads / 32);
+            if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
+            EDEN_DISPATCH_HALF(a->type, return launch(ctx, "t_join_plain", bytes, wide ? k_join_plain<T_, true> : k_join_plain<T_, false>, dim3((uint32_t)blocks),
+                                                      kPlainThreads, 0, 1, p));
+        }
+        JoinView p{per_value ? nullptr : a->gate, a->x, a->x_stride, before ? a->y : nullptr, a->y_stride,
+                   {a->after.weight, a->after.bias, a->after_stats, a->after.eps, a->after.kind},
                    {a->before.weight, a->before.bias, a->before_stats, a->before.eps, a->before.kind}, {}, a->scale, 0};
         p.drop = drop_view(a->drop, &p.has_drop);
-        const Grid g = grid_of(a->m, a->n, after || before, 2 * (uint64_t)ctx->sm_count);
-        const double bytes = 2.0 * a->m * a->n * (1 + (a->residual ? 1 : 0) + (p.gate_stride ? 1 : 0) + (a->x ? 1 : 0) + (before ? 1 : 0));
-        EDEN_DISPATCH_HALF(a->type, EDEN_DISPATCH_NORMS(after, before, return (join<T_, AFTER_, BEFORE_>(ctx, p, g, bytes))));
+        Source source[kMaxSources] = {};
+        source[kSourceH] = matrix_source(a->h, a->h_stride);
+        if (a->residual) source[kSourceResidual] = matrix_source(a->residual, a->residual_stride);
+        if (per_value) source[kSourceGate] = matrix_source(a->gate, per_value);
+        const bool f = full(a->after) || full(a->before) || per_value;
+        const Grid g = grid_of(ctx, a->m, a->n, source, kJoinThreads / 32, f);
+        EDEN_DISPATCH_HALF(a->type, EDEN_DISPATCH_NORMS(after, before, return (join<T_, AFTER_, BEFORE_>(ctx, p, g, f, bytes))));
     });
 }
 
@@ -170,31 +210,56 @@ extern "C" int eden_block_join_backward(eden_ctx* ctx, const eden_block_join_bac
         out.n = (uint32_t)a->n;
         out.accumulate = a->accumulate;
         if (a->m > 0 && (wanted || a->d_residual || a->dh || a->d_gate)) {
-            JoinBackwardView p{};
-            p.dx = a->dx; p.dx_stride = a->dx_stride;
-            if (before) p.dy = a->dy, p.dy_stride = a->dy_stride, p.x = kept_view(a->x);
-            if (after || a->gate) p.h = kept_view(a->h);
-            p.gate = a->gate; p.gate_stride = gate_stride(a->gate, a->gate_per_value, a->gate_stride);
-            p.d_residual = a->d_residual; p.d_residual_stride = a->d_residual_stride;
-            p.dh = a->dh; p.dh_stride = a->dh_stride;
-            p.d_gate = a->d_gate; p.d_gate_stride = a->d_gate_stride;
-            p.after = {a->after.weight, a->after.bias, const_cast<float*>(a->after_stats), a->after.eps, a->after.kind};
-            p.before = {a->before.weight, a->before.bias, const_cast<float*>(a->before_stats), a->before.eps, a->before.kind};
-            p.drop = drop_view(a->drop, &p.has_drop);
-            p.scale = a->scale;
-            p.wanted = wanted;
-            const Grid g = grid_of(a->m, a->n, after || before, slots_of(ctx));
-            if (wanted) {
-                out.parts = g.parts;
-                p.partial = Scratch(ctx).take<float>((uint64_t)g.parts * out.sums * a->n);
-                if (!p.partial) return EDEN_ERR_WORKSPACE;
-                out.partial = p.partial;
-            }
-            const double each = (double)a->m * a->n;
-            const double bytes = each * (2.0 * (!!a->dx + before + !!p.gate_stride + !!a->d_residual + !!a->dh + !!a->d_gate) +
-                                         (before ? (a->x.data ? 2 : 1) : 0) + (after || a->gate ? (a->h.data ? 2 : 1) : 0));
+            const uint64_t per_value = gate_stride(a->gate, a->gate_per_value, a->gate_stride);
+            const double bytes = (double)a->m * a->n * (2.0 * (!!a->dx + before + !!per_value + !!a->d_residual + !!a->dh + !!a->d_gate) +
+                                                        (before ? (a->x.data ? 2 : 1) : 0) + (after || a->gate ? (a->h.data ? 2 : 1) : 0));
+            int has_drop;
+            const DropView drop = drop_view(a->drop, &has_drop);
+            auto partial = [&](uint64_t parts) {
+                out.parts = (uint32_t)parts;
+                float* const to = wanted ? Scratch(ctx).take<float>(parts * out.sums * a->n) : nullptr;
+                out.partial = to;
+                return to;
+            };
             int rc = EDEN_OK;
-            EDEN_DISPATCH_HALF(a->type, EDEN_DISPATCH_NORMS(after, before, rc = (join_backward<T_, AFTER_, BEFORE_>(ctx, p, g, bytes))));
+            if (!after && !before) {
+                const uint64_t strips = (a->n + 8 * kPlainThreads - 1) / (8 * kPlainThreads);
+                const uint64_t want = std::min<uint64_t>(kMaxRuns, std::max<uint64_t>(1, 8ull * ctx->sm_count / strips));
+                const uint64_t rows_per_run = std::max<uint64_t>(4, (a->m + want - 1) / want), runs = (a->m + rows_per_run - 1) / rows_per_run;
+                PlainBackwardView p{a->dx, a->dx_stride, a->gate ? kept_view(a->h) : KeptView{}, a->gate, per_value, a->d_residual, a->d_residual_stride, a->dh, a->dh_stride,
+                                    a->d_gate, a->d_gate_stride, partial(runs), drop, a->scale, has_drop, (uint32_t)a->m, (uint32_t)a->n, (uint32_t)rows_per_run};
+                if (wanted && !p.partial) return EDEN_ERR_WORKSPACE;
+                const bool wide = rows_on_16(p.dx, p.dx_stride) && rows_on_16(p.h.data, p.h.stride) && (!per_value || rows_on_16(p.gate, per_value)) &&
+                                  rows_on_16(p.d_residual, p.d_residual_stride) && rows_on_16(p.dh, p.dh_stride) && rows_on_16(p.d_gate, p.d_gate_stride);
+                EDEN_DISPATCH_HALF(a->type, rc = launch(ctx, "t_join_plain_backward", bytes, wide ? k_join_plain_backward<T_, true> : k_join_plain_backward<T_, false>,
+                                                        dim3((uint32_t)strips, (uint32_t)runs), kPlainThreads, 0, 1, p));
+            } else {
+                Source source[kMaxSources] = {};
+                auto kept = [&](int at, const eden_kept& k) {
+                    if (k.data) {
+                        source[at] = matrix_source(k.data, k.stride);
+                    } else {
+                        source[at] = {(const char*)k.codes, k.codes_stride, 1, 1, 0, aligned(k.codes, 16) && k.codes_stride % 16 == 0};
+                        source[at + 1] = {(const char*)k.exps, k.exps_stride, 1, (uint32_t)kGroup, 0, 0};
+                    }
+                };
+                if (a->dx) source[kSourceDx] = matrix_source(a->dx, a->dx_stride);
+                if (before) {
+                    source[kSourceDy] = matrix_source(a->dy, a->dy_stride);
+                    kept(kSourceX, a->x);
+                    source[kSourceBefore] = stats_source(a->before_stats);
+                }
+                if (after || a->gate) kept(kSourceKeptH, a->h);
+                if (after) source[kSourceAfter] = stats_source(a->after_stats);
+                if (per_value) source[kSourceGateMatrix] = matrix_source(a->gate, per_value);
+                const bool f = full(a->after) || full(a->before) || per_value || (wanted & (1u << kBeforeBias | 1u << kAfterBias));
+                const Grid g = grid_of(ctx, a->m, a->n, source, kJoinBackwardThreads / 32, f);
+                JoinBackwardView p{per_value ? nullptr : a->gate, a->d_residual, a->d_residual_stride, a->dh, a->dh_stride, a->d_gate, a->d_gate_stride,
+                                   partial(g.parts), wanted, {a->after.weight, a->after.bias, nullptr, a->after.eps, a->after.kind},
+                                   {a->before.weight, a->before.bias, nullptr, a->before.eps, a->before.kind}, drop, a->scale, has_drop};
+                if (wanted && !p.partial) return EDEN_ERR_WORKSPACE;
+                EDEN_DISPATCH_HALF(a->type, EDEN_DISPATCH_NORMS(after, before, rc = (join_backward<T_, AFTER_, BEFORE_>(ctx, p, g, f, bytes))));
+            }
             if (rc) return rc;
         }
         if (!wanted) return EDEN_OK;

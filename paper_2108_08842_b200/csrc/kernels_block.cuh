@@ -14,11 +14,27 @@
 
 namespace eden {
 
-// A thread takes 8 columns (one Philox call) of its team's rows; a team is the warps that hold a row,
-// 256 columns each.  A block has as many teams as fit into 16 warps.  Rows of more than 4096 columns
-// are shared by the blocks of a cluster (their sums go through distributed shared memory), or, where
-// no norm needs a row's sums, by independent blocks.
-constexpr int kBlockThreads = 512, kBlockWarps = kBlockThreads / 32, kBlockColumns = 8 * kBlockThreads, kBlockCluster = 8;
+// A thread takes K pieces of 8 columns (a Philox call each) of its team's rows, 256 columns apart; a
+// team is the up to 16 warps that hold a row.  Rows that 16
+// warps do not hold are shared by the blocks of a cluster (their sums go through distributed shared
+// memory).  K = 2 halves the shuffles and waits per value and leaves another team to run while one
+// waits; K = 1 spreads a few rows over more warps.
+//
+// What a row needs is brought to shared memory by bulk copies, the next rows of the team while this
+// one is worked on.  Copies start on 16 bytes: a row's first and last chunks may hold bytes of its
+// neighbours, which are not used.
+//
+// FULL: a mean is taken off, biases are added, or a gate is a matrix.  WIDE: every row starts on 16
+// bytes and has a multiple of 8 columns; a thread then has all 8 columns of a piece or none, and reads
+// zeros where there are none.  A kernel that asked for both at run time took 1230 instructions for 256
+// values of a row's gradients and four rows at a time did not fit the instruction cache: 780 us for the
+// gradients of 16384 x 4096, and 364 with FULL alone.
+//
+// The vectors over the columns (weights, biases, a gate) lie in shared memory as well: in registers,
+// they made the gradients' kernel spill, and left the forward one 16 warps on an SM.  Forward 24 warps of
+// 80 registers, backward 16 of 128, which hold the column sums.
+constexpr int kTeamWarps = 16, kJoinThreads = 768, kJoinBackwardThreads = 512, kBlockCluster = 8;
+constexpr int kMaxSources = 9, kMaxStages = 4, kMaxTeams = 24;
 
 struct NormView {
     const void* weight;                // or null: 1
@@ -28,11 +44,30 @@ struct NormView {
     int kind;                          // EDEN_NORM_*
 };
 
+// What a row needs of a matrix: `number` bytes for `columns` columns (statistics: 8 bytes, columns 0).
+struct Source {
+    const char* base;                  // or null: not wanted
+    uint64_t stride;                   // bytes from row to row
+    uint32_t number, columns;
+    uint32_t at;                       // in a row's place in shared memory
+    uint32_t aligned;                  // all rows start on 16 bytes
+    __device__ __forceinline__ uint32_t begin(uint32_t first) const { return columns ? first / columns * number : 0; }
+    __host__ __device__ __forceinline__ uint32_t bytes_of(uint32_t cols) const { return columns ? (cols * number + columns - 1) / columns : number; }
+    // what a row's place begins with that is not the row's
+    __device__ __forceinline__ uint32_t skew(uint32_t r, uint32_t first) const
+    {
+        return aligned ? 0 : ((uint32_t)(uintptr_t)base + r * (uint32_t)stride + begin(first)) & 15u;
+    }
+};
+
 struct BlockShape {
     uint32_t m, n;
     uint32_t warps, teams;             // of a team, of a block
     uint32_t span;                     // columns of a block
     uint32_t blocks;                   // of a cluster
+    uint32_t stages, row_bytes;
+    uint32_t vectors;                  // where those begin in shared memory, behind the rows
+    Source source[kMaxSources];
 };
 
 struct DropView {
@@ -42,17 +77,11 @@ struct DropView {
     float factor;                      // 65536 / keep, 0 for 0
 };
 
-__device__ __forceinline__ float warp_sum_f(float v)
-{
-#pragma unroll
-    for (int i = 16; i > 0; i /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, i);
-    return v;
-}
-
 // Where a thread stands: its team, its columns.
+template <int K>
 struct Place {
-    uint32_t team, warp, lane, rank, first, col;
-    int count;                         // of its 8 columns exist
+    uint32_t team, warp, lane, rank, first, col, width;
+    int count[K];                      // of its 8 columns at col + 256 * i exist
     __device__ __forceinline__ explicit Place(const BlockShape& s)
     {
         const uint32_t w = threadIdx.x / 32;
@@ -60,115 +89,732 @@ struct Place {
         team = w / s.warps;
         warp = w - team * s.warps;
         rank = s.blocks > 1 ? cluster_rank() : 0;
-        first = (s.blocks > 1 ? rank : blockIdx.y) * s.span;
-        col = first + warp * 256 + lane * 8;
-        count = col < s.n ? (int)min(s.n - col, 8u) : 0;
+        first = rank * s.span;
+        width = first < s.n ? min(s.n - first, s.span) : 0;
+        col = first + warp * (256 * K) + lane * 8;
+#pragma unroll
+        for (int i = 0; i < K; ++i) count[i] = col + 256 * i < s.n ? (int)min(s.n - col - 256 * i, 8u) : 0;
     }
 };
 
-// Sums over a row.  Each warp leaves a pair of its own; `take(i, pair)` then gets warp i's, every
-// lane some of them, alike in all warps.  Two places in turn: a place is written again after the
-// next exchange, which nobody passes before all have read this one.
-struct Exchange {
-    float2 places[2][kBlockWarps * kBlockCluster];
-};
+template <int K>
+using Values = Pair[K][4];
 
-template <typename F>
-__device__ __forceinline__ void exchange(Exchange& e, uint32_t& turn, const BlockShape& s, const Place& at, float2 mine, F&& take)
+// ---- sums over rows -----------------------------------------------------------------
+__device__ __forceinline__ float warp_total(float a)
 {
-    if (s.blocks == 1 && s.warps == 1) {
-        if (at.lane == 0) take(0u, mine);
-        return;
-    }
+#pragma unroll
+    for (int i = 16; i > 0; i /= 2) a += __shfl_xor_sync(0xFFFFFFFFu, a, i);
+    return a;
+}
+
+// Each warp leaves a pair; `take(i, pair)` then gets warp i's, each lane some of them (without a
+// cluster one, alike in both halves of the warp), alike in all warps.  Two places in turn: a place is
+// written again after the next exchange, which nobody passes before all have read this one.
+struct Exchange {
+    float2 places[2][kTeamWarps * kBlockCluster];
+};
+
+template <int K, typename F>
+__device__ __forceinline__ void exchange(Exchange& e, uint32_t& turn, const BlockShape& s, const Place<K>& at, float2 mine, F&& take)
+{
     float2* const place = e.places[turn];
     turn ^= 1;
     if (s.blocks == 1) {
         float2* const team = place + at.team * s.warps;
         if (at.lane == 0) team[at.warp] = mine;
         __syncwarp();
-        asm volatile("barrier.sync %0, %1;" ::"r"(at.team + 1), "r"(s.warps * 32) : "memory");
-        if (at.lane < s.warps) take(at.lane, team[at.lane]);
+        if (s.warps > 1) asm volatile("barrier.sync %0, %1;" ::"r"(at.team + 1), "r"(s.warps * 32) : "memory");
+        const uint32_t i = at.lane % kTeamWarps;
+        if (i < s.warps) take(i, team[i]);
+        __syncwarp();
         return;
     }
     if (at.lane < s.blocks) {
-        const uint32_t to = address_in(shared_address(place + at.rank * kBlockWarps + at.warp), at.lane);
+        const uint32_t to = address_in(shared_address(place + at.rank * kTeamWarps + at.warp), at.lane);
         asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(mine.x), "f"(mine.y) : "memory");
     }
     cluster_arrive_wait();
-    for (uint32_t i = at.lane; i < s.blocks * kBlockWarps; i += 32) {
-        const uint32_t w = i % kBlockWarps;
-        if (w < s.warps) take(i / kBlockWarps * s.warps + w, place[i]);
+    for (uint32_t i = at.lane; i < s.blocks * kTeamWarps; i += 32) {
+        const uint32_t w = i % kTeamWarps;
+        if (w < s.warps) take(i / kTeamWarps * s.warps + w, place[i]);
     }
+    __syncwarp();
+}
+
+// what the lanes hold after an exchange, added up
+__device__ __forceinline__ float lanes_total(const BlockShape& s, float a)
+{
+#pragma unroll
+    for (int i = kTeamWarps / 2; i > 0; i /= 2) a += __shfl_xor_sync(0xFFFFFFFFu, a, i);
+    if (s.blocks > 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, 16);
+    return a;
 }
 
 // columns of warp i (in the order of `exchange`)
+template <int K>
 __device__ __forceinline__ float columns_of(const BlockShape& s, uint32_t i)
 {
-    const uint32_t begin = i / s.warps * s.span + i % s.warps * 256;
-    return begin < s.n ? (float)min(s.n - begin, 256u) : 0.f;
+    const uint32_t begin = i / s.warps * s.span + i % s.warps * (256 * K);
+    return begin < s.n ? (float)min(s.n - begin, 256u * K) : 0.f;
+}
+
+__device__ __forceinline__ float both(Pair a)
+{
+    float x, y;
+    a.get(x, y);
+    return x + y;
+}
+
+// Sums over a row's columns: of b, and (FULL) of a.
+template <bool FULL, int K>
+__device__ __forceinline__ float2 row_sums(Exchange& e, uint32_t& turn, const BlockShape& s, const Place<K>& at, Pair a, Pair b)
+{
+    float2 total = make_float2(0.f, 0.f);
+    exchange<K>(e, turn, s, at, make_float2(FULL ? warp_total(both(a)) : 0.f, warp_total(both(b))), [&](uint32_t, float2 w) {
+        if (FULL) total.x += w.x;
+        total.y += w.y;
+    });
+    return make_float2(FULL ? lanes_total(s, total.x) : 0.f, lanes_total(s, total.y));
 }
 
 // Mean and rate of a row.  "layer": each warp's mean and the sum of squares around it, put together
 // around the row's mean, so that no difference of large squares makes a small one.
-__device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, const BlockShape& s, const Place& at, const NormView& norm, const float (&v)[8])
+template <bool FULL, int K>
+__device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, const BlockShape& s, const Place<K>& at, const NormView& norm, const Values<K>& v)
 {
-    const float n = (float)s.n;
-    if (norm.kind == EDEN_NORM_RMS) {
-        float q = 0.f;
+    const float over_n = 1.f / (float)s.n;
+    if (!FULL || norm.kind == EDEN_NORM_RMS) {
+        Pair q(0.f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q = fmaf(v[j], v[j], q);               // columns that do not exist hold 0
-        float total = 0.f;
-        exchange(e, turn, s, at, make_float2(warp_sum_f(q), 0.f), [&](uint32_t, float2 w) { total += w.x; });
-        return make_float2(0.f, rsqrtf(warp_sum_f(total) / n + norm.eps));
+        for (int i = 0; i < K; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q = fma(v[i][j], v[i][j], q);          // columns that do not exist hold 0
+        return make_float2(0.f, rsqrtf(fmaf(row_sums<false, K>(e, turn, s, at, q, q).y, over_n, norm.eps)));
     }
-    float sum = 0.f, q = 0.f;
+    Pair t(0.f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += v[j];
-    sum = warp_sum_f(sum);
-    const float own = columns_of(s, (s.blocks > 1 ? at.rank : 0) * s.warps + at.warp), middle = own > 0.f ? sum / own : 0.f;
+    for (int i = 0; i < K; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < at.count) q = fmaf(v[j] - middle, v[j] - middle, q);
-    float2 held[kBlockCluster * kBlockWarps / 32];
-    float columns[kBlockCluster * kBlockWarps / 32];
+        for (int j = 0; j < 4; ++j) t = t + v[i][j];
+    const float sum = warp_total(both(t)), own = columns_of<K>(s, at.rank * s.warps + at.warp), middle = own > 0.f ? sum / own : 0.f;
+    float q = 0.f;
 #pragma unroll
-    for (int i = 0; i < kBlockCluster * kBlockWarps / 32; ++i) held[i] = make_float2(0.f, 0.f), columns[i] = 0.f;
+    for (int i = 0; i < K; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x, y;
+            (v[i][j] + Pair(-middle)).get(x, y);
+            if (2 * j < at.count[i]) q = fmaf(x, x, q);
+            if (2 * j + 1 < at.count[i]) q = fmaf(y, y, q);
+        }
+    constexpr int kHeld = kBlockCluster * kTeamWarps / 32;
+    float2 held[kHeld];
+    float columns[kHeld], total = 0.f;
     int got = 0;
-    float total = 0.f;
-    exchange(e, turn, s, at, make_float2(sum, warp_sum_f(q)), [&](uint32_t i, float2 w) {
 #pragma unroll
-        for (int k = 0; k < kBlockCluster * kBlockWarps / 32; ++k)
-            if (k == got) held[k] = w, columns[k] = columns_of(s, i);
+    for (int i = 0; i < kHeld; ++i) columns[i] = 0.f;
+    exchange<K>(e, turn, s, at, make_float2(sum, warp_total(q)), [&](uint32_t i, float2 w) {
+        const float c = columns_of<K>(s, i);
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            if (k == got) held[k] = w, columns[k] = c;
         ++got;
         total += w.x;
     });
-    const float mean = warp_sum_f(total) / n;
+    const float mean = lanes_total(s, total) * over_n;
     q = 0.f;
 #pragma unroll
-    for (int k = 0; k < kBlockCluster * kBlockWarps / 32; ++k)
+    for (int k = 0; k < kHeld; ++k)
         if (columns[k] > 0.f) {
             const float off = held[k].x / columns[k] - mean;
             q += fmaf(columns[k] * off, off, held[k].y);
         }
-    return make_float2(mean, rsqrtf(warp_sum_f(q) / n + norm.eps));
+    return make_float2(mean, rsqrtf(fmaf(lanes_total(s, q), over_n, norm.eps)));
 }
 
-// both sums over the row
-__device__ __forceinline__ float2 row_sums(Exchange& e, uint32_t& turn, const BlockShape& s, const Place& at, float a, float b)
+// ---- rows in shared memory ----------------------------------------------------------
+// A row of every source, `stages` times for each team: a row's copies are counted by its stage's barrier.
+template <int K>
+struct Stages {
+    const BlockShape& s;
+    const Place<K>& at;
+    char* buffers;
+    uint32_t bars;                     // this team's
+    __device__ __forceinline__ Stages(const BlockShape& s, const Place<K>& at, char* buffers, uint32_t bars)
+        : s(s), at(at), buffers(buffers + at.team * s.stages * s.row_bytes), bars(bars + at.team * kMaxStages * 8) {}
+
+    // the team's first warp, a source per lane
+    __device__ __forceinline__ void fetch(uint32_t stage, uint32_t row) const
+    {
+        const uint32_t bar = bars + 8 * stage;
+        uint32_t size = 0;
+        const char* from = nullptr;
+        if (at.lane < kMaxSources) {
+            const Source& source = s.source[at.lane];
+            if (source.base && at.width) {
+                from = source.base + (uint64_t)row * source.stride + source.begin(at.first);
+                const uint32_t skew = (uint32_t)(uintptr_t)from & 15u;
+                from -= skew;
+                size = (skew + source.bytes_of(at.width) + 15) & ~15u;
+            }
+        }
+        const uint32_t bytes = __reduce_add_sync(0xFFFFFFFFu, size);
+        if (at.lane == 0) barrier_expect(bar, bytes);
+        __syncwarp();
+        if (size)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(shared_address(buffers + stage * s.row_bytes) + s.source[at.lane].at), "l"(from), "r"(size), "r"(bar) : "memory");
+        __syncwarp();
+    }
+
+    __device__ __forceinline__ const char* place(uint32_t stage, const Source& source) const { return buffers + stage * s.row_bytes + source.at; }
+
+    // The thread's values of 16 bits, zeros where there is no column.
+    template <typename T, bool WIDE>
+    __device__ __forceinline__ void values(Values<K>& v, uint32_t stage, uint32_t row, const Source& source) const
+    {
+        const char* const begin = place(stage, source) + (at.col - at.first) * 2;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            const char* const from = begin + 512 * i;
+            if constexpr (WIDE) {
+                const uint4 q = *(const uint4*)from;
+                w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+            } else if (at.count[i] > 0) {
+                // words from the last one that starts at or before the values
+                const uint32_t skew = source.skew(row, at.first), shift = (skew & 2u) * 8;
+                const uint32_t* const word = (const uint32_t*)(from + (skew & ~3u));
+                uint32_t c[5];
+#pragma unroll
+                for (int j = 0; j < 5; ++j) c[j] = word[j];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(c[j], c[j + 1], shift);
+                if (at.count[i] < 8) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] &= at.count[i] >= 2 * j + 2 ? 0xFFFFFFFFu : at.count[i] == 2 * j + 1 ? 0xFFFFu : 0u;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x, y;
+                unpack<T>(w[j], x, y);
+                v[i][j] = Pair(x, y);
+            }
+        }
+    }
+
+    // The same from a checkpoint, times `factor`.
+    template <bool WIDE>
+    __device__ __forceinline__ void coded(Values<K>& v, uint32_t stage, uint32_t row, const Source& codes, const Source& exps, float factor) const
+    {
+        const char* const begin = place(stage, codes) + (at.col - at.first);
+        const uint8_t* const exp = (const uint8_t*)place(stage, exps) + exps.skew(row, at.first) + (at.col - at.first) / kGroup;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            uint32_t a = 0, b = 0, e = 1;
+            const char* const from = begin + 256 * i;
+            if constexpr (WIDE) {
+                const uint2 q = *(const uint2*)from;
+                const bool there = at.count[i] > 0;
+                e = exp[256 / kGroup * i];
+                a = there ? q.x : 0u, b = there ? q.y : 0u, e = there ? e : 1u;
+            } else if (at.count[i] > 0) {
+                const uint32_t skew = codes.skew(row, at.first), shift = (skew & 3u) * 8;
+                const uint32_t* const word = (const uint32_t*)(from + (skew & ~3u));
+                const uint32_t c = word[1];
+                a = __funnelshift_r(word[0], c, shift);
+                b = __funnelshift_r(c, word[2], shift);
+                e = exp[256 / kGroup * i];
+                if (at.count[i] < 8) {
+                    a &= at.count[i] >= 4 ? 0xFFFFFFFFu : 0xFFFFFFFFu >> (32 - 8 * at.count[i]);
+                    b &= at.count[i] > 4 ? 0xFFFFFFFFu >> (64 - 8 * at.count[i]) : 0u;
+                }
+            }
+            const Pair scale(group_scale(e) * factor);
+            code_values(a, scale, v[i][0], v[i][1]);
+            code_values(b, scale, v[i][2], v[i][3]);
+        }
+    }
+
+    // Zeros behind the last value of every row's place, up to the team's last column: no copy reaches
+    // there.  The whole block.
+    __device__ __forceinline__ void clear(char* block) const
+    {
+        for (int i = 0; i < kMaxSources; ++i) {
+            const Source& source = s.source[i];
+            if (!source.base || !source.columns) continue;
+            const uint32_t begin = (source.bytes_of(at.width) + 15) & ~15u, end = source.bytes_of(s.span);
+            if (begin >= end) continue;
+            for (uint32_t row = 0; row < s.teams * s.stages; ++row)
+                for (uint32_t to = begin + threadIdx.x * 4; to < end; to += blockDim.x * 4) *(uint32_t*)(block + row * s.row_bytes + source.at + to) = 0;
+        }
+    }
+
+    // A vector over the columns is vector `which` of the block: ones where there is none.  The whole block.
+    template <typename T>
+    __device__ __forceinline__ void keep_vector(char* block, int which, const void* v) const
+    {
+        const uint32_t one = pack<T>(1.f, 1.f);
+        for (uint32_t c = threadIdx.x * 8; c < s.span; c += blockDim.x * 8) {
+            const uint32_t col = at.first + c;
+            const int count = col < s.n ? (int)min(s.n - col, 8u) : 0;
+            *(uint4*)(block + s.vectors + (which * s.span + c) * 2) = v ? load_shifted_8((const T*)v + col, count) : make_uint4(one, one, one, one);
+        }
+    }
+
+    template <typename T>
+    __device__ __forceinline__ void vector(Values<K>& v, const char* block, int which) const
+    {
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const uint4 q = *(const uint4*)(block + s.vectors + (which * s.span + at.col - at.first + 256 * i) * 2);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x, y;
+                unpack<T>(w[j], x, y);
+                v[i][j] = Pair(x, y);
+            }
+        }
+    }
+
+    // A row's statistics.
+    __device__ __forceinline__ float2 pair(uint32_t stage, uint32_t row, const Source& source) const
+    {
+        return *(const float2*)(place(stage, source) + source.skew(row, 0));
+    }
+
+    // After a wait that ran out: the copies still on their way land before the block ends.
+    __device__ __forceinline__ void drain(uint32_t first, uint32_t step) const
+    {
+        const uint32_t rows = first < s.m ? (s.m - first + step - 1) / step : 0;
+        for (uint32_t i = 0; i < s.stages && i < rows; ++i) barrier_wait(bars + 8 * i, (rows - 1 - i) / s.stages & 1);
+    }
+};
+
+// The lane's 8 values to p, of which `count` exist.  Without WIDE they go round the warp in shared
+// memory (`buffer`, its own 132 words) and are stored side by side, whole words wherever the matrix
+// has them.
+template <typename T, bool WIDE>
+__device__ __forceinline__ void store_row_8(T* p, int count, const Pair (&v)[4], uint32_t* buffer, uint32_t lane)
 {
-    float2 total = make_float2(0.f, 0.f);
-    exchange(e, turn, s, at, make_float2(warp_sum_f(a), warp_sum_f(b)), [&](uint32_t, float2 w) { total.x += w.x; total.y += w.y; });
-    return make_float2(warp_sum_f(total.x), warp_sum_f(total.y));
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x, y;
+        v[j].get(x, y);
+        w[j] = pack<T>(x, y);
+    }
+    if constexpr (WIDE) {
+        if (count > 0) *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+        return;
+    }
+    __syncwarp();
+    *(uint4*)(buffer + 4 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+    __syncwarp();
+    const int in_warp = __reduce_add_sync(0xFFFFFFFFu, count);             // lanes' columns follow one another
+    uint16_t* const row = (uint16_t*)p - lane * 8;
+    const int skew = ((uintptr_t)row & 3) != 0;                            // the first value is a word's second half
+    uint32_t* const words = (uint32_t*)(row - skew);
+#pragma unroll
+    for (int j = 0; j < 5; ++j) {
+        const int i = j * 32 + (int)lane, a = 2 * i - skew;                // the word holds values a and a + 1
+        if (j == 4 && i > 128) break;
+        const uint32_t low = a >= 0 && a < in_warp ? ((const uint16_t*)buffer)[a] : 0u, high = a + 1 < in_warp ? ((const uint16_t*)buffer)[a + 1] : 0u;
+        if (a >= 0 && a + 1 < in_warp) words[i] = low | high << 16;
+        else if (a >= 0 && a < in_warp) row[a] = (uint16_t)low;
+        else if (a == -1 && in_warp > 0) row[0] = (uint16_t)high;
+    }
 }
 
-template <typename T>
-__device__ __forceinline__ void widen_8(const uint4& w, float (&v)[8])
+// The eight numbers that decide on 8 values.
+__device__ __forceinline__ uint4 drop_numbers(const DropView& d, uint64_t seed, uint32_t row, uint32_t col)
 {
-    unpack<T>(w.x, v[0], v[1]);
-    unpack<T>(w.y, v[2], v[3]);
-    unpack<T>(w.z, v[4], v[5]);
-    unpack<T>(w.w, v[6], v[7]);
+    return philox_stream(seed, 3u, (uint64_t)(d.first_row + row) << 32 | col / 8);
 }
+
+// Dropped values are 0, whatever they were; the others are multiplied by `factor`.  A number's half of a
+// word is compared at the word's top (keep is below 65536 where anything is dropped).
+__device__ __forceinline__ void drop_values(Pair (&v)[4], const uint4& numbers, uint32_t keep, float factor)
+{
+    const uint32_t w[4] = {numbers.x, numbers.y, numbers.z, numbers.w}, below = keep << 16;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x, y;
+        (v[j] * Pair(factor)).get(x, y);
+        v[j] = Pair(w[j] << 16 < below ? x : 0.f, w[j] < below ? y : 0.f);
+    }
+}
+
+// columns that do not exist are 0
+template <bool WIDE>
+__device__ __forceinline__ void mask_values(Pair (&v)[4], int count)
+{
+    if (count == 8) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x, y;
+        v[j].get(x, y);
+        v[j] = WIDE ? Pair(0.f) : Pair(2 * j < count ? x : 0.f, 2 * j + 1 < count ? y : 0.f);
+    }
+}
+
+// A row's pieces to p, the first one's place.
+template <typename T, bool WIDE, int K>
+__device__ __forceinline__ void store_row(T* p, const Place<K>& at, const Values<K>& v, uint32_t* buffer)
+{
+#pragma unroll
+    for (int i = 0; i < K; ++i) store_row_8<T, WIDE>(p + 256 * i, at.count[i], v[i], buffer, at.lane);
+}
+
+// Vectors of a block.
+enum { kAfterWeights = 0, kBeforeWeights = 1, kGateVector = 2, kAfterBiases = 3, kBeforeBiases = 4 };
+template <bool FULL> constexpr int kVectors = FULL ? 5 : 3;
+
+// f(i, j) for a thread's K x 4 pairs
+template <int K, typename F>
+__device__ __forceinline__ void each(F&& f)
+{
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f(i, j);
+}
+
+enum { kSourceH = 0, kSourceResidual = 1, kSourceGate = 2 };
+
+struct JoinView {
+    const void* gate;                  // a vector, or null
+    void* x;               uint64_t x_stride;              // or null
+    void* y;               uint64_t y_stride;              // before.kind != none
+    NormView after, before;
+    DropView drop;
+    float scale;
+    int has_drop;
+};
+
+__device__ __forceinline__ void stages_init(uint32_t bars, uint32_t teams)
+{
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < teams * kMaxStages; ++i) barrier_init(bars + 8 * i, 1);
+        barrier_init_done();
+    }
+    __syncthreads();
+}
+
+template <typename T, bool AFTER, bool BEFORE, bool FULL, bool WIDE, int K>
+__global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __grid_constant__ BlockShape s, uint32_t* status)
+{
+    __shared__ Exchange sums;
+    __shared__ uint32_t buffers[WIDE ? 1 : kMaxTeams][132];
+    __shared__ __align__(8) uint64_t bars[kMaxTeams * kMaxStages];
+    extern __shared__ __align__(16) char rows_of_block[];
+    const Place<K> at(s);
+    const Stages<K> stages(s, at, rows_of_block, shared_address(bars));
+    if constexpr (WIDE) stages.clear(rows_of_block);
+    stages_init(shared_address(bars), s.teams);
+    dependency_wait();
+    dependency_release();
+    uint32_t* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
+    const uint64_t seed = p.drop.seed_at ? *p.drop.seed_at : p.drop.seed;
+    const uint32_t step = gridDim.x / s.blocks * s.teams, first = blockIdx.x / s.blocks * s.teams + at.team;
+    if (at.warp == 0)
+        for (uint32_t i = 0; i < s.stages; ++i)
+            if (first + i * (uint64_t)step < s.m) stages.fetch(i, first + i * step);
+    stages.template keep_vector<T>(rows_of_block, kGateVector, p.gate);
+    if (AFTER) stages.template keep_vector<T>(rows_of_block, kAfterWeights, p.after.weight);
+    if (BEFORE) stages.template keep_vector<T>(rows_of_block, kBeforeWeights, p.before.weight);
+    if (FULL && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
+    if (FULL && BEFORE && p.before.bias) stages.template keep_vector<T>(rows_of_block, kBeforeBiases, p.before.bias);
+    __syncthreads();
+    auto vector = [&](Values<K>& v, int which) { stages.template vector<T>(v, rows_of_block, which); };
+    uint32_t turn = 0, stage = 0, phase = 0;
+    bool ok = true;
+    for (uint32_t row = first; row < s.m; row += step) {
+        // a wait that ran out: the row is worked on all the same, so that every warp and every block of
+        // the cluster meets at the same barriers; the status says that the results are not to be used
+        ok = barrier_wait(stages.bars + 8 * stage, phase) && ok;
+        // everybody has done the row before this one: its stage is free
+        auto refill = [&] {
+            const uint64_t next = row + (uint64_t)step * (s.stages - 1);
+            if (at.warp == 0 && row != first && next < s.m) stages.fetch(stage == 0 ? s.stages - 1 : stage - 1, (uint32_t)next);
+        };
+        Values<K> v, w;
+        stages.template values<T, WIDE>(v, stage, row, s.source[kSourceH]);
+        if constexpr (AFTER) {
+            const float2 st = row_statistics<FULL, K>(sums, turn, s, at, p.after, v);
+            refill();
+            if (p.after.stats && at.col == 0) *(float2*)(p.after.stats + 2 * (uint64_t)row) = st;
+            vector(w, kAfterWeights);
+            each<K>([&](int i, int j) {
+                if (FULL) v[i][j] = v[i][j] + Pair(-st.x);
+                v[i][j] = v[i][j] * Pair(st.y) * w[i][j];
+            });
+            if (FULL && p.after.bias) {
+                vector(w, kAfterBiases);
+                each<K>([&](int i, int j) { v[i][j] = v[i][j] + w[i][j]; });
+            }
+        }
+        if (p.has_drop) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) drop_values(v[i], drop_numbers(p.drop, seed, row, at.col + 256 * i), p.drop.keep, p.drop.factor);
+        }
+        if (FULL && s.source[kSourceGate].base) {
+            stages.template values<T, WIDE>(w, stage, row, s.source[kSourceGate]);
+            each<K>([&](int i, int j) { v[i][j] = v[i][j] * w[i][j]; });
+        } else if (p.gate) {
+            vector(w, kGateVector);
+            each<K>([&](int i, int j) { v[i][j] = v[i][j] * w[i][j]; });
+        }
+        if (s.source[kSourceResidual].base) {
+            stages.template values<T, WIDE>(w, stage, row, s.source[kSourceResidual]);
+            each<K>([&](int i, int j) { v[i][j] = fma(w[i][j], Pair(p.scale), v[i][j]); });
+        }
+        if (p.x) store_row<T, WIDE, K>((T*)p.x + (uint64_t)row * p.x_stride + at.col, at, v, buffer);
+        if constexpr (BEFORE) {
+            if (FULL) {
+#pragma unroll
+                for (int i = 0; i < K; ++i) mask_values<WIDE>(v[i], at.count[i]);
+            }
+            const float2 st = row_statistics<FULL, K>(sums, turn, s, at, p.before, v);
+            if (!AFTER) refill();
+            if (p.before.stats && at.col == 0) *(float2*)(p.before.stats + 2 * (uint64_t)row) = st;
+            vector(w, kBeforeWeights);
+            each<K>([&](int i, int j) {
+                if (FULL) v[i][j] = v[i][j] + Pair(-st.x);
+                v[i][j] = v[i][j] * Pair(st.y) * w[i][j];
+            });
+            if (FULL && p.before.bias) {
+                vector(w, kBeforeBiases);
+                each<K>([&](int i, int j) { v[i][j] = v[i][j] + w[i][j]; });
+            }
+            store_row<T, WIDE, K>((T*)p.y + (uint64_t)row * p.y_stride + at.col, at, v, buffer);
+        }
+        // a team of one warp has no barrier: its lanes meet before the stage is filled again
+        __syncwarp();
+        if (++stage == s.stages) stage = 0, phase ^= 1;
+    }
+    if (!ok) {
+        stages.drain(first, step);
+        if (at.lane == 0) atomicOr(status, EDEN_STATUS_TIMEOUT);
+    }
+    // a block's places are written by the others of its cluster as long as they run
+    if (s.blocks > 1) cluster_arrive_wait();
+}
+
+// ---- backward -----------------------------------------------------------------------
+enum { kBeforeWeight = 0, kBeforeBias = 1, kAfterWeight = 2, kAfterBias = 3, kGateSum = 4, kJoinSums = 5 };
+enum { kSourceDx = 0, kSourceDy = 1, kSourceX = 2, kSourceXExps = 3, kSourceBefore = 4, kSourceKeptH = 5, kSourceHExps = 6, kSourceAfter = 7, kSourceGateMatrix = 8 };
+
+struct JoinBackwardView {
+    const void* gate;                  // a vector, or null
+    void* d_residual;      uint64_t d_residual_stride;     // or null
+    void* dh;              uint64_t dh_stride;             // or null
+    void* d_gate;          uint64_t d_gate_stride;         // a matrix gate's gradient, or null
+    float* partial;                    // sums over rows that are wanted: [part][number of them][n]
+    uint32_t wanted;
+    NormView after, before;
+    DropView drop;
+    float scale;
+    int has_drop;
+};
+
+// Each team keeps the sums of its rows over the columns in registers and leaves them in its part of
+// `partial`, which k_join_sums adds up.
+template <typename T, bool AFTER, bool BEFORE, bool FULL, bool WIDE, int K>
+__global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinBackwardView p, const __grid_constant__ BlockShape s, uint32_t* status)
+{
+    __shared__ Exchange sums;
+    __shared__ uint32_t buffers[WIDE ? 1 : kMaxTeams][132];
+    __shared__ __align__(8) uint64_t bars[kMaxTeams * kMaxStages];
+    extern __shared__ __align__(16) char rows_of_block[];
+    const Place<K> at(s);
+    const Stages<K> stages(s, at, rows_of_block, shared_address(bars));
+    if constexpr (WIDE) stages.clear(rows_of_block);
+    stages_init(shared_address(bars), s.teams);
+    dependency_wait();
+    dependency_release();
+    uint32_t* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
+    const uint64_t seed = p.drop.seed_at ? *p.drop.seed_at : p.drop.seed;
+    const uint32_t group = blockIdx.x / s.blocks, step = gridDim.x / s.blocks * s.teams, first = group * s.teams + at.team;
+    if (at.warp == 0)
+        for (uint32_t i = 0; i < s.stages; ++i)
+            if (first + i * (uint64_t)step < s.m) stages.fetch(i, first + i * step);
+    const float over_n = 1.f / (float)s.n;
+    stages.template keep_vector<T>(rows_of_block, kGateVector, p.gate);
+    if (AFTER) stages.template keep_vector<T>(rows_of_block, kAfterWeights, p.after.weight);
+    if (BEFORE) stages.template keep_vector<T>(rows_of_block, kBeforeWeights, p.before.weight);
+    if (FULL && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
+    __syncthreads();
+    auto vector = [&](Values<K>& v, int which) { stages.template vector<T>(v, rows_of_block, which); };
+    const bool matrix_gate = FULL && s.source[kSourceGateMatrix].base, gated = p.gate || matrix_gate;
+    Values<K> total[kJoinSums];
+#pragma unroll
+    for (int k = 0; k < kJoinSums; ++k) each<K>([&](int i, int j) { total[k][i][j] = Pair(0.f); });
+    // the normalised row of an activation that was kept
+    auto unit = [&](Values<K>& v, int which, uint32_t stage, uint32_t row, float2 st) {
+        const bool coded = s.source[which + 1].base;
+        if (coded) stages.template coded<WIDE>(v, stage, row, s.source[which], s.source[which + 1], FULL ? 1.f : st.y);
+        else stages.template values<T, WIDE>(v, stage, row, s.source[which]);
+        if (FULL) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                const Pair rate(at.count[i] > 0 ? st.y : 0.f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = (v[i][j] + Pair(-st.x)) * rate;
+                if (!WIDE) mask_values<false>(v[i], at.count[i]);
+            }
+        } else if (!coded) {
+            each<K>([&](int i, int j) { v[i][j] = v[i][j] * Pair(st.y); });
+        }
+    };
+    uint32_t turn = 0, stage = 0, phase = 0;
+    bool ok = true;
+    for (uint32_t row = first; row < s.m; row += step) {
+        ok = barrier_wait(stages.bars + 8 * stage, phase) && ok;
+        auto refill = [&] {
+            const uint64_t next = row + (uint64_t)step * (s.stages - 1);
+            if (at.warp == 0 && row != first && next < s.m) stages.fetch(stage == 0 ? s.stages - 1 : stage - 1, (uint32_t)next);
+        };
+        Values<K> d, g, u;
+        if constexpr (BEFORE) {
+            const float2 st = stages.pair(stage, row, s.source[kSourceBefore]);
+            stages.template values<T, WIDE>(g, stage, row, s.source[kSourceDy]);
+            unit(u, kSourceX, stage, row, st);
+            Pair a(0.f), b(0.f);
+            vector(d, kBeforeWeights);
+            each<K>([&](int i, int j) {
+                total[kBeforeWeight][i][j] = fma(g[i][j], u[i][j], total[kBeforeWeight][i][j]);
+                if (FULL) total[kBeforeBias][i][j] = total[kBeforeBias][i][j] + g[i][j];
+                g[i][j] = g[i][j] * d[i][j];
+                if (FULL) a = a + g[i][j];
+                b = fma(g[i][j], u[i][j], b);
+            });
+            const float2 mean = row_sums<FULL, K>(sums, turn, s, at, a, b);
+            refill();
+            const Pair off(p.before.kind == EDEN_NORM_LAYER ? -mean.x * over_n : 0.f), inner(-mean.y * over_n), rate(st.y);
+            if (s.source[kSourceDx].base) stages.template values<T, WIDE>(d, stage, row, s.source[kSourceDx]);
+            else each<K>([&](int i, int j) { d[i][j] = Pair(0.f); });
+            each<K>([&](int i, int j) {
+                if (FULL) g[i][j] = g[i][j] + off;
+                d[i][j] = fma(fma(u[i][j], inner, g[i][j]), rate, d[i][j]);
+            });
+        } else {
+            stages.template values<T, WIDE>(d, stage, row, s.source[kSourceDx]);
+        }
+        if (p.d_residual) {
+            each<K>([&](int i, int j) { g[i][j] = d[i][j] * Pair(p.scale); });
+            store_row<T, WIDE, K>((T*)p.d_residual + (uint64_t)row * p.d_residual_stride + at.col, at, g, buffer);
+        }
+        uint4 numbers[K];
+        if (p.has_drop) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                numbers[i] = drop_numbers(p.drop, seed, row, at.col + 256 * i);
+                drop_values(d[i], numbers[i], p.drop.keep, p.drop.factor);
+            }
+        }
+        const float2 st = AFTER ? stages.pair(stage, row, s.source[kSourceAfter]) : make_float2(0.f, 1.f);
+        if (AFTER || gated) unit(u, kSourceKeptH, stage, row, st);
+        if (gated) {
+            if (AFTER) {
+                vector(g, kAfterWeights);
+                each<K>([&](int i, int j) { g[i][j] = g[i][j] * u[i][j]; });
+            } else {
+                each<K>([&](int i, int j) { g[i][j] = u[i][j]; });
+            }
+            if (FULL && AFTER && p.after.bias) {
+                Values<K> bias;
+                vector(bias, kAfterBiases);
+                each<K>([&](int i, int j) { g[i][j] = g[i][j] + bias[i][j]; });
+            }
+            each<K>([&](int i, int j) { g[i][j] = g[i][j] * d[i][j]; });
+            // a value of h that was dropped, whatever it is; behind a norm it would have made all of the row NaN
+            if (!AFTER && p.has_drop) {
+#pragma unroll
+                for (int i = 0; i < K; ++i) drop_values(g[i], numbers[i], p.drop.keep, 1.f);
+            }
+            if (matrix_gate) {
+                if (p.d_gate) store_row<T, WIDE, K>((T*)p.d_gate + (uint64_t)row * p.d_gate_stride + at.col, at, g, buffer);
+                stages.template values<T, WIDE>(g, stage, row, s.source[kSourceGateMatrix]);
+                each<K>([&](int i, int j) { d[i][j] = d[i][j] * g[i][j]; });
+            } else {
+                each<K>([&](int i, int j) { total[kGateSum][i][j] = total[kGateSum][i][j] + g[i][j]; });
+                vector(g, kGateVector);
+                each<K>([&](int i, int j) { d[i][j] = d[i][j] * g[i][j]; });
+            }
+        }
+        if constexpr (AFTER) {
+            Pair a(0.f), b(0.f);
+            if (FULL) {
+#pragma unroll
+                for (int i = 0; i < K; ++i) mask_values<WIDE>(d[i], at.count[i]);
+            }
+            vector(g, kAfterWeights);
+            each<K>([&](int i, int j) {
+                total[kAfterWeight][i][j] = fma(d[i][j], u[i][j], total[kAfterWeight][i][j]);
+                if (FULL) total[kAfterBias][i][j] = total[kAfterBias][i][j] + d[i][j];
+                d[i][j] = d[i][j] * g[i][j];
+                if (FULL) a = a + d[i][j];
+                b = fma(d[i][j], u[i][j], b);
+            });
+            const float2 mean = row_sums<FULL, K>(sums, turn, s, at, a, b);
+            if (!BEFORE) refill();
+            const Pair off(p.after.kind == EDEN_NORM_LAYER ? -mean.x * over_n : 0.f), inner(-mean.y * over_n), rate(st.y);
+            each<K>([&](int i, int j) {
+                if (FULL) d[i][j] = d[i][j] + off;
+                d[i][j] = fma(u[i][j], inner, d[i][j]) * rate;
+            });
+        }
+        if (p.dh) store_row<T, WIDE, K>((T*)p.dh + (uint64_t)row * p.dh_stride + at.col, at, d, buffer);
+        __syncwarp();
+        if (++stage == s.stages) stage = 0, phase ^= 1;
+    }
+    if (p.wanted) {
+        float* to = p.partial + (uint64_t)(group * s.teams + at.team) * __popc(p.wanted) * s.n + at.col;
+#pragma unroll
+        for (int k = 0; k < kJoinSums; ++k) {
+            if (!(p.wanted >> k & 1)) continue;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) total[k][i][j].get(x[2 * j], x[2 * j + 1]);
+                if (WIDE) {
+                    if (at.count[i] > 0) *(float4*)(to + 256 * i) = make_float4(x[0], x[1], x[2], x[3]), *(float4*)(to + 256 * i + 4) = make_float4(x[4], x[5], x[6], x[7]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < at.count[i]) to[256 * i + j] = x[j];
+                }
+            }
+            to += s.n;
+        }
+    }
+    if (!ok) {
+        stages.drain(first, step);
+        if (at.lane == 0) atomicOr(status, EDEN_STATUS_TIMEOUT);
+    }
+    if (s.blocks > 1) cluster_arrive_wait();
+}
+
+// ---- without norms -------------------------------------------------------------------
+// Nothing is summed over a row, so a block takes 256 columns a warp of its own choice and any rows:
+// kPlainRows of them at a time, all of their loads on their way together.
+constexpr int kPlainRows = 4, kPlainThreads = 256;
+
+struct PlainView {
+    const void* h;         uint64_t h_stride;
+    const void* residual;  uint64_t residual_stride;       // or null
+    const void* gate;      uint64_t gate_stride;           // or null; stride 0: a vector
+    void* x;               uint64_t x_stride;
+    DropView drop;
+    float scale;
+    int has_drop;
+    uint32_t m, n, warps_across;       // warps that cover a row
+};
 
 // 8 values at p, of which `count` exist (zeros after them); WIDE: on 16 bytes
 template <bool WIDE, typename T>
@@ -178,160 +824,63 @@ __device__ __forceinline__ uint4 load_row_8(const T* p, int count)
     return load_shifted_8(p, count);
 }
 
-// The lane's 8 values to p, of which `count` exist.  Without WIDE the warp hands them round in shared
-// memory (`buffer`, its own 128 words) and stores them side by side.
-template <bool WIDE, typename T>
-__device__ __forceinline__ void store_row_8(T* p, int count, const float (&v)[8], uint4* buffer, uint32_t lane)
+template <typename T>
+__device__ __forceinline__ void widen_8(const uint4& q, Pair (&v)[4])
 {
-    const uint4 w = make_uint4(pack<T>(v[0], v[1]), pack<T>(v[2], v[3]), pack<T>(v[4], v[5]), pack<T>(v[6], v[7]));
-    if constexpr (WIDE) {
-        if (count == 8) {
-            *(uint4*)p = w;
-            return;
-        }
-        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < count) ((uint16_t*)p)[j] = (uint16_t)(words[j / 2] >> 16 * (j % 2));
-        return;
-    }
-    __syncwarp();
-    buffer[lane] = w;
-    __syncwarp();
-    const int in_warp = __reduce_add_sync(0xFFFFFFFFu, count);             // lanes' columns follow one another
-    uint16_t* const row = (uint16_t*)p - lane * 8;
-    if (((uintptr_t)row & 3) == 0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = j * 32 + (int)lane;
-            if (2 * i + 1 < in_warp) ((uint32_t*)row)[i] = ((const uint32_t*)buffer)[i];
-            else if (2 * i < in_warp) row[2 * i] = ((const uint16_t*)buffer)[2 * i];
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = j * 32 + (int)lane;
-            if (i < in_warp) row[i] = ((const uint16_t*)buffer)[i];
-        }
-    }
-}
-
-// factors of the 8 values: 0 or 65536 / keep
-__device__ __forceinline__ uint32_t kept_bits(const DropView& d, uint64_t seed, uint32_t row, uint32_t col)
-{
-    const uint4 r = philox_stream(seed, 3u, (uint64_t)(d.first_row + row) << 32 | col / 8);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-    uint32_t bits = 0;
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        bits |= (w[j] & 0xFFFFu) < d.keep ? 1u << 2 * j : 0u;
-        bits |= w[j] >> 16 < d.keep ? 2u << 2 * j : 0u;
+        float x, y;
+        unpack<T>(w[j], x, y);
+        v[j] = Pair(x, y);
     }
-    return bits;
 }
 
-struct JoinView {
-    const void* h;         uint64_t h_stride;
-    const void* residual;  uint64_t residual_stride;       // or null
-    const void* gate;      uint64_t gate_stride;           // or null; stride 0: a vector
-    void* x;               uint64_t x_stride;              // or null
-    void* y;               uint64_t y_stride;              // before.kind != none
-    NormView after, before;
-    DropView drop;
-    float scale;
-    int has_drop;
-};
-
-template <typename T, bool WIDE, bool AFTER, bool BEFORE>
-__global__ void __launch_bounds__(kBlockThreads, 2) k_join(JoinView p, BlockShape s)
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kPlainThreads) k_join_plain(PlainView p)
 {
-    __shared__ Exchange sums;
-    __shared__ uint4 buffers[WIDE ? 1 : kBlockWarps][32];
+    __shared__ uint32_t buffers[WIDE ? 1 : kPlainThreads / 32][132];
     dependency_wait();
     dependency_release();
-    const Place at(s);
-    uint4* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
+    const uint32_t lane = threadIdx.x % 32;
+    uint32_t* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
+    const uint64_t unit = (uint64_t)blockIdx.x * (kPlainThreads / 32) + threadIdx.x / 32, row0 = unit / p.warps_across * kPlainRows;
+    if (row0 >= p.m) return;
+    const uint32_t col = (uint32_t)(unit % p.warps_across) * 256 + lane * 8;
+    const int count = col < p.n ? (int)min(p.n - col, 8u) : 0, rows = (int)min((uint64_t)p.m - row0, (uint64_t)kPlainRows);
     const uint64_t seed = p.drop.seed_at ? *p.drop.seed_at : p.drop.seed;
-    const uint32_t step = gridDim.x / s.blocks * s.teams;
-    uint32_t turn = 0, row = blockIdx.x / s.blocks * s.teams + at.team;
-    auto vector = [&](const void* v) { return load_shifted_8((const T*)v + at.col, v ? at.count : 0); };
-    uint4 after_weight, after_bias, before_weight, before_bias, gate = vector(p.gate_stride ? nullptr : p.gate);
-    if (AFTER) after_weight = vector(p.after.weight), after_bias = vector(p.after.bias);
-    if (BEFORE) before_weight = vector(p.before.weight), before_bias = vector(p.before.bias);
-    auto affine = [&](float (&v)[8], const NormView& norm, const uint4& weight, const uint4& bias) {
-        float w[8];
-        if (norm.weight) {
-            widen_8<T>(weight, w);
+    uint4 h[kPlainRows], residual[kPlainRows], gate[kPlainRows];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= w[j];
-        }
-        if (norm.bias) {
-            widen_8<T>(bias, w);
+    for (int r = 0; r < kPlainRows; ++r) {
+        const int here = r < rows ? count : 0;
+        h[r] = load_row_8<WIDE>((const T*)p.h + (row0 + r) * p.h_stride + col, here);
+        if (p.residual) residual[r] = load_row_8<WIDE>((const T*)p.residual + (row0 + r) * p.residual_stride + col, here);
+        if (p.gate) gate[r] = p.gate_stride ? load_row_8<WIDE>((const T*)p.gate + (row0 + r) * p.gate_stride + col, here) : load_shifted_8((const T*)p.gate + col, here);
+    }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += w[j];
-        }
-    };
-    // the next row waits as it lies in memory
-    uint4 next_h, next_residual, next_gate;
-    auto fetch = [&](uint32_t r) {
-        const int count = r < s.m ? at.count : 0;
-        next_h = load_row_8<WIDE>((const T*)p.h + (uint64_t)r * p.h_stride + at.col, count);
-        if (p.residual) next_residual = load_row_8<WIDE>((const T*)p.residual + (uint64_t)r * p.residual_stride + at.col, count);
-        if (p.gate_stride) next_gate = load_row_8<WIDE>((const T*)p.gate + (uint64_t)r * p.gate_stride + at.col, count);
-    };
-    fetch(row);
-    for (; row < s.m; row += step) {
-        float v[8], residual[8], g[8];
-        widen_8<T>(next_h, v);
-        if (p.residual) widen_8<T>(next_residual, residual);
-        if (p.gate) widen_8<T>(p.gate_stride ? next_gate : gate, g);
-        fetch(row + step);
-        if constexpr (AFTER) {
-            const float2 st = row_statistics(sums, turn, s, at, p.after, v);
-            if (p.after.stats && at.col == 0) *(float2*)(p.after.stats + 2 * (uint64_t)row) = st;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (v[j] - st.x) * st.y;
-            affine(v, p.after, after_weight, after_bias);
-        }
-        if (p.has_drop) {
-            const uint32_t bits = kept_bits(p.drop, seed, row, at.col);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = bits >> j & 1 ? v[j] * p.drop.factor : 0.f;
-        }
+    for (int r = 0; r < kPlainRows; ++r) {
+        if (r >= rows) break;
+        Pair v[4], w[4];
+        widen_8<T>(h[r], v);
+        if (p.has_drop) drop_values(v, drop_numbers(p.drop, seed, (uint32_t)row0 + r, col), p.drop.keep, p.drop.factor);
         if (p.gate) {
+            widen_8<T>(gate[r], w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= g[j];
+            for (int j = 0; j < 4; ++j) v[j] = v[j] * w[j];
         }
         if (p.residual) {
+            widen_8<T>(residual[r], w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = fmaf(p.scale, residual[j], v[j]);
+            for (int j = 0; j < 4; ++j) v[j] = fma(w[j], Pair(p.scale), v[j]);
         }
-        if (p.x) store_row_8<WIDE>((T*)p.x + (uint64_t)row * p.x_stride + at.col, at.count, v, buffer, at.lane);
-        if constexpr (BEFORE) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < at.count ? v[j] : 0.f;
-            const float2 st = row_statistics(sums, turn, s, at, p.before, v);
-            if (p.before.stats && at.col == 0) *(float2*)(p.before.stats + 2 * (uint64_t)row) = st;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (v[j] - st.x) * st.y;
-            affine(v, p.before, before_weight, before_bias);
-            store_row_8<WIDE>((T*)p.y + (uint64_t)row * p.y_stride + at.col, at.count, v, buffer, at.lane);
-        }
+        store_row_8<T, WIDE>((T*)p.x + (row0 + r) * p.x_stride + col, count, v, buffer, lane);
     }
-    // a block's places are written by the others of its cluster as long as they run
-    if (s.blocks > 1) cluster_arrive_wait();
 }
 
-// ---- backward -----------------------------------------------------------------------
 // An activation that was kept: a matrix of 16-bit values, or a checkpoint.
 struct KeptView {
     const void* data;      uint64_t stride;                // null: the checkpoint
     CheckpointView held;
-};
-
-struct KeptRaw {
-    uint4 w;                           // 16-bit values; or two words of codes
-    uint32_t exp;
 };
 
 // 8 bytes at any address, of which `count` exist
@@ -350,197 +899,87 @@ __device__ __forceinline__ uint2 load_bytes_8(const int8_t* p, int count)
 }
 
 template <bool WIDE, typename T>
-__device__ __forceinline__ KeptRaw load_kept(const KeptView& k, uint32_t row, uint32_t col, int count)
-{
-    KeptRaw raw;
-    if (k.data) {
-        raw.w = load_row_8<WIDE>((const T*)k.data + (uint64_t)row * k.stride + col, count);
-        raw.exp = 0;
-    } else {
-        const int8_t* const codes = k.held.codes + (uint64_t)row * k.held.codes_stride + col;
-        const uint2 w = WIDE && count == 8 ? *(const uint2*)codes : load_bytes_8(codes, count);
-        raw.w = make_uint4(w.x, w.y, 0, 0);
-        raw.exp = count > 0 ? k.held.exps[(uint64_t)row * k.held.exps_stride + col / kGroup] : 1u;
-    }
-    return raw;
-}
-
-template <typename T>
-__device__ __forceinline__ void kept_values(const KeptView& k, const KeptRaw& raw, float (&v)[8])
+__device__ __forceinline__ void load_kept(const KeptView& k, uint64_t row, uint32_t col, int count, Pair (&v)[4])
 {
     if (k.data) {
-        widen_8<T>(raw.w, v);
+        widen_8<T>(load_row_8<WIDE>((const T*)k.data + row * k.stride + col, count), v);
         return;
     }
-    const Pair scale(group_scale(raw.exp));
-    Pair a, b;
-    code_values(raw.w.x, scale, a, b);
-    a.get(v[0], v[1]);
-    b.get(v[2], v[3]);
-    code_values(raw.w.y, scale, a, b);
-    a.get(v[4], v[5]);
-    b.get(v[6], v[7]);
+    const uint2 w = load_bytes_8(k.held.codes + row * k.held.codes_stride + col, count);
+    const Pair scale(group_scale(count > 0 ? k.held.exps[row * k.held.exps_stride + col / kGroup] : 1u));
+    code_values(w.x, scale, v[0], v[1]);
+    code_values(w.y, scale, v[2], v[3]);
 }
 
-enum { kBeforeWeight = 0, kBeforeBias = 1, kAfterWeight = 2, kAfterBias = 3, kGateSum = 4, kJoinSums = 5 };
-
-struct JoinBackwardView {
-    const void* dx;        uint64_t dx_stride;             // or null: 0
-    const void* dy;        uint64_t dy_stride;             // before.kind != none
-    KeptView h, x;                                         // h: after.kind != none or a gate
+struct PlainBackwardView {
+    const void* dx;        uint64_t dx_stride;
+    KeptView h;                        // with a gate
     const void* gate;      uint64_t gate_stride;
-    void* d_residual;      uint64_t d_residual_stride;     // or null
-    void* dh;              uint64_t dh_stride;             // or null
-    void* d_gate;          uint64_t d_gate_stride;         // a matrix gate's gradient, or null
-    float* partial;        uint32_t wanted;                // sums over rows that are wanted: [part][number of them][n]
-    NormView after, before;
+    void* d_residual;      uint64_t d_residual_stride;
+    void* dh;              uint64_t dh_stride;
+    void* d_gate;          uint64_t d_gate_stride;
+    float* partial;                    // a vector gate's sums: [run][n], or null
     DropView drop;
     float scale;
     int has_drop;
+    uint32_t m, n, rows_per_run;
 };
 
-// Each team keeps the sums of its rows over the columns in registers and leaves them in its part of
-// `partial`, which k_join_sums adds up.
-template <typename T, bool WIDE, bool AFTER, bool BEFORE>
-__global__ void __launch_bounds__(kBlockThreads, 1) k_join_backward(JoinBackwardView p, BlockShape s)
+// Eight warps side by side along the columns walk down a run of rows.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kPlainThreads) k_join_plain_backward(PlainBackwardView p)
 {
-    __shared__ Exchange sums;
-    __shared__ uint4 buffers[WIDE ? 1 : kBlockWarps][32];
+    __shared__ uint32_t buffers[WIDE ? 1 : kPlainThreads / 32][132];
     dependency_wait();
     dependency_release();
-    const Place at(s);
-    uint4* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
+    const uint32_t lane = threadIdx.x % 32, col = blockIdx.x * (kPlainThreads * 8) + threadIdx.x * 8;
+    uint32_t* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
+    const int count = col < p.n ? (int)min(p.n - col, 8u) : 0;
+    const uint64_t begin = (uint64_t)blockIdx.y * p.rows_per_run, end = min((uint64_t)p.m, begin + p.rows_per_run);
     const uint64_t seed = p.drop.seed_at ? *p.drop.seed_at : p.drop.seed;
-    const uint32_t group = blockIdx.x / s.blocks, step = gridDim.x / s.blocks * s.teams;
-    uint32_t turn = 0, row = group * s.teams + at.team;
-    const float n = (float)s.n;
-    auto vector = [&](const void* v) { return load_shifted_8((const T*)v + at.col, v ? at.count : 0); };
-    uint4 after_weight, after_bias, before_weight, gate = vector(p.gate_stride ? nullptr : p.gate);
-    if (AFTER) after_weight = vector(p.after.weight), after_bias = vector(p.after.bias);
-    if (BEFORE) before_weight = vector(p.before.weight);
-    const bool needs_h = AFTER || p.gate;
-    float total[kJoinSums][8];
+    Pair total[4];
 #pragma unroll
-    for (int i = 0; i < kJoinSums; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) total[i][j] = 0.f;
-
-    uint4 next_dx = make_uint4(0, 0, 0, 0), next_dy, next_gate;
-    KeptRaw next_x, next_h;
-    float2 next_before, next_after;
-    auto fetch = [&](uint32_t r) {
-        const int count = r < s.m ? at.count : 0;
-        if (p.dx) next_dx = load_row_8<WIDE>((const T*)p.dx + (uint64_t)r * p.dx_stride + at.col, count);
-        if (BEFORE) {
-            next_dy = load_row_8<WIDE>((const T*)p.dy + (uint64_t)r * p.dy_stride + at.col, count);
-            next_x = load_kept<WIDE, T>(p.x, r, at.col, count);
-            next_before = r < s.m ? *(const float2*)(p.before.stats + 2 * (uint64_t)r) : make_float2(0.f, 0.f);
-        }
-        if (needs_h) next_h = load_kept<WIDE, T>(p.h, r, at.col, count);
-        if (AFTER) next_after = r < s.m ? *(const float2*)(p.after.stats + 2 * (uint64_t)r) : make_float2(0.f, 0.f);
-        if (p.gate_stride) next_gate = load_row_8<WIDE>((const T*)p.gate + (uint64_t)r * p.gate_stride + at.col, count);
-    };
-    fetch(row);
-    for (; row < s.m; row += step) {
-        float d[8], h[8], g[8], dy[8], x[8];
-        widen_8<T>(next_dx, d);
-        if (needs_h) kept_values<T>(p.h, next_h, h);
-        if (p.gate) widen_8<T>(p.gate_stride ? next_gate : gate, g);
-        if (BEFORE) widen_8<T>(next_dy, dy), kept_values<T>(p.x, next_x, x);
-        const float2 before = next_before, after = next_after;
-        fetch(row + step);
-        if constexpr (BEFORE) {
-            float w[8], sum = 0.f, dot = 0.f;
-            widen_8<T>(before_weight, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = (x[j] - before.x) * before.y;
-                total[kBeforeWeight][j] = fmaf(dy[j], x[j], total[kBeforeWeight][j]);
-                total[kBeforeBias][j] += dy[j];
-                if (p.before.weight) dy[j] *= w[j];
-                if (j < at.count) {
-                    sum += dy[j];
-                    dot = fmaf(dy[j], x[j], dot);
-                }
-            }
-            float2 mean = row_sums(sums, turn, s, at, sum, dot);
-            mean.x = p.before.kind == EDEN_NORM_LAYER ? mean.x / n : 0.f;
-            mean.y /= n;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = fmaf(before.y, dy[j] - mean.x - x[j] * mean.y, d[j]);
-        }
+    for (int j = 0; j < 4; ++j) total[j] = Pair(0.f);
+    uint4 vector = make_uint4(0, 0, 0, 0);
+    if (p.gate && !p.gate_stride) vector = load_shifted_8((const T*)p.gate + col, count);
+#pragma unroll 2
+    for (uint64_t row = begin; row < end; ++row) {
+        Pair v[4], w[4], h[4];
+        widen_8<T>(load_row_8<WIDE>((const T*)p.dx + row * p.dx_stride + col, count), v);
+        if (p.gate) load_kept<WIDE, T>(p.h, row, col, count, h);
         if (p.d_residual) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = p.scale * d[j];
-            store_row_8<WIDE>((T*)p.d_residual + (uint64_t)row * p.d_residual_stride + at.col, at.count, x, buffer, at.lane);
+            for (int j = 0; j < 4; ++j) w[j] = v[j] * Pair(p.scale);
+            store_row_8<T, WIDE>((T*)p.d_residual + row * p.d_residual_stride + col, count, w, buffer, lane);
         }
-        if constexpr (AFTER) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] = (h[j] - after.x) * after.y;
-        }
-        const uint32_t bits = p.has_drop ? kept_bits(p.drop, seed, row, at.col) : 0xFFu;
-        if (p.gate) {
-            float u[8], w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = h[j];
-            if (AFTER && p.after.weight) {
-                widen_8<T>(after_weight, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) u[j] *= w[j];
-            }
-            if (AFTER && p.after.bias) {
-                widen_8<T>(after_bias, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) u[j] += w[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = bits >> j & 1 ? u[j] * p.drop.factor * d[j] : 0.f;
-            if (p.gate_stride) {
-                if (p.d_gate) store_row_8<WIDE>((T*)p.d_gate + (uint64_t)row * p.d_gate_stride + at.col, at.count, u, buffer, at.lane);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) total[kGateSum][j] += u[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] *= g[j];
-        }
+        uint4 numbers;
         if (p.has_drop) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = bits >> j & 1 ? d[j] * p.drop.factor : 0.f;
+            numbers = drop_numbers(p.drop, seed, (uint32_t)row, col);
+            drop_values(v, numbers, p.drop.keep, p.drop.factor);
         }
-        if constexpr (AFTER) {
-            float w[8], sum = 0.f, dot = 0.f;
-            widen_8<T>(after_weight, w);
+        if (p.gate) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                total[kAfterWeight][j] = fmaf(d[j], h[j], total[kAfterWeight][j]);
-                total[kAfterBias][j] += d[j];
-                if (p.after.weight) d[j] *= w[j];
-                if (j < at.count) {
-                    sum += d[j];
-                    dot = fmaf(d[j], h[j], dot);
-                }
+            for (int j = 0; j < 4; ++j) h[j] = h[j] * v[j];
+            if (p.has_drop) drop_values(h, numbers, p.drop.keep, 1.f);
+            widen_8<T>(p.gate_stride ? load_row_8<WIDE>((const T*)p.gate + row * p.gate_stride + col, count) : vector, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = v[j] * w[j];
+                total[j] = total[j] + h[j];
             }
-            float2 mean = row_sums(sums, turn, s, at, sum, dot);
-            mean.x = p.after.kind == EDEN_NORM_LAYER ? mean.x / n : 0.f;
-            mean.y /= n;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = after.y * (d[j] - mean.x - h[j] * mean.y);
+            if (p.d_gate) store_row_8<T, WIDE>((T*)p.d_gate + row * p.d_gate_stride + col, count, h, buffer, lane);
         }
-        if (p.dh) store_row_8<WIDE>((T*)p.dh + (uint64_t)row * p.dh_stride + at.col, at.count, d, buffer, at.lane);
+        if (p.dh) store_row_8<T, WIDE>((T*)p.dh + row * p.dh_stride + col, count, v, buffer, lane);
     }
-    if (p.wanted) {
-        float* to = p.partial + (uint64_t)(group * s.teams + at.team) * __popc(p.wanted) * s.n + at.col;
+    if (!p.partial) return;
+    float* const to = p.partial + (uint64_t)blockIdx.y * p.n + col;
 #pragma unroll
-        for (int i = 0; i < kJoinSums; ++i) {
-            if (!(p.wanted >> i & 1)) continue;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < at.count) to[j] = total[i][j];
-            to += s.n;
-        }
+    for (int j = 0; j < 4; ++j) {
+        float x, y;
+        total[j].get(x, y);
+        if (2 * j < count) to[2 * j] = x;
+        if (2 * j + 1 < count) to[2 * j + 1] = y;
     }
-    if (s.blocks > 1) cluster_arrive_wait();
 }
 
 struct JoinSumsView {
