@@ -554,7 +554,7 @@ int eden_linear_weight_grad(eden_ctx* ctx, const eden_linear_weight_grad_args* a
 #define EDEN_NORM_NONE  0
 #define EDEN_NORM_RMS   1
 #define EDEN_NORM_LAYER 2
-#define EDEN_NORM_MAX_FEATURES 65536u
+#define EDEN_NORM_MAX_FEATURES 32768u
 
 typedef struct eden_norm {
     const void* weight;                                 /* n values, or NULL: 1 */

@@ -11,7 +11,7 @@ namespace {
 
 constexpr uint64_t kMaxSlots = 192;             // blocks of a launch with norms, whatever the device
 constexpr uint64_t kMaxRuns = 512;              // runs of rows of a backward launch without norms
-constexpr uint64_t kMaxNormColumns = 512ull * kTeamWarps * kBlockCluster;
+constexpr uint64_t kMaxNormColumns = 512ull * kTeamWarps * kBlockCluster / 2;   // whatever a row needs fits a cluster
 static_assert(kMaxNormColumns == EDEN_NORM_MAX_FEATURES, "as documented");
 
 bool rows_on_16(const void* p, uint64_t stride) { return !p || (aligned(p, 16) && stride % 8 == 0); }
@@ -38,8 +38,8 @@ DropView drop_view(const eden_drop& d, int* has)
 // stride 0 where one vector serves all rows
 uint64_t gate_stride(const void* gate, int per_value, uint64_t stride) { return gate && per_value ? stride : 0; }
 
-Source matrix_source(const void* p, uint64_t stride) { return {(const char*)p, stride * 2, 2, 1, 0, rows_on_16(p, stride)}; }
-Source stats_source(const float* p) { return {(const char*)p, 8, 8, 0, 0, 0}; }
+Source matrix_source(const void* p, uint64_t stride) { return {(const char*)p, stride * 2, 2, 0, 0, 0, rows_on_16(p, stride)}; }
+Source stats_source(const float* p) { return {(const char*)p, 8, 8, 0, 1, 0, 0}; }
 
 // Rows over teams, blocks and clusters: see kernels_block.cuh.
 struct Grid {
@@ -54,7 +54,6 @@ constexpr uint32_t kRowsShared = (227 - 17) * 1024;
 Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)[kMaxSources], uint32_t warps, bool full)
 {
     Grid g{};
-    g.wide = n % 8 == 0;
     BlockShape& s = g.s;
     s.m = (uint32_t)m;
     s.n = (uint32_t)n;
@@ -62,22 +61,27 @@ Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)
     // Two pieces a thread where that leaves a row for every SM, or where one would need a cluster.
     g.pieces = n > 256 * kTeamWarps || (n > 256 && m >= sms) ? 2 : 1;
     const uint64_t columns = 256ull * kTeamWarps * g.pieces;
-    s.blocks = 1;
-    while (s.blocks * columns < n) s.blocks *= 2;
-    s.warps = (uint32_t)(((n + s.blocks - 1) / s.blocks + 256 * g.pieces - 1) / (256 * g.pieces));
-    s.teams = s.blocks > 1 ? 1 : warps / s.warps;                  // a cluster's blocks work on one row
-    s.span = s.warps * 256 * g.pieces;
-    const uint32_t width = (uint32_t)std::min<uint64_t>(n, s.span);
-    for (int i = 0; i < kMaxSources; ++i) {
-        s.source[i] = source[i];
-        if (!source[i].base) continue;
-        s.source[i].at = s.row_bytes;
-        // up to 15 bytes of a neighbour, and whole words behind the last value; all of the team's columns
-        s.row_bytes += (uint32_t)align_to(std::max(source[i].bytes_of(width) + 48, source[i].bytes_of(s.span)), 16);
-        if (source[i].columns && source[i].columns != (uint32_t)kGroup) g.wide = g.wide && source[i].aligned;
+    uint32_t vectors = 0;
+    for (s.blocks = 1;; s.blocks *= 2) {
+        s.warps = (uint32_t)(((n + s.blocks - 1) / s.blocks + 256 * g.pieces - 1) / (256 * g.pieces));
+        s.span = s.warps * 256 * g.pieces;
+        vectors = (full ? kVectors<true> : kVectors<false>) * s.span * 4;
+        const uint32_t width = (uint32_t)std::min<uint64_t>(n, s.span);
+        s.row_bytes = 0;
+        g.wide = n % 8 == 0;
+        for (int i = 0; i < kMaxSources; ++i) {
+            s.source[i] = source[i];
+            if (!source[i].base) continue;
+            s.source[i].at = s.row_bytes;
+            // up to 15 bytes of a neighbour, and whole words behind the last value; all of the team's columns
+            s.row_bytes += (uint32_t)align_to(std::max(source[i].bytes_of(width) + 48, source[i].bytes_of(s.span)), 16);
+            if (!source[i].fixed && !source[i].shift) g.wide = g.wide && source[i].aligned;
+        }
+        if (s.blocks * columns >= n && 2 * s.row_bytes + vectors <= kRowsShared) break;
+        if (s.blocks == kBlockCluster) return g;                  // not reached: rows of that many columns are refused
     }
+    s.teams = s.blocks > 1 ? 1 : warps / s.warps;                  // a cluster's blocks work on one row
     // few rows: a team of each block has one before a block has two
-    const uint32_t vectors = (full ? kVectors<true> : kVectors<false>) * s.span * 2;
     while (s.teams > 1 && (2 * s.row_bytes * s.teams + vectors > kRowsShared || (uint64_t)s.teams * (sms / s.blocks) >= 2 * m)) s.teams = (s.teams + 1) / 2;
     s.stages = std::min<uint32_t>(kMaxStages, (kRowsShared - vectors) / (s.row_bytes * s.teams));
     s.vectors = s.teams * s.stages * s.row_bytes;
@@ -239,8 +243,9 @@ extern "C" int eden_block_join_backward(eden_ctx* ctx, const eden_block_join_bac
                     if (k.data) {
                         source[at] = matrix_source(k.data, k.stride);
                     } else {
-                        source[at] = {(const char*)k.codes, k.codes_stride, 1, 1, 0, aligned(k.codes, 16) && k.codes_stride % 16 == 0};
-                        source[at + 1] = {(const char*)k.exps, k.exps_stride, 1, (uint32_t)kGroup, 0, 0};
+                        source[at] = {(const char*)k.codes, k.codes_stride, 1, 0, 0, 0, aligned(k.codes, 16) && k.codes_stride % 16 == 0};
+                        source[at + 1] = {(const char*)k.exps, k.exps_stride, 1, 5, 0, 0, 0};
+                        static_assert(kGroup == 1 << 5, "a byte for 2^shift columns");
                     }
                 };
                 if (a->dx) source[kSourceDx] = matrix_source(a->dx, a->dx_stride);

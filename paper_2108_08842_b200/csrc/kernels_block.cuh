@@ -44,15 +44,15 @@ struct NormView {
     int kind;                          // EDEN_NORM_*
 };
 
-// What a row needs of a matrix: `number` bytes for `columns` columns (statistics: 8 bytes, columns 0).
+// What a row needs of a matrix: `number` bytes for 2^shift columns; or, `fixed`, those bytes.
 struct Source {
     const char* base;                  // or null: not wanted
     uint64_t stride;                   // bytes from row to row
-    uint32_t number, columns;
+    uint32_t number, shift, fixed;
     uint32_t at;                       // in a row's place in shared memory
     uint32_t aligned;                  // all rows start on 16 bytes
-    __device__ __forceinline__ uint32_t begin(uint32_t first) const { return columns ? first / columns * number : 0; }
-    __host__ __device__ __forceinline__ uint32_t bytes_of(uint32_t cols) const { return columns ? (cols * number + columns - 1) / columns : number; }
+    __host__ __device__ __forceinline__ uint32_t begin(uint32_t first) const { return fixed ? 0 : (first >> shift) * number; }
+    __host__ __device__ __forceinline__ uint32_t bytes_of(uint32_t cols) const { return fixed ? number : ((cols + (1u << shift) - 1) >> shift) * number; }
     // what a row's place begins with that is not the row's
     __device__ __forceinline__ uint32_t skew(uint32_t r, uint32_t first) const
     {
@@ -240,41 +240,46 @@ struct Stages {
     const BlockShape& s;
     const Place<K>& at;
     char* buffers;
+    const char* row;                   // the place of the row that is worked on
     uint32_t bars;                     // this team's
-    __device__ __forceinline__ Stages(const BlockShape& s, const Place<K>& at, char* buffers, uint32_t bars)
-        : s(s), at(at), buffers(buffers + at.team * s.stages * s.row_bytes), bars(bars + at.team * kMaxStages * 8) {}
+    const char* from;                  // a lane's source: its first row's bytes for this block, how many, and their place
+    uint64_t stride;
+    uint32_t bytes, to;
+    __device__ __forceinline__ Stages(const BlockShape& s, const Place<K>& at, char* block, uint32_t bars)
+        : s(s), at(at), buffers(block + at.team * s.stages * s.row_bytes), row(buffers), bars(bars + at.team * kMaxStages * 8), from(nullptr), stride(0), bytes(0), to(0)
+    {
+        if (at.lane >= kMaxSources || !at.width) return;
+        const Source& source = s.source[at.lane];
+        if (!source.base) return;
+        from = source.base + source.begin(at.first);
+        stride = source.stride;
+        bytes = source.bytes_of(at.width);
+        to = shared_address(buffers) + source.at;
+    }
 
     // the team's first warp, a source per lane
-    __device__ __forceinline__ void fetch(uint32_t stage, uint32_t row) const
+    __device__ __forceinline__ void fetch(uint32_t stage, uint32_t r) const
     {
         const uint32_t bar = bars + 8 * stage;
-        uint32_t size = 0;
-        const char* from = nullptr;
-        if (at.lane < kMaxSources) {
-            const Source& source = s.source[at.lane];
-            if (source.base && at.width) {
-                from = source.base + (uint64_t)row * source.stride + source.begin(at.first);
-                const uint32_t skew = (uint32_t)(uintptr_t)from & 15u;
-                from -= skew;
-                size = (skew + source.bytes_of(at.width) + 15) & ~15u;
-            }
-        }
-        const uint32_t bytes = __reduce_add_sync(0xFFFFFFFFu, size);
-        if (at.lane == 0) barrier_expect(bar, bytes);
+        const char* const begin = from + r * stride;
+        const uint32_t skew = (uint32_t)(uintptr_t)begin & 15u, size = bytes ? (skew + bytes + 15) & ~15u : 0;
+        const uint32_t all = __reduce_add_sync(0xFFFFFFFFu, size);
+        if (at.lane == 0) barrier_expect(bar, all);
         __syncwarp();
         if (size)
             asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                         ::"r"(shared_address(buffers + stage * s.row_bytes) + s.source[at.lane].at), "l"(from), "r"(size), "r"(bar) : "memory");
+                         ::"r"(to + stage * s.row_bytes), "l"(begin - skew), "r"(size), "r"(bar) : "memory");
         __syncwarp();
     }
 
-    __device__ __forceinline__ const char* place(uint32_t stage, const Source& source) const { return buffers + stage * s.row_bytes + source.at; }
+    __device__ __forceinline__ void go_to(uint32_t stage) { row = buffers + stage * s.row_bytes; }
+    __device__ __forceinline__ const char* place(const Source& source) const { return row + source.at; }
 
     // The thread's values of 16 bits, zeros where there is no column.
     template <typename T, bool WIDE>
-    __device__ __forceinline__ void values(Values<K>& v, uint32_t stage, uint32_t row, const Source& source) const
+    __device__ __forceinline__ void values(Values<K>& v, uint32_t r, const Source& source) const
     {
-        const char* const begin = place(stage, source) + (at.col - at.first) * 2;
+        const char* const begin = place(source) + (at.col - at.first) * 2;
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             uint32_t w[4] = {0, 0, 0, 0};
@@ -284,7 +289,7 @@ struct Stages {
                 w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
             } else if (at.count[i] > 0) {
                 // words from the last one that starts at or before the values
-                const uint32_t skew = source.skew(row, at.first), shift = (skew & 2u) * 8;
+                const uint32_t skew = source.skew(r, at.first), shift = (skew & 2u) * 8;
                 const uint32_t* const word = (const uint32_t*)(from + (skew & ~3u));
                 uint32_t c[5];
 #pragma unroll
@@ -307,10 +312,10 @@ struct Stages {
 
     // The same from a checkpoint, times `factor`.
     template <bool WIDE>
-    __device__ __forceinline__ void coded(Values<K>& v, uint32_t stage, uint32_t row, const Source& codes, const Source& exps, float factor) const
+    __device__ __forceinline__ void coded(Values<K>& v, uint32_t r, const Source& codes, const Source& exps, float factor) const
     {
-        const char* const begin = place(stage, codes) + (at.col - at.first);
-        const uint8_t* const exp = (const uint8_t*)place(stage, exps) + exps.skew(row, at.first) + (at.col - at.first) / kGroup;
+        const char* const begin = place(codes) + (at.col - at.first);
+        const uint8_t* const exp = (const uint8_t*)place(exps) + exps.skew(r, at.first) + (at.col - at.first) / kGroup;
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             uint32_t a = 0, b = 0, e = 1;
@@ -321,7 +326,7 @@ struct Stages {
                 e = exp[256 / kGroup * i];
                 a = there ? q.x : 0u, b = there ? q.y : 0u, e = there ? e : 1u;
             } else if (at.count[i] > 0) {
-                const uint32_t skew = codes.skew(row, at.first), shift = (skew & 3u) * 8;
+                const uint32_t skew = codes.skew(r, at.first), shift = (skew & 3u) * 8;
                 const uint32_t* const word = (const uint32_t*)(from + (skew & ~3u));
                 const uint32_t c = word[1];
                 a = __funnelshift_r(word[0], c, shift);
@@ -344,7 +349,7 @@ struct Stages {
     {
         for (int i = 0; i < kMaxSources; ++i) {
             const Source& source = s.source[i];
-            if (!source.base || !source.columns) continue;
+            if (!source.base || source.fixed) continue;
             const uint32_t begin = (source.bytes_of(at.width) + 15) & ~15u, end = source.bytes_of(s.span);
             if (begin >= end) continue;
             for (uint32_t row = 0; row < s.teams * s.stages; ++row)
@@ -352,38 +357,42 @@ struct Stages {
         }
     }
 
-    // A vector over the columns is vector `which` of the block: ones where there is none.  The whole block.
+    // A vector over the columns is vector `which` of the block, in 32 bits; ones where there is none.
+    // The whole block.
     template <typename T>
     __device__ __forceinline__ void keep_vector(char* block, int which, const void* v) const
     {
-        const uint32_t one = pack<T>(1.f, 1.f);
         for (uint32_t c = threadIdx.x * 8; c < s.span; c += blockDim.x * 8) {
             const uint32_t col = at.first + c;
-            const int count = col < s.n ? (int)min(s.n - col, 8u) : 0;
-            *(uint4*)(block + s.vectors + (which * s.span + c) * 2) = v ? load_shifted_8((const T*)v + col, count) : make_uint4(one, one, one, one);
+            const uint4 q = load_shifted_8((const T*)v + col, v && col < s.n ? (int)min(s.n - col, 8u) : 0);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) unpack<T>(w[j], x[2 * j], x[2 * j + 1]);
+            // the halves of a thread's 8 apart: its lanes meet all banks once
+            float4* const to = (float4*)(block + s.vectors + (which * s.span + (c & ~255u)) * 4) + c % 256 / 8;
+            to[0] = v ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(1.f, 1.f, 1.f, 1.f);
+            to[32] = v ? make_float4(x[4], x[5], x[6], x[7]) : make_float4(1.f, 1.f, 1.f, 1.f);
         }
     }
 
-    template <typename T>
     __device__ __forceinline__ void vector(Values<K>& v, const char* block, int which) const
     {
+        const ulonglong2* const from = (const ulonglong2*)(block + s.vectors + (which * s.span + at.warp * 256 * K) * 4) + at.lane;
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-            const uint4 q = *(const uint4*)(block + s.vectors + (which * s.span + at.col - at.first + 256 * i) * 2);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (int i = 0; i < K; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float x, y;
-                unpack<T>(w[j], x, y);
-                v[i][j] = Pair(x, y);
+            for (int j = 0; j < 2; ++j) {
+                const ulonglong2 q = from[64 * i + 32 * j];
+                v[i][2 * j].bits = q.x;
+                v[i][2 * j + 1].bits = q.y;
             }
-        }
     }
 
     // A row's statistics.
-    __device__ __forceinline__ float2 pair(uint32_t stage, uint32_t row, const Source& source) const
+    __device__ __forceinline__ float2 pair(uint32_t r, const Source& source) const
     {
-        return *(const float2*)(place(stage, source) + source.skew(row, 0));
+        return *(const float2*)(place(source) + source.skew(r, 0));
     }
 
     // After a wait that ran out: the copies still on their way land before the block ends.
@@ -512,7 +521,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __gr
     __shared__ __align__(8) uint64_t bars[kMaxTeams * kMaxStages];
     extern __shared__ __align__(16) char rows_of_block[];
     const Place<K> at(s);
-    const Stages<K> stages(s, at, rows_of_block, shared_address(bars));
+    Stages<K> stages(s, at, rows_of_block, shared_address(bars));
     if constexpr (WIDE) stages.clear(rows_of_block);
     stages_init(shared_address(bars), s.teams);
     dependency_wait();
@@ -529,20 +538,21 @@ __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __gr
     if (FULL && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
     if (FULL && BEFORE && p.before.bias) stages.template keep_vector<T>(rows_of_block, kBeforeBiases, p.before.bias);
     __syncthreads();
-    auto vector = [&](Values<K>& v, int which) { stages.template vector<T>(v, rows_of_block, which); };
+    auto vector = [&](Values<K>& v, int which) { stages.vector(v, rows_of_block, which); };
     uint32_t turn = 0, stage = 0, phase = 0;
     bool ok = true;
     for (uint32_t row = first; row < s.m; row += step) {
         // a wait that ran out: the row is worked on all the same, so that every warp and every block of
         // the cluster meets at the same barriers; the status says that the results are not to be used
         ok = barrier_wait(stages.bars + 8 * stage, phase) && ok;
+        stages.go_to(stage);
         // everybody has done the row before this one: its stage is free
         auto refill = [&] {
             const uint64_t next = row + (uint64_t)step * (s.stages - 1);
             if (at.warp == 0 && row != first && next < s.m) stages.fetch(stage == 0 ? s.stages - 1 : stage - 1, (uint32_t)next);
         };
         Values<K> v, w;
-        stages.template values<T, WIDE>(v, stage, row, s.source[kSourceH]);
+        stages.template values<T, WIDE>(v, row, s.source[kSourceH]);
         if constexpr (AFTER) {
             const float2 st = row_statistics<FULL, K>(sums, turn, s, at, p.after, v);
             refill();
@@ -562,14 +572,14 @@ __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __gr
             for (int i = 0; i < K; ++i) drop_values(v[i], drop_numbers(p.drop, seed, row, at.col + 256 * i), p.drop.keep, p.drop.factor);
         }
         if (FULL && s.source[kSourceGate].base) {
-            stages.template values<T, WIDE>(w, stage, row, s.source[kSourceGate]);
+            stages.template values<T, WIDE>(w, row, s.source[kSourceGate]);
             each<K>([&](int i, int j) { v[i][j] = v[i][j] * w[i][j]; });
         } else if (p.gate) {
             vector(w, kGateVector);
             each<K>([&](int i, int j) { v[i][j] = v[i][j] * w[i][j]; });
         }
         if (s.source[kSourceResidual].base) {
-            stages.template values<T, WIDE>(w, stage, row, s.source[kSourceResidual]);
+            stages.template values<T, WIDE>(w, row, s.source[kSourceResidual]);
             each<K>([&](int i, int j) { v[i][j] = fma(w[i][j], Pair(p.scale), v[i][j]); });
         }
         if (p.x) store_row<T, WIDE, K>((T*)p.x + (uint64_t)row * p.x_stride + at.col, at, v, buffer);
@@ -631,7 +641,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
     __shared__ __align__(8) uint64_t bars[kMaxTeams * kMaxStages];
     extern __shared__ __align__(16) char rows_of_block[];
     const Place<K> at(s);
-    const Stages<K> stages(s, at, rows_of_block, shared_address(bars));
+    Stages<K> stages(s, at, rows_of_block, shared_address(bars));
     if constexpr (WIDE) stages.clear(rows_of_block);
     stages_init(shared_address(bars), s.teams);
     dependency_wait();
@@ -648,16 +658,16 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
     if (BEFORE) stages.template keep_vector<T>(rows_of_block, kBeforeWeights, p.before.weight);
     if (FULL && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
     __syncthreads();
-    auto vector = [&](Values<K>& v, int which) { stages.template vector<T>(v, rows_of_block, which); };
+    auto vector = [&](Values<K>& v, int which) { stages.vector(v, rows_of_block, which); };
     const bool matrix_gate = FULL && s.source[kSourceGateMatrix].base, gated = p.gate || matrix_gate;
     Values<K> total[kJoinSums];
 #pragma unroll
     for (int k = 0; k < kJoinSums; ++k) each<K>([&](int i, int j) { total[k][i][j] = Pair(0.f); });
     // the normalised row of an activation that was kept
-    auto unit = [&](Values<K>& v, int which, uint32_t stage, uint32_t row, float2 st) {
+    auto unit = [&](Values<K>& v, int which, uint32_t row, float2 st) {
         const bool coded = s.source[which + 1].base;
-        if (coded) stages.template coded<WIDE>(v, stage, row, s.source[which], s.source[which + 1], FULL ? 1.f : st.y);
-        else stages.template values<T, WIDE>(v, stage, row, s.source[which]);
+        if (coded) stages.template coded<WIDE>(v, row, s.source[which], s.source[which + 1], FULL ? 1.f : st.y);
+        else stages.template values<T, WIDE>(v, row, s.source[which]);
         if (FULL) {
 #pragma unroll
             for (int i = 0; i < K; ++i) {
@@ -674,15 +684,16 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
     bool ok = true;
     for (uint32_t row = first; row < s.m; row += step) {
         ok = barrier_wait(stages.bars + 8 * stage, phase) && ok;
+        stages.go_to(stage);
         auto refill = [&] {
             const uint64_t next = row + (uint64_t)step * (s.stages - 1);
             if (at.warp == 0 && row != first && next < s.m) stages.fetch(stage == 0 ? s.stages - 1 : stage - 1, (uint32_t)next);
         };
         Values<K> d, g, u;
         if constexpr (BEFORE) {
-            const float2 st = stages.pair(stage, row, s.source[kSourceBefore]);
-            stages.template values<T, WIDE>(g, stage, row, s.source[kSourceDy]);
-            unit(u, kSourceX, stage, row, st);
+            const float2 st = stages.pair(row, s.source[kSourceBefore]);
+            stages.template values<T, WIDE>(g, row, s.source[kSourceDy]);
+            unit(u, kSourceX, row, st);
             Pair a(0.f), b(0.f);
             vector(d, kBeforeWeights);
             each<K>([&](int i, int j) {
@@ -695,14 +706,14 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
             const float2 mean = row_sums<FULL, K>(sums, turn, s, at, a, b);
             refill();
             const Pair off(p.before.kind == EDEN_NORM_LAYER ? -mean.x * over_n : 0.f), inner(-mean.y * over_n), rate(st.y);
-            if (s.source[kSourceDx].base) stages.template values<T, WIDE>(d, stage, row, s.source[kSourceDx]);
+            if (s.source[kSourceDx].base) stages.template values<T, WIDE>(d, row, s.source[kSourceDx]);
             else each<K>([&](int i, int j) { d[i][j] = Pair(0.f); });
             each<K>([&](int i, int j) {
                 if (FULL) g[i][j] = g[i][j] + off;
                 d[i][j] = fma(fma(u[i][j], inner, g[i][j]), rate, d[i][j]);
             });
         } else {
-            stages.template values<T, WIDE>(d, stage, row, s.source[kSourceDx]);
+            stages.template values<T, WIDE>(d, row, s.source[kSourceDx]);
         }
         if (p.d_residual) {
             each<K>([&](int i, int j) { g[i][j] = d[i][j] * Pair(p.scale); });
@@ -716,8 +727,8 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
                 drop_values(d[i], numbers[i], p.drop.keep, p.drop.factor);
             }
         }
-        const float2 st = AFTER ? stages.pair(stage, row, s.source[kSourceAfter]) : make_float2(0.f, 1.f);
-        if (AFTER || gated) unit(u, kSourceKeptH, stage, row, st);
+        const float2 st = AFTER ? stages.pair(row, s.source[kSourceAfter]) : make_float2(0.f, 1.f);
+        if (AFTER || gated) unit(u, kSourceKeptH, row, st);
         if (gated) {
             if (AFTER) {
                 vector(g, kAfterWeights);
@@ -738,7 +749,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
             }
             if (matrix_gate) {
                 if (p.d_gate) store_row<T, WIDE, K>((T*)p.d_gate + (uint64_t)row * p.d_gate_stride + at.col, at, g, buffer);
-                stages.template values<T, WIDE>(g, stage, row, s.source[kSourceGateMatrix]);
+                stages.template values<T, WIDE>(g, row, s.source[kSourceGateMatrix]);
                 each<K>([&](int i, int j) { d[i][j] = d[i][j] * g[i][j]; });
             } else {
                 each<K>([&](int i, int j) { total[kGateSum][i][j] = total[kGateSum][i][j] + g[i][j]; });
