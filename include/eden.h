@@ -635,9 +635,10 @@ int eden_block_join_backward(eden_ctx* ctx, const eden_block_join_backward_args*
  *   - A matrix of `rows` rows of `features` values in this form (eden_mx4): codes, two a byte, the
  *     low half first, code = sign << 3 | place of the magnitude in the list, rows of
  *     eden_mx4_code_bytes(features) bytes, codes past the last value 0; exponents, the byte e + 127
- *     (255: NaN; 0 stands for 2^-127), in tiles of 128 rows x 256 values: group g of row r is byte
+ *     (1 to 254; 255: NaN, with codes 0), in tiles of 128 rows x 256 values: group g of row r is byte
  *         (r / 128 * ceil(features / 256) + g / 8) * 1024 + g / 4 % 2 * 512 + r % 32 * 16 + r / 32 % 4 * 4 + g % 4
- *     of eden_mx4_exponent_bytes(rows, features); no byte of a tile may be 255 but for a NaN group.
+ *     of eden_mx4_exponent_bytes(rows, features); no byte of a tile may be 255 but for a
+ *     NaN group.
  *     Codes start on 16 bytes, as do their rows (codes_stride, in bytes) and the exponents.
  *   - The sums run along the groups, so each product of a layer's training step reads its operands in
  *     another form, and eden_mx4_quantize writes one or both from one read of the matrix: `rows` has
@@ -645,8 +646,10 @@ int eden_block_join_backward(eden_ctx* ctx, const eden_block_join_backward_args*
  *       forward       y  = x W^T     x and W by rows
  *       input grad    dx = dz W      dz by rows, W by columns (weight_t [k, n])
  *       weight grad   dW = dz^T x    dz and x by columns (dz_t [n, m], x_t [k, m])
- *   - The products of two codes and their scales are exact, sums are held in fp32 as for the
- *     products above (codes and 32-bit results: in parts of 2048 added up, rounded to nearest). */
+ *   - The products of two codes and their scales are exact; sums are held in fp32.  Weight gradients
+ *     are added up in parts of 2048, rounded to nearest; within a part, and elsewhere, the tensor
+ *     cores cut off what the fp32 sum of 64 products more cannot hold, which shows only where the
+ *     sum's terms span more than 24 bits. */
 typedef struct eden_mx4 {
     uint8_t* codes;        uint64_t codes_stride;
     uint8_t* exps;

@@ -730,6 +730,66 @@ __device__ __forceinline__ void few_product(float (&c)[4], uint32_t a0, uint32_t
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// The block's sums, and (SHARED) those of the cluster's blocks, added up in their order, and what
+// follows them.  c[r][i]: a warp's sums of 16 rows of W from n0 + 16 * r and tokens from 8 * i.
+template <typename T, int NT, int R, bool SHARED>
+__device__ __forceinline__ void few_finish(const float (&c)[R][NT][4], const LinearEpilogue& p, uint64_t n0, uint32_t blocks, uint32_t part)
+{
+    constexpr int kWarps = kFewThreads / 32;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    // eight tokens at a time, [warp][token][row of W]; warp 0's place then takes the block's sums
+    __shared__ float sums[kWarps][8][16 * R + 1];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        if (8 * i >= p.rows) break;                        // alike in all blocks of a cluster
+        if (i > 0) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sums[warp][2 * t][16 * r + g] = c[r][i][0];
+            sums[warp][2 * t + 1][16 * r + g] = c[r][i][1];
+            sums[warp][2 * t][16 * r + g + 8] = c[r][i][2];
+            sums[warp][2 * t + 1][16 * r + g + 8] = c[r][i][3];
+        }
+        __syncthreads();
+        const bool mine = threadIdx.x < 128 * R;
+        const uint32_t in_tile = threadIdx.x / (16 * R), in = threadIdx.x % (16 * R), token = 8 * i + in_tile;
+        float v = 0.f;
+        if (mine) {
+#pragma unroll
+            for (int j = 0; j < kWarps; ++j) v += sums[j][in_tile][in];
+        }
+        if constexpr (SHARED) {
+            if (mine) sums[0][in_tile][in] = v;            // its own reader's value: no other thread's
+            cluster_arrive_wait();
+            if (mine && part == 0 && token < p.rows) {     // what is fetched is stored, and so waited for
+                for (uint32_t j = 1; j < blocks; ++j) v += cluster_load(address_in(shared_address(&sums[0][in_tile][in]), j));
+            }
+        }
+        if (mine && part == 0) {
+            const uint64_t col = n0 + in;
+            const bool live = token < p.rows && col < p.cols;
+            if (p.bias && live) v += to_float(((const T*)p.bias)[col]);
+            auto save = [&]() {                            // R = 2: the warp holds a token's group
+                const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, live ? magnitude_bits(v) : 0u));
+                if (!live) return;
+                p.ckpt.codes[token * p.ckpt.codes_stride + col] = (int8_t)group_code(v, group_inverse(e));
+                if (in == 0) p.ckpt.exps[token * p.ckpt.exps_stride + n0 / kGroup] = (uint8_t)e;
+            };
+            if (R == 2 && p.save == EDEN_SAVE_PRE) save();
+            with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
+            if (p.residual && live) v += to_float(((const T*)p.residual)[token * p.residual_stride + col]);
+            const T y = from_float<T>(v);
+            if (R == 2 && p.save == EDEN_SAVE_OUT) {
+                v = to_float(y);
+                save();
+            }
+            if (live) ((T*)p.out)[token * p.out_stride + col] = y;
+        }
+        // the sums were used (also where nothing was stored) before their blocks go on
+        if constexpr (SHARED) cluster_arrive_wait();
+    }
+}
+
 template <typename T, int NT, int R, bool VEC, bool SHARED>
 __global__ void __launch_bounds__(kFewThreads, NT <= 2 ? 2 : 1) k_linear_few(const T* x, uint64_t x_stride, const T* w, uint64_t w_stride, uint32_t k,
                                                            LinearEpilogue p)
@@ -785,57 +845,7 @@ __global__ void __launch_bounds__(kFewThreads, NT <= 2 ? 2 : 1) k_linear_few(con
                         few_product<T>(c[r][i], u.z, v.z, u.w, v.w, z.z, z.w);
                     }
     }
-    // eight tokens at a time, [warp][token][row of W]; warp 0's place then takes the block's sums
-    __shared__ float sums[kWarps][8][16 * R + 1];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        if (8 * i >= p.rows) break;                        // alike in all blocks of a cluster
-        if (i > 0) __syncthreads();
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            sums[warp][2 * t][16 * r + g] = c[r][i][0];
-            sums[warp][2 * t + 1][16 * r + g] = c[r][i][1];
-            sums[warp][2 * t][16 * r + g + 8] = c[r][i][2];
-            sums[warp][2 * t + 1][16 * r + g + 8] = c[r][i][3];
-        }
-        __syncthreads();
-        const bool mine = threadIdx.x < 128 * R;
-        const uint32_t in_tile = threadIdx.x / (16 * R), in = threadIdx.x % (16 * R), token = 8 * i + in_tile;
-        float v = 0.f;
-        if (mine) {
-#pragma unroll
-            for (int j = 0; j < kWarps; ++j) v += sums[j][in_tile][in];
-        }
-        if constexpr (SHARED) {
-            if (mine) sums[0][in_tile][in] = v;            // its own reader's value: no other thread's
-            cluster_arrive_wait();
-            if (mine && part == 0 && token < p.rows) {     // what is fetched is stored, and so waited for
-                for (uint32_t j = 1; j < blocks; ++j) v += cluster_load(address_in(shared_address(&sums[0][in_tile][in]), j));
-            }
-        }
-        if (mine && part == 0) {
-            const uint64_t col = n0 + in;
-            const bool live = token < p.rows && col < p.cols;
-            if (p.bias && live) v += to_float(((const T*)p.bias)[col]);
-            auto save = [&]() {                            // R = 2: the warp holds a token's group
-                const uint32_t e = group_exponent(__reduce_max_sync(0xFFFFFFFFu, live ? magnitude_bits(v) : 0u));
-                if (!live) return;
-                p.ckpt.codes[token * p.ckpt.codes_stride + col] = (int8_t)group_code(v, group_inverse(e));
-                if (in == 0) p.ckpt.exps[token * p.ckpt.exps_stride + n0 / kGroup] = (uint8_t)e;
-            };
-            if (R == 2 && p.save == EDEN_SAVE_PRE) save();
-            with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
-            if (p.residual && live) v += to_float(((const T*)p.residual)[token * p.residual_stride + col]);
-            const T y = from_float<T>(v);
-            if (R == 2 && p.save == EDEN_SAVE_OUT) {
-                v = to_float(y);
-                save();
-            }
-            if (live) ((T*)p.out)[token * p.out_stride + col] = y;
-        }
-        // the sums were used (also where nothing was stored) before their blocks go on
-        if constexpr (SHARED) cluster_arrive_wait();
-    }
+    few_finish<T, NT, R, SHARED>(c, p, n0, blocks, part);
 }
 
 // ---- operands -----------------------------------------------------------------------

@@ -163,32 +163,43 @@ __global__ void __launch_bounds__(kMx4Threads) k_mx4_quantize(const T* x, uint64
     }
 }
 
-// codes -> x [m][n]; four lanes to 128 values of a row
+// codes -> x [m][n]; four lanes to 128 values of a row.  Without WIDE a warp hands its 8 x 128 values
+// round in shared memory and stores each row's side by side.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kMx4Threads) k_mx4_restore(T* x, uint64_t x_stride, Mx4View q, uint32_t m, uint32_t n, uint32_t blocks_x)
 {
+    __shared__ T values[WIDE ? 1 : kMx4Threads / 32][8][128 + 8 / sizeof(T)];
     dependency_wait();
     dependency_release();
-    const uint32_t block_y = blockIdx.x / blocks_x, group = (blockIdx.x - block_y * blocks_x) * 4 + threadIdx.x % 4;
+    const uint32_t block_y = blockIdx.x / blocks_x, col0 = (blockIdx.x - block_y * blocks_x) * 128, group = col0 / 32 + threadIdx.x % 4;
     const uint32_t row = block_y * 64 + threadIdx.x / 4, col = group * 32;
-    if (row >= m || col >= n) return;
-    const int count = (int)min(n - col, 32u);
-    const uint4 w = *(const uint4*)(q.codes + (uint64_t)row * q.stride + group * 16);
-    const uint32_t e = q.exps[mx4_exponent_at(q.tiles, row, group)], words[4] = {w.x, w.y, w.z, w.w};
-    const float scale = e == 0u ? 5.877471754111438e-39f : group_scale(e);
-    T* const to = x + (uint64_t)row * x_stride + col;
+    const int count = row < m && col < n ? (int)min(n - col, 32u) : 0, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (count > 0) {
+        const uint4 w = *(const uint4*)(q.codes + (uint64_t)row * q.stride + group * 16);
+        const uint32_t e = q.exps[mx4_exponent_at(q.tiles, row, group)], words[4] = {w.x, w.y, w.z, w.w};
+        const float scale = group_scale(e);
+        T* const to = x + (uint64_t)row * x_stride + col;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        float v[16];
+        for (int h = 0; h < 2; ++h) {
+            float v[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = saturated<T>(mx4_value(words[2 * h + j / 8] >> 4 * (j % 8)) * scale);
-        if constexpr (WIDE) {
-            if (count >= 16 * h + 1) store_values(to + 16 * h, min(count - 16 * h, 16), v);
-        } else {
+            for (int j = 0; j < 16; ++j) v[j] = saturated<T>(mx4_value(words[2 * h + j / 8] >> 4 * (j % 8)) * scale);
+            if constexpr (WIDE) {
+                if (count >= 16 * h + 1) store_values(to + 16 * h, min(count - 16 * h, 16), v);
+            } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (16 * h + j < count) to[16 * h + j] = from_float<T>(v[j]);
+                for (int j = 0; j < 16; ++j) values[warp][lane / 4][32 * (lane % 4) + 16 * h + j] = from_float<T>(v[j]);
+            }
         }
+    }
+    if constexpr (!WIDE) {
+        __syncwarp();
+        const uint32_t row0 = block_y * 64 + warp * 8;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (row0 + r < m && col0 + 32 * j + lane < n) x[(uint64_t)(row0 + r) * x_stride + col0 + 32 * j + lane] = values[warp][r][32 * j + lane];
     }
 }
 
@@ -464,6 +475,163 @@ k_mx4_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if constexpr (CG == 2) cluster_arrive_wait(); else __syncthreads();
     tmem_fence_after();
     if (warp == 2) tmem_free<CG>(sums, S::kColumns);
+}
+
+// ---- few tokens ---------------------------------------------------------------------
+// y [m, n] for m <= 8: as k_linear_few, every weight is read once, straight to registers.  A lane
+// reads 8 codes of a group (its row's group lies with the four lanes of the row); their values are fed
+// as fp16 to two products of 16 x 8 x 16, in the same order of the sum's index for W and x.  The
+// products of a group are exact and added up in fp32 by themselves, then times both powers of two.
+//   FROM_MATRIX   x is a matrix of 16-bit values, which the block quantises into its shared memory
+//                 first, while its weights are on their way; else x is in 4 bits.
+// Instructions bound it: values by shifts and masks of fp16 numbers with an exponent 14 too low, with
+// the powers of two checked for 0 and NaN, took 9.1 us for 1 x 4096 x 4096.  16 tokens took 28 us, more than
+// the tiles' 16.
+__device__ __forceinline__ void mx4_halves(uint32_t w, uint32_t (&h)[4])
+{
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+
+// 2^e of byte `group`; infinity for 255, whose group's products are 0: their product is NaN
+__device__ __forceinline__ float mx4_scale(uint32_t word, int group)
+{
+    return __uint_as_float((group < 3 ? word << (23 - 8 * group) : word >> 1) & 0x7F800000u);
+}
+
+struct Mx4Few {
+    const void* x;         uint64_t x_stride;              // FROM_MATRIX
+    Mx4View held;                                          // else
+    Mx4View weight;
+    uint32_t k;
+};
+
+// a row of x's codes in shared memory is 16 bytes longer than it is: eight rows meet all banks once
+__host__ __device__ __forceinline__ uint32_t mx4_few_pitch(uint32_t k) { return (k + 127) / 128 * 64 + 16; }
+__host__ __device__ __forceinline__ uint32_t mx4_few_shared(uint32_t m, uint32_t k) { return m * (mx4_few_pitch(k) + (k + 127) / 128 * 4); }
+
+template <typename T, int R, bool FROM_MATRIX, bool SHARED>
+__global__ void __launch_bounds__(kFewThreads, R == 1 ? 2 : 1) k_mx4_few(Mx4Few q, LinearEpilogue p)
+{
+    constexpr int kWarps = kFewThreads / 32;
+    extern __shared__ __align__(16) uint8_t held[];
+    dependency_wait();
+    dependency_release();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    const uint64_t n0 = (uint64_t)blockIdx.x * (16 * R);
+    const uint32_t groups = (q.k + 31) / 32, steps = (q.k + 127) / 128, tokens = (uint32_t)p.rows;
+    uint32_t blocks = 1, part = 0, first_step = 0, last_step = steps;       // of the cluster: 2, 4 or 8
+    if constexpr (SHARED) {
+        blocks = gridDim.y;
+        part = blockIdx.y;
+        const uint32_t shift = 31 - __clz(blocks);
+        first_step = steps * part >> shift;
+        last_step = steps * (part + 1) >> shift;
+    }
+    const uint8_t *codes[2 * R], *exps[2 * R];             // past the end: any row, its sums are dropped
+#pragma unroll
+    for (int i = 0; i < 2 * R; ++i) {
+        const uint64_t row = min(n0 + g + 8 * i, p.cols - 1);
+        codes[i] = q.weight.codes + row * q.weight.stride + 4 * t;
+        exps[i] = q.weight.exps + mx4_exponent_at(q.weight.tiles, row, 0);
+    }
+    constexpr int kAhead = R == 1 ? 2 : 1;                 // steps of 128 on their way
+    uint32_t w[kAhead][2 * R][4], we[kAhead][2 * R];
+    auto fetch = [&](uint32_t step, int s) {
+        if (step >= last_step) return;
+#pragma unroll
+        for (int i = 0; i < 2 * R; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[s][i][j] = 4 * step + j < groups ? *(const uint32_t*)(codes[i] + 64 * step + 16 * j) : 0u;
+            we[s][i] = *(const uint32_t*)(exps[i] + step / 2 * kMx4TileBytes + step % 2 * 512);
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) fetch(first_step + warp + s * kWarps, s);
+    const uint32_t pitch = mx4_few_pitch(q.k);
+    if constexpr (FROM_MATRIX) {
+        uint8_t* const held_exps = held + tokens * pitch;
+        const uint32_t per_row = steps * 16, begin = first_step * 16, mine = last_step * 16 - begin;        // units of 8 values, four to a group
+        for (uint32_t u = threadIdx.x; u < (tokens * mine + 31) / 32 * 32; u += kFewThreads) {
+            const uint32_t token = u / mine, unit = begin + u - token * mine, col = unit * 8;
+            const bool live = token < tokens;
+            const uint4 raw = load_shifted_8((const T*)q.x + (live ? token * q.x_stride : 0) + col, live && col < q.k ? (int)min(q.k - col, 8u) : 0);
+            float v[8];
+            unpack<T>(raw.x, v[0], v[1]);
+            unpack<T>(raw.y, v[2], v[3]);
+            unpack<T>(raw.z, v[4], v[5]);
+            unpack<T>(raw.w, v[6], v[7]);
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) top = max_magnitude(top, v[j], v[j + 1]);
+            uint32_t most = magnitude_bits(top);
+            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+            const uint32_t e = mx4_exponent(most);
+            if (!live) continue;
+            *(uint32_t*)(held + token * pitch + unit * 4) = mx4_codes(v, group_inverse(e));
+            if (unit % 4 == 0) held_exps[token * (steps * 4) + unit / 4] = (uint8_t)e;
+        }
+        __syncthreads();
+    }
+    float c[R][1][4];
+#pragma unroll
+    for (int r = 0; r < R; ++r) c[r][0][0] = c[r][0][1] = c[r][0][2] = c[r][0][3] = 0.f;
+    // this lane's codes are token g's; its sums belong to tokens 2 t and 2 t + 1
+    const uint8_t *x_codes, *x_exps[2];
+    if constexpr (FROM_MATRIX) {
+        x_codes = held + min((uint32_t)g, tokens - 1) * pitch + 4 * t;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) x_exps[s] = held + tokens * pitch + min((uint32_t)(2 * t + s), tokens - 1) * (steps * 4);
+    } else {
+        x_codes = q.held.codes + min((uint32_t)g, tokens - 1) * q.held.stride + 4 * t;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) x_exps[s] = q.held.exps + mx4_exponent_at(q.held.tiles, min((uint32_t)(2 * t + s), tokens - 1), 0);
+    }
+    for (uint32_t step0 = first_step + warp; step0 < last_step; step0 += kWarps * kAhead) {
+#pragma unroll
+        for (int ahead = 0; ahead < kAhead; ++ahead) {
+            const uint32_t step = step0 + ahead * kWarps;
+            if (step >= last_step) break;
+            uint32_t a[2 * R][4], ae[2 * R], b[4], be[2];
+#pragma unroll
+            for (int i = 0; i < 2 * R; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) a[i][j] = w[ahead][i][j];
+                ae[i] = we[ahead][i];
+            }
+            fetch(step + kWarps * kAhead, ahead);
+            // tokens that do not exist multiply another one's codes: their sums are dropped
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = 4 * step + j < groups ? *(const uint32_t*)(x_codes + 64 * step + 16 * j) : 0u;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) be[s] = *(const uint32_t*)(x_exps[s] + (FROM_MATRIX ? 4 * step : step / 2 * kMx4TileBytes + step % 2 * 512));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t z[4];
+                mx4_halves(b[j], z);
+                const float sx[2] = {mx4_scale(be[0], j), mx4_scale(be[1], j)};
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    uint32_t u[4], v[4];
+                    mx4_halves(a[2 * r][j], u);
+                    mx4_halves(a[2 * r + 1][j], v);
+                    float d[4] = {0.f, 0.f, 0.f, 0.f};
+                    few_product<__half>(d, u[0], v[0], u[1], v[1], z[0], z[1]);
+                    few_product<__half>(d, u[2], v[2], u[3], v[3], z[2], z[3]);
+                    const float sw[2] = {mx4_scale(ae[2 * r], j), mx4_scale(ae[2 * r + 1], j)};
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) c[r][0][s] = fmaf(d[s] * sx[s % 2], sw[s / 2], c[r][0][s]);
+                }
+            }
+        }
+    }
+    few_finish<T, 1, R, SHARED>(c, p, n0, blocks, part);
 }
 
 }  // namespace eden

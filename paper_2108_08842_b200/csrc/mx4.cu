@@ -11,6 +11,8 @@ using namespace eden;
 
 namespace {
 
+constexpr uint32_t kFewShared = 64 * 1024;      // of a block that quantises x
+
 uint64_t tiles_along(uint64_t features) { return (features + kMx4TileDepth - 1) / kMx4TileDepth; }
 uint64_t tiles_across(uint64_t rows) { return (rows + kMx4TileRows - 1) / kMx4TileRows; }
 uint64_t exponent_bytes(uint64_t rows, uint64_t features) { return tiles_across(rows) * tiles_along(features) * kMx4TileBytes; }
@@ -109,6 +111,33 @@ int launch_mx4(eden_ctx* ctx, const Mx4Product& q)
                   (uint32_t*)ctx->ws);
 }
 
+// The cheapest form by a model of its time in microseconds, fitted to sums of 256 to 4096 on 16 to 8192
+// tiles: a launch's fixed part, and for each wave of tiles a step of 256 along the sum (and the gap
+// between two tiles' products) or the epilogue, whichever is longer.  8192 x 8192 results over 4096: 96 us
+// in pairs, 139 and 246 in the others; 128 x 4096 over 4096: 11.3, 9.1 and 7.8.
+template <int OP>
+int choose_form(const eden_ctx* ctx, const Mx4Product& q)
+{
+    const int form = ctx->linear_form;
+    if (form == EDEN_LINEAR_PAIR || form == EDEN_LINEAR_SINGLE || form == EDEN_LINEAR_NARROW) return form;
+    // epilogues: a store of 16 bits, an activation or a residual, a slope with its sums, a store of 32 bits
+    const int kind = OP == kWeightGrad ? 3 : OP == kInputGrad && (q.p.act || q.p.column_sums) ? 2 : q.p.act || q.p.residual || q.p.save ? 1 : 0;
+    static const struct { int form; uint64_t rows, cols, blocks; double fixed, gap, step, finish[4]; } forms[] = {
+        {EDEN_LINEAR_PAIR, 256, 256, 2, 4.5, 1.7, 0.32, {3.2, 4.0, 8.6, 3.8}},
+        {EDEN_LINEAR_SINGLE, 128, 128, 1, 3.8, 0.8, 0.26, {1.8, 2.9, 5.5, 1.7}},
+        {EDEN_LINEAR_NARROW, 128, 64, 1, 3.1, 0.45, 0.246, {0.8, 1.4, 2.9, 0.9}}};
+    const double steps = (double)tiles_along(q.a.features);
+    int best = EDEN_LINEAR_PAIR;
+    double least = 1e300;
+    for (const auto& f : forms) {
+        const uint64_t tiles = ((q.p.rows + f.rows - 1) / f.rows) * ((q.p.cols + f.cols - 1) / f.cols), slots = ctx->sm_count / f.blocks;
+        const double waves = (double)((tiles + slots - 1) / slots);
+        const double cost = f.fixed + f.finish[kind] - f.finish[0] + waves * std::max(f.gap + f.step * steps, f.finish[kind]);
+        if (cost < least) least = cost, best = f.form;
+    }
+    return best;
+}
+
 template <int OP, typename T>
 int product(eden_ctx* ctx, Mx4Product q)
 {
@@ -117,11 +146,39 @@ int product(eden_ctx* ctx, Mx4Product q)
     p.grain_residual = row_grain(p.residual, p.residual_stride, 2);
     p.grain_codes = row_grain(p.ckpt.codes, p.ckpt.codes_stride, 1);
     p.grain_bias = row_grain(p.bias, 0, 2);
-    const bool exact = OP == kWeightGrad || (OP == kInputGrad ? p.column_sums != nullptr : p.save != EDEN_SAVE_NONE);
-    const int form = ctx->linear_form;
-    if (form == EDEN_LINEAR_SINGLE) return exact ? launch_mx4<OP, T, 1, 128, true, 2>(ctx, q) : launch_mx4<OP, T, 1, 128, OP == kWeightGrad, 2>(ctx, q);
-    if (form == EDEN_LINEAR_NARROW) return exact ? launch_mx4<OP, T, 1, 64, true, 2>(ctx, q) : launch_mx4<OP, T, 1, 64, OP == kWeightGrad, 2>(ctx, q);
-    return exact ? launch_mx4<OP, T, 2, 256, true, 2>(ctx, q) : launch_mx4<OP, T, 2, 256, OP == kWeightGrad, 2>(ctx, q);
+    // Weight gradients, of 32 bits, are added up in runs.  Column sums are not: sums of 4-bit products are
+    // mostly exact in fp32 as they come (no error at all over 16384 normal or Laplace values), and the runs'
+    // registers cost an epilogue half its warps: 8192 x 4096 over 4096 with gelu's slope 76 us, 128 in runs.
+    constexpr bool runs = OP == kWeightGrad;
+    switch (choose_form<OP>(ctx, q)) {
+        case EDEN_LINEAR_SINGLE: return launch_mx4<OP, T, 1, 128, runs, 2>(ctx, q);
+        case EDEN_LINEAR_NARROW: return launch_mx4<OP, T, 1, 64, runs, 2>(ctx, q);
+        default: break;
+    }
+    // sixteen epilogue warps wherever it is more than a store
+    if constexpr (!runs) {
+        if (p.act || p.residual || p.save || p.column_sums) return launch_mx4<OP, T, 2, 256, false, 4>(ctx, q);
+    }
+    return launch_mx4<OP, T, 2, 256, runs, 2>(ctx, q);
+}
+
+// A block for each SM where there are fewer rows of W than that, as long as its warps have a step each.
+uint32_t few_parts(const eden_ctx* ctx, uint64_t blocks, uint64_t steps)
+{
+    uint32_t parts = 1;
+    while (parts < 8 && blocks * parts * 2 <= (uint64_t)ctx->sm_count && steps >= 16 * 2 * parts) parts *= 2;
+    return parts;
+}
+
+template <typename T, int R>
+int launch_few(eden_ctx* ctx, const Mx4Few& q, const LinearEpilogue& p, double bytes)
+{
+    const uint64_t blocks = (p.cols + 16 * R - 1) / (16 * R);
+    const uint32_t parts = few_parts(ctx, blocks, (q.k + 127) / 128), shared = q.x ? mx4_few_shared((uint32_t)p.rows, q.k) : 0;
+    const auto kernel = q.x ? (parts > 1 ? k_mx4_few<T, R, true, true> : k_mx4_few<T, R, true, false>)
+                            : (parts > 1 ? k_mx4_few<T, R, false, true> : k_mx4_few<T, R, false, false>);
+    if (shared > 32 * 1024) CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
+    return launch(ctx, "t_mx4_linear", bytes, kernel, dim3((uint32_t)blocks, parts), kFewThreads, shared, parts, q, p);
 }
 
 // A matrix of 16-bit values as an operand: quantised into the workspace.
@@ -186,14 +243,23 @@ extern "C" int eden_mx4_linear(eden_ctx* ctx, const eden_mx4_linear_args* a)
     if (a->save != EDEN_SAVE_NONE && !checkpoint_ok(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride, a->n)) return EDEN_ERR_INVALID_ARG;
     return guarded(ctx, [&]() -> int {
         Scratch scratch(ctx);
-        Mx4Operand x = operand_of(a->held, a->m, a->k);
-        if (a->x) {
-            if (int rc = quantized(ctx, scratch, a->type, a->x, a->x_stride, a->m, a->k, &x)) return rc;
-        }
         LinearEpilogue p{a->bias, a->residual, a->residual_stride, a->y, a->y_stride, view(a->saved, a->saved_stride, a->saved_exp, a->saved_exp_stride),
                          nullptr, a->m, a->n, a->act, a->save, 0};
         const double bytes = 17.0 * groups_of(a->k) * ((double)a->m + a->n) + 2.0 * (a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
                              (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
+        const bool few = a->m <= 8 && (ctx->linear_form == EDEN_LINEAR_AUTO || ctx->linear_form == EDEN_LINEAR_FEW);
+        // a few rows of x are quantised by the blocks that use them, as long as two of those share an SM
+        const bool fused = few && a->x && mx4_few_shared((uint32_t)a->m, (uint32_t)a->k) <= kFewShared;
+        Mx4Operand x = operand_of(a->held, a->m, a->k);
+        if (a->x && !fused) {
+            if (int rc = quantized(ctx, scratch, a->type, a->x, a->x_stride, a->m, a->k, &x)) return rc;
+        }
+        if (few) {
+            const Mx4Few q{fused ? a->x : nullptr, a->x_stride, {const_cast<uint8_t*>(x.codes), x.stride, const_cast<uint8_t*>(x.exps), tiles_along(a->k)},
+                           mx4_view(a->weight, a->k), (uint32_t)a->k};
+            // groups of 32 results are saved by a warp that holds them: two times 16 rows of W
+            EDEN_DISPATCH_HALF(a->type, return (a->save ? launch_few<T_, 2>(ctx, q, p, bytes) : launch_few<T_, 1>(ctx, q, p, bytes)));
+        }
         const Mx4Product q{"t_mx4_linear", a->type, x, operand_of(a->weight, a->n, a->k), p, bytes};
         EDEN_DISPATCH_HALF(a->type, return (product<kForward, T_>(ctx, q)));
     });
