@@ -740,3 +740,33 @@ def eden_linear_input_grad(ctx: Context, dz, weight, residual=None, pre=None, ac
 
 def eden_linear_weight_grad(ctx: Context, dz, x, out=None, accumulate=False):
     return ctx.linear_weight_grad(dz, x, out, accumulate)
+
+
+def eden_block_join(ctx: Context, h, residual=None, after=None, before=None, gate=None, scale=1.0, drop=0.0, seed=0, first_row=0, out=None,
+                    normed=None, stats=False):
+    return ctx.block_join(h, residual, after, before, gate, scale, drop, seed, first_row, out, normed, stats)
+
+
+def eden_block_join_backward(ctx: Context, dx, dy, h=None, x=None, after_stats=None, before_stats=None, **rest):
+    return ctx.block_join_backward(dx, dy, h, x, after_stats, before_stats, **rest)
+
+
+def eden_mx4_quantize(ctx: Context, x, rows=None, columns=False):
+    """rows, columns: an Mx4 to write, None (made) or False (left out)."""
+    return _binding.mx4_quantize(ctx._native, x, rows, columns)
+
+
+def eden_mx4_restore(ctx: Context, q, dtype, out=None):
+    return ctx.mx4_restore(q, dtype, out)
+
+
+def eden_mx4_linear(ctx: Context, x, weight, bias=None, act="none", residual=None, out=None, save="none", saved=None, dtype=None):
+    return ctx.mx4_linear(x, weight, bias, act, residual, out, save, saved, dtype)
+
+
+def eden_mx4_linear_input_grad(ctx: Context, dz, weight_t, residual=None, pre=None, act="none", out=None, bias_grad=None, accumulate=False, dtype=None):
+    return ctx.mx4_linear_input_grad(dz, weight_t, residual, pre, act, out, bias_grad, accumulate, dtype)
+
+
+def eden_mx4_linear_weight_grad(ctx: Context, dz_t, x_t, out=None, accumulate=False):
+    return ctx.mx4_linear_weight_grad(dz_t, x_t, out, accumulate)
