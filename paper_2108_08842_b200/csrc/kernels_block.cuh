@@ -179,58 +179,70 @@ __device__ __forceinline__ float2 row_sums(Exchange& e, uint32_t& turn, const Bl
 }
 
 // Mean and rate of a row.  "layer": each warp's mean and the sum of squares around it, put together
-// around the row's mean, so that no difference of large squares makes a small one.
+// around the row's mean, so that no difference of large squares makes a small one.  Sums that pass
+// fp32's largest number (bf16 values beyond 10^17) are made again of smaller values: all threads of a row
+// hold the same sum, and go round together.
 template <bool FULL, int K>
 __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, const BlockShape& s, const Place<K>& at, const NormView& norm, const Values<K>& v)
 {
     const float over_n = 1.f / (float)s.n;
-    if (!FULL || norm.kind == EDEN_NORM_RMS) {
-        Pair q(0.f);
+    constexpr float kSmaller = 8.271806125530277e-25f;     // 2^-80
+    float mean = 0.f, square = 0.f, scale = 1.f;
+#pragma unroll 1
+    for (;; scale = kSmaller) {
+        const Pair by(scale);
+        if (!FULL || norm.kind == EDEN_NORM_RMS) {
+            Pair q(0.f);
 #pragma unroll
-        for (int i = 0; i < K; ++i)
+            for (int i = 0; i < K; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q = fma(v[i][j], v[i][j], q);          // columns that do not exist hold 0
-        return make_float2(0.f, rsqrtf(fmaf(row_sums<false, K>(e, turn, s, at, q, q).y, over_n, norm.eps)));
+                for (int j = 0; j < 4; ++j) q = fma(v[i][j] * by, v[i][j] * by, q);          // columns that do not exist hold 0
+            square = row_sums<false, K>(e, turn, s, at, q, q).y * over_n;
+        } else {
+            Pair t(0.f);
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t = fma(v[i][j], by, t);
+            const float sum = warp_total(both(t)), own = columns_of<K>(s, at.rank * s.warps + at.warp), middle = own > 0.f ? sum / own : 0.f;
+            float q = 0.f;
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float x, y;
+                    fma(v[i][j], by, Pair(-middle)).get(x, y);
+                    if (2 * j < at.count[i]) q = fmaf(x, x, q);
+                    if (2 * j + 1 < at.count[i]) q = fmaf(y, y, q);
+                }
+            constexpr int kHeld = kBlockCluster * kTeamWarps / 32;
+            float2 held[kHeld];
+            float columns[kHeld], total = 0.f;
+            int got = 0;
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) columns[i] = 0.f;
+            exchange<K>(e, turn, s, at, make_float2(sum, warp_total(q)), [&](uint32_t i, float2 w) {
+                const float c = columns_of<K>(s, i);
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k)
+                    if (k == got) held[k] = w, columns[k] = c;
+                ++got;
+                total += w.x;
+            });
+            mean = lanes_total(s, total) * over_n;
+            q = 0.f;
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k)
+                if (columns[k] > 0.f) {
+                    const float off = held[k].x / columns[k] - mean;
+                    q += fmaf(columns[k] * off, off, held[k].y);
+                }
+            square = lanes_total(s, q) * over_n;
+        }
+        if (square < 3.0e38f || scale != 1.f) break;
     }
-    Pair t(0.f);
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) t = t + v[i][j];
-    const float sum = warp_total(both(t)), own = columns_of<K>(s, at.rank * s.warps + at.warp), middle = own > 0.f ? sum / own : 0.f;
-    float q = 0.f;
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float x, y;
-            (v[i][j] + Pair(-middle)).get(x, y);
-            if (2 * j < at.count[i]) q = fmaf(x, x, q);
-            if (2 * j + 1 < at.count[i]) q = fmaf(y, y, q);
-        }
-    constexpr int kHeld = kBlockCluster * kTeamWarps / 32;
-    float2 held[kHeld];
-    float columns[kHeld], total = 0.f;
-    int got = 0;
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) columns[i] = 0.f;
-    exchange<K>(e, turn, s, at, make_float2(sum, warp_total(q)), [&](uint32_t i, float2 w) {
-        const float c = columns_of<K>(s, i);
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k)
-            if (k == got) held[k] = w, columns[k] = c;
-        ++got;
-        total += w.x;
-    });
-    const float mean = lanes_total(s, total) * over_n;
-    q = 0.f;
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-        if (columns[k] > 0.f) {
-            const float off = held[k].x / columns[k] - mean;
-            q += fmaf(columns[k] * off, off, held[k].y);
-        }
-    return make_float2(mean, rsqrtf(fmaf(lanes_total(s, q), over_n, norm.eps)));
+    if (scale == 1.f) return make_float2(mean, rsqrtf(square + norm.eps));
+    return make_float2(mean / kSmaller, rsqrtf(square) * kSmaller);        // eps is nothing beside such squares
 }
 
 // ---- rows in shared memory ----------------------------------------------------------
