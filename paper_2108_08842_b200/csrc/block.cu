@@ -51,7 +51,7 @@ struct Grid {
 // What a block has beside its rows and vectors: places for sums, store buffers and barriers.
 constexpr uint32_t kRowsShared = (227 - 17) * 1024;
 
-Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)[kMaxSources], uint32_t warps, bool full)
+Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)[kMaxSources], uint32_t warps, bool full, uint32_t sums)
 {
     Grid g{};
     BlockShape& s = g.s;
@@ -59,7 +59,8 @@ Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)
     s.n = (uint32_t)n;
     const uint64_t sms = std::min<uint64_t>(ctx->sm_count, kMaxSlots);
     // Two pieces a thread where that leaves a row for every SM, or where one would need a cluster.
-    g.pieces = n > 256 * kTeamWarps || (n > 256 && m >= sms) ? 2 : 1;
+    // (gradients with everything do not fit the registers with two: 200 to 600 bytes of spills)
+    g.pieces = n > 256 * kTeamWarps || (n > 256 && m >= sms && !(full && sums)) ? 2 : 1;
     const uint64_t columns = 256ull * kTeamWarps * g.pieces;
     uint32_t vectors = 0;
     for (s.blocks = 1;; s.blocks *= 2) {
@@ -88,8 +89,8 @@ Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)
     const uint64_t groups = std::min<uint64_t>((m + s.teams - 1) / s.teams, std::max<uint64_t>(1, sms / s.blocks));
     g.blocks = (uint32_t)groups * s.blocks;
     g.threads = s.teams * s.warps * 32;
-    g.shared = s.vectors + vectors;
-    g.parts = (uint32_t)groups * s.teams;
+    g.shared = std::max(s.vectors + vectors, s.teams * sums * s.span * 4);     // the teams' sums, at most 160 KB
+    g.parts = (uint32_t)groups;
     return g;
 }
 
@@ -181,7 +182,7 @@ extern "C" int eden_block_join(eden_ctx* ctx, const eden_block_join_args* a)
         if (a->residual) source[kSourceResidual] = matrix_source(a->residual, a->residual_stride);
         if (per_value) source[kSourceGate] = matrix_source(a->gate, per_value);
         const bool f = full(a->after) || full(a->before) || per_value;
-        const Grid g = grid_of(ctx, a->m, a->n, source, kJoinThreads / 32, f);
+        const Grid g = grid_of(ctx, a->m, a->n, source, kJoinThreads / 32, f, 0);
         EDEN_DISPATCH_HALF(a->type, EDEN_DISPATCH_NORMS(after, before, return (join<T_, AFTER_, BEFORE_>(ctx, p, g, f, bytes))));
     });
 }
@@ -258,7 +259,7 @@ extern "C" int eden_block_join_backward(eden_ctx* ctx, const eden_block_join_bac
                 if (after) source[kSourceAfter] = stats_source(a->after_stats);
                 if (per_value) source[kSourceGateMatrix] = matrix_source(a->gate, per_value);
                 const bool f = full(a->after) || full(a->before) || per_value || (wanted & (1u << kBeforeBias | 1u << kAfterBias));
-                const Grid g = grid_of(ctx, a->m, a->n, source, kJoinBackwardThreads / 32, f);
+                const Grid g = grid_of(ctx, a->m, a->n, source, kJoinBackwardThreads / 32, f, kJoinSums);
                 JoinBackwardView p{per_value ? nullptr : a->gate, a->d_residual, a->d_residual_stride, a->dh, a->dh_stride, a->d_gate, a->d_gate_stride,
                                    partial(g.parts), wanted, {a->after.weight, a->after.bias, nullptr, a->after.eps, a->after.kind},
                                    {a->before.weight, a->before.bias, nullptr, a->before.eps, a->before.kind}, drop, a->scale, has_drop};

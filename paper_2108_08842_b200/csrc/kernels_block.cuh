@@ -643,8 +643,8 @@ struct JoinBackwardView {
     int has_drop;
 };
 
-// Each team keeps the sums of its rows over the columns in registers and leaves them in its part of
-// `partial`, which k_join_sums adds up.
+// Each team keeps the sums of its rows over the columns in registers; a block leaves them in its part
+// of `partial`, which k_join_sums adds up.
 template <typename T, bool AFTER, bool BEFORE, bool FULL, bool WIDE, int K>
 __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinBackwardView p, const __grid_constant__ BlockShape s, uint32_t* status)
 {
@@ -795,8 +795,15 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
         __syncwarp();
         if (++stage == s.stages) stage = 0, phase ^= 1;
     }
+    if (!ok) {
+        stages.drain(first, step);
+        if (at.lane == 0) atomicOr(status, EDEN_STATUS_TIMEOUT);
+    }
     if (p.wanted) {
-        float* to = p.partial + (uint64_t)(group * s.teams + at.team) * __popc(p.wanted) * s.n + at.col;
+        // the teams' sums meet in the rows' place, and are added up in the teams' order
+        const uint32_t sums_wanted = __popc(p.wanted);
+        __syncthreads();
+        float* to = (float*)rows_of_block + at.team * sums_wanted * s.span + at.col - at.first;
 #pragma unroll
         for (int k = 0; k < kJoinSums; ++k) {
             if (!(p.wanted >> k & 1)) continue;
@@ -805,20 +812,20 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) total[k][i][j].get(x[2 * j], x[2 * j + 1]);
-                if (WIDE) {
-                    if (at.count[i] > 0) *(float4*)(to + 256 * i) = make_float4(x[0], x[1], x[2], x[3]), *(float4*)(to + 256 * i + 4) = make_float4(x[4], x[5], x[6], x[7]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < at.count[i]) to[256 * i + j] = x[j];
-                }
+                *(float4*)(to + 256 * i) = make_float4(x[0], x[1], x[2], x[3]);
+                *(float4*)(to + 256 * i + 4) = make_float4(x[4], x[5], x[6], x[7]);
             }
-            to += s.n;
+            to += s.span;
         }
-    }
-    if (!ok) {
-        stages.drain(first, step);
-        if (at.lane == 0) atomicOr(status, EDEN_STATUS_TIMEOUT);
+        __syncthreads();
+        float* const part = p.partial + (uint64_t)group * sums_wanted * s.n + at.first;
+        const float* const held = (const float*)rows_of_block;
+        for (uint32_t k = 0; k < sums_wanted; ++k)
+            for (uint32_t c = threadIdx.x; c < at.width; c += blockDim.x) {
+                float sum = 0.f;
+                for (uint32_t team = 0; team < s.teams; ++team) sum += held[(team * sums_wanted + k) * s.span + c];
+                part[(uint64_t)k * s.n + c] = sum;
+            }
     }
     if (s.blocks > 1) cluster_arrive_wait();
 }

@@ -89,7 +89,7 @@ template <typename T> constexpr uint32_t kMx4Pitch = 128 * sizeof(T) / 4 + 1;
 template <typename T, bool COLUMNS> constexpr uint32_t kMx4Shared = COLUMNS ? 128 * kMx4Pitch<T> * 4 + 128 * 64 : 0;
 
 template <typename T, bool WIDE, bool COLUMNS>
-__global__ void __launch_bounds__(kMx4Threads) k_mx4_quantize(const T* x, uint64_t x_stride, Mx4View rows, Mx4View columns, uint32_t m, uint32_t n,
+__global__ void __launch_bounds__(kMx4Threads, sizeof(T) == 2 ? 4 : 2) k_mx4_quantize(const T* x, uint64_t x_stride, Mx4View rows, Mx4View columns, uint32_t m, uint32_t n,
                                                              uint32_t blocks_x)
 {
     __shared__ __align__(16) uint8_t exps[2][512];
@@ -97,24 +97,29 @@ __global__ void __launch_bounds__(kMx4Threads) k_mx4_quantize(const T* x, uint64
     dependency_wait();
     dependency_release();
     const uint32_t block_y = blockIdx.x / blocks_x, block_x = blockIdx.x - block_y * blocks_x, row0 = block_y * 128, col0 = block_x * 128;
+    const uint32_t g = threadIdx.x % 4, col = col0 + 32 * g;
+    auto count_of = [&](uint32_t row) { return row < m && col < n ? (int)min(n - col, 32u) : 0; };
+    uint32_t raw[2][8 * sizeof(T)];                        // both groups on their way together
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const uint32_t r = i * 64 + threadIdx.x / 4, g = threadIdx.x % 4, row = row0 + r, col = col0 + 32 * g;
-        const int count = row < m && col < n ? (int)min(n - col, 32u) : 0;
-        uint32_t raw[8 * sizeof(T)];
-        load_group<WIDE>(x + (count ? (uint64_t)row * x_stride + col : 0), count, raw);
+        const uint32_t row = row0 + i * 64 + threadIdx.x / 4;
+        load_group<WIDE>(x + (count_of(row) ? (uint64_t)row * x_stride + col : 0), count_of(row), raw[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t r = i * 64 + threadIdx.x / 4, row = row0 + r;
         if constexpr (COLUMNS) {
 #pragma unroll
-            for (int j = 0; j < 8 * (int)sizeof(T); ++j) tile[r * kMx4Pitch<T> + g * 8 * sizeof(T) + j] = raw[j];
+            for (int j = 0; j < 8 * (int)sizeof(T); ++j) tile[r * kMx4Pitch<T> + g * 8 * sizeof(T) + j] = raw[i][j];
         }
         if (rows.codes) {
             float v[32];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) widen<T>(*(uint32_t(*)[4 * sizeof(T)])(raw + h * 4 * sizeof(T)), *(float(*)[16])(v + 16 * h));
+            for (int h = 0; h < 2; ++h) widen<T>(*(uint32_t(*)[4 * sizeof(T)])(raw[i] + h * 4 * sizeof(T)), *(float(*)[16])(v + 16 * h));
             const uint32_t e = mx4_exponent(largest_bits(v));
             const float inverse = group_inverse(e);
             exps[0][r % 32 * 16 + r / 32 * 4 + g] = (uint8_t)e;
-            if (count)
+            if (count_of(row))
                 *(uint4*)(rows.codes + (uint64_t)row * rows.stride + col / 2) =
                     make_uint4(mx4_codes(v, inverse), mx4_codes(v + 8, inverse), mx4_codes(v + 16, inverse), mx4_codes(v + 24, inverse));
         }
