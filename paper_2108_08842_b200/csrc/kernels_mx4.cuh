@@ -551,67 +551,106 @@ __global__ void __launch_bounds__(kFewThreads, R == 1 ? 2 : 1) k_mx4_few(Mx4Few 
         first_step = steps * part >> shift;
         last_step = steps * (part + 1) >> shift;
     }
-    const uint8_t *codes[2 * R], *exps[2 * R];             // past the end: any row, its sums are dropped
+    // A warp's steps are kWarps apart, an even number: the bytes from one to the next are the same for all.
+    constexpr uint32_t kCodesOn = 64 * kWarps, kExpsOn = kMx4TileBytes * kWarps / 2;
+    const uint32_t mine = first_step + warp;
+    const uint8_t *codes[2 * R], *exps[2 * R];             // of the next step to fetch; past the end: any row, its sums are dropped
 #pragma unroll
     for (int i = 0; i < 2 * R; ++i) {
         const uint64_t row = min(n0 + g + 8 * i, p.cols - 1);
-        codes[i] = q.weight.codes + row * q.weight.stride + 4 * t;
-        exps[i] = q.weight.exps + mx4_exponent_at(q.weight.tiles, row, 0);
+        codes[i] = q.weight.codes + row * q.weight.stride + 64 * mine + 4 * t;
+        exps[i] = q.weight.exps + mx4_exponent_at(q.weight.tiles, row, 4 * mine);
     }
-    constexpr int kAhead = R == 1 ? 2 : 1;                 // steps of 128 on their way
+    // four words of a row, of which the last step may have fewer
+    auto load_words = [&](uint32_t (&to)[4], const uint8_t* from, uint32_t step) {
+        if (4 * step + 4 <= groups) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[j] = *(const uint32_t*)(from + 16 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[j] = 4 * step + j < groups ? *(const uint32_t*)(from + 16 * j) : 0u;
+        }
+    };
+    constexpr int kAhead = 1;                              // steps of 128 on their way: with two, registers spill (8 us for 6.5)
     uint32_t w[kAhead][2 * R][4], we[kAhead][2 * R];
     auto fetch = [&](uint32_t step, int s) {
         if (step >= last_step) return;
 #pragma unroll
         for (int i = 0; i < 2 * R; ++i) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[s][i][j] = 4 * step + j < groups ? *(const uint32_t*)(codes[i] + 64 * step + 16 * j) : 0u;
-            we[s][i] = *(const uint32_t*)(exps[i] + step / 2 * kMx4TileBytes + step % 2 * 512);
+            load_words(w[s][i], codes[i], step);
+            we[s][i] = *(const uint32_t*)exps[i];
+            codes[i] += kCodesOn;
+            exps[i] += kExpsOn;
         }
     };
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s) fetch(first_step + warp + s * kWarps, s);
+    for (int s = 0; s < kAhead; ++s) fetch(mine + s * kWarps, s);
+    // what the end reads comes nearer meanwhile
+    if (threadIdx.x < tokens) {
+        if (p.residual) asm volatile("prefetch.global.L2 [%0];" ::"l"((const T*)p.residual + threadIdx.x * p.residual_stride + n0));
+        if (p.bias) asm volatile("prefetch.global.L2 [%0];" ::"l"((const T*)p.bias + n0));
+    }
     const uint32_t pitch = mx4_few_pitch(q.k);
     if constexpr (FROM_MATRIX) {
         uint8_t* const held_exps = held + tokens * pitch;
-        const uint32_t per_row = steps * 16, begin = first_step * 16, mine = last_step * 16 - begin;        // units of 8 values, four to a group
-        for (uint32_t u = threadIdx.x; u < (tokens * mine + 31) / 32 * 32; u += kFewThreads) {
-            const uint32_t token = u / mine, unit = begin + u - token * mine, col = unit * 8;
-            const bool live = token < tokens;
-            const uint4 raw = load_shifted_8((const T*)q.x + (live ? token * q.x_stride : 0) + col, live && col < q.k ? (int)min(q.k - col, 8u) : 0);
-            float v[8];
-            unpack<T>(raw.x, v[0], v[1]);
-            unpack<T>(raw.y, v[2], v[3]);
-            unpack<T>(raw.z, v[4], v[5]);
-            unpack<T>(raw.w, v[6], v[7]);
-            float top = 0.f;
+        const uint32_t begin = first_step * 16, per_row = last_step * 16 - begin;        // units of 8 values, four to a group
+        const uint32_t units = tokens * per_row;
+        for (uint32_t u0 = threadIdx.x; u0 < (units + 31) / 32 * 32; u0 += 4 * kFewThreads) {
+            uint4 raw[4];                                  // on their way together
+            auto place = [&](int i, uint32_t& token, uint32_t& unit) {
+                const uint32_t u = u0 + i * kFewThreads;
+                token = u / per_row;
+                unit = begin + u - token * per_row;
+                return u < units;
+            };
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) top = max_magnitude(top, v[j], v[j + 1]);
-            uint32_t most = magnitude_bits(top);
-            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-            const uint32_t e = mx4_exponent(most);
-            if (!live) continue;
-            *(uint32_t*)(held + token * pitch + unit * 4) = mx4_codes(v, group_inverse(e));
-            if (unit % 4 == 0) held_exps[token * (steps * 4) + unit / 4] = (uint8_t)e;
+            for (int i = 0; i < 4; ++i) {
+                if (u0 - lane + i * kFewThreads >= units) break;                  // all lanes together
+                uint32_t token, unit;
+                const bool live = place(i, token, unit);
+                const int count = live && unit * 8 < q.k ? (int)min(q.k - unit * 8, 8u) : 0;
+                raw[i] = load_shifted_8((const T*)q.x + (count ? token * q.x_stride + unit * 8 : 0), count);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (u0 - lane + i * kFewThreads >= units) break;
+                uint32_t token, unit;
+                const bool live = place(i, token, unit);
+                float v[8];
+                unpack<T>(raw[i].x, v[0], v[1]);
+                unpack<T>(raw[i].y, v[2], v[3]);
+                unpack<T>(raw[i].z, v[4], v[5]);
+                unpack<T>(raw[i].w, v[6], v[7]);
+                float top = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) top = max_magnitude(top, v[j], v[j + 1]);
+                uint32_t most = magnitude_bits(top);
+                most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+                most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+                const uint32_t e = mx4_exponent(most);
+                if (!live) continue;
+                *(uint32_t*)(held + token * pitch + unit * 4) = mx4_codes(v, group_inverse(e));
+                if (unit % 4 == 0) held_exps[token * (steps * 4) + unit / 4] = (uint8_t)e;
+            }
         }
         __syncthreads();
     }
     float c[R][1][4];
 #pragma unroll
     for (int r = 0; r < R; ++r) c[r][0][0] = c[r][0][1] = c[r][0][2] = c[r][0][3] = 0.f;
-    // this lane's codes are token g's; its sums belong to tokens 2 t and 2 t + 1
+    // This lane's codes are token g's; its sums belong to tokens 2 t and 2 t + 1.  Tokens that do not
+    // exist multiply another one's codes: their sums are dropped.
     const uint8_t *x_codes, *x_exps[2];
     if constexpr (FROM_MATRIX) {
-        x_codes = held + min((uint32_t)g, tokens - 1) * pitch + 4 * t;
+        x_codes = held + min((uint32_t)g, tokens - 1) * pitch + 64 * mine + 4 * t;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) x_exps[s] = held + tokens * pitch + min((uint32_t)(2 * t + s), tokens - 1) * (steps * 4);
+        for (int s = 0; s < 2; ++s) x_exps[s] = held + tokens * pitch + min((uint32_t)(2 * t + s), tokens - 1) * (steps * 4) + 4 * mine;
     } else {
-        x_codes = q.held.codes + min((uint32_t)g, tokens - 1) * q.held.stride + 4 * t;
+        x_codes = q.held.codes + min((uint32_t)g, tokens - 1) * q.held.stride + 64 * mine + 4 * t;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) x_exps[s] = q.held.exps + mx4_exponent_at(q.held.tiles, min((uint32_t)(2 * t + s), tokens - 1), 0);
+        for (int s = 0; s < 2; ++s) x_exps[s] = q.held.exps + mx4_exponent_at(q.held.tiles, min((uint32_t)(2 * t + s), tokens - 1), 4 * mine);
     }
-    for (uint32_t step0 = first_step + warp; step0 < last_step; step0 += kWarps * kAhead) {
+    for (uint32_t step0 = mine; step0 < last_step; step0 += kWarps * kAhead) {
 #pragma unroll
         for (int ahead = 0; ahead < kAhead; ++ahead) {
             const uint32_t step = step0 + ahead * kWarps;
@@ -624,11 +663,18 @@ __global__ void __launch_bounds__(kFewThreads, R == 1 ? 2 : 1) k_mx4_few(Mx4Few 
                 ae[i] = we[ahead][i];
             }
             fetch(step + kWarps * kAhead, ahead);
-            // tokens that do not exist multiply another one's codes: their sums are dropped
+            if constexpr (FROM_MATRIX) {                   // zeros behind the last value
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = 4 * step + j < groups ? *(const uint32_t*)(x_codes + 64 * step + 16 * j) : 0u;
+                for (int j = 0; j < 4; ++j) b[j] = *(const uint32_t*)(x_codes + 16 * j);
+            } else {
+                load_words(b, x_codes, step);
+            }
+            x_codes += kCodesOn;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) be[s] = *(const uint32_t*)(x_exps[s] + (FROM_MATRIX ? 4 * step : step / 2 * kMx4TileBytes + step % 2 * 512));
+            for (int s = 0; s < 2; ++s) {
+                be[s] = *(const uint32_t*)x_exps[s];
+                x_exps[s] += FROM_MATRIX ? 4 * kWarps : kExpsOn;
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t z[4];

@@ -11,7 +11,7 @@ using namespace eden;
 
 namespace {
 
-constexpr uint32_t kFewShared = 64 * 1024;      // of a block that quantises x
+constexpr uint64_t kFewFused = 16384;           // values of x that every block of a product with few tokens quantises
 
 uint64_t tiles_along(uint64_t features) { return (features + kMx4TileDepth - 1) / kMx4TileDepth; }
 uint64_t tiles_across(uint64_t rows) { return (rows + kMx4TileRows - 1) / kMx4TileRows; }
@@ -177,7 +177,6 @@ int launch_few(eden_ctx* ctx, const Mx4Few& q, const LinearEpilogue& p, double b
     const uint32_t parts = few_parts(ctx, blocks, (q.k + 127) / 128), shared = q.x ? mx4_few_shared((uint32_t)p.rows, q.k) : 0;
     const auto kernel = q.x ? (parts > 1 ? k_mx4_few<T, R, true, true> : k_mx4_few<T, R, true, false>)
                             : (parts > 1 ? k_mx4_few<T, R, false, true> : k_mx4_few<T, R, false, false>);
-    if (shared > 32 * 1024) CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
     return launch(ctx, "t_mx4_linear", bytes, kernel, dim3((uint32_t)blocks, parts), kFewThreads, shared, parts, q, p);
 }
 
@@ -248,8 +247,9 @@ extern "C" int eden_mx4_linear(eden_ctx* ctx, const eden_mx4_linear_args* a)
         const double bytes = 17.0 * groups_of(a->k) * ((double)a->m + a->n) + 2.0 * (a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
                              (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
         const bool few = a->m <= 8 && (ctx->linear_form == EDEN_LINEAR_AUTO || ctx->linear_form == EDEN_LINEAR_FEW);
-        // a few rows of x are quantised by the blocks that use them, as long as two of those share an SM
-        const bool fused = few && a->x && mx4_few_shared((uint32_t)a->m, (uint32_t)a->k) <= kFewShared;
+        // A token's values are quantised by the blocks that use them (1 x 4096 x 4096 in 6.5 us, as a launch of
+        // its own 9.5); of many, each block would do too much (8 tokens: 12.7 us, and 10).
+        const bool fused = few && a->x && a->m * a->k <= kFewFused;
         Mx4Operand x = operand_of(a->held, a->m, a->k);
         if (a->x && !fused) {
             if (int rc = quantized(ctx, scratch, a->type, a->x, a->x_stride, a->m, a->k, &x)) return rc;
