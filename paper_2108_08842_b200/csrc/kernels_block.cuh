@@ -181,29 +181,29 @@ __device__ __forceinline__ float2 row_sums(Exchange& e, uint32_t& turn, const Bl
 // Mean and rate of a row.  "layer": each warp's mean and the sum of squares around it, put together
 // around the row's mean, so that no difference of large squares makes a small one.  Sums that pass
 // fp32's largest number (bf16 values beyond 10^17) are made again of smaller values: all threads of a row
-// hold the same sum, and go round together.
+// hold the same sum, and take the second way together.
 template <bool FULL, int K>
 __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, const BlockShape& s, const Place<K>& at, const NormView& norm, const Values<K>& v)
 {
     const float over_n = 1.f / (float)s.n;
     constexpr float kSmaller = 8.271806125530277e-25f;     // 2^-80
-    float mean = 0.f, square = 0.f, scale = 1.f;
-#pragma unroll 1
-    for (;; scale = kSmaller) {
-        const Pair by(scale);
+    float mean = 0.f, square = 0.f;
+    auto sums = [&](auto scaled) {
+        const Pair by(decltype(scaled)::value ? kSmaller : 1.f);
+        auto times = [&](Pair a) { return decltype(scaled)::value ? a * by : a; };
         if (!FULL || norm.kind == EDEN_NORM_RMS) {
             Pair q(0.f);
 #pragma unroll
             for (int i = 0; i < K; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) q = fma(v[i][j] * by, v[i][j] * by, q);          // columns that do not exist hold 0
+                for (int j = 0; j < 4; ++j) q = fma(times(v[i][j]), times(v[i][j]), q);      // columns that do not exist hold 0
             square = row_sums<false, K>(e, turn, s, at, q, q).y * over_n;
         } else {
             Pair t(0.f);
 #pragma unroll
             for (int i = 0; i < K; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) t = fma(v[i][j], by, t);
+                for (int j = 0; j < 4; ++j) t = t + times(v[i][j]);
             const float sum = warp_total(both(t)), own = columns_of<K>(s, at.rank * s.warps + at.warp), middle = own > 0.f ? sum / own : 0.f;
             float q = 0.f;
 #pragma unroll
@@ -211,7 +211,7 @@ __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, co
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float x, y;
-                    fma(v[i][j], by, Pair(-middle)).get(x, y);
+                    (times(v[i][j]) + Pair(-middle)).get(x, y);
                     if (2 * j < at.count[i]) q = fmaf(x, x, q);
                     if (2 * j + 1 < at.count[i]) q = fmaf(y, y, q);
                 }
@@ -239,9 +239,10 @@ __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, co
                 }
             square = lanes_total(s, q) * over_n;
         }
-        if (square < 3.0e38f || scale != 1.f) break;
-    }
-    if (scale == 1.f) return make_float2(mean, rsqrtf(square + norm.eps));
+    };
+    sums(std::false_type());
+    if (square < 3.0e38f) return make_float2(mean, rsqrtf(square + norm.eps));
+    sums(std::true_type());
     return make_float2(mean / kSmaller, rsqrtf(square) * kSmaller);        // eps is nothing beside such squares
 }
 
