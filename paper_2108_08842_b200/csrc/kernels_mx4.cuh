@@ -52,11 +52,16 @@ __device__ __forceinline__ uint32_t mx4_codes(const float* v, float inverse)
     return inverse == 0.f ? 0u : w;
 }
 
-// The value of a code: its three bits of magnitude are the top of an fp32 number whose exponent is
-// 126 too low (0.5 is its largest subnormal step), so one product by 2^126 makes the value.
-__device__ __forceinline__ float mx4_value(uint32_t code)
+// fp16 values of eight codes, exact: h[j] holds 2 j and 2 j + 1
+__device__ __forceinline__ void mx4_halves(uint32_t w, uint32_t (&h)[4])
 {
-    return __uint_as_float((code & 8u) << 28 | (code & 7u) << 22) * 8.507059173023462e37f;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
 
 __device__ __forceinline__ uint32_t largest_bits(const float (&v)[32])
@@ -74,6 +79,9 @@ __device__ __forceinline__ void load_group(const T* p, int count, uint32_t (&w)[
     if (WIDE && count == 32) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T); ++i) load_32b((const char*)p + 32 * i, *(uint32_t(*)[8])(w + 8 * i));
+    } else if (count == 32 && ((uintptr_t)p & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) *(uint4*)(w + 4 * i) = ((const uint4*)p)[i];
     } else {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T); ++i) load_shifted((const char*)p + 32 * i, min(max(count * (int)sizeof(T) - 32 * i, 0), 32), *(uint32_t(*)[8])(w + 8 * i));
@@ -181,6 +189,9 @@ __global__ void __launch_bounds__(kMx4Threads, sizeof(T) == 2 ? 3 : 2) k_mx4_qua
     }
 }
 
+// groups whose exponent byte is below this cannot pass the largest number: 6 * 2^e
+template <typename T> constexpr uint32_t kMx4Saturates = std::is_same_v<T, __half> ? 127 + 14 : 127 + 126;
+
 // codes -> x [m][n]; four lanes to 128 values of a row.  Without WIDE a warp hands its 8 x 128 values
 // round in shared memory and stores each row's side by side.
 template <typename T, bool WIDE>
@@ -201,7 +212,20 @@ __global__ void __launch_bounds__(kMx4Threads) k_mx4_restore(T* x, uint64_t x_st
         for (int h = 0; h < 2; ++h) {
             float v[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = saturated<T>(mx4_value(words[2 * h + j / 8] >> 4 * (j % 8)) * scale);
+            for (int i = 0; i < 2; ++i) {
+                uint32_t halves[4];
+                mx4_halves(words[2 * h + i], halves);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float lo, hi;
+                    unpack<__half>(halves[j], lo, hi);
+                    (Pair(lo, hi) * Pair(scale)).get(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]);
+                }
+            }
+            if (e >= kMx4Saturates<T>) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = saturated<T>(v[j]);
+            }
             if constexpr (WIDE) {
                 if (count >= 16 * h + 1) store_values(to + 16 * h, min(count - 16 * h, 16), v);
             } else {
@@ -505,17 +529,6 @@ k_mx4_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 // Instructions bound it: values by shifts and masks of fp16 numbers with an exponent 14 too low, with
 // the powers of two checked for 0 and NaN, took 9.1 us for 1 x 4096 x 4096.  16 tokens took 28 us, more than
 // the tiles' 16.
-__device__ __forceinline__ void mx4_halves(uint32_t w, uint32_t (&h)[4])
-{
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "mov.b32 {a, b, c, d}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
-        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
-}
-
 // 2^e of byte `group`; infinity for 255, whose group's products are 0: their product is NaN
 __device__ __forceinline__ float mx4_scale(uint32_t word, int group)
 {
