@@ -370,9 +370,9 @@ int eden_force_generic_kernels(eden_ctx* ctx, int on);
                                      one slab's second pass can overlap the next slab's first */
 /*   EDEN_OPT_LINEAR_FORM   EDEN_LINEAR_AUTO (default): the linear products choose their kernel by
  *                          size; else that form wherever it can run (EDEN_LINEAR_FEW: up to 32
- *                          tokens of eden_linear).
+ *                          tokens of eden_linear, up to 8 of eden_mx4_linear).
  *   EDEN_OPT_LINEAR_SPLITS 0 (default): by size; 1, 2, 4 or 8: parts that a tile's sum is cut
- *                          into (at most one for each 64 of its length, and blocks of at most
+ *                          into, but for 4-bit products (at most one for each 64 of its length, and blocks of at most
  *                          eight SMs). */
 #define EDEN_OPT_LINEAR_FORM   9
 #define EDEN_OPT_LINEAR_SPLITS 10
@@ -567,7 +567,7 @@ typedef struct eden_drop {
     double rate;                                        /* 0 to 1; 0: no dropout */
     uint64_t seed;
     const uint64_t* seed_at;                            /* dev, or NULL: seed */
-    uint64_t first_row;
+    uint64_t first_row;                                 /* below 2^31 */
 } eden_drop;
 
 /* Device workspace of eden_block_join_backward for rows of n values (eden_block_join needs none). */
