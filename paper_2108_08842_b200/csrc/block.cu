@@ -1,5 +1,6 @@
 // C ABI of what joins a client's blocks (declared in include/eden.h): argument checks, workspace
 // carving and launches.
+#include <atomic>
 #include <cmath>
 
 #include "kernels_block.cuh"
@@ -94,32 +95,39 @@ Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)
     return g;
 }
 
-template <typename View>
-int launch_rows(eden_ctx* ctx, const char* name, double bytes, void (*kernel)(View, BlockShape, uint32_t*), const View& p, const Grid& g)
+template <auto kernel, typename View>
+int launch_rows(eden_ctx* ctx, const char* name, double bytes, const View& p, const Grid& g)
 {
-    CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowsShared));
+    static std::atomic<uint64_t> asked{0};       // devices on which this kernel may use its shared memory
+    const uint64_t device = 1ull << (ctx->device & 63);
+    if (!(asked.load(std::memory_order_relaxed) & device) || ctx->device > 63) {
+        CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowsShared));
+        asked.fetch_or(device, std::memory_order_relaxed);
+    }
     return launch(ctx, name, bytes, kernel, dim3(g.blocks), g.threads, g.shared, g.s.blocks, p, g.s, (uint32_t*)ctx->ws);
 }
 
 bool full(const eden_norm& n) { return n.kind == EDEN_NORM_LAYER || (n.kind != EDEN_NORM_NONE && n.bias); }
 
-#define EDEN_JOIN_PIECES(kernel, f, w, pieces) ((pieces) == 2 ? kernel<T, AFTER, BEFORE, f, w, 2> : kernel<T, AFTER, BEFORE, f, w, 1>)
-#define EDEN_JOIN_KERNEL(kernel, f, w, pieces)                                                                  \
-    ((f) ? ((w) ? EDEN_JOIN_PIECES(kernel, true, true, pieces) : EDEN_JOIN_PIECES(kernel, true, false, pieces))  \
-         : ((w) ? EDEN_JOIN_PIECES(kernel, false, true, pieces) : EDEN_JOIN_PIECES(kernel, false, false, pieces)))
+// The launch of the kernel for everything or less, aligned rows or any, and one or two pieces a thread.
+#define EDEN_JOIN_PIECES(kernel, f, w, pieces, ...) \
+    ((pieces) == 2 ? launch_rows<kernel<T, AFTER, BEFORE, f, w, 2>>(__VA_ARGS__) : launch_rows<kernel<T, AFTER, BEFORE, f, w, 1>>(__VA_ARGS__))
+#define EDEN_JOIN_KERNEL(kernel, f, w, pieces, ...)                                                                                             \
+    ((f) ? ((w) ? EDEN_JOIN_PIECES(kernel, true, true, pieces, __VA_ARGS__) : EDEN_JOIN_PIECES(kernel, true, false, pieces, __VA_ARGS__))       \
+         : ((w) ? EDEN_JOIN_PIECES(kernel, false, true, pieces, __VA_ARGS__) : EDEN_JOIN_PIECES(kernel, false, false, pieces, __VA_ARGS__)))
 
 template <typename T, bool AFTER, bool BEFORE>
 int join(eden_ctx* ctx, const JoinView& p, const Grid& g, bool f, double bytes)
 {
     const bool wide = g.wide && rows_on_16(p.x, p.x_stride) && rows_on_16(p.y, p.y_stride);
-    return launch_rows(ctx, "t_join", bytes, EDEN_JOIN_KERNEL(k_join, f, wide, g.pieces), p, g);
+    return EDEN_JOIN_KERNEL(k_join, f, wide, g.pieces, ctx, "t_join", bytes, p, g);
 }
 
 template <typename T, bool AFTER, bool BEFORE>
 int join_backward(eden_ctx* ctx, const JoinBackwardView& p, const Grid& g, bool f, double bytes)
 {
     const bool wide = g.wide && rows_on_16(p.d_residual, p.d_residual_stride) && rows_on_16(p.dh, p.dh_stride) && rows_on_16(p.d_gate, p.d_gate_stride);
-    return launch_rows(ctx, "t_join_backward", bytes, EDEN_JOIN_KERNEL(k_join_backward, f, wide, g.pieces), p, g);
+    return EDEN_JOIN_KERNEL(k_join_backward, f, wide, g.pieces, ctx, "t_join_backward", bytes, p, g);
 }
 
 #define EDEN_DISPATCH_NORMS(after, before, CALL)                                                   \

@@ -94,7 +94,11 @@ struct Place {
         col = first + warp * (256 * K) + lane * 8;
 #pragma unroll
         for (int i = 0; i < K; ++i) count[i] = col + 256 * i < s.n ? (int)min(s.n - col - 256 * i, 8u) : 0;
+        columns = s.n;
     }
+    uint32_t columns;
+    // columns of the warp's piece that exist
+    __device__ __forceinline__ int in_warp(int i) const { return min(max((int)columns - (int)(col - lane * 8 + 256 * i), 0), 256); }
 };
 
 template <int K>
@@ -293,6 +297,7 @@ struct Stages {
     __device__ __forceinline__ void values(Values<K>& v, uint32_t r, const Source& source) const
     {
         const char* const begin = place(source) + (at.col - at.first) * 2;
+        const uint32_t skew = WIDE ? 0 : source.skew(r, at.first);
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             uint32_t w[4] = {0, 0, 0, 0};
@@ -301,14 +306,16 @@ struct Stages {
                 const uint4 q = *(const uint4*)from;
                 w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
             } else if (at.count[i] > 0) {
-                // words from the last one that starts at or before the values
-                const uint32_t skew = source.skew(r, at.first), shift = (skew & 2u) * 8;
-                const uint32_t* const word = (const uint32_t*)(from + (skew & ~3u));
-                uint32_t c[5];
+                // The chunks that hold them, shifted by the row's skew, the same for all lanes.  Five words a
+                // lane, 16 bytes apart across the lanes, would meet four times in a bank.
+                const uint4 lo = *(const uint4*)from, hi = *(const uint4*)(from + 16);
+                uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-                for (int j = 0; j < 5; ++j) c[j] = word[j];
+                for (int j = 0; j < 6; ++j) c[j] = skew & 8u ? c[j + 2] : c[j];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(c[j], c[j + 1], shift);
+                for (int j = 0; j < 5; ++j) c[j] = skew & 4u ? c[j + 1] : c[j];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(c[j], c[j + 1], (skew & 2u) * 8);
                 if (at.count[i] < 8) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) w[j] &= at.count[i] >= 2 * j + 2 ? 0xFFFFFFFFu : at.count[i] == 2 * j + 1 ? 0xFFFFu : 0u;
@@ -328,6 +335,7 @@ struct Stages {
     __device__ __forceinline__ void coded(Values<K>& v, uint32_t r, const Source& codes, const Source& exps, float factor) const
     {
         const char* const begin = place(codes) + (at.col - at.first);
+        const uint32_t skew = WIDE ? 0 : codes.skew(r, at.first);
         const uint8_t* const exp = (const uint8_t*)place(exps) + exps.skew(r, at.first) + (at.col - at.first) / kGroup;
 #pragma unroll
         for (int i = 0; i < K; ++i) {
@@ -339,11 +347,10 @@ struct Stages {
                 e = exp[256 / kGroup * i];
                 a = there ? q.x : 0u, b = there ? q.y : 0u, e = there ? e : 1u;
             } else if (at.count[i] > 0) {
-                const uint32_t skew = codes.skew(r, at.first), shift = (skew & 3u) * 8;
-                const uint32_t* const word = (const uint32_t*)(from + (skew & ~3u));
-                const uint32_t c = word[1];
-                a = __funnelshift_r(word[0], c, shift);
-                b = __funnelshift_r(c, word[2], shift);
+                const uint2 lo = *(const uint2*)(from + (skew & 8u)), hi = *(const uint2*)(from + (skew & 8u) + 8);
+                const uint32_t c0 = skew & 4u ? lo.y : lo.x, c1 = skew & 4u ? hi.x : lo.y, c2 = skew & 4u ? hi.y : hi.x;
+                a = __funnelshift_r(c0, c1, (skew & 3u) * 8);
+                b = __funnelshift_r(c1, c2, (skew & 3u) * 8);
                 e = exp[256 / kGroup * i];
                 if (at.count[i] < 8) {
                     a &= at.count[i] >= 4 ? 0xFFFFFFFFu : 0xFFFFFFFFu >> (32 - 8 * at.count[i]);
@@ -418,9 +425,9 @@ struct Stages {
 
 // The lane's 8 values to p, of which `count` exist.  Without WIDE they go round the warp in shared
 // memory (`buffer`, its own 132 words) and are stored side by side, whole words wherever the matrix
-// has them.
+// has them; `in_warp` of the warp's 256 columns exist.
 template <typename T, bool WIDE>
-__device__ __forceinline__ void store_row_8(T* p, int count, const Pair (&v)[4], uint32_t* buffer, uint32_t lane)
+__device__ __forceinline__ void store_row_8(T* p, int count, int in_warp, const Pair (&v)[4], uint32_t* buffer, uint32_t lane)
 {
     uint32_t w[4];
 #pragma unroll
@@ -436,19 +443,19 @@ __device__ __forceinline__ void store_row_8(T* p, int count, const Pair (&v)[4],
     __syncwarp();
     *(uint4*)(buffer + 4 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
     __syncwarp();
-    const int in_warp = __reduce_add_sync(0xFFFFFFFFu, count);             // lanes' columns follow one another
     uint16_t* const row = (uint16_t*)p - lane * 8;
     const int skew = ((uintptr_t)row & 3) != 0;                            // the first value is a word's second half
     uint32_t* const words = (uint32_t*)(row - skew);
 #pragma unroll
-    for (int j = 0; j < 5; ++j) {
-        const int i = j * 32 + (int)lane, a = 2 * i - skew;                // the word holds values a and a + 1
-        if (j == 4 && i > 128) break;
-        const uint32_t low = a >= 0 && a < in_warp ? ((const uint16_t*)buffer)[a] : 0u, high = a + 1 < in_warp ? ((const uint16_t*)buffer)[a + 1] : 0u;
-        if (a >= 0 && a + 1 < in_warp) words[i] = low | high << 16;
-        else if (a >= 0 && a < in_warp) row[a] = (uint16_t)low;
-        else if (a == -1 && in_warp > 0) row[0] = (uint16_t)high;
+    for (int j = 0; j < 4; ++j) {
+        const int i = j * 32 + (int)lane, first = 2 * i - skew;            // the word holds values first and first + 1
+        const uint32_t here = buffer[i], before = buffer[i > 0 ? i - 1 : 0];
+        if (first >= 0 && first + 1 < in_warp) words[i] = skew ? __funnelshift_r(before, here, 16) : here;
     }
+    // a first and a last value that share their words with others
+    const int last = in_warp - 1;
+    if (lane == 0 && skew && in_warp > 0) row[0] = (uint16_t)buffer[0];
+    if (lane == 1 && last >= skew && ((last + skew) & 1) == 0) row[last] = ((const uint16_t*)buffer)[last];
 }
 
 // The eight numbers that decide on 8 values.
@@ -488,7 +495,7 @@ template <typename T, bool WIDE, int K>
 __device__ __forceinline__ void store_row(T* p, const Place<K>& at, const Values<K>& v, uint32_t* buffer)
 {
 #pragma unroll
-    for (int i = 0; i < K; ++i) store_row_8<T, WIDE>(p + 256 * i, at.count[i], v[i], buffer, at.lane);
+    for (int i = 0; i < K; ++i) store_row_8<T, WIDE>(p + 256 * i, at.count[i], at.in_warp(i), v[i], buffer, at.lane);
 }
 
 // Vectors of a block.
@@ -878,7 +885,7 @@ __global__ void __launch_bounds__(kPlainThreads) k_join_plain(PlainView p)
     const uint64_t unit = (uint64_t)blockIdx.x * (kPlainThreads / 32) + threadIdx.x / 32, row0 = unit / p.warps_across * kPlainRows;
     if (row0 >= p.m) return;
     const uint32_t col = (uint32_t)(unit % p.warps_across) * 256 + lane * 8;
-    const int count = col < p.n ? (int)min(p.n - col, 8u) : 0, rows = (int)min((uint64_t)p.m - row0, (uint64_t)kPlainRows);
+    const int in_warp = min(max((int)p.n - (int)(col - lane * 8), 0), 256), count = col < p.n ? (int)min(p.n - col, 8u) : 0, rows = (int)min((uint64_t)p.m - row0, (uint64_t)kPlainRows);
     const uint64_t seed = p.drop.seed_at ? *p.drop.seed_at : p.drop.seed;
     uint4 h[kPlainRows], residual[kPlainRows], gate[kPlainRows];
 #pragma unroll
@@ -904,7 +911,7 @@ __global__ void __launch_bounds__(kPlainThreads) k_join_plain(PlainView p)
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = fma(w[j], Pair(p.scale), v[j]);
         }
-        store_row_8<T, WIDE>((T*)p.x + (row0 + r) * p.x_stride + col, count, v, buffer, lane);
+        store_row_8<T, WIDE>((T*)p.x + (row0 + r) * p.x_stride + col, count, in_warp, v, buffer, lane);
     }
 }
 
@@ -965,7 +972,7 @@ __global__ void __launch_bounds__(kPlainThreads) k_join_plain_backward(PlainBack
     dependency_release();
     const uint32_t lane = threadIdx.x % 32, col = blockIdx.x * (kPlainThreads * 8) + threadIdx.x * 8;
     uint32_t* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
-    const int count = col < p.n ? (int)min(p.n - col, 8u) : 0;
+    const int in_warp = min(max((int)p.n - (int)(col - lane * 8), 0), 256), count = col < p.n ? (int)min(p.n - col, 8u) : 0;
     const uint64_t begin = (uint64_t)blockIdx.y * p.rows_per_run, end = min((uint64_t)p.m, begin + p.rows_per_run);
     const uint64_t seed = p.drop.seed_at ? *p.drop.seed_at : p.drop.seed;
     Pair total[4];
@@ -981,7 +988,7 @@ __global__ void __launch_bounds__(kPlainThreads) k_join_plain_backward(PlainBack
         if (p.d_residual) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = v[j] * Pair(p.scale);
-            store_row_8<T, WIDE>((T*)p.d_residual + row * p.d_residual_stride + col, count, w, buffer, lane);
+            store_row_8<T, WIDE>((T*)p.d_residual + row * p.d_residual_stride + col, count, in_warp, w, buffer, lane);
         }
         uint4 numbers;
         if (p.has_drop) {
@@ -998,9 +1005,9 @@ __global__ void __launch_bounds__(kPlainThreads) k_join_plain_backward(PlainBack
                 v[j] = v[j] * w[j];
                 total[j] = total[j] + h[j];
             }
-            if (p.d_gate) store_row_8<T, WIDE>((T*)p.d_gate + row * p.d_gate_stride + col, count, h, buffer, lane);
+            if (p.d_gate) store_row_8<T, WIDE>((T*)p.d_gate + row * p.d_gate_stride + col, count, in_warp, h, buffer, lane);
         }
-        if (p.dh) store_row_8<T, WIDE>((T*)p.dh + row * p.dh_stride + col, count, v, buffer, lane);
+        if (p.dh) store_row_8<T, WIDE>((T*)p.dh + row * p.dh_stride + col, count, in_warp, v, buffer, lane);
     }
     if (!p.partial) return;
     float* const to = p.partial + (uint64_t)blockIdx.y * p.n + col;

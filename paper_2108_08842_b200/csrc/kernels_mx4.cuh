@@ -64,12 +64,31 @@ __device__ __forceinline__ void mx4_halves(uint32_t w, uint32_t (&h)[4])
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
 
-__device__ __forceinline__ uint32_t largest_bits(const float (&v)[32])
+// The largest magnitudes of 16-bit values, two a word, of the low and the high halves: as whole numbers
+// without their signs, which NaN tops.
+__device__ __forceinline__ uint32_t halves_max(uint32_t most, uint32_t a, uint32_t b) { return __vimax3_u16x2(most, a & 0x7FFF7FFFu, b & 0x7FFF7FFFu); }
+
+template <typename T>
+__device__ __forceinline__ uint32_t half_magnitude_bits(uint32_t half)
 {
-    float top = 0.f;
+    float lo, hi;
+    unpack<T>(half & 0xFFFFu, lo, hi);
+    return __float_as_uint(lo);
+}
+
+// 32 values as 16 bytes of codes; value(j) is value j
+template <typename F>
+__device__ __forceinline__ uint4 mx4_group(float inverse, F&& value)
+{
+    uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 32; j += 2) top = max_magnitude(top, v[j], v[j + 1]);
-    return magnitude_bits(top);
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = value(8 * i + j);
+        w[i] = mx4_codes(v, inverse);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // 32 values at p, of which `count` exist, zeros after them; WIDE: on 32 bytes
@@ -109,7 +128,7 @@ __device__ __forceinline__ uint32_t mx4_chunk(uint32_t row, uint32_t c)
 __device__ __forceinline__ uint32_t mx4_result(uint32_t c, uint32_t g) { return (c * 4 + g) ^ (c >> 1 & 3) ^ (c >> 3 & 1) << 2; }
 
 template <typename T, bool WIDE, bool COLUMNS>
-__global__ void __launch_bounds__(kMx4Threads, sizeof(T) == 2 ? 3 : 2) k_mx4_quantize(const T* x, uint64_t x_stride, Mx4View rows, Mx4View columns, uint32_t m, uint32_t n,
+__global__ void __launch_bounds__(kMx4Threads, sizeof(T) == 2 ? 4 : 2) k_mx4_quantize(const T* x, uint64_t x_stride, Mx4View rows, Mx4View columns, uint32_t m, uint32_t n,
                                                              uint32_t blocks_x)
 {
     __shared__ __align__(16) uint8_t exps[2][512];
@@ -134,15 +153,27 @@ __global__ void __launch_bounds__(kMx4Threads, sizeof(T) == 2 ? 3 : 2) k_mx4_qua
                 ((uint4*)tile)[mx4_chunk<T>(r, g * 2 * sizeof(T) + j)] = make_uint4(raw[i][4 * j], raw[i][4 * j + 1], raw[i][4 * j + 2], raw[i][4 * j + 3]);
         }
         if (rows.codes) {
-            float v[32];
+            uint32_t most = 0;
+            if constexpr (sizeof(T) == 4) {
+                float top = 0.f;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) widen<T>(*(uint32_t(*)[4 * sizeof(T)])(raw[i] + h * 4 * sizeof(T)), *(float(*)[16])(v + 16 * h));
-            const uint32_t e = mx4_exponent(largest_bits(v));
+                for (int j = 0; j < 32; j += 2) top = max_magnitude(top, __uint_as_float(raw[i][j]), __uint_as_float(raw[i][j + 1]));
+                most = magnitude_bits(top);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) most = halves_max(most, raw[i][j], raw[i][j + 1]);
+                most = half_magnitude_bits<T>(max(most & 0xFFFFu, most >> 16));
+            }
+            const uint32_t e = mx4_exponent(most);
             const float inverse = group_inverse(e);
             exps[0][r % 32 * 16 + r / 32 * 4 + g] = (uint8_t)e;
             if (count_of(row))
-                *(uint4*)(rows.codes + (uint64_t)row * rows.stride + col / 2) =
-                    make_uint4(mx4_codes(v, inverse), mx4_codes(v + 8, inverse), mx4_codes(v + 16, inverse), mx4_codes(v + 24, inverse));
+                *(uint4*)(rows.codes + (uint64_t)row * rows.stride + col / 2) = mx4_group(inverse, [&](int j) {
+                    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[i][j]);
+                    float pair[2];
+                    unpack<T>(raw[i][j / 2], pair[0], pair[1]);
+                    return pair[j % 2];
+                });
         }
     }
     __syncthreads();
@@ -155,21 +186,29 @@ __global__ void __launch_bounds__(kMx4Threads, sizeof(T) == 2 ? 3 : 2) k_mx4_qua
             uint32_t raw[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) raw[j] = tile[mx4_chunk<T>(32 * g + j, word / 4) * 4 + word % 4];
+            uint32_t most[2] = {0, 0};
+            if constexpr (sizeof(T) == 4) {
+                float top = 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) top = max_magnitude(top, __uint_as_float(raw[j]), __uint_as_float(raw[j + 1]));
+                most[0] = magnitude_bits(top);
+            } else {
+                uint32_t both = 0;
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) both = halves_max(both, raw[j], raw[j + 1]);
+                most[0] = half_magnitude_bits<T>(both & 0xFFFFu);
+                most[1] = half_magnitude_bits<T>(both >> 16);
+            }
 #pragma unroll
             for (int h = 0; h < kTogether; ++h) {
-                float v[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    float pair[2];
-                    if constexpr (sizeof(T) == 4) pair[0] = __uint_as_float(raw[j]);
-                    else unpack<T>(raw[j], pair[0], pair[1]);
-                    v[j] = pair[h];
-                }
-                const uint32_t c = word * kTogether + h, e = mx4_exponent(largest_bits(v));
-                const float inverse = group_inverse(e);
+                const uint32_t c = word * kTogether + h, e = mx4_exponent(most[h]);
                 exps[1][c % 32 * 16 + c / 32 * 4 + g] = (uint8_t)e;
-                out[mx4_result(c, g)] =
-                    make_uint4(mx4_codes(v, inverse), mx4_codes(v + 8, inverse), mx4_codes(v + 16, inverse), mx4_codes(v + 24, inverse));
+                out[mx4_result(c, g)] = mx4_group(group_inverse(e), [&](int j) {
+                    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[j]);
+                    float pair[2];
+                    unpack<T>(raw[j], pair[0], pair[1]);
+                    return pair[h];
+                });
             }
         }
         __syncthreads();

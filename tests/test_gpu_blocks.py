@@ -6,6 +6,7 @@ import torch
 from tests import blocks_reference as B
 from tests import training_reference as R
 from tests.test_gpu_training import gen, normal, untouched, within
+from tests.test_gpu_training_guards import Guarded
 
 pytestmark = pytest.mark.gpu
 
@@ -225,6 +226,28 @@ def test_results_in_place(ctx, n):
     a, b = dx.clone(), dy.clone()
     got = ctx.block_join_backward(a, b, *args, residual=a, out=b, **c.how())
     assert all(torch.equal(p, q) for p, q in zip(got, want)) and got.residual is a and got.h is b
+
+
+@pytest.mark.parametrize("extra,offset", [(0, 0), (1, 1), (2, 3), (8, 8)])
+@pytest.mark.parametrize("after,before,gate", [("rms", "layer", "matrix"), ("none", "rms", "vector"), ("layer", "none", "none"), ("none", "none", "matrix")])
+def test_calls_write_their_outputs_only(ctx, after, before, gate, extra, offset):
+    for m, n in ((1, 1), (3, 33), (40, 257), (9, 520), (2, 8200)):
+        c = Case(m, n, torch.bfloat16, after, before, gate, bias=True)
+        x, y = Guarded(m, n, torch.bfloat16, extra, offset), Guarded(m, n, torch.bfloat16, extra, offset)
+        want = ctx.block_join(c.h, c.residual, stats=True, **c.how())
+        got = ctx.block_join(c.h, c.residual, out=x.view, normed=y.view if c.before else None, stats=True, **c.how())
+        assert torch.equal(got.x, want.x) and (got.y is None or torch.equal(got.y, want.y))
+        for guarded in (x, y):
+            guarded.check()
+        dx, dy = make(5, m, n, torch.bfloat16), make(6, m, n, torch.bfloat16) if c.before else None
+        halves = {name: Guarded(m, n, torch.bfloat16, extra, offset) for name in ("residual", "out") + (("gate_grad",) if gate == "matrix" else ())}
+        sums = {name: Guarded(1, n, torch.float32, 0, offset) for name, there in (("after_weight_grad", c.after), ("after_bias_grad", c.after),
+                                                                                  ("before_weight_grad", c.before), ("before_bias_grad", c.before)) if there}
+        args = (dx, dy, c.h, want.x, want.after_stats, want.before_stats)
+        d = ctx.block_join_backward(*args, **{k: g.view for k, g in halves.items()}, **{k: g.view[0] for k, g in sums.items()}, **c.how())
+        for guarded in (*halves.values(), *sums.values()):
+            guarded.check()
+        assert all(p is None and q is None or torch.equal(p, q) for p, q in zip(d, ctx.block_join_backward(*args, **c.how())))
 
 
 # ------------------------------------------------------------------------------- dropout
