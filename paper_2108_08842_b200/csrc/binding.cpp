@@ -489,19 +489,24 @@ uint64_t count_of(PyObject* o, const char* name)
     return v;
 }
 
-// a norm (weight, bias, kind, eps), or None
-eden_norm norm_of(const Native* n, PyObject* o, const char* name, int64_t cols, at::ScalarType t)
+// a norm (weight, bias, kind, eps), or None; the names of it and of its parts
+struct NormNames {
+    const char *norm, *weight, *bias, *kind, *eps;
+};
+constexpr NormNames kAfterNames{"after", "the weight of after", "the bias of after", "the kind of after", "eps of after"};
+constexpr NormNames kBeforeNames{"before", "the weight of before", "the bias of before", "the kind of before", "eps of before"};
+
+eden_norm norm_of(const Native* n, PyObject* o, const NormNames& names, int64_t cols, at::ScalarType t)
 {
     eden_norm r;
     std::memset(&r, 0, sizeof(r));
     if (!given(o)) return r;
-    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) refuse(std::string(name) + " has to be a Norm");
-    const std::string at = std::string(" of ") + name;
-    if (given(PyTuple_GET_ITEM(o, 0))) r.weight = vector_of(n, PyTuple_GET_ITEM(o, 0), ("the weight" + at).c_str(), cols, t);
-    if (given(PyTuple_GET_ITEM(o, 1))) r.bias = vector_of(n, PyTuple_GET_ITEM(o, 1), ("the bias" + at).c_str(), cols, t);
-    r.kind = name_of(PyTuple_GET_ITEM(o, 2), ("the kind" + at).c_str(), kNorms, 3);
-    r.eps = (float)number_of(PyTuple_GET_ITEM(o, 3), ("eps" + at).c_str());
-    if (!(r.eps >= 0.f) || r.eps > 1e30f) refuse("eps" + at + " has to be a finite number from 0 on");
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) refuse(std::string(names.norm) + " has to be a Norm");
+    if (given(PyTuple_GET_ITEM(o, 0))) r.weight = vector_of(n, PyTuple_GET_ITEM(o, 0), names.weight, cols, t);
+    if (given(PyTuple_GET_ITEM(o, 1))) r.bias = vector_of(n, PyTuple_GET_ITEM(o, 1), names.bias, cols, t);
+    r.kind = name_of(PyTuple_GET_ITEM(o, 2), names.kind, kNorms, 3);
+    r.eps = (float)number_of(PyTuple_GET_ITEM(o, 3), names.eps);
+    if (!(r.eps >= 0.f) || r.eps > 1e30f) refuse(std::string(names.eps) + " has to be a finite number from 0 on");
     if (r.kind == EDEN_NORM_NONE) r.weight = r.bias = nullptr;
     return r;
 }
@@ -564,8 +569,8 @@ PyObject* join(PyObject*, PyObject* const* v, Py_ssize_t count)
         a.type = type_of(h, false, "h");
         const Matrix mh(n, h, "h", m, cols, t);
         a.h = mh.data; a.h_stride = mh.stride;
-        a.after = norm_of(n, v[3], "after", cols, t);
-        a.before = norm_of(n, v[4], "before", cols, t);
+        a.after = norm_of(n, v[3], kAfterNames, cols, t);
+        a.before = norm_of(n, v[4], kBeforeNames, cols, t);
         a.gate = gate_of(n, v[5], m, cols, t, &a.gate_stride, &a.gate_per_value);
         a.scale = (float)number_of(v[6], "scale");
         a.drop = drop_of(n, v[7], v[8], v[9]);
@@ -637,8 +642,8 @@ PyObject* join_backward(PyObject*, PyObject* const* v, Py_ssize_t count)
         eden_block_join_backward_args a;
         std::memset(&a, 0, sizeof(a));
         a.type = type_of(leading, false, given(v[1]) ? "dx" : "dy");
-        a.after = norm_of(n, v[7], "after", cols, t);
-        a.before = norm_of(n, v[8], "before", cols, t);
+        a.after = norm_of(n, v[7], kAfterNames, cols, t);
+        a.before = norm_of(n, v[8], kBeforeNames, cols, t);
         a.gate = gate_of(n, v[9], m, cols, t, &a.gate_stride, &a.gate_per_value);
         a.scale = (float)number_of(v[10], "scale");
         a.drop = drop_of(n, v[11], v[12], v[13]);
@@ -726,16 +731,15 @@ Mx4 mx4_of(const Native* n, PyObject* o, const char* name, int64_t rows, int64_t
         PyErr_Clear();
         refuse(std::string("the features of ") + name + " have to be a whole number from 1 on");
     }
-    const std::string at = std::string(" of ") + name;
     if (q.codes.dim() != 2 || (features >= 0 && q.features != features) || (rows >= 0 && q.codes.size(0) != rows))
         refuse(std::string(name) + " has to hold [" + (rows >= 0 ? std::to_string(rows) : "rows") + ", " + (features >= 0 ? std::to_string(features) : "features") +
                "] values, got features " + std::to_string(q.features) + " and codes " + described(q.codes));
-    const Matrix codes(n, q.codes, ("the codes" + at).c_str(), q.codes.size(0), groups_of(q.features) * 16, at::kByte);
-    if ((uintptr_t)codes.data & 15 || codes.stride & 15) refuse("the rows of the codes" + at + " have to start on 16 bytes");
+    const Matrix codes(n, q.codes, name, q.codes.size(0), groups_of(q.features) * 16, at::kByte);
+    if ((uintptr_t)codes.data & 15 || codes.stride & 15) refuse(std::string("the rows of the codes of ") + name + " have to start on 16 bytes");
     const int64_t across = tiles_of(q.codes.size(0), 128), along = tiles_of(q.features, 256);
     if (q.exps.dim() != 3 || q.exps.scalar_type() != at::kByte || q.exps.size(0) != across || q.exps.size(1) != along || q.exps.size(2) != 1024 || !q.exps.is_cuda() ||
         q.exps.get_device() != n->device || !q.exps.is_contiguous() || (uintptr_t)q.exps.data_ptr() & 15)
-        refuse("the exponents" + at + " have to be contiguous Byte [" + std::to_string(across) + ", " + std::to_string(along) + ", 1024] on cuda:" +
+        refuse(std::string("the exponents of ") + name + " have to be contiguous Byte [" + std::to_string(across) + ", " + std::to_string(along) + ", 1024] on cuda:" +
                std::to_string(n->device) + " and 16 bytes, got " + described(q.exps));
     return q;
 }

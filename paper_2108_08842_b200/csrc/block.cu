@@ -176,7 +176,7 @@ extern "C" int eden_block_join(eden_ctx* ctx, const eden_block_join_args* a)
             p.drop = drop_view(a->drop, &p.has_drop);
             const bool wide = rows_on_16(p.h, p.h_stride) && rows_on_16(p.residual, p.residual_stride) && (!per_value || rows_on_16(p.gate, per_value)) &&
                               rows_on_16(p.x, p.x_stride);
-            const uint64_t blocks = ((a->m + kPlainRows - 1) / kPlainRows * p.warps_across + kPlainThreads / 32 - 1) / (kPlainThreads / 32);
+            const uint64_t rows = wide ? kPlainRows<true> : kPlainRows<false>, blocks = ((a->m + rows - 1) / rows * p.warps_across + kPlainThreads / 32 - 1) / (kPlainThreads / 32);
             if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;
             EDEN_DISPATCH_HALF(a->type, return launch(ctx, "t_join_plain", bytes, wide ? k_join_plain<T_, true> : k_join_plain<T_, false>, dim3((uint32_t)blocks),
                                                       kPlainThreads, 0, 1, p));

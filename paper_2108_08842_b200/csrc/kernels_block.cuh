@@ -250,6 +250,23 @@ __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, co
     return make_float2(mean / kSmaller, rsqrtf(square) * kSmaller);        // eps is nothing beside such squares
 }
 
+// The 16 bytes that begin `skew` bytes, an even number, into two chunks.  One branch where the skew is
+// the same for all lanes, as it is for a row.
+__device__ __forceinline__ void shift_words(uint32_t (&w)[4], const uint4& lo, const uint4& hi, uint32_t skew)
+{
+    const uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, bits = (skew & 2u) * 8;
+    auto from = [&](auto first) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(c[decltype(first)::value + j], c[decltype(first)::value + j + 1], bits);
+    };
+    switch (skew >> 2) {
+        case 0: from(std::integral_constant<int, 0>()); break;
+        case 1: from(std::integral_constant<int, 1>()); break;
+        case 2: from(std::integral_constant<int, 2>()); break;
+        default: from(std::integral_constant<int, 3>()); break;
+    }
+}
+
 // ---- rows in shared memory ----------------------------------------------------------
 // A row of every source, `stages` times for each team: a row's copies are counted by its stage's barrier.
 template <int K>
@@ -308,14 +325,7 @@ struct Stages {
             } else if (at.count[i] > 0) {
                 // The chunks that hold them, shifted by the row's skew, the same for all lanes.  Five words a
                 // lane, 16 bytes apart across the lanes, would meet four times in a bank.
-                const uint4 lo = *(const uint4*)from, hi = *(const uint4*)(from + 16);
-                uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-                for (int j = 0; j < 6; ++j) c[j] = skew & 8u ? c[j + 2] : c[j];
-#pragma unroll
-                for (int j = 0; j < 5; ++j) c[j] = skew & 4u ? c[j + 1] : c[j];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(c[j], c[j + 1], (skew & 2u) * 8);
+                shift_words(w, *(const uint4*)from, *(const uint4*)(from + 16), skew);
                 if (at.count[i] < 8) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) w[j] &= at.count[i] >= 2 * j + 2 ? 0xFFFFFFFFu : at.count[i] == 2 * j + 1 ? 0xFFFFu : 0u;
@@ -449,8 +459,9 @@ __device__ __forceinline__ void store_row_8(T* p, int count, int in_warp, const 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int i = j * 32 + (int)lane, first = 2 * i - skew;            // the word holds values first and first + 1
-        const uint32_t here = buffer[i], before = buffer[i > 0 ? i - 1 : 0];
-        if (first >= 0 && first + 1 < in_warp) words[i] = skew ? __funnelshift_r(before, here, 16) : here;
+        uint32_t word = buffer[i];
+        if (skew) word = __funnelshift_r(buffer[i > 0 ? i - 1 : 0], word, 16);
+        if ((j > 0 || first >= 0) && (in_warp == 256 || first + 1 < in_warp)) words[i] = word;
     }
     // a first and a last value that share their words with others
     const int last = in_warp - 1;
@@ -840,8 +851,10 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
 
 // ---- without norms -------------------------------------------------------------------
 // Nothing is summed over a row, so a block takes 256 columns a warp of its own choice and any rows:
-// kPlainRows of them at a time, all of their loads on their way together.
-constexpr int kPlainRows = 4, kPlainThreads = 256;
+// kPlainRows of them at a time, all of their loads on their way together (twice as many a row where rows
+// do not start on 16 bytes).
+constexpr int kPlainThreads = 256;
+template <bool WIDE> constexpr int kPlainRows = WIDE ? 4 : 2;
 
 struct PlainView {
     const void* h;         uint64_t h_stride;
@@ -854,12 +867,41 @@ struct PlainView {
     uint32_t m, n, warps_across;       // warps that cover a row
 };
 
-// 8 values at p, of which `count` exist (zeros after them); WIDE: on 16 bytes
+// 8 values of 16 bits as they lie in memory: a chunk, or the two that hold them.
+template <bool WIDE>
+struct Raw8 {
+    uint4 lo, hi;
+    uint32_t skew;
+    int count;
+    template <typename T>
+    __device__ __forceinline__ void load(const T* p, int n)
+    {
+        count = n;
+        lo = hi = make_uint4(0, 0, 0, 0);
+        skew = WIDE ? 0 : (uint32_t)(uintptr_t)p & 15u;
+        const uint4* const chunk = (const uint4*)((uintptr_t)p - skew);
+        if (n > 0) lo = chunk[0];
+        if (!WIDE && (int)skew + 2 * n > 16) hi = chunk[1];
+    }
+    // zeros after those that exist
+    __device__ __forceinline__ uint4 get() const
+    {
+        uint32_t w[4] = {lo.x, lo.y, lo.z, lo.w};
+        if (!WIDE) shift_words(w, lo, hi, skew);
+        if (count < 8) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] &= count >= 2 * j + 2 ? 0xFFFFFFFFu : count == 2 * j + 1 ? 0xFFFFu : 0u;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
 template <bool WIDE, typename T>
 __device__ __forceinline__ uint4 load_row_8(const T* p, int count)
 {
-    if (WIDE && count == 8) return *(const uint4*)p;
-    return load_shifted_8(p, count);
+    Raw8<WIDE> raw;
+    raw.load(p, count);
+    return raw.get();
 }
 
 template <typename T>
@@ -875,31 +917,33 @@ __device__ __forceinline__ void widen_8(const uint4& q, Pair (&v)[4])
 }
 
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kPlainThreads) k_join_plain(PlainView p)
+__global__ void __launch_bounds__(kPlainThreads, 3) k_join_plain(PlainView p)
 {
+    constexpr int kRows = kPlainRows<WIDE>;
     __shared__ uint32_t buffers[WIDE ? 1 : kPlainThreads / 32][132];
     dependency_wait();
     dependency_release();
     const uint32_t lane = threadIdx.x % 32;
     uint32_t* const buffer = buffers[WIDE ? 0 : threadIdx.x / 32];
-    const uint64_t unit = (uint64_t)blockIdx.x * (kPlainThreads / 32) + threadIdx.x / 32, row0 = unit / p.warps_across * kPlainRows;
+    const uint64_t unit = (uint64_t)blockIdx.x * (kPlainThreads / 32) + threadIdx.x / 32, row0 = unit / p.warps_across * kRows;
     if (row0 >= p.m) return;
     const uint32_t col = (uint32_t)(unit % p.warps_across) * 256 + lane * 8;
-    const int in_warp = min(max((int)p.n - (int)(col - lane * 8), 0), 256), count = col < p.n ? (int)min(p.n - col, 8u) : 0, rows = (int)min((uint64_t)p.m - row0, (uint64_t)kPlainRows);
+    const int in_warp = min(max((int)p.n - (int)(col - lane * 8), 0), 256), count = col < p.n ? (int)min(p.n - col, 8u) : 0, rows = (int)min((uint64_t)p.m - row0, (uint64_t)kRows);
     const uint64_t seed = p.drop.seed_at ? *p.drop.seed_at : p.drop.seed;
-    uint4 h[kPlainRows], residual[kPlainRows], gate[kPlainRows];
+    Raw8<WIDE> h[kRows], residual[kRows];
+    uint4 gate[kRows];
 #pragma unroll
-    for (int r = 0; r < kPlainRows; ++r) {
+    for (int r = 0; r < kRows; ++r) {
         const int here = r < rows ? count : 0;
-        h[r] = load_row_8<WIDE>((const T*)p.h + (row0 + r) * p.h_stride + col, here);
-        if (p.residual) residual[r] = load_row_8<WIDE>((const T*)p.residual + (row0 + r) * p.residual_stride + col, here);
+        h[r].load((const T*)p.h + (row0 + r) * p.h_stride + col, here);
+        if (p.residual) residual[r].load((const T*)p.residual + (row0 + r) * p.residual_stride + col, here);
         if (p.gate) gate[r] = p.gate_stride ? load_row_8<WIDE>((const T*)p.gate + (row0 + r) * p.gate_stride + col, here) : load_shifted_8((const T*)p.gate + col, here);
     }
 #pragma unroll
-    for (int r = 0; r < kPlainRows; ++r) {
+    for (int r = 0; r < kRows; ++r) {
         if (r >= rows) break;
         Pair v[4], w[4];
-        widen_8<T>(h[r], v);
+        widen_8<T>(h[r].get(), v);
         if (p.has_drop) drop_values(v, drop_numbers(p.drop, seed, (uint32_t)row0 + r, col), p.drop.keep, p.drop.factor);
         if (p.gate) {
             widen_8<T>(gate[r], w);
@@ -907,7 +951,7 @@ __global__ void __launch_bounds__(kPlainThreads) k_join_plain(PlainView p)
             for (int j = 0; j < 4; ++j) v[j] = v[j] * w[j];
         }
         if (p.residual) {
-            widen_8<T>(residual[r], w);
+            widen_8<T>(residual[r].get(), w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = fma(w[j], Pair(p.scale), v[j]);
         }
@@ -965,7 +1009,7 @@ struct PlainBackwardView {
 
 // Eight warps side by side along the columns walk down a run of rows.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kPlainThreads) k_join_plain_backward(PlainBackwardView p)
+__global__ void __launch_bounds__(kPlainThreads, 3) k_join_plain_backward(PlainBackwardView p)
 {
     __shared__ uint32_t buffers[WIDE ? 1 : kPlainThreads / 32][132];
     dependency_wait();
