@@ -95,8 +95,11 @@ struct Place {
 #pragma unroll
         for (int i = 0; i < K; ++i) count[i] = col + 256 * i < s.n ? (int)min(s.n - col - 256 * i, 8u) : 0;
         columns = s.n;
+        const uint32_t begin = first + warp * (256 * K);
+        over_own = begin < s.n ? 1.f / (float)min(s.n - begin, 256u * K) : 0.f;
     }
     uint32_t columns;
+    float over_own;                    // one over the number of the warp's columns that exist
     // columns of the warp's piece that exist
     __device__ __forceinline__ int in_warp(int i) const { return min(max((int)columns - (int)(col - lane * 8 + 256 * i), 0), 256); }
 };
@@ -159,7 +162,7 @@ __device__ __forceinline__ float lanes_total(const BlockShape& s, float a)
 template <int K>
 __device__ __forceinline__ float columns_of(const BlockShape& s, uint32_t i)
 {
-    const uint32_t begin = i / s.warps * s.span + i % s.warps * (256 * K);
+    const uint32_t begin = s.blocks == 1 ? i * (256 * K) : i / s.warps * s.span + i % s.warps * (256 * K);
     return begin < s.n ? (float)min(s.n - begin, 256u * K) : 0.f;
 }
 
@@ -186,7 +189,7 @@ __device__ __forceinline__ float2 row_sums(Exchange& e, uint32_t& turn, const Bl
 // around the row's mean, so that no difference of large squares makes a small one.  Sums that pass
 // fp32's largest number (bf16 values beyond 10^17) are made again of smaller values: all threads of a row
 // hold the same sum, and take the second way together.
-template <bool FULL, int K>
+template <bool FULL, bool WIDE, int K>
 __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, const BlockShape& s, const Place<K>& at, const NormView& norm, const Values<K>& v)
 {
     const float over_n = 1.f / (float)s.n;
@@ -208,40 +211,42 @@ __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, co
             for (int i = 0; i < K; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) t = t + times(v[i][j]);
-            const float sum = warp_total(both(t)), own = columns_of<K>(s, at.rank * s.warps + at.warp), middle = own > 0.f ? sum / own : 0.f;
+            const float sum = warp_total(both(t)), middle = sum * at.over_own;
             float q = 0.f;
 #pragma unroll
-            for (int i = 0; i < K; ++i)
+            for (int i = 0; i < K; ++i) {
+                Pair part(0.f);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float x, y;
-                    (times(v[i][j]) + Pair(-middle)).get(x, y);
-                    if (2 * j < at.count[i]) q = fmaf(x, x, q);
-                    if (2 * j + 1 < at.count[i]) q = fmaf(y, y, q);
+                    Pair off = times(v[i][j]) + Pair(-middle);
+                    if (!WIDE && at.count[i] < 8) {
+                        float x, y;
+                        off.get(x, y);
+                        off = Pair(2 * j < at.count[i] ? x : 0.f, 2 * j + 1 < at.count[i] ? y : 0.f);
+                    }
+                    part = fma(off, off, part);
                 }
-            constexpr int kHeld = kBlockCluster * kTeamWarps / 32;
-            float2 held[kHeld];
-            float columns[kHeld], total = 0.f;
-            int got = 0;
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i) columns[i] = 0.f;
+                q += at.count[i] > 0 ? both(part) : 0.f;
+            }
+            // the lane's warps (one, without a cluster) as one: columns, their mean, the squares around it
+            float columns = 0.f, mid = 0.f, squares = 0.f, total = 0.f;
             exchange<K>(e, turn, s, at, make_float2(sum, warp_total(q)), [&](uint32_t i, float2 w) {
                 const float c = columns_of<K>(s, i);
-#pragma unroll
-                for (int k = 0; k < kHeld; ++k)
-                    if (k == got) held[k] = w, columns[k] = c;
-                ++got;
+                if (c == 0.f) return;
+                const float m = w.x / c;
                 total += w.x;
+                if (columns == 0.f) {
+                    columns = c, mid = m, squares = w.y;
+                    return;
+                }
+                const float off = m - mid, part = c / (columns + c);
+                squares += fmaf(off * off * columns, part, w.y);
+                mid = fmaf(off, part, mid);
+                columns += c;
             });
             mean = lanes_total(s, total) * over_n;
-            q = 0.f;
-#pragma unroll
-            for (int k = 0; k < kHeld; ++k)
-                if (columns[k] > 0.f) {
-                    const float off = held[k].x / columns[k] - mean;
-                    q += fmaf(columns[k] * off, off, held[k].y);
-                }
-            square = lanes_total(s, q) * over_n;
+            const float off = mid - mean;
+            square = lanes_total(s, columns > 0.f ? fmaf(columns * off, off, squares) : 0.f) * over_n;
         }
     };
     sums(std::false_type());
@@ -585,7 +590,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __gr
         Values<K> v, w;
         stages.template values<T, WIDE>(v, row, s.source[kSourceH]);
         if constexpr (AFTER) {
-            const float2 st = row_statistics<FULL, K>(sums, turn, s, at, p.after, v);
+            const float2 st = row_statistics<FULL, WIDE, K>(sums, turn, s, at, p.after, v);
             refill();
             if (p.after.stats && at.col == 0) *(float2*)(p.after.stats + 2 * (uint64_t)row) = st;
             vector(w, kAfterWeights);
@@ -619,7 +624,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __gr
 #pragma unroll
                 for (int i = 0; i < K; ++i) mask_values<WIDE>(v[i], at.count[i]);
             }
-            const float2 st = row_statistics<FULL, K>(sums, turn, s, at, p.before, v);
+            const float2 st = row_statistics<FULL, WIDE, K>(sums, turn, s, at, p.before, v);
             if (!AFTER) refill();
             if (p.before.stats && at.col == 0) *(float2*)(p.before.stats + 2 * (uint64_t)row) = st;
             vector(w, kBeforeWeights);
