@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libeden.so")
 BINDING = os.path.join(HERE, "_binding.so")
-SOURCES = ["eden.cu", "train.cu", "block.cu", "mx4.cu", "lloyd_max.cpp", "uniform_family.cpp"]
+SOURCES = ["eden.cu", "train.cu", "block.cu", "block_backward.cu", "mx4.cu", "lloyd_max.cpp", "uniform_family.cpp"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -668,10 +668,11 @@ struct JoinBackwardView {
 };
 
 // Each team keeps the sums of its rows over the columns in registers; a block leaves them in its part
-// of `partial`, which k_join_sums adds up.
-template <typename T, bool AFTER, bool BEFORE, bool FULL, bool WIDE, int K>
+// of `partial`, which k_join_sums adds up.  LEVEL: 1 FULL but for biases, 2 with their sums as well.
+template <typename T, bool AFTER, bool BEFORE, int LEVEL, bool WIDE, int K>
 __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinBackwardView p, const __grid_constant__ BlockShape s, uint32_t* status)
 {
+    constexpr bool FULL = LEVEL > 0, BIASES = LEVEL > 1;
     __shared__ Exchange sums;
     __shared__ uint32_t buffers[WIDE ? 1 : kMaxTeams][132];
     __shared__ __align__(8) uint64_t bars[kMaxTeams * kMaxStages];
@@ -692,7 +693,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
     stages.template keep_vector<T>(rows_of_block, kGateVector, p.gate);
     if (AFTER) stages.template keep_vector<T>(rows_of_block, kAfterWeights, p.after.weight);
     if (BEFORE) stages.template keep_vector<T>(rows_of_block, kBeforeWeights, p.before.weight);
-    if (FULL && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
+    if (BIASES && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
     __syncthreads();
     auto vector = [&](Values<K>& v, int which) { stages.vector(v, rows_of_block, which); };
     const bool matrix_gate = FULL && s.source[kSourceGateMatrix].base, gated = p.gate || matrix_gate;
@@ -734,7 +735,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
             vector(d, kBeforeWeights);
             each<K>([&](int i, int j) {
                 total[kBeforeWeight][i][j] = fma(g[i][j], u[i][j], total[kBeforeWeight][i][j]);
-                if (FULL) total[kBeforeBias][i][j] = total[kBeforeBias][i][j] + g[i][j];
+                if (BIASES) total[kBeforeBias][i][j] = total[kBeforeBias][i][j] + g[i][j];
                 g[i][j] = g[i][j] * d[i][j];
                 if (FULL) a = a + g[i][j];
                 b = fma(g[i][j], u[i][j], b);
@@ -772,7 +773,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
             } else {
                 each<K>([&](int i, int j) { g[i][j] = u[i][j]; });
             }
-            if (FULL && AFTER && p.after.bias) {
+            if (BIASES && AFTER && p.after.bias) {
                 Values<K> bias;
                 vector(bias, kAfterBiases);
                 each<K>([&](int i, int j) { g[i][j] = g[i][j] + bias[i][j]; });
@@ -802,7 +803,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
             vector(g, kAfterWeights);
             each<K>([&](int i, int j) {
                 total[kAfterWeight][i][j] = fma(d[i][j], u[i][j], total[kAfterWeight][i][j]);
-                if (FULL) total[kAfterBias][i][j] = total[kAfterBias][i][j] + d[i][j];
+                if (BIASES) total[kAfterBias][i][j] = total[kAfterBias][i][j] + d[i][j];
                 d[i][j] = d[i][j] * g[i][j];
                 if (FULL) a = a + d[i][j];
                 b = fma(d[i][j], u[i][j], b);
@@ -1078,7 +1079,7 @@ struct JoinSumsView {
 
 // out[i][col] (+)= the sum of the parts' sums i: 32 columns per block, each warp every eighth
 // part, the eight added in order
-__global__ void __launch_bounds__(256) k_join_sums(JoinSumsView p)
+static __global__ void __launch_bounds__(256) k_join_sums(JoinSumsView p)
 {
     dependency_wait();
     dependency_release();
