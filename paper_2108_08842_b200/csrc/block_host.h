@@ -61,7 +61,7 @@ Grid grid_of(const eden_ctx* ctx, uint64_t m, uint64_t n, const Source (&source)
     const uint64_t sms = std::min<uint64_t>(ctx->sm_count, kMaxSlots);
     // Two pieces a thread where that leaves a row for every SM, or where one would need a cluster.
     // (Gradients with the sums of biases do not fit the registers with two: 200 to 600 bytes of spills; with a
-    // matrix gate two teams leave room for two rows each: 387 us for 16384 x 4096, against 305.)
+    // matrix gate two teams leave room for two rows each: 387 us for 16384 x 4096, against 288.)
     const bool alone = sums && (level == 2 || source[kSourceGateMatrix].base);
     g.pieces = n > 256 * kTeamWarps || (n > 256 && m >= sms && !alone) ? 2 : 1;
     const uint64_t columns = 256ull * kTeamWarps * g.pieces;

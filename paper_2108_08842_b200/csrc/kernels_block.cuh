@@ -15,9 +15,8 @@
 namespace eden {
 
 // A thread takes K pieces of 8 columns (a Philox call each) of its team's rows, 256 columns apart; a
-// team is the up to 16 warps that hold a row.  Rows that 16
-// warps do not hold are shared by the blocks of a cluster (their sums go through distributed shared
-// memory).  K = 2 halves the shuffles and waits per value and leaves another team to run while one
+// team is the warps, up to 16, that hold a row.  Rows that 16 warps do not hold are shared by the blocks
+// of a cluster (their sums go through distributed shared memory).  K = 2 halves the shuffles and waits per value and leaves another team to run while one
 // waits; K = 1 spreads a few rows over more warps.
 //
 // What a row needs is brought to shared memory by bulk copies, the next rows of the team while this
