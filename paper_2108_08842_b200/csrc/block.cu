@@ -38,7 +38,8 @@ extern "C" int eden_block_join(eden_ctx* ctx, const eden_block_join_args* a)
             PlainView p{a->h, a->h_stride, a->residual, a->residual_stride, a->gate, per_value, a->x, a->x_stride, {}, a->scale, 0,
                         (uint32_t)a->m, (uint32_t)a->n, (uint32_t)((a->n + 255) / 256)};
             p.drop = drop_view(a->drop, &p.has_drop);
-            const bool wide = rows_on_16(p.h, p.h_stride) && rows_on_16(p.residual, p.residual_stride) && (!per_value || rows_on_16(p.gate, per_value)) &&
+            // (rows that end inside a chunk are not stored in chunks: what lies behind them is not the call's)
+            const bool wide = a->n % 8 == 0 && rows_on_16(p.h, p.h_stride) && rows_on_16(p.residual, p.residual_stride) && (!per_value || rows_on_16(p.gate, per_value)) &&
                               rows_on_16(p.x, p.x_stride);
             const uint64_t rows = wide ? kPlainRows<true> : kPlainRows<false>, blocks = ((a->m + rows - 1) / rows * p.warps_across + kPlainThreads / 32 - 1) / (kPlainThreads / 32);
             if (blocks > kMaxCount) return EDEN_ERR_TOO_LARGE;

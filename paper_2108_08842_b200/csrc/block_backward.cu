@@ -72,7 +72,7 @@ extern "C" int eden_block_join_backward(eden_ctx* ctx, const eden_block_join_bac
                 PlainBackwardView p{a->dx, a->dx_stride, a->gate ? kept_view(a->h) : KeptView{}, a->gate, per_value, a->d_residual, a->d_residual_stride, a->dh, a->dh_stride,
                                     a->d_gate, a->d_gate_stride, partial(runs), drop, a->scale, has_drop, (uint32_t)a->m, (uint32_t)a->n, (uint32_t)rows_per_run};
                 if (wanted && !p.partial) return EDEN_ERR_WORKSPACE;
-                const bool wide = rows_on_16(p.dx, p.dx_stride) && rows_on_16(p.h.data, p.h.stride) && (!per_value || rows_on_16(p.gate, per_value)) &&
+                const bool wide = a->n % 8 == 0 && rows_on_16(p.dx, p.dx_stride) && rows_on_16(p.h.data, p.h.stride) && (!per_value || rows_on_16(p.gate, per_value)) &&
                                   rows_on_16(p.d_residual, p.d_residual_stride) && rows_on_16(p.dh, p.dh_stride) && rows_on_16(p.d_gate, p.d_gate_stride);
                 EDEN_DISPATCH_HALF(a->type, rc = launch(ctx, "t_join_plain_backward", bytes, wide ? k_join_plain_backward<T_, true> : k_join_plain_backward<T_, false>,
                                                         dim3((uint32_t)strips, (uint32_t)runs), kPlainThreads, 0, 1, p));

@@ -439,7 +439,8 @@ struct Stages {
 
 // The lane's 8 values to p, of which `count` exist.  Without WIDE they go round the warp in shared
 // memory (`buffer`, its own 132 words) and are stored side by side, whole words wherever the matrix
-// has them; `in_warp` of the warp's 256 columns exist.
+// has them; `in_warp` of the warp's 256 columns exist.  With it the row's length is a multiple of 8: all
+// 8 exist or none.
 template <typename T, bool WIDE>
 __device__ __forceinline__ void store_row_8(T* p, int count, int in_warp, const Pair (&v)[4], uint32_t* buffer, uint32_t lane)
 {
