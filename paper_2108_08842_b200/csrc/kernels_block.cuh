@@ -549,6 +549,13 @@ __device__ __forceinline__ void stages_init(uint32_t bars, uint32_t teams)
     __syncthreads();
 }
 
+// The block's vectors lie in shared memory; in a cluster, all of its blocks have started, whose shared
+// memory the others write to from their first sums on.
+__device__ __forceinline__ void block_ready(uint32_t blocks)
+{
+    if (blocks > 1) cluster_arrive_wait(); else __syncthreads();
+}
+
 template <typename T, bool AFTER, bool BEFORE, bool FULL, bool WIDE, int K>
 __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __grid_constant__ BlockShape s, uint32_t* status)
 {
@@ -573,7 +580,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __gr
     if (BEFORE) stages.template keep_vector<T>(rows_of_block, kBeforeWeights, p.before.weight);
     if (FULL && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
     if (FULL && BEFORE && p.before.bias) stages.template keep_vector<T>(rows_of_block, kBeforeBiases, p.before.bias);
-    __syncthreads();
+    block_ready(s.blocks);
     auto vector = [&](Values<K>& v, int which) { stages.vector(v, rows_of_block, which); };
     uint32_t turn = 0, stage = 0, phase = 0;
     bool ok = true;
@@ -694,7 +701,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
     if (AFTER) stages.template keep_vector<T>(rows_of_block, kAfterWeights, p.after.weight);
     if (BEFORE) stages.template keep_vector<T>(rows_of_block, kBeforeWeights, p.before.weight);
     if (BIASES && AFTER && p.after.bias) stages.template keep_vector<T>(rows_of_block, kAfterBiases, p.after.bias);
-    __syncthreads();
+    block_ready(s.blocks);
     auto vector = [&](Values<K>& v, int which) { stages.vector(v, rows_of_block, which); };
     const bool matrix_gate = FULL && s.source[kSourceGateMatrix].base, gated = p.gate || matrix_gate;
     Values<K> total[kJoinSums];
