@@ -423,10 +423,10 @@ struct Stages {
             }
     }
 
-    // A row's statistics.
+    // A row's statistics; 0 for a cluster's block without columns, which nothing was brought to.
     __device__ __forceinline__ float2 pair(uint32_t r, const Source& source) const
     {
-        return *(const float2*)(place(source) + source.skew(r, 0));
+        return at.width ? *(const float2*)(place(source) + source.skew(r, 0)) : make_float2(0.f, 0.f);
     }
 
     // After a wait that ran out: the copies still on their way land before the block ends.

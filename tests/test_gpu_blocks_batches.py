@@ -28,3 +28,18 @@ BOTH = [("rms", "rms", "vector", True, 0.25), ("layer", "layer", "matrix", True,
 def test_clusters_take_several_rows(ctx, parts, m, n, extra, offset, held):
     T.check_join(ctx, T.Case(m, n, torch.bfloat16, *parts, bias=n % 2 == 0, extra=extra, offset=offset))
     T.test_join_backward(ctx, torch.bfloat16, *parts, m, n, extra, offset, held)
+
+
+# rows that the first seven blocks of a cluster hold
+@pytest.mark.parametrize("m,n,extra,offset,parts", [(40, 20488, 0, 0, ("layer", "layer", "matrix", True, 0.1)), (40, 20488, 0, 0, ("rms", "rms", "matrix", True, 0.0)),
+                                                    (40, 24584, 0, 0, ("layer", "layer", "none", True, 0.2)), (40, 24584, 0, 0, ("layer", "rms", "vector", True, 0.0)),
+                                                    (20, 24583, 1, 1, ("layer", "layer", "matrix", False, 0.1))], ids=str)
+def test_gradients_of_clusters_whose_last_block_has_no_columns(ctx, m, n, extra, offset, parts):
+    """Nothing of what earlier calls left in shared memory (NaN, here) reaches the others' sums."""
+    from paper_2108_08842_b200 import eden
+
+    nan = torch.full((300, 8192), float("nan"), dtype=torch.bfloat16, device="cuda")
+    norm = eden.Norm(nan[0], nan[1], "layer")
+    ctx.block_join_backward(nan, nan, nan, nan, torch.full((300, 2), float("nan"), device="cuda"), torch.full((300, 2), float("nan"), device="cuda"),
+                            after=norm, before=norm, gate=nan)
+    T.test_join_backward(ctx, torch.bfloat16, *parts, m, n, extra, offset, False)
