@@ -377,13 +377,15 @@ struct Stages {
         }
     }
 
-    // Zeros behind the last value of every row's place, up to the team's last column: no copy reaches
-    // there.  The whole block.
+    // Zeros behind the last value of every row's place of 16-bit values, up to the team's last column: no
+    // copy reaches there, as their rows start on 16 bytes (a checkpoint's exponents may lie up to 15 bytes
+    // further back, where a copy would meet these stores; what is not there is left out as it is read).
+    // The whole block.
     __device__ __forceinline__ void clear(char* block) const
     {
         for (int i = 0; i < kMaxSources; ++i) {
             const Source& source = s.source[i];
-            if (!source.base || source.fixed) continue;
+            if (!source.base || source.fixed || source.number != 2) continue;
             const uint32_t begin = (source.bytes_of(at.width) + 15) & ~15u, end = source.bytes_of(s.span);
             if (begin >= end) continue;
             for (uint32_t row = 0; row < s.teams * s.stages; ++row)

@@ -43,3 +43,9 @@ def test_gradients_of_clusters_whose_last_block_has_no_columns(ctx, m, n, extra,
     ctx.block_join_backward(nan, nan, nan, nan, torch.full((300, 2), float("nan"), device="cuda"), torch.full((300, 2), float("nan"), device="cuda"),
                             after=norm, before=norm, gate=nan)
     T.test_join_backward(ctx, torch.bfloat16, *parts, m, n, extra, offset, False)
+
+
+@pytest.mark.parametrize("parts", BOTH, ids=lambda p: "-".join(map(str, p)))
+def test_exponents_of_a_cluster_at_any_place_of_16_bytes(ctx, parts):
+    """Rows of 271 exponents, the second block's 127 of which reach past 128 bytes of their place."""
+    T.test_join_backward(ctx, torch.bfloat16, *parts, 150, 8672, 0, 0, True)
