@@ -1041,9 +1041,12 @@ __global__ void __launch_bounds__(kPlainThreads, 3) k_join_plain_backward(PlainB
     if (p.gate && !p.gate_stride) vector = load_shifted_8((const T*)p.gate + col, count);
 #pragma unroll 2
     for (uint64_t row = begin; row < end; ++row) {
+        // all of a row's loads before its stores: a result may lie over any of the inputs
         Pair v[4], w[4], h[4];
+        uint4 gate = vector;
         widen_8<T>(load_row_8<WIDE>((const T*)p.dx + row * p.dx_stride + col, count), v);
         if (p.gate) load_kept<WIDE, T>(p.h, row, col, count, h);
+        if (p.gate && p.gate_stride) gate = load_row_8<WIDE>((const T*)p.gate + row * p.gate_stride + col, count);
         if (p.d_residual) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = v[j] * Pair(p.scale);
@@ -1058,7 +1061,7 @@ __global__ void __launch_bounds__(kPlainThreads, 3) k_join_plain_backward(PlainB
 #pragma unroll
             for (int j = 0; j < 4; ++j) h[j] = h[j] * v[j];
             if (p.has_drop) drop_values(h, numbers, p.drop.keep, 1.f);
-            widen_8<T>(p.gate_stride ? load_row_8<WIDE>((const T*)p.gate + row * p.gate_stride + col, count) : vector, w);
+            widen_8<T>(gate, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 v[j] = v[j] * w[j];
