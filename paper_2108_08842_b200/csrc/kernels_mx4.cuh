@@ -727,23 +727,45 @@ __global__ void __launch_bounds__(kFewThreads, R == 1 ? 2 : 1) k_mx4_few(Mx4Few 
                 be[s] = *(const uint32_t*)x_exps[s];
                 x_exps[s] += FROM_MATRIX ? 4 * kWarps : kExpsOn;
             }
+            // d * sx is exact down to 2^-126; with one of x's powers from 2^65 on it could pass the range though the
+            // result does not, and the smaller of the two powers comes first
+            const bool large = ((be[0] & be[0] << 1 | be[1] & be[1] << 1) & 0x80808080u) != 0;
+            // the products of two groups, then what they are scaled by
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t z[4];
-                mx4_halves(b[j], z);
-                const float sx[2] = {mx4_scale(be[0], j), mx4_scale(be[1], j)};
+            for (int j0 = 0; j0 < 4; j0 += 2) {
+                float d[2][R][4];
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    uint32_t u[4], v[4];
-                    mx4_halves(a[2 * r][j], u);
-                    mx4_halves(a[2 * r + 1][j], v);
-                    float d[4] = {0.f, 0.f, 0.f, 0.f};
-                    few_product<__half>(d, u[0], v[0], u[1], v[1], z[0], z[1]);
-                    few_product<__half>(d, u[2], v[2], u[3], v[3], z[2], z[3]);
-                    const float sw[2] = {mx4_scale(ae[2 * r], j), mx4_scale(ae[2 * r + 1], j)};
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t z[4];
+                    mx4_halves(b[j0 + h], z);
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) c[r][0][s] = fmaf(d[s] * sx[s % 2], sw[s / 2], c[r][0][s]);
+                    for (int r = 0; r < R; ++r) {
+                        uint32_t u[4], v[4];
+                        mx4_halves(a[2 * r][j0 + h], u);
+                        mx4_halves(a[2 * r + 1][j0 + h], v);
+                        d[h][r][0] = d[h][r][1] = d[h][r][2] = d[h][r][3] = 0.f;
+                        few_product<__half>(d[h][r], u[0], v[0], u[1], v[1], z[0], z[1]);
+                        few_product<__half>(d[h][r], u[2], v[2], u[3], v[3], z[2], z[3]);
+                    }
                 }
+                auto add = [&](auto ordered) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float sx[2] = {mx4_scale(be[0], j0 + h), mx4_scale(be[1], j0 + h)};
+#pragma unroll
+                        for (int r = 0; r < R; ++r)
+#pragma unroll
+                            for (int s = 0; s < 4; s += 2) {
+                                const float sw = mx4_scale(ae[2 * r + s / 2], j0 + h);
+                                float(&sum)[4] = c[r][0];
+                                const Pair first = decltype(ordered)::value ? Pair(fminf(sx[0], sw), fminf(sx[1], sw)) : Pair(sx[0], sx[1]);
+                                const Pair second = decltype(ordered)::value ? Pair(fmaxf(sx[0], sw), fmaxf(sx[1], sw)) : Pair(sw);
+                                fma(Pair(d[h][r][s], d[h][r][s + 1]) * first, second, Pair(sum[s], sum[s + 1])).get(sum[s], sum[s + 1]);
+                            }
+                    }
+                };
+                if (__builtin_expect(large, 0)) add(std::true_type());
+                else add(std::false_type());
             }
         }
     }
