@@ -251,7 +251,8 @@ __device__ __forceinline__ float2 row_statistics(Exchange& e, uint32_t& turn, co
     sums(std::false_type());
     if (square < 3.0e38f) return make_float2(mean, rsqrtf(square + norm.eps));
     sums(std::true_type());
-    return make_float2(mean / kSmaller, rsqrtf(square) * kSmaller);        // eps is nothing beside such squares
+    // eps is nothing beside such squares, but all there is where only the sum of the values was too large
+    return make_float2(mean / kSmaller, square == 0.f ? rsqrtf(norm.eps) : rsqrtf(fmaf(norm.eps * kSmaller, kSmaller, square)) * kSmaller);
 }
 
 // The 16 bytes that begin `skew` bytes, an even number, into two chunks.  One branch where the skew is
