@@ -630,7 +630,8 @@ __global__ void __launch_bounds__(kJoinThreads, 1) k_join(JoinView p, const __gr
         }
         if (p.x) store_row<T, WIDE, K>((T*)p.x + (uint64_t)row * p.x_stride + at.col, at, v, buffer);
         if constexpr (BEFORE) {
-            if (FULL) {
+            // (without a mean, columns that do not exist are 0 but for a row whose norm after is NaN)
+            if (FULL || AFTER) {
 #pragma unroll
                 for (int i = 0; i < K; ++i) mask_values<WIDE>(v[i], at.count[i]);
             }
@@ -806,7 +807,7 @@ __global__ void __launch_bounds__(kJoinBackwardThreads, 1) k_join_backward(JoinB
         }
         if constexpr (AFTER) {
             Pair a(0.f), b(0.f);
-            if (FULL) {
+            if (FULL || BEFORE) {
 #pragma unroll
                 for (int i = 0; i < K; ++i) mask_values<WIDE>(d[i], at.count[i]);
             }

@@ -1,4 +1,4 @@
-"""Joins of rows whose values or sums lie at the ends of the range."""
+"""Joins of rows whose values or sums lie at the ends of the range, and of what a mask leaves of them."""
 import numpy as np
 import pytest
 import torch
@@ -50,3 +50,36 @@ def test_rows_whose_squares_pass_the_range(ctx):
         y, stats = ctx.norm(rows, eden.Norm(None, None, kind, 1e-6), stats=True)
         value, off, mean, rate, mean_off, rate_off = B.norm(R.f64(rows), np.zeros(rows.shape), kind, None, None, 1e-6)
         B.near(y, (value, off), R.UNIT[torch.bfloat16], R.TINY[torch.bfloat16])
+
+
+# ------------------------------------------------------------------------------- masks
+def all_dropped(m, n, drop, seed):
+    gone = torch.from_numpy((B.kept(m, n, drop, seed) == 0).all(axis=1)).cuda()
+    assert gone.any() and not gone.all()
+    return gone
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("n", [1, 5, 8, 16])
+def test_rows_of_which_the_mask_leaves_nothing(ctx, dtype, kind, n):
+    """They are the residual's, whatever the block made; their gradients are 0, whatever came back."""
+    from paper_2108_08842_b200 import eden
+
+    m, drop, seed = 300, 0.9, 21
+    gone = all_dropped(m, n, drop, seed)
+    h, r, gate = normal(1, m, n, dtype=dtype), normal(2, m, n, dtype=dtype), normal(3, n, dtype=dtype)
+    after, before = eden.Norm(normal(4, n, dtype=dtype), None, kind), eden.Norm(normal(5, n, dtype=dtype), None, kind)
+    how = dict(after=after, before=before, gate=gate, drop=drop, seed=seed)
+    clean = ctx.block_join(h, r, stats=True, **how)
+    for bad in (float("nan"), float("inf")):
+        broken = torch.where(gone[:, None], torch.full_like(h, bad), h)
+        j = ctx.block_join(broken, r, stats=True, **how)
+        assert torch.equal(j.x, clean.x) and torch.equal(j.y, clean.y) and torch.equal(j.before_stats, clean.before_stats)
+    args = (h, clean.x, clean.after_stats, clean.before_stats)
+    dx, dy = normal(6, m, n, dtype=dtype), normal(7, m, n, dtype=dtype)
+    want = ctx.block_join_backward(dx, dy, *args, **how)
+    assert (want.h[gone] == 0).all()
+    for bad in (float("nan"), float("inf")):
+        d = ctx.block_join_backward(dx, torch.where(gone[:, None], torch.full_like(dy, bad), dy), *args, **how)
+        assert torch.equal(d.h, want.h) and torch.equal(d.after_weight, want.after_weight) and torch.equal(d.gate, want.gate)
