@@ -287,9 +287,9 @@ struct Stages {
     __device__ __forceinline__ Stages(const BlockShape& s, const Place<K>& at, char* block, uint32_t bars)
         : s(s), at(at), buffers(block + at.team * s.stages * s.row_bytes), row(buffers), bars(bars + at.team * kMaxStages * 8), from(nullptr), stride(0), bytes(0), to(0)
     {
-        if (at.lane >= kMaxSources || !at.width) return;
+        if (at.lane >= kMaxSources) return;
         const Source& source = s.source[at.lane];
-        if (!source.base) return;
+        if (!source.base || (!at.width && !source.fixed)) return;          // a cluster's block without columns reads a row's statistics too
         from = source.base + source.begin(at.first);
         stride = source.stride;
         bytes = source.bytes_of(at.width);
@@ -426,10 +426,10 @@ struct Stages {
             }
     }
 
-    // A row's statistics; 0 for a cluster's block without columns, which nothing was brought to.
+    // A row's statistics.
     __device__ __forceinline__ float2 pair(uint32_t r, const Source& source) const
     {
-        return at.width ? *(const float2*)(place(source) + source.skew(r, 0)) : make_float2(0.f, 0.f);
+        return *(const float2*)(place(source) + source.skew(r, 0));
     }
 
     // After a wait that ran out: the copies still on their way land before the block ends.
