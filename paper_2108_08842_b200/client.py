@@ -57,6 +57,7 @@ class FeedForward:
                 gated.fill_(0.5)
         self.load(self.vector)
         self._held: List = []
+        self._first = None                                    # with norms: the network's input and its statistics
 
     def _vectors(self, parts: List[torch.Tensor], b: int):
         """(weight, bias) of the norm before block b and of the one after it, and its gate, out of parts()."""
@@ -110,7 +111,7 @@ class FeedForward:
         return dict(after=self._norm(b, True), before=self._norm(b + 1, False), gate=self._norms[b][2], drop=drop, seed=(seed * self.blocks + b) % 2 ** 64)
 
     def _forward_joined(self, x: torch.Tensor, train: bool, seed: int) -> torch.Tensor:
-        ctx, self._held, mx4 = self.ctx, [], self.products == "mx4"
+        ctx, self._held, self._first, mx4 = self.ctx, [], None, self.products == "mx4"
         if train:
             y, stats = ctx.norm(x, self._norm(0, False), stats=True)
             self._first, self._seed = (ctx.checkpoint_save(x), stats), seed
@@ -141,9 +142,15 @@ class FeedForward:
             x, y = j.x, j.y
         return x
 
-    def held_bytes(self) -> int:
-        """What the kept activations take."""
-        return sum(t.numel() for held in self._held for c in held if isinstance(c, tuple) for t in c[:2])
+    def held_bytes(self, whole: bool = False) -> int:
+        """What the blocks' kept activations take; whole: with the network's input, which blocks without norms
+        count as the first one's, and the norms' statistics: all that is kept for `backward`."""
+        kept = sum(t.numel() for held in self._held for c in held if isinstance(c, tuple) for t in c[:2])
+        if whole and self._first:
+            x, stats = self._first
+            kept += sum(t.numel() for t in x)
+            kept += sum(4 * t.numel() for held in [(stats,)] + self._held for t in held if isinstance(t, torch.Tensor))
+        return kept
 
     def backward(self, dy: torch.Tensor, gradient: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
         """The gradient of <dy, forward(x)> with respect to the parameters, as one fp32 vector
@@ -224,7 +231,7 @@ def run(clients: int = 4, rounds: int = 20, bits: float = 1.0, tokens: int = 204
         student.load(student.vector - rate / width * mean)
         losses.append(float(total) / clients)
         say("round %d: loss %.5f  (%d clients, d = %d, %.3g bits; held activations %.1f MB a client)" % (
-            r, losses[-1], clients, d, bits, student.held_bytes() / 1e6))
+            r, losses[-1], clients, d, bits, student.held_bytes(whole=True) / 1e6))
     assert ctx.status() == 0
     ctx.close()
     return losses
