@@ -77,13 +77,14 @@ class FeedForward:
         return [v.view(s) for v, s in zip(vector.split(self.sizes), self.shapes)]
 
     def load(self, vector: torch.Tensor):
-        """Takes fp32 parameters: the products run on copies in the 16-bit type, or in 4 bits."""
+        """Takes fp32 parameters: the products run on copies in the 16-bit type, or in 4 bits (each rounded once)."""
         self.vector = vector
-        self.work = [p.to(self.dtype) for p in self.parts(vector)]
+        parts = self.parts(vector)
+        self.work = [p.to(self.dtype) for p in parts]
         if self.norm != "none":
             self._norms = [self._vectors(self.work, b) for b in range(self.blocks)]
         if self.products == "mx4":                            # each by rows and, for the input's gradient, by columns
-            self._mx4 = [self.ctx.mx4_quantize_both(p) for p in self.work[: 4 * self.blocks] if p.dim() == 2]
+            self._mx4 = [self.ctx.mx4_quantize_both(p) for p in parts[: 4 * self.blocks] if p.dim() == 2]
 
     def forward(self, x: torch.Tensor, train: bool = True, seed: int = 0) -> torch.Tensor:
         """x [tokens, width] -> [tokens, width]; train: the checkpoints for `backward` are kept, and
