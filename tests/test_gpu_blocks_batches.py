@@ -30,6 +30,31 @@ def test_clusters_take_several_rows(ctx, parts, m, n, extra, offset, held):
     T.test_join_backward(ctx, torch.bfloat16, *parts, m, n, extra, offset, held)
 
 
+# teams of a warp to all of a block's, of one piece a thread and of two, aligned rows and others: 4 to 16 rows a
+# team, in 2 to 4 places
+@pytest.mark.parametrize("parts", BOTH + [("rms", "none", "matrix", True, 0.3), ("none", "layer", "vector", False, 0.0)], ids=lambda p: "-".join(map(str, p)))
+@pytest.mark.parametrize("m,n,extra,offset,held", [(30000, 40, 0, 0, True), (8000, 513, 0, 0, False), (1600, 4096, 0, 0, True), (1200, 4104, 8, 8, False)])
+def test_teams_take_several_rows(ctx, parts, m, n, extra, offset, held):
+    T.check_join(ctx, T.Case(m, n, torch.bfloat16, *parts, bias=n % 2 == 0, extra=extra, offset=offset))
+    T.test_join_backward(ctx, torch.bfloat16, *parts, m, n, extra, offset, held)
+
+
+def test_a_batch_is_its_rows(ctx):
+    """The rows of a batch, joined in parts of one row a team, are the same bit for bit, forward and backward."""
+    m, n, part = 8000, 520, 800
+    c = T.Case(m, n, torch.float16, "layer", "rms", "vector", drop=0.2, bias=True)
+    j = ctx.block_join(c.h, c.residual, stats=True, **c.how())
+    dx, dy = T.make(5, m, n, torch.float16), T.make(6, m, n, torch.float16)
+    sums = dict(after_bias_grad=False, before_bias_grad=False)        # which would have the parts take fewer values a thread
+    d = ctx.block_join_backward(dx, dy, c.h, j.x, j.after_stats, j.before_stats, **sums, **c.how())
+    for i in range(0, m, part):
+        s, how = slice(i, i + part), {**c.how(), "first_row": i}
+        a = ctx.block_join(c.h[s], c.residual[s], stats=True, **how)
+        assert all(torch.equal(p, q[s]) for p, q in zip(a, j))
+        b = ctx.block_join_backward(dx[s], dy[s], c.h[s], j.x[s], j.after_stats[s], j.before_stats[s], **sums, **how)
+        assert torch.equal(b.h, d.h[s]) and torch.equal(b.residual, d.residual[s])
+
+
 # rows that the first seven blocks of a cluster hold
 @pytest.mark.parametrize("m,n,extra,offset,parts", [(40, 20488, 0, 0, ("layer", "layer", "matrix", True, 0.1)), (40, 20488, 0, 0, ("rms", "rms", "matrix", True, 0.0)),
                                                     (40, 24584, 0, 0, ("layer", "layer", "none", True, 0.2)), (40, 24584, 0, 0, ("layer", "rms", "vector", True, 0.0)),
