@@ -600,6 +600,7 @@ typedef struct eden_kept {
  *   d_residual = scale * t, dh, and d_gate (gate_per_value), in `type`;
  *   the sums over the rows in fp32 (accumulate: added to what is there): the norms' weights and
  *   biases, gate_sum (a vector gate).
+ * What was dropped adds nothing to a gate's gradient, whatever it was, but for a NaN that the norm after made.
  * Each output may be NULL.  h: with a norm after or a gate; x: with a norm before. */
 typedef struct eden_block_join_backward_args {
     const void* dx;        uint64_t dx_stride;

@@ -247,8 +247,8 @@ extern "C" int eden_mx4_linear(eden_ctx* ctx, const eden_mx4_linear_args* a)
         const double bytes = 17.0 * groups_of(a->k) * ((double)a->m + a->n) + 2.0 * (a->n + (double)a->m * a->n * (a->residual ? 2 : 1)) +
                              (a->save ? (double)a->m * (a->n + groups_of(a->n)) : 0.0);
         const bool few = a->m <= 8 && (ctx->linear_form == EDEN_LINEAR_AUTO || ctx->linear_form == EDEN_LINEAR_FEW);
-        // A token's values are quantised by the blocks that use them (1 x 4096 x 4096 in 6.5 us, as a launch of
-        // its own 9.5); of many, each block would do too much (8 tokens: 12.7 us, and 10).
+        // A token's values are quantised by the blocks that use them (1 x 4096 x 4096 in 7.0 us, as a launch of
+        // its own 8.9; 3 tokens 9.2 and 9.4); of many, each block would do too much (8 tokens 13.9 and 9.4).
         const bool fused = few && a->x && a->m * a->k <= kFewFused;
         Mx4Operand x = operand_of(a->held, a->m, a->k);
         if (a->x && !fused) {
